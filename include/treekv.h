@@ -257,10 +257,93 @@ treekv_status treekv_export_state(treekv_ctx* ctx, void* dev_image, int64_t* hos
 treekv_status treekv_import_state(treekv_ctx* ctx, const void* dev_image, const int64_t* host_tokens_seen,
                                   void* stream);
 
+/*
+ * ---- Drafted decoding ------------------------------------------------------------------------------------------------
+ * A step that drafts several tokens ahead: treekv_norm_rope makes q, k, v of the drafted tokens, treekv_verify_tree
+ * attends to the cache and to the draft's own tree without changing the cache, the caller picks the path it accepts, and
+ * treekv_accept_path takes that path's tokens into the cache.  treekv_fork_sequences copies sequences within the batch.
+ * (The paper has no counterpart: Section 3.1's attention and Algorithm 1's updates, applied to a tree of tokens.)  These
+ * four calls need the context's device to be the current one (TREEKV_ERR_BAD_STATE otherwise).
+ */
+
+/*
+ * q, k, v of `tokens` tokens out of a packed projection, in one pass: the rows' heads are separated, every q and k head is
+ * normalised, n = x * rsqrt(mean(x^2) + eps) * weight, and rotated to its token's position with the numeric contract of
+ * treekv_set_positions, in fp32 with one rounding at the end; v heads are copied.
+ *   dev_qkv      [tokens] rows of (n_heads + 2 n_kv_heads) * head_dim elements - q heads, k heads, v heads - row_stride
+ *                elements apart (a multiple of 16 bytes, at least the row)
+ *   dev_q_weight, dev_k_weight  [head_dim], the context's dtype; NULL = no norm for that tensor
+ *   dev_cos, dev_sin            [slots][head_dim/2] float as in treekv_set_positions; both NULL = no rotation (what a
+ *                context with in-cache positions takes)
+ *   dev_pos      [tokens] int32: each token's row of the tables.  A negative one marks padding: the token's rows of the
+ *                outputs are not written.  One past the tables is not followed: its rows are not written, and device_error
+ *                gets bit 256.  May be NULL without tables.
+ *   dev_q [tokens][n_heads][head_dim], dev_k, dev_v [tokens][n_kv_heads][head_dim]; dev_v NULL = v is not wanted.  The
+ *                outputs must not overlap the input.
+ * The cache takes no part: of the context the call uses the head layout, the dtype and the error word.
+ */
+treekv_status treekv_norm_rope(treekv_ctx* ctx, const void* dev_qkv, int64_t row_stride, const void* dev_q_weight,
+                               const void* dev_k_weight, float eps, const float* dev_cos, const float* dev_sin, int slots,
+                               const int32_t* dev_pos, void* dev_q, void* dev_k, void* dev_v, int tokens, void* stream);
+
+/*
+ * Attention of a tree of drafted tokens over the cache, which stays as it is: drafted token i of a sequence attends to
+ * every cached token and to the drafted tokens j whose bit j is set in mask word i - normally its ancestors and itself.
+ *   dev_q, dev_out  [batch][stride][n_heads][head_dim]     dev_k, dev_v  [batch][stride][n_kv_heads][head_dim]
+ *   dev_mask        [batch][stride] 64-bit words; bits at and above the sequence's draft length are ignored.  NULL = a
+ *                   chain: token i sees tokens 0..i
+ *   dev_lse         [batch][stride][n_heads] float: natural logarithm of the sum of exp(q k / sqrt(head_dim)) over what
+ *                   the token sees, as treekv_accept_path takes it; may be NULL
+ *   host_lens       [batch] int32 in 0..stride (0 = sequence not in this call); NULL = all `stride`.  Read before
+ *                   returning.  stride: 1..64
+ * A token that sees nothing (an empty cache and an empty word) gets an output of zeros and a log-sum-exp of minus
+ * infinity.  Rows beyond a sequence's length are neither read as keys nor written.  With in-cache positions a drafted token
+ * is encoded behind the cache, at slot L + (number of drafted tokens it sees) - 1 - where it will sit if its path is
+ * accepted - which needs tables of at least budget + stride slots (TREEKV_ERR_UNSUPPORTED otherwise).
+ */
+treekv_status treekv_verify_tree(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v,
+                                 const uint64_t* dev_mask, void* dev_out, float* dev_lse, const int32_t* host_lens,
+                                 int stride, void* stream);
+
+/*
+ * The accepted path of a draft enters the cache: as treekv_prefill_chunk with the path's tokens as the chunk, in path
+ * order - append, S and C, evictions - except that no output is computed (treekv_verify_tree has left it).
+ *   dev_q, dev_k, dev_v, stride, dev_lse   as they were in the treekv_verify_tree call, on the same cache content
+ *   dev_path   [batch][path_stride] int32: the accepted drafted tokens, first to last; each must have seen the cache, the
+ *              path's tokens in front of it and itself, nothing else.  An index outside 0..stride-1 is not followed: token 0
+ *              stands in and device_error gets bit 256 (the context must then be reset)
+ *   host_lens  [batch] int32 in 0..min(path_stride, stride, max_chunk): tokens accepted (0 = none); NULL = all path_stride.
+ *              Read before returning
+ * Not while the stream is being captured (TREEKV_ERR_BAD_STATE): the host-side token counts advance with the call.
+ */
+treekv_status treekv_accept_path(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v,
+                                 const float* dev_lse, int stride, const int32_t* dev_path, int path_stride,
+                                 const int32_t* host_lens, void* stream);
+
+/*
+ * Copies between the sequences of the batch, all at once: sequence b becomes what sequence host_source[b] was before the
+ * call (cached tokens, scores, positions, counters); host_source[b] = b leaves it, -1 empties it.  A source may itself be
+ * replaced or emptied by the same call and may have any number of copies: beams take their parents' caches, one prompt
+ * becomes several samples, a shrinking batch is packed.
+ *   host_source  [batch] int32 in -1..batch-1.  Read before returning
+ * treekv_stats.evictions stays (copies are no evictions).  Not while the stream is being captured (TREEKV_ERR_BAD_STATE).
+ */
+treekv_status treekv_fork_sequences(treekv_ctx* ctx, const int32_t* host_source, void* stream);
+
+/*
+ * Self-test of the order in which treekv_fork_sequences copies (host only).  Fills ops with rows of four - component, source,
+ * destination, tokens seen - at most 3 * batch / 2 of them, and returns their number (-1 on bad arguments).  A destination
+ * of 65535 keeps the source's content aside, a source of 65535 is the content kept, a source of 65534 empties the
+ * destination.
+ */
+int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64_t* host_seen, int32_t* ops);
+
 /* Counters and error words.  Synchronises `stream` to read the device-side counters.  *host_out is filled
  * whenever the read itself succeeded; the return value is TREEKV_ERR_TIMEOUT when device_error is non-zero, i.e.
  * when a kernel's bounded wait gave up (bits: 4 TMA producer, 8 MMA issuer, 16 softmax / epilogue warps of the
- * tensor-core prefill kernels, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v).  treekv_reset clears it. */
+ * tensor-core prefill kernels, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v), or
+ * TREEKV_ERR_INVALID_ARG when its only bit is 256: an index in device memory was out of range and was not followed
+ * (treekv_norm_rope, treekv_accept_path).  treekv_reset clears it. */
 treekv_status treekv_get_stats(treekv_ctx* ctx, treekv_stats* host_out, void* stream);
 
 /*

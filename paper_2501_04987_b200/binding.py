@@ -27,6 +27,7 @@ EXPORTS = [
     "treekv_destroy", "treekv_status_string", "treekv_version",
     "treekv_state_bytes", "treekv_export_state", "treekv_import_state", "treekv_selftest_wait_giveup",
     "treekv_set_protection", "treekv_prefill_oneshot", "treekv_set_positions",
+    "treekv_norm_rope", "treekv_verify_tree", "treekv_accept_path", "treekv_fork_sequences", "treekv_selftest_fork_plan",
 ]
 
 
@@ -102,6 +103,16 @@ def _load():
     lib.treekv_set_protection.argtypes = [vp, i32, i32]
     lib.treekv_selftest_wait_giveup.restype = i32
     lib.treekv_selftest_wait_giveup.argtypes = [vp, i32, vp]
+    lib.treekv_norm_rope.restype = i32
+    lib.treekv_norm_rope.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_float, vp, vp, i32, vp, vp, vp, vp, i32, vp]
+    lib.treekv_verify_tree.restype = i32
+    lib.treekv_verify_tree.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.POINTER(C.c_int32), i32, vp]
+    lib.treekv_accept_path.restype = i32
+    lib.treekv_accept_path.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, C.POINTER(C.c_int32), vp]
+    lib.treekv_fork_sequences.restype = i32
+    lib.treekv_fork_sequences.argtypes = [vp, C.POINTER(C.c_int32), vp]
+    lib.treekv_selftest_fork_plan.restype = i32
+    lib.treekv_selftest_fork_plan.argtypes = [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
     return lib
 
 
@@ -221,6 +232,30 @@ def treekv_import_state(ctx, dev_image, tokens_seen, stream=0) -> int:
     return lib.treekv_import_state(ctx, dev_image, seen, stream)
 
 
+def treekv_norm_rope(ctx, qkv, row_stride, q_weight, k_weight, eps, cos, sin, slots, pos, q, k, v, tokens, stream=0) -> int:
+    return lib.treekv_norm_rope(ctx, qkv, row_stride, q_weight, k_weight, eps, cos, sin, slots, pos, q, k, v, tokens, stream)
+
+
+def treekv_verify_tree(ctx, q, k, v, mask, out, lse, lens, stride, stream=0) -> int:
+    return lib.treekv_verify_tree(ctx, q, k, v, mask, out, lse, _i32(lens), stride, stream)
+
+
+def treekv_accept_path(ctx, q, k, v, lse, stride, path, path_stride, lens, stream=0) -> int:
+    return lib.treekv_accept_path(ctx, q, k, v, lse, stride, path, path_stride, _i32(lens), stream)
+
+
+def treekv_fork_sequences(ctx, source, stream=0) -> int:
+    return lib.treekv_fork_sequences(ctx, _i32(source), stream)
+
+
+def treekv_selftest_fork_plan(source, seen):
+    """The copy operations of treekv_fork_sequences as (component, source, destination, tokens seen) rows."""
+    n = len(source)
+    ops = (C.c_int32 * (4 * (n + n // 2 + 1)))()
+    count = lib.treekv_selftest_fork_plan(_i32(source), n, (C.c_int64 * n)(*[int(x) for x in seen]), ops)
+    return None if count < 0 else [tuple(ops[4 * o:4 * o + 4]) for o in range(count)]
+
+
 def treekv_selftest_wait_giveup(ctx, attempts, stream=0) -> int:
     return lib.treekv_selftest_wait_giveup(ctx, attempts, stream)
 
@@ -329,6 +364,85 @@ class TreeKV:
         _check(treekv_prefill_chunk_host(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), out.data_ptr(), chunk_lens,
                                          q.shape[1], self._stream()), "treekv_prefill_chunk_host")
         return out
+
+    def _lens(self, lens, what):
+        if lens is not None and len(lens) != self.batch:
+            raise ValueError("expected %d %s, got %d" % (self.batch, what, len(lens)))
+        return lens
+
+    def _int(self, x, dtype, shape, what):
+        if not (x.is_cuda and x.is_contiguous() and x.dtype == dtype and tuple(x.shape) == tuple(shape)):
+            raise ValueError("expected %s as a contiguous %s CUDA tensor of shape %s, got %s %s" %
+                             (what, dtype, tuple(shape), x.dtype, tuple(x.shape)))
+
+    def norm_rope(self, qkv, q_weight=None, k_weight=None, cos=None, sin=None, positions=None, eps=1e-6, q=None, k=None, v=None):
+        """(q, k, v) of the tokens of a packed projection [tokens, (n_heads + 2 n_kv_heads) * head_dim], whose rows may lie
+        in wider ones: every q and k head normalised (where its weight [head_dim] is given) and rotated to the token's
+        position (where tables [slots, head_dim/2] are given)."""
+        t = self.torch
+        Hq, Hkv, d = self.n_heads, self.n_kv_heads, self.head_dim
+        if not (qkv.is_cuda and qkv.dim() == 2 and qkv.dtype == self.tdtype and qkv.shape[1] == (Hq + 2 * Hkv) * d
+                and (qkv.stride(1) == 1 or qkv.numel() == 0)):
+            raise ValueError("expected a %s CUDA tensor [tokens, %d] with adjacent columns, got %s %s" %
+                             (self.tdtype, (Hq + 2 * Hkv) * d, qkv.dtype, tuple(qkv.shape)))
+        n = qkv.shape[0]
+        for w in (q_weight, k_weight):
+            if w is not None:
+                self._chk(w, (d,))
+        if (cos is None) != (sin is None) or (cos is not None and positions is None):
+            raise ValueError("a rotation takes cos, sin and positions")
+        for x in (cos, sin):
+            if x is not None:
+                self._int(x, t.float32, (cos.shape[0], d // 2), "cos and sin")
+        if positions is not None:
+            self._int(positions, t.int32, (n,), "positions")
+        q = t.empty((n, Hq, d), dtype=self.tdtype, device=qkv.device) if q is None else q
+        k = t.empty((n, Hkv, d), dtype=self.tdtype, device=qkv.device) if k is None else k
+        v = t.empty((n, Hkv, d), dtype=self.tdtype, device=qkv.device) if v is None else v
+        self._chk(q, (n, Hq, d)); self._chk(k, (n, Hkv, d)); self._chk(v, (n, Hkv, d))
+        ptr = lambda x: None if x is None else x.data_ptr()
+        # (torch reports any stride for the rows of a tensor of one row)
+        stride = qkv.stride(0) if n > 1 else (Hq + 2 * Hkv) * d
+        _check(treekv_norm_rope(self._h, qkv.data_ptr(), stride, ptr(q_weight), ptr(k_weight), eps, ptr(cos), ptr(sin),
+                                0 if cos is None else cos.shape[0], ptr(positions), q.data_ptr(), k.data_ptr(), v.data_ptr(), n,
+                                self._stream()), "treekv_norm_rope")
+        return q, k, v
+
+    def verify_tree(self, q, k, v, mask=None, lens=None, out=None, lse=None):
+        """(out, lse) of drafted tokens [batch, stride, heads, head_dim] over the cache and the drafted tokens that each
+        one's mask word (int64 [batch, stride], bit j = drafted token j) names; without masks a chain."""
+        t = self.torch
+        B, Hq, Hkv, d = self.batch, self.n_heads, self.n_kv_heads, self.head_dim
+        n = q.shape[1]
+        self._chk(q, (B, n, Hq, d)); self._chk(k, (B, n, Hkv, d)); self._chk(v, (B, n, Hkv, d))
+        if mask is not None:
+            self._int(mask, t.int64, (B, n), "mask")
+        if out is None:
+            out = t.empty_like(q)
+        if lse is None:
+            lse = t.empty((B, n, Hq), dtype=t.float32, device=q.device)
+        self._chk(out, (B, n, Hq, d))
+        self._int(lse, t.float32, (B, n, Hq), "lse")
+        _check(treekv_verify_tree(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if mask is None else mask.data_ptr(),
+                                  out.data_ptr(), lse.data_ptr(), self._lens(lens, "draft lengths"), n, self._stream()),
+               "treekv_verify_tree")
+        return out, lse
+
+    def accept_path(self, q, k, v, lse, path, lens=None):
+        """The drafted tokens path[b, :lens[b]] (int32) of every sequence enter the cache; q, k, v, lse as in verify_tree."""
+        t = self.torch
+        B, Hq, Hkv, d = self.batch, self.n_heads, self.n_kv_heads, self.head_dim
+        n = q.shape[1]
+        self._chk(q, (B, n, Hq, d)); self._chk(k, (B, n, Hkv, d)); self._chk(v, (B, n, Hkv, d))
+        self._int(lse, t.float32, (B, n, Hq), "lse")
+        self._int(path, t.int32, (B, path.shape[1]), "path")
+        _check(treekv_accept_path(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), lse.data_ptr(), n, path.data_ptr(),
+                                  path.shape[1], self._lens(lens, "accepted lengths"), self._stream()), "treekv_accept_path")
+
+    def fork_sequences(self, source):
+        """Sequence b becomes what sequence source[b] was (b: stays, -1: emptied), all at once."""
+        _check(treekv_fork_sequences(self._h, self._lens([int(x) for x in source], "sources"), self._stream()),
+               "treekv_fork_sequences")
 
     def retained_positions(self):
         t = self.torch

@@ -151,7 +151,7 @@ treekv_status treekv_create(treekv_ctx** out, int budget, int n_heads, int n_kv_
     ctx->ps.colsum = reinterpret_cast<float*>(base + L.colsum);
     // (rows in flight during compaction stay in registers: the context has no staging rows; PrefillScratch's
     //  staging pointers are only used by the entry point that brings its own scratch)
-    ctx->ps.QT = L.QT; ctx->ps.n_max = L.n_max; ctx->ps.max_chunk = max_chunk; ctx->ps.window = 0;
+    ctx->ps.QT = L.QT; ctx->ps.n_max = L.n_max; ctx->ps.max_chunk = max_chunk; ctx->ps.window = 0; ctx->ps.slices = 0;
     ctx->st_q = base + L.st_q; ctx->st_k = base + L.st_k; ctx->st_v = base + L.st_v; ctx->st_out = base + L.st_out;
     ctx->dt = dtype; ctx->max_chunk = max_chunk; ctx->G = n_heads / n_kv_heads;
     ctx->elem = dtype == TREEKV_F32 ? 4 : 2;
@@ -579,7 +579,8 @@ treekv_status treekv_get_stats(treekv_ctx* ctx, treekv_stats* host_out, void* st
     host_out->kernel_launches = ctx->launches;
     host_out->device_error = ds.error;
     host_out->last_cuda_error = ctx->last_cuda_error;
-    return ds.error ? TREEKV_ERR_TIMEOUT : TREEKV_OK;
+    if (ds.error & ~kErrBadIndex) return TREEKV_ERR_TIMEOUT;
+    return ds.error ? TREEKV_ERR_INVALID_ARG : TREEKV_OK;
 }
 
 int64_t treekv_tokens_seen(const treekv_ctx* ctx, int b) {
@@ -614,7 +615,7 @@ treekv_status treekv_set_positions(treekv_ctx* ctx, const float* dev_cos, const 
     // slots in use: 0 .. budget during decode (the query sits in slot budget), 0 .. budget + chunk - 1 during prefill
     const int need = ctx->cv.c + (ctx->max_chunk > 1 ? ctx->max_chunk : 1);
     if (slots < need) return TREEKV_ERR_INVALID_ARG;
-    ctx->cv.rope_cos = dev_cos; ctx->cv.rope_sin = dev_sin;
+    ctx->cv.rope_cos = dev_cos; ctx->cv.rope_sin = dev_sin; ctx->rope_slots = slots;
     return TREEKV_OK;
 }
 

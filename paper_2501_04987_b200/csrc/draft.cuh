@@ -1,0 +1,68 @@
+// Shared by the kernels of drafted decoding: what a call brings, and where its keys lie.
+#pragma once
+
+#include "common.cuh"
+
+namespace treekv {
+
+constexpr int kMaxDraft = 64;  // drafted tokens of a sequence: one 64-bit word of visibility per token
+
+// a draft's tensors as the caller passed them
+struct DraftView {
+    const void* q;          // [B][stride][Hq][d]
+    const void* k;          // [B][stride][Hkv][d]
+    const void* v;
+    const uint64_t* mask;   // [B][stride] bit j: the token sees drafted token j; nullptr: a chain (token i sees 0..i)
+    int stride;
+};
+
+#ifdef __CUDACC__
+__device__ inline uint64_t low_bits(int n) { return n >= 64 ? ~0ull : ((1ull << n) - 1ull); }
+// drafted tokens of sequence b (n of them) that drafted token i sees
+__device__ inline uint64_t draft_sees(const DraftView& dv, int b, int i, int n) {
+    const uint64_t m = dv.mask ? dv.mask[(size_t)b * dv.stride + i] : low_bits(i + 1);
+    return m & low_bits(n);
+}
+// in-cache positions: a drafted token comes behind the cache by as many slots as it has ancestors (the drafted tokens it
+// sees, itself not counted)
+__device__ inline int draft_depth(uint64_t sees) { return max(__popcll(sees) - 1, 0); }
+
+// One key row in fp32, `slot` >= 0: encoded at that slot (see rope_apply).  Piece c of VEC channels and its partner
+// c + half come together: f(channel, value) is called for both.
+template <typename T, int D, typename F>
+__device__ inline void for_key_row(const T* row, const CacheView& cv, int slot, F&& f) {
+    constexpr int VEC = Elem<T>::kVec, HALF = D / 2 / VEC;
+    for (int c = 0; c < HALF; ++c) {
+        float x[VEC], y[VEC];
+        Elem<T>::unpack(ld_plain(row + c * VEC), x);
+        Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
+        if (cv.rope_cos) {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) {
+                const float cs = __ldg(cv.rope_cos + (size_t)slot * (D / 2) + c * VEC + e);
+                const float sn = __ldg(cv.rope_sin + (size_t)slot * (D / 2) + c * VEC + e);
+                const float x1 = x[e], x2 = y[e];
+                x[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
+                y[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
+            }
+        }
+        f(c * VEC, x);
+        f(D / 2 + c * VEC, y);
+    }
+}
+#endif
+
+// draft lengths of a verify call, accepted lengths of an accept call: 0..64
+struct DraftLens {
+    uint8_t n[kMaxBatch];
+};
+
+cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
+                               void* out, float* lse, cudaStream_t stream);
+// S gains what the accepted rows give to every live row; the accepted tokens' rows are appended.  Column sums go to
+// slice 0 of ps.colsum.
+cudaError_t launch_accept_scores(const CacheView& cv, treekv_dtype dt, const PrefillScratch& ps, const DraftView& dv,
+                                 const float* lse, const int32_t* path, int path_stride, const DraftLens& lens, int max_n,
+                                 cudaStream_t stream);
+
+}  // namespace treekv

@@ -1,0 +1,153 @@
+// Sequences of a batch become copies of others, all at once (beam reorder, one prompt for several samples, batch
+// compaction), or are freed.
+//
+// A copy has the geometry of its source, so physical row r of the source goes to physical row r of the copy.  One thread
+// therefore owns a 16-byte piece of row r in every sequence of a component of the copy graph and plays the component's
+// operations in the order the host put them in: a sequence is overwritten after everything that copies from it has read
+// it, and a ring of sequences is cut by one value kept in registers.  No thread reads what another writes: no staging
+// memory, no barrier, every source read once however many copies it has.  Bound by memory traffic.
+#include "common.cuh"
+
+namespace treekv {
+
+namespace {
+
+constexpr int kForkThreads = 256;
+constexpr int kForkUnroll = 4;  // rows of a thread per block
+
+template <int D16, int MAXB>
+__global__ void __launch_bounds__(kForkThreads) fork_kernel(CacheView cv, ForkPlan<MAXB> plan) {
+    constexpr int RPB = kForkThreads / D16;     // rows of a block per unrolled step
+    constexpr int ROWS = RPB * kForkUnroll;     // rows of a block
+    pdl_trigger();
+    pdl_wait();
+    const int kh = blockIdx.y, first = plan.start[blockIdx.z], last = plan.start[blockIdx.z + 1];
+    const int piece = threadIdx.x % D16, r0 = blockIdx.x * ROWS, rt = r0 + threadIdx.x / D16;
+    uint4* K = reinterpret_cast<uint4*>(cv.K);
+    uint4* V = reinterpret_cast<uint4*>(cv.V);
+    auto unit = [&](int b) { return (size_t)(b * cv.Hkv + kh); };
+
+    // ---- K and V
+    uint4 k[kForkUnroll], v[kForkUnroll], ks[kForkUnroll], vs[kForkUnroll];
+    for (int o = first; o < last; ++o) {
+        const int src = plan.src[o], dst = plan.dst[o];
+        if (src == kForkEmpty) continue;
+        const UnitState st = unit_state(plan.seen[o], cv);
+        const int end = st.L + st.i;
+        if (r0 >= end) continue;
+        const bool fresh = src != kForkKept && (o == first || plan.src[o - 1] != src);
+#pragma unroll
+        for (int u = 0; u < kForkUnroll; ++u) {
+            const int r = rt + u * RPB;
+            if (r < st.a || (r >= st.a + st.i && r < end)) {
+                if (fresh) {
+                    const size_t at = (unit(src) * cv.R + r) * D16 + piece;
+                    k[u] = ld_stream(K + at);
+                    v[u] = ld_stream(V + at);
+                }
+            }
+        }
+#pragma unroll
+        for (int u = 0; u < kForkUnroll; ++u) {
+            const int r = rt + u * RPB;
+            if (r < st.a || (r >= st.a + st.i && r < end)) {
+                if (dst == kForkKept) {
+                    ks[u] = k[u]; vs[u] = v[u];
+                } else {
+                    const size_t at = (unit(dst) * cv.R + r) * D16 + piece;
+                    K[at] = src == kForkKept ? ks[u] : k[u];
+                    V[at] = src == kForkKept ? vs[u] : v[u];
+                }
+            }
+        }
+    }
+    // ---- S, stream positions, and the sequence's own counters
+    if (threadIdx.x < ROWS) {
+        const int r = r0 + threadIdx.x;
+        float s = 0.f, s_kept = 0.f;
+        int p = 0, p_kept = 0, w0 = 0, w0_kept = 0;
+        for (int o = first; o < last; ++o) {
+            const int src = plan.src[o], dst = plan.dst[o];
+            const UnitState st = unit_state(plan.seen[o], cv);
+            const bool live = r < st.a || (r >= st.a + st.i && r < st.L + st.i);
+            if (src == kForkKept) { s = s_kept; p = p_kept; w0 = w0_kept; }
+            else if (src != kForkEmpty) {
+                if (live) { s = cv.S[unit(src) * cv.R + r]; p = cv.pos[unit(src) * cv.R + r]; }
+                if (r == 0) w0 = cv.w0[unit(src)];
+            } else w0 = 0;
+            if (dst == kForkKept) { s_kept = s; p_kept = p; w0_kept = w0; continue; }
+            if (live && src != kForkEmpty) { cv.S[unit(dst) * cv.R + r] = s; cv.pos[unit(dst) * cv.R + r] = p; }
+            if (r == 0) { cv.n_seen[unit(dst)] = plan.seen[o]; cv.w0[unit(dst)] = w0; }
+        }
+    }
+}
+
+template <int D16, int MAXB>
+cudaError_t launch_fork_b(const CacheView& cv, const ForkPlanHost& p, cudaStream_t stream) {
+    ForkPlan<MAXB> plan;
+    int rows = 1;
+    for (int o = 0; o < p.n_ops; ++o) {
+        plan.src[o] = p.src[o]; plan.dst[o] = p.dst[o]; plan.seen[o] = p.seen[o];
+        const UnitState st = unit_state(p.seen[o], cv);
+        if (st.L + st.i > rows) rows = st.L + st.i;
+    }
+    for (int c = 0; c <= p.n_comps; ++c) plan.start[c] = p.start[c];
+    constexpr int ROWS = kForkThreads / D16 * kForkUnroll;
+    return launch_pdl(fork_kernel<D16, MAXB>, dim3((rows + ROWS - 1) / ROWS, cv.Hkv, p.n_comps), dim3(kForkThreads), 0, stream, cv, plan);
+}
+
+template <int D16>
+cudaError_t launch_fork_t(const CacheView& cv, const ForkPlanHost& p, cudaStream_t stream) {
+    // the plan travels as a kernel parameter: a small one for the usual batch
+    return p.n_ops <= 64 ? launch_fork_b<D16, 64>(cv, p, stream) : launch_fork_b<D16, kForkMaxOps>(cv, p, stream);
+}
+
+}  // namespace
+
+// The copy graph has an edge from each destination to its source; a component is a tree of copies hanging on a sequence
+// that stays (or is freed), or trees hanging on one ring.  A sequence's copies are written together, deepest sequences
+// first; in a ring the content of one member is kept at the start and its copies are written at the end.
+void make_fork_plan(const int32_t* source, int B, const int64_t* seen, ForkPlanHost& plan) {
+    int16_t comp[kMaxBatch], order[kMaxBatch], child[kMaxBatch], next[kMaxBatch];
+    bool used[kMaxBatch] = {};
+    for (int b = 0; b < B; ++b) { comp[b] = -1; child[b] = -1; }
+    auto copies = [&](int b) { return source[b] >= 0 && source[b] != b; };
+    for (int b = B - 1; b >= 0; --b)
+        if (copies(b)) { next[b] = child[source[b]]; child[source[b]] = (int16_t)b; used[b] = used[source[b]] = true; }
+    plan.n_ops = plan.n_comps = 0;
+    auto put = [&](int src, int dst, int64_t n) {
+        plan.src[plan.n_ops] = (uint16_t)src; plan.dst[plan.n_ops] = (uint16_t)dst; plan.seen[plan.n_ops] = (int32_t)n;
+        ++plan.n_ops;
+    };
+    for (int b0 = 0; b0 < B; ++b0) {
+        if (comp[b0] >= 0 || !(used[b0] || source[b0] < 0)) continue;
+        // the root: where the way up from b0 ends, or a member of the ring that it runs into
+        int root = b0, steps = 0;
+        while (copies(root) && steps <= B) { root = source[root]; ++steps; }
+        const bool ring = copies(root);
+        plan.start[plan.n_comps] = (uint16_t)plan.n_ops;
+        if (ring) put(root, kForkKept, seen[root]);
+        // breadth first from the root (a ring closes at the root, which is already there); copies of later ones go first
+        int n = 0;
+        order[n++] = (int16_t)root; comp[root] = (int16_t)plan.n_comps;
+        for (int x = 0; x < n; ++x)
+            for (int d = child[order[x]]; d >= 0; d = next[d])
+                if (comp[d] < 0) { comp[d] = (int16_t)plan.n_comps; order[n++] = (int16_t)d; }
+        for (int x = n - 1; x >= 0; --x) {
+            const int a = order[x];
+            for (int d = child[a]; d >= 0; d = next[d]) put(ring && a == root ? kForkKept : a, d, seen[a]);
+        }
+        if (source[root] < 0) put(kForkEmpty, root, 0);
+        ++plan.n_comps;
+    }
+    plan.start[plan.n_comps] = (uint16_t)plan.n_ops;
+}
+
+cudaError_t launch_fork(const CacheView& cv, treekv_dtype dt, const ForkPlanHost& p, cudaStream_t stream) {
+    const int pieces = cv.d * (dt == TREEKV_F32 ? 4 : 2) / 16;
+    if (pieces == 8) return launch_fork_t<8>(cv, p, stream);
+    if (pieces == 16) return launch_fork_t<16>(cv, p, stream);
+    return launch_fork_t<32>(cv, p, stream);
+}
+
+}  // namespace treekv

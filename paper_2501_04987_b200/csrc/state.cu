@@ -358,7 +358,7 @@ chunk_update_evict_kernel(CacheView cv, PrefillScratch ps, ChunkLens lens) {
     // ---- score update (Algorithm 1: S <- S + a, summed over the chunk's steps; group mean): tiles added in a
     //      fixed order so the result does not depend on scheduling
     {
-        const int qt = (m * G + kQTileRows - 1) / kQTileRows;
+        const int qt = ps.slices > 0 ? ps.slices : (m * G + kQTileRows - 1) / kQTileRows;
         const float inv_g = 1.0f / (float)G;
         for (int lam = rank * kEvictThreads + threadIdx.x; lam < n; lam += kEvictCluster * kEvictThreads) {
             const float* part = ps.colsum + (size_t)unit * ps.QT * ps.n_max + lam;
