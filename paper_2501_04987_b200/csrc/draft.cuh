@@ -59,6 +59,10 @@ struct DraftLens {
 
 cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
                                void* out, float* lse, cudaStream_t stream);
+// bf16, no in-cache positions; tmK, tmV: maps over the slabs in boxes of the kernel's key tile (make_verify_maps)
+bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV);
+cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,
+                             int max_n, void* out, float* lse, int sms, cudaStream_t stream);
 // S gains what the accepted rows give to every live row; the accepted tokens' rows are appended.  Column sums go to
 // slice 0 of ps.colsum.
 cudaError_t launch_accept_scores(const CacheView& cv, treekv_dtype dt, const PrefillScratch& ps, const DraftView& dv,

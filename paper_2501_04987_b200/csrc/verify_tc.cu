@@ -1,0 +1,457 @@
+// Attention of a tree of drafted tokens over the cache on the 5th-generation tensor cores (bf16).
+//
+// A tile of 128 query rows (row = token * G + head-in-group) of one unit (sequence, KV head) attends to every cached row
+// and to the drafted tokens its mask names, in one pass over key tiles of 64:
+//     S = Q K^T        both from TMA-fed, 128-byte-swizzled shared memory, S in tensor memory (lane = query row)
+//     p = exp2(S c - m)  one thread per row: the running maximum m never leaves the thread
+//     O += P V         P goes back to tensor memory over S, as the matrix operand; O accumulates there
+// The reference m is moved - and O rescaled - only when a row's maximum outgrows it by 2^8: the weights stay within fp32's
+// and bf16's range, their relative precision is the same, and after the first tiles rescaling is rare.
+//
+// Memory bound up to about 128 rows per KV head, so what matters is bytes in flight: a block takes under half an SM's
+// shared memory and half its tensor memory, two run per SM, and each hides the other's exponentials, first loads and
+// epilogue.  When there are fewer units than the machine holds, the keys of a unit are dealt to a cluster of blocks, whose
+// partial results (maximum, sum, O) meet in shared memory, every block joining its share of the rows.
+//
+// The drafted tokens are one key tile.  Their rows come from the caller's tensors through registers (rows behind the draft
+// become zeros; a value that is not finite is taken out of the tile, where a weight of zero would spread it as NaN, and
+// added to the rows that see it at the end).
+//
+// Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
+#include <algorithm>
+
+#include "draft.cuh"
+#include "tma.cuh"
+
+namespace treekv {
+
+namespace {
+
+constexpr int kThreads = 192;
+constexpr int kKeys = 64;                  // keys of a tile
+constexpr int kMaxSplit = 8;
+constexpr int kMaxSlots = 8;
+constexpr uint32_t kTmemCols = 256;        // S 64, S 64, O 128: two blocks share an SM's 512 columns
+constexpr size_t kSmemMin = 80 * 1024;     // never a third block on an SM: it would wait for tensor memory inside a cluster
+constexpr size_t kSmemMax = 112 * 1024;
+constexpr float kSlack = 8.f;              // log2 by which a row's maximum may outgrow its reference
+
+enum Bar { Q_FULL = 0, S_FULL = 1, P_FULL = 3, PV_DONE = 5, FULL = 6, EMPTY = FULL + kMaxSlots, N_BARS = EMPTY + kMaxSlots };
+
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// D[tmem] (+)= A[tmem] * B[smem desc]
+__device__ inline void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
+    asm volatile(
+        "{\n\t.reg .pred p;\n\t"
+        "setp.ne.b32 p, %4, 0;\n\t"
+        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}"
+        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u) : "memory");
+}
+__device__ inline void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
+        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
+          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
+          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
+}
+__device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
+
+// A block's key tiles: cached rows in two segments (rows = index below the split point a, index + i behind it), then the
+// drafted tokens as the last tile of the unit.  The block that owns that one takes it first.
+struct Tiles {
+    int a, i, L, nA, nB, t0, count;
+    bool draft;  // this block's tile 0 is the drafted one
+};
+__device__ inline Tiles my_tiles(const UnitState& st, int rank, int split) {
+    Tiles t;
+    t.a = min(st.a, st.L); t.i = st.i; t.L = st.L;
+    t.nA = (t.a + kKeys - 1) / kKeys;
+    t.nB = (st.L - t.a + kKeys - 1) / kKeys;
+    const int all = t.nA + t.nB + 1, per = (all + split - 1) / split;
+    t.t0 = min(rank * per, all);
+    t.count = min(per, all - t.t0);
+    t.draft = t.count > 0 && t.t0 + t.count == all;
+    return t;
+}
+// cached tile j of the block: first slab row and rows that exist
+__device__ inline void cached_tile(const Tiles& t, int j, int& row0, int& valid) {
+    const int x = t.t0 + j - (t.draft ? 1 : 0);
+    if (x < t.nA) { row0 = x * kKeys; valid = min(kKeys, t.a - row0); }
+    else { const int lam = t.a + (x - t.nA) * kKeys; row0 = lam + t.i; valid = min(kKeys, t.L - lam); }
+}
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2)
+verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                 CacheView cv, DraftView dv, DraftLens lens, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
+                 int q_rows, int q_bytes, int slots, int split) {
+    constexpr int HALVES = D / 64, SLOT = kKeys * D * 2, VHALF = kKeys * 128, PITCH = D + 4;
+    const int unit = blockIdx.z, b = unit / cv.Hkv, kh = unit % cv.Hkv, rank = blockIdx.x;
+    const int G = cv.Hq / cv.Hkv, n = lens.n[b], r0 = blockIdx.y * 128, rows = min(128, n * G - r0);
+    pdl_trigger();
+    if (rows <= 0) { pdl_wait(); return; }  // the whole cluster
+
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[N_BARS];
+    __shared__ uint32_t tmem_slot;
+    __shared__ uint32_t s_bad[2];       // drafted tokens with a value that is not finite (this block staged them)
+    __shared__ __align__(8) float s_bad_all[2];  // the same, from the block that did
+    const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char* base_ptr = smem_raw + (base - smem_addr_u32(smem_raw));
+    const uint32_t sQ = base, sRing = base + HALVES * q_rows * 128;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bar0 = smem_addr_u32(&bars[0]);
+    auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
+
+    if (tid == 0) {
+        mbar_init(bar(Q_FULL), 1); mbar_init(bar(PV_DONE), 1);
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(S_FULL + s), 1); mbar_init(bar(P_FULL + s), 4); }
+        for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
+        s_bad[0] = s_bad[1] = 0u;
+        mbar_fence_init();
+    }
+    if (warp == 1) { tmem_alloc(smem_addr_u32(&tmem_slot), kTmemCols); tmem_relinquish(); }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tmO = tmem + 128;  // S / P of tile j at column 64 (j & 1)
+    pdl_wait();
+    const UnitState st = unit_state(cv.n_seen[unit], cv);
+    const Tiles t = my_tiles(st, rank, split);
+    const int NT = t.count;
+
+    bool ok = true;
+    float m_ref = -INFINITY, l_run = 0.f;
+    if (warp == 0) {
+        // ================= TMA producer: K_j in ring load 2j, V_j in ring load 2j + 1
+        if (lane == 0 && NT > 0) {
+            mbar_arrive_expect_tx(bar(Q_FULL), q_bytes);
+            for (int h = 0; h < HALVES; ++h)
+                tma_load_3d(sQ + h * q_rows * 128, &tmQ, 64 * h, kh * G, b * dv.stride + r0 / G, bar(Q_FULL));
+            int issued = 0;
+            for (int x = t.draft ? 2 : 0; x < 2 * NT; ++x) {
+                const int slot = x % slots;
+                if (!mbar_wait(bar(EMPTY + slot), ((x / slots) & 1) ^ 1)) { ok = false; break; }
+                int row0, valid;
+                cached_tile(t, x >> 1, row0, valid);
+                const int grow = unit * cv.R + row0;
+                const uint32_t dst = sRing + slot * SLOT;
+                mbar_arrive_expect_tx(bar(FULL + slot), SLOT);
+                const CUtensorMap* map = x & 1 ? &tmV : &tmK;
+                for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * VHALF, map, 64 * h, grow, bar(FULL + slot));
+                issued = x + 1;
+            }
+            // nothing may still be on its way into this block's memory when it ends, whatever gave up
+            ok = mbar_wait(bar(Q_FULL), 0) && ok;
+            for (int x = max(t.draft ? 2 : 0, issued - slots); x < issued; ++x) ok = mbar_wait(bar(FULL + x % slots), (x / slots) & 1) && ok;
+            if (!ok) atomicOr(&cv.stats->error, 4u);
+        }
+    } else if (warp == 1) {
+        // ================= MMA issuer
+        if (lane == 0 && NT > 0) {
+            constexpr uint32_t idesc_s = umma_idesc_bf16(128, kKeys, 0, 0);  // both operands K-major (rows x channels)
+            constexpr uint32_t idesc_o = umma_idesc_bf16(128, D, 0, 1);      // P from tensor memory, V MN-major
+            auto issue_s = [&](int j) {
+                const int x = 2 * j, slot = x % slots;
+                if (!(ok = ok && mbar_wait(bar(FULL + slot), (x / slots) & 1))) return;
+                tc_fence_after();
+                const uint32_t sK = sRing + slot * SLOT;
+#pragma unroll
+                for (int kk = 0; kk < D / 16; ++kk)
+                    umma_bf16(tmem + 64 * (j & 1), umma_desc_sw128(sQ + (kk >> 2) * q_rows * 128 + (kk & 3) * 32, 16, 1024),
+                              umma_desc_sw128(sK + (kk >> 2) * VHALF + (kk & 3) * 32, 16, 1024), idesc_s, kk > 0);
+                umma_commit(bar(EMPTY + slot));
+                umma_commit(bar(S_FULL + (j & 1)));
+            };
+            ok = mbar_wait(bar(Q_FULL), 0);
+            for (int j = 0; j < 2 && j < NT; ++j) issue_s(j);
+            for (int j = 0; j < NT && ok; ++j) {
+                const int x = 2 * j + 1, slot = x % slots;
+                ok = mbar_wait(bar(P_FULL + (j & 1)), (j >> 1) & 1) && mbar_wait(bar(FULL + slot), (x / slots) & 1);
+                if (!ok) break;
+                tc_fence_after();
+                const uint32_t sV = sRing + slot * SLOT;
+#pragma unroll
+                for (int kk = 0; kk < kKeys / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes, 8 columns of packed P
+                    umma_bf16_ta(tmO, tmem + 64 * (j & 1) + 8 * kk, umma_desc_sw128(sV + kk * 2048, VHALF, 1024), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+                umma_commit(bar(EMPTY + slot));
+                umma_commit(bar(PV_DONE));
+                if (j + 2 < NT) {  // S_{j+2} overwrites P_j
+                    if (!(ok = mbar_wait(bar(PV_DONE), j & 1))) break;
+                    issue_s(j + 2);
+                }
+            }
+            // every MMA of this block has finished before its memory and tensor memory are given to anything else
+            if (ok) ok = mbar_wait(bar(PV_DONE), (NT - 1) & 1);
+            if (!ok) atomicOr(&cv.stats->error, 8u);
+        }
+    } else {
+        // ================= softmax warps
+        const int quarter = warp & 3, row = quarter * 32 + lane, st_tid = tid - 64;
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+        const float sc2 = kLog2e * rsqrtf((float)D);
+        const bool live = quarter * 32 < rows;  // of the warp
+        uint64_t sees = 0ull;
+        if (t.draft) {
+            if (row < rows) sees = draft_sees(dv, b, (r0 + row) / G, n);
+            // the drafted tokens' K and V into ring loads 0 and 1
+            const uint4* ks = reinterpret_cast<const uint4*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * (D / 8);
+            const uint4* vs = reinterpret_cast<const uint4*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * (D / 8);
+            unsigned char* ring = base_ptr + HALVES * q_rows * 128;
+            for (int e = st_tid; e < kKeys * (D / 8); e += 128) {
+                const int r = e / (D / 8), c = e % (D / 8);
+                uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
+                if (r < n) {
+                    kx = ks[(size_t)r * cv.Hkv * (D / 8) + c];
+                    vx = vs[(size_t)r * cv.Hkv * (D / 8) + c];
+                    uint32_t* w = &vx.x;
+#pragma unroll
+                    for (int u = 0; u < 4; ++u) {
+                        const uint32_t lo = (w[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                        if (lo | hi) { w[u] &= ~(lo | hi); atomicOr(&s_bad[r >> 5], 1u << (r & 31)); }
+                    }
+                }
+                const int off = (c >> 3) * VHALF + r * 128 + (((c & 7) ^ (r & 7)) << 4);
+                *reinterpret_cast<uint4*>(ring + off) = kx;
+                *reinterpret_cast<uint4*>(ring + SLOT + off) = vx;
+            }
+            fence_proxy_async_smem();
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (st_tid == 0) { mbar_arrive(bar(FULL)); mbar_arrive(bar(FULL + 1)); }
+        }
+        for (int j = 0; j < NT && ok; ++j) {
+            const uint32_t tmS = tmem + 64 * (j & 1) + lane_off;
+            const bool draft = t.draft && j == 0;
+            int row0 = 0, valid = kKeys;
+            if (!draft) cached_tile(t, j, row0, valid);
+            if (!mbar_wait(bar(S_FULL + (j & 1)), (j >> 1) & 1)) { ok = false; break; }
+            tc_fence_after();
+            if (live) {
+                uint32_t s0[32], s1[32];
+                tmem_ld32(tmS, s0);
+                tmem_ld32(tmS + 32, s1);
+                tmem_ld_wait_for(s0);
+                tmem_ld_wait_for(s1);
+                if (draft || valid < kKeys) {
+                    const uint64_t see = draft ? sees : low_bits(valid);
+                    const uint32_t see0 = (uint32_t)see, see1 = (uint32_t)(see >> 32);
+#pragma unroll
+                    for (int e = 0; e < 32; ++e) {
+                        if (!(see0 >> e & 1u)) s0[e] = 0xff800000u;
+                        if (!(see1 >> e & 1u)) s1[e] = 0xff800000u;
+                    }
+                }
+                float mx0 = __uint_as_float(s0[0]), mx1 = __uint_as_float(s1[0]);
+#pragma unroll
+                for (int e = 1; e < 32; ++e) { mx0 = fmaxf(mx0, __uint_as_float(s0[e])); mx1 = fmaxf(mx1, __uint_as_float(s1[e])); }
+                const float mx = fmaxf(mx0, mx1) * sc2;
+                const bool grow = mx > m_ref + kSlack;  // also from minus infinity to anything
+                if (__any_sync(0xffffffffu, grow)) {
+                    const float f = grow ? ex2(m_ref - mx) : 1.f;
+                    if (grow) { m_ref = mx; l_run *= f; }
+                    if (j > 0) {
+                        if (!mbar_wait(bar(PV_DONE), (j - 1) & 1)) ok = false;
+                        tc_fence_after();
+#pragma unroll
+                        for (int cg = 0; cg < D / 32; ++cg) {
+                            uint32_t o[32];
+                            tmem_ld32(tmO + lane_off + cg * 32, o);
+                            tmem_ld_wait_for(o);
+#pragma unroll
+                            for (int e = 0; e < 32; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * f);
+                            tmem_st32(tmO + lane_off + cg * 32, o);
+                        }
+                    }
+                }
+                const float mr = m_ref == -INFINITY ? 0.f : m_ref;
+                float sum0 = 0.f, sum1 = 0.f;
+                uint32_t p[32];
+#pragma unroll
+                for (int e = 0; e < 16; ++e) {
+                    const float a = ex2(fmaf(__uint_as_float(s0[2 * e]), sc2, -mr)), c = ex2(fmaf(__uint_as_float(s0[2 * e + 1]), sc2, -mr));
+                    const float g = ex2(fmaf(__uint_as_float(s1[2 * e]), sc2, -mr)), h = ex2(fmaf(__uint_as_float(s1[2 * e + 1]), sc2, -mr));
+                    sum0 += a + c; sum1 += g + h;
+                    p[e] = rope_pack_bf16(a, c); p[16 + e] = rope_pack_bf16(g, h);
+                }
+                l_run += sum0 + sum1;
+                tmem_st32(tmS, p);
+                tmem_st_wait();
+            }
+            if (!draft && valid < kKeys) {
+                // rows of the slab that hold no token of this unit may hold anything: their weight is zero, their values
+                // must not be NaN
+                const int x = 2 * j + 1, slot = x % slots;
+                if (!mbar_wait(bar(FULL + slot), (x / slots) & 1)) { ok = false; break; }
+                unsigned char* v = base_ptr + HALVES * q_rows * 128 + slot * SLOT;
+                for (int e = st_tid; e < (kKeys - valid) * (D / 8); e += 128) {
+                    const int r = valid + e / (D / 8), c = e % (D / 8);
+                    *reinterpret_cast<uint4*>(v + (c >> 3) * VHALF + r * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+                }
+                fence_proxy_async_smem();
+            }
+            tc_fence_before();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(P_FULL + (j & 1)));
+        }
+        if (ok && NT > 0) ok = mbar_wait(bar(PV_DONE), (NT - 1) & 1);
+        if (!ok && lane == 0) atomicOr(&cv.stats->error, 16u);
+        tc_fence_after();
+    }
+    __syncwarp();
+
+    // ---- the cluster's partial results meet: a block joins rpo rows, and gets from every block m, l and O of those rows
+    const int rpo = (rows + split - 1) / split;
+    const uint32_t sPart = base, sStat = base + split * rpo * PITCH * 4;  // [split][rpo][PITCH], [split][rpo][2]
+    if (split > 1) cluster_sync_all(); else __syncthreads();              // (1) every block's tiles are consumed
+    if (warp >= 2) {
+        const int quarter = warp & 3, row = quarter * 32 + lane;
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+        if (quarter * 32 < rows) {
+            const int owner = row / rpo, at = rank * rpo + row % rpo;
+            const uint32_t dst = map_to_cta(sPart, min(owner, split - 1)) + at * PITCH * 4;
+#pragma unroll
+            for (int cg = 0; cg < D / 32; ++cg) {
+                uint32_t o[32];
+                if (NT > 0) { tmem_ld32(tmO + lane_off + cg * 32, o); tmem_ld_wait_for(o); }
+                if (row < rows) {
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const bool z = NT == 0;
+                        st_remote_v4(dst + (cg * 32 + e) * 4, z ? 0.f : __uint_as_float(o[e]), z ? 0.f : __uint_as_float(o[e + 1]),
+                                     z ? 0.f : __uint_as_float(o[e + 2]), z ? 0.f : __uint_as_float(o[e + 3]));
+                    }
+                }
+            }
+            if (row < rows) st_remote_v2(map_to_cta(sStat, min(owner, split - 1)) + at * 8, m_ref, l_run);
+        }
+        if (t.draft && tid - 64 < split)
+            st_remote_v2(map_to_cta(smem_addr_u32(s_bad_all), tid - 64), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
+    }
+    __syncwarp();
+    if (split > 1) cluster_sync_all(); else __syncthreads();  // (2) all parts have arrived
+    {
+        const float* part = reinterpret_cast<const float*>(base_ptr);
+        const float* stat = part + split * rpo * PITCH;
+        const uint64_t bad = (uint64_t)__float_as_uint(s_bad_all[0]) | (uint64_t)__float_as_uint(s_bad_all[1]) << 32;
+        constexpr int LPR = D / 8;  // threads per row, eight channels each
+        for (int e = tid; e < rpo * LPR; e += kThreads) {
+            const int rl = e / LPR, c = e % LPR, row = rank * rpo + rl;
+            if (row >= rows) continue;
+            float M = -INFINITY;
+            for (int s = 0; s < split; ++s) M = fmaxf(M, stat[(s * rpo + rl) * 2]);
+            float l = 0.f, o[8];
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] = 0.f;
+            for (int s = 0; s < split; ++s) {
+                const float ms = stat[(s * rpo + rl) * 2];
+                const float f = ms == -INFINITY ? 0.f : ex2(ms - M);
+                l += stat[(s * rpo + rl) * 2 + 1] * f;
+                const float4 x = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8);
+                const float4 y = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8 + 4);
+                o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
+                o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+            }
+            const float inv = l == 0.f ? 0.f : 1.0f / l;  // l = 0: the row sees nothing
+            const int tok = (r0 + row) / G, h = (r0 + row) % G;
+#pragma unroll
+            for (int u = 0; u < 8; ++u) o[u] *= inv;
+            if (bad) {
+                for (uint64_t left = bad & draft_sees(dv, b, tok, n); left; left &= left - 1) {
+                    const int d = __ffsll((long long)left) - 1;
+                    const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(dv.v) + (((size_t)b * dv.stride + d) * cv.Hkv + kh) * D + c * 8;
+#pragma unroll
+                    for (int u = 0; u < 8; ++u) {
+                        const float x = __bfloat162float(vr[u]);
+                        if (!(fabsf(x) < INFINITY)) o[u] += x;
+                    }
+                }
+            }
+            const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
+            *reinterpret_cast<uint4*>(out + at * D + c * 8) =
+                make_uint4(rope_pack_bf16(o[0], o[1]), rope_pack_bf16(o[2], o[3]), rope_pack_bf16(o[4], o[5]), rope_pack_bf16(o[6], o[7]));
+            if (lse && c == 0) lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * (1.0f / kLog2e);
+        }
+    }
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
+}
+
+// Blocks of a cluster (key splits): the machine holds two blocks per SM; a split costs every block its start and end,
+// worth about four tiles, once more.
+int pick_split(long blocks, int tiles, int sms) {
+    int best = 1;
+    long least = -1;
+    for (int s = 1; s <= kMaxSplit; s *= 2) {
+        const long waves = (blocks * s + 2L * sms - 1) / (2L * sms), cost = waves * ((tiles + s - 1) / s + 4);
+        if (least < 0 || cost < least) { least = cost; best = s; }
+    }
+    return best;
+}
+
+template <int D>
+cudaError_t launch_t(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens, int max_n,
+                     void* out, float* lse, int sms, cudaStream_t stream) {
+    const int G = cv.Hq / cv.Hkv, box = std::min(128 / G, dv.stride);
+    CUtensorMap tmQ;
+    const uint64_t dims[3] = {(uint64_t)D, (uint64_t)cv.Hq, (uint64_t)cv.B * dv.stride};
+    const uint64_t strides[2] = {(uint64_t)D * 2, (uint64_t)cv.Hq * D * 2};
+    const uint32_t boxes[3] = {64u, (uint32_t)G, (uint32_t)box};
+    if (!make_tensor_map_bf16(&tmQ, dv.q, 3, dims, strides, boxes)) return cudaErrorInvalidValue;
+    const int q_rows = box * G <= 32 ? 32 : box * G <= 64 ? 64 : 128;
+    const size_t q_area = (size_t)(D / 64) * q_rows * 128, slot = (size_t)kKeys * D * 2;
+    const int slots = (int)std::min<size_t>(kMaxSlots, (kSmemMax - 1024 - q_area) / slot);
+    // The queries' matrix operand is read as 128 rows.  With fewer loaded the others are what lies behind them in the ring:
+    // such a row has a lane of its own, which nobody looks at.
+    const size_t smem = std::max(kSmemMin, 1024 + q_area + slots * slot);
+    auto kern = verify_tc_kernel<D>;
+    static bool smem_set[64] = {};  // per device: the opt-in is needed once
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    if (!smem_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
+        if (e != cudaSuccess) return e;
+        smem_set[dev] = true;
+    }
+    const int tiles_r = (max_n * G + 127) / 128;
+    const int split = pick_split((long)cv.B * cv.Hkv * tiles_r, (cv.c + kKeys - 1) / kKeys + 2, sms);
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(split, tiles_r, cv.B * cv.Hkv);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, tmQ, tmK, tmV, cv, dv, lens, reinterpret_cast<__nv_bfloat16*>(out), lse, q_rows,
+                              (D / 64) * box * G * 128, slots, split);
+}
+
+}  // namespace
+
+bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV) {
+    const uint64_t dims[2] = {(uint64_t)cv.d, (uint64_t)cv.B * cv.Hkv * cv.R};
+    const uint64_t strides[1] = {(uint64_t)cv.d * 2};
+    const uint32_t box[2] = {64u, (uint32_t)kKeys};
+    return make_tensor_map_bf16(tmK, cv.K, 2, dims, strides, box) && make_tensor_map_bf16(tmV, cv.V, 2, dims, strides, box);
+}
+
+cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,
+                             int max_n, void* out, float* lse, int sms, cudaStream_t stream) {
+    return cv.d == 64 ? launch_t<64>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream)
+                      : launch_t<128>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream);
+}
+
+}  // namespace treekv
