@@ -1,116 +1,339 @@
-// The accepted path of a draft enters the cache: the part in front of the evictions.  The path's tokens are appended as a
-// chunk of prefill would append them, and every live row's score gains the attention it received from them:
-// S_j += mean over the group of sum over the path's rows of exp(q k_j / sqrt d - lse), with the log-sum-exp that the
-// tree's attention left for each row (a row of the path saw the cache and the path up to itself, so no second softmax
-// pass and no values are needed: keys are read once).
+// The accepted path of a draft enters the cache, one launch: the path's tokens are appended as a chunk of prefill would
+// append them, every live row's score gains the attention it received from them, and Algorithm 1's evictions follow.
+//     S_j += mean over the group of sum over the path's rows of exp(q k_j / sqrt d - lse)
+// with the log-sum-exp that the tree's attention left for each row (a row of the path saw the cache and the path up to
+// itself): no second softmax pass and no values are needed, so the keys are read once and that is what bounds it.
+//
+// A cluster of blocks owns a unit (sequence, KV head).  bf16: a warp takes 16 keys at a time as the rows of mma.m16n8k16,
+// the path's queries, 8 at a time, as its columns.  The contraction runs over channels in any order, so a lane loads its
+// key fragments straight from memory as 16-byte pieces (channels 32u + 8t.. of rows g and g + 8) and the queries' the same
+// way from shared memory: no transposition, no shared-memory pass of the keys, and the next 16 keys are on their way
+// while these are used.  fp32: a thread per key, queries broadcast from shared memory.
+#include <cooperative_groups.h>
+
 #include "draft.cuh"
+#include "evict.cuh"
 
 namespace treekv {
 
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kRows = 8;      // rows of a pass over a thread's key
+constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kStage32 = 32;  // fp32: query rows in shared memory at a time
 
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
+// D(16x8, f32) += A(16x16, bf16, row) * B(16x8, bf16, col)
+__device__ inline void mma_bf16(float (&d)[4], uint32_t a0, uint32_t a1, uint32_t a2, uint32_t a3, uint32_t b0, uint32_t b1) {
+    asm volatile("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, {%8,%9}, {%0,%1,%2,%3};"
+                 : "+f"(d[0]), "+f"(d[1]), "+f"(d[2]), "+f"(d[3])
+                 : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
+}
+
+// What the blocks of a unit share: where its rows are and which drafted tokens are on the path.
+struct Path {
+    UnitState st;
+    int unit, b, kh, n, G, N, total;
+    const int* node;  // [n] in shared memory
+};
+
+// key row of live index lam (0 <= lam < total): cached, or the path's token lam - L as the caller passed it
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
-accept_scores_kernel(CacheView cv, PrefillScratch ps, DraftView dv, const float* __restrict__ lse, const int32_t* __restrict__ path,
-                     int path_stride, DraftLens lens) {
-    constexpr int VEC = Elem<T>::kVec;
+__device__ inline const T* key_row(const CacheView& cv, const DraftView& dv, const Path& p, int lam) {
+    if (lam < p.st.L) return reinterpret_cast<const T*>(cv.K) + ((size_t)p.unit * cv.R + phys_row(lam, p.st)) * D;
+    return reinterpret_cast<const T*>(dv.k) + (((size_t)p.b * dv.stride + p.node[lam - p.st.L]) * cv.Hkv + p.kh) * D;
+}
+template <typename T, int D>
+__device__ inline size_t draft_row(const CacheView& cv, const DraftView& dv, const Path& p, int j) {
+    return (((size_t)p.b * dv.stride + p.node[j]) * cv.Hkv + p.kh) * D;
+}
+
+// query row pitch in shared memory, bytes: rows g and g + 1 half the banks apart, so that eight lanes' 16-byte reads (two
+// rows, four pieces) meet no conflict
+template <int D> constexpr int q_pitch() { return D * 2 + 64; }
+
+template <int D, bool ROPE>
+__device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, const Path& p, const float* __restrict__ lse, int rank, int nblocks,
+                                   unsigned char* smem, int rows8) {
+    using T = __nv_bfloat16;
+    constexpr int NU = D / 32, PITCH = q_pitch<D>();
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
+    const int rows = p.n * p.G, tiles_r = (rows + 7) / 8, lg = __ffs(p.G) - 1;
+    float* s_lse = reinterpret_cast<float*>(smem + (size_t)rows8 * PITCH);
+    const float scale = kLog2e * rsqrtf((float)D);
+    const int ntiles = (p.total + 15) / 16, step = nblocks * kWarps;
+
+    uint4 kf[2][NU], kn[2][NU];
+    float s_old = 0.f, s_next = 0.f;
+    auto fetch = [&](int tile) {  // keys g and g + 8 of the tile; lane t = 0 / 1 also their scores
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+            const int lam = tile * 16 + g + 8 * h;
+            if (lam < p.total) {
+                const T* row = key_row<T, D>(cv, dv, p, lam);
+#pragma unroll
+                for (int u = 0; u < NU; ++u) kn[h][u] = ld_stream(row + 32 * u + 8 * t);
+                if (t == h) s_next = lam < p.st.L ? cv.S[(size_t)p.unit * cv.R + phys_row(lam, p.st)] : 0.f;
+            } else {
+#pragma unroll
+                for (int u = 0; u < NU; ++u) kn[h][u] = make_uint4(0, 0, 0, 0);
+            }
+        }
+    };
+    const int first = rank * kWarps + warp;
+    if (first < ntiles) fetch(first);
+
+    // ---- the path's queries (encoded at their slots with in-cache positions) and their log-sum-exps
+    for (int e = tid; e < tiles_r * 8 * (D / 16); e += kThreads) {
+        const int r = e / (D / 16), c = e % (D / 16);
+        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
+        if (r < rows) {
+            const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
+            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(dv.q) + at * D);
+            lo = src[c]; hi = src[c + D / 16];
+            if (ROPE) rope_piece_pair(lo, hi, cv.rope_cos + (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 8, cv.rope_sin + (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 8);
+            if (c == 0) s_lse[r] = lse[at] * kLog2e;
+        } else if (c == 0) {
+            s_lse[r] = INFINITY;  // weight 0
+        }
+        *reinterpret_cast<uint4*>(smem + r * PITCH + c * 16) = lo;
+        *reinterpret_cast<uint4*>(smem + r * PITCH + (c + D / 16) * 16) = hi;
+    }
+    __syncthreads();
+
+    for (int tile = first; tile < ntiles; tile += step) {
+#pragma unroll
+        for (int h = 0; h < 2; ++h)
+#pragma unroll
+            for (int u = 0; u < NU; ++u) kf[h][u] = kn[h][u];
+        s_old = s_next;
+        if (tile + step < ntiles) fetch(tile + step);
+        const int lam0 = tile * 16;
+        const bool has_new = lam0 + 16 > p.st.L;
+        if (has_new) {  // append: the lane's pieces of the key row, as they came
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int j = lam0 + g + 8 * h - p.st.L;
+                if (j >= 0 && j < p.n) {
+                    const size_t row = ((size_t)p.unit * cv.R + p.st.L + p.st.i + j) * D;
+                    const T* v = reinterpret_cast<const T*>(dv.v) + draft_row<T, D>(cv, dv, p, j);
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) {
+                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(cv.K) + row + 32 * u + 8 * t) = kf[h][u];
+                        *reinterpret_cast<uint4*>(reinterpret_cast<T*>(cv.V) + row + 32 * u + 8 * t) = ld_plain(v + 32 * u + 8 * t);
+                    }
+                }
+            }
+        }
+        if (ROPE) {  // the key of live index lam is encoded at slot lam; a channel's partner is this lane's too
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const int slot = min(lam0 + g + 8 * h, p.total - 1);
+#pragma unroll
+                for (int u = 0; u < NU / 2; ++u)
+                    rope_piece_pair(kf[h][u], kf[h][u + NU / 2], cv.rope_cos + (size_t)slot * (D / 2) + 32 * u + 8 * t,
+                                    cv.rope_sin + (size_t)slot * (D / 2) + 32 * u + 8 * t);
+            }
+        }
+        float sum0 = 0.f, sum1 = 0.f;  // keys g, g + 8; this lane's rows
+        const int j0 = lam0 + g - p.st.L;
+        for (int rt = 0; rt < tiles_r; ++rt) {
+            float c[4] = {0.f, 0.f, 0.f, 0.f};
+            const unsigned char* qrow = smem + (rt * 8 + g) * PITCH + t * 16;
+#pragma unroll
+            for (int u = 0; u < NU; ++u) {
+                const uint4 q = *reinterpret_cast<const uint4*>(qrow + u * 64);
+                mma_bf16(c, kf[0][u].x, kf[1][u].x, kf[0][u].y, kf[1][u].y, q.x, q.y);
+                mma_bf16(c, kf[0][u].z, kf[1][u].z, kf[0][u].w, kf[1][u].w, q.z, q.w);
+            }
+            const float2 ls = *reinterpret_cast<const float2*>(s_lse + rt * 8 + 2 * t);
+            float p0 = ex2(fmaf(c[0], scale, -ls.x)), p1 = ex2(fmaf(c[1], scale, -ls.y));
+            float p2 = ex2(fmaf(c[2], scale, -ls.x)), p3 = ex2(fmaf(c[3], scale, -ls.y));
+            if (has_new) {  // a path token is seen from itself on
+                const int ra = (rt * 8 + 2 * t) >> lg, rb = (rt * 8 + 2 * t + 1) >> lg;
+                if (ra < j0) p0 = 0.f;
+                if (rb < j0) p1 = 0.f;
+                if (ra < j0 + 8) p2 = 0.f;
+                if (rb < j0 + 8) p3 = 0.f;
+            }
+            sum0 += p0 + p1; sum1 += p2 + p3;
+        }
+        sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
+        sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
+        if (t < 2) {
+            const int lam = lam0 + g + 8 * t;
+            if (lam < p.total) {
+                const size_t row = (size_t)p.unit * cv.R + (lam < p.st.L ? phys_row(lam, p.st) : lam + p.st.i);
+                cv.S[row] = s_old + (t ? sum1 : sum0) * (1.0f / (float)p.G);
+                if (lam >= p.st.L) cv.pos[row] = p.N + lam - p.st.L;
+            }
+        }
+    }
+}
+
+template <int D>
+__device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, const Path& p, const float* __restrict__ lse, int rank, int nblocks,
+                                  unsigned char* smem) {
+    float* sq = reinterpret_cast<float*>(smem);  // [kStage32][D]
+    float* s_lse = sq + kStage32 * D;
+    const int rows = p.n * p.G, tid = threadIdx.x, lg = __ffs(p.G) - 1;
+    const float scale = kLog2e * rsqrtf((float)D);
+    for (int base = rank * kThreads; base < p.total; base += nblocks * kThreads) {
+        const int lam = base + tid, j = lam - p.st.L;
+        const float* krow = lam < p.total ? key_row<float, D>(cv, dv, p, lam) : nullptr;
+        float sum = 0.f;
+        for (int r0 = 0; r0 < rows; r0 += kStage32) {
+            __syncthreads();
+            for (int e = tid; e < kStage32 * (D / 2); e += kThreads) {  // queries: encoded at their slots, scaled
+                const int r = r0 + e / (D / 2), c = e % (D / 2);
+                float x = 0.f, y = 0.f;
+                if (r < rows) {
+                    const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
+                    const float* row = reinterpret_cast<const float*>(dv.q) + at * D;
+                    x = row[c]; y = row[c + D / 2];
+                    if (cv.rope_cos) {
+                        const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c;
+                        const float cs = __ldg(cv.rope_cos + tab), sn = __ldg(cv.rope_sin + tab), x1 = x, x2 = y;
+                        x = __fmaf_rn(x1, cs, -__fmul_rn(x2, sn));
+                        y = __fmaf_rn(x2, cs, __fmul_rn(x1, sn));
+                    }
+                    if (c == 0) s_lse[r - r0] = lse[at] * kLog2e;
+                }
+                sq[(r - r0) * D + c] = x * scale; sq[(r - r0) * D + c + D / 2] = y * scale;
+            }
+            __syncthreads();
+            if (lam < p.total) {
+                for (int r8 = 0; r8 < kStage32 && r0 + r8 < rows; r8 += 8) {
+                    float a[8];
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) a[r] = 0.f;
+                    for_key_row<float, D>(krow, cv, lam, [&](int c, const float (&x)[4]) {
+#pragma unroll
+                        for (int r = 0; r < 8; ++r) {
+                            const float4 q4 = *reinterpret_cast<const float4*>(sq + (r8 + r) * D + c);
+                            a[r] = fmaf(q4.x, x[0], fmaf(q4.y, x[1], fmaf(q4.z, x[2], fmaf(q4.w, x[3], a[r]))));
+                        }
+                    });
+#pragma unroll
+                    for (int r = 0; r < 8; ++r)
+                        if (r0 + r8 + r < rows && ((r0 + r8 + r) >> lg) >= j) sum += exp2f(a[r] - s_lse[r8 + r]);
+                }
+            }
+        }
+        if (lam < p.total) {
+            const size_t row = (size_t)p.unit * cv.R + (j < 0 ? phys_row(lam, p.st) : lam + p.st.i);
+            cv.S[row] = (j < 0 ? cv.S[row] : 0.f) + sum * (1.0f / (float)p.G);
+            if (j >= 0) {  // append
+                const uint4* ks = reinterpret_cast<const uint4*>(krow);
+                const uint4* vs = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(dv.v) + draft_row<float, D>(cv, dv, p, j));
+                for (int e = 0; e < D / 4; ++e) {
+                    reinterpret_cast<uint4*>(cv.K)[row * (D / 4) + e] = ks[e];
+                    reinterpret_cast<uint4*>(cv.V)[row * (D / 4) + e] = vs[e];
+                }
+                cv.pos[row] = p.N + j;
+            }
+        }
+    }
+}
+
+template <typename T, int D, int CL, bool ROPE>
+__global__ void __launch_bounds__(kThreads, 2)
+accept_kernel(CacheView cv, DraftView dv, const float* __restrict__ lse, const int32_t* __restrict__ path, int path_stride, DraftLens lens,
+              int rows8) {
+    namespace cg = cooperative_groups;
+    extern __shared__ __align__(16) unsigned char smem[];
+    __shared__ int s_node[kMaxDraft];
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.y, b = unit / cv.Hkv, kh = unit % cv.Hkv;
-    const int n = lens.n[b], G = cv.Hq / cv.Hkv;
-    if (n == 0) return;
-    const int N = cv.n_seen[unit];
-    const UnitState st = unit_state(N, cv);
-    const int total = st.L + n, lam = blockIdx.x * kThreads + threadIdx.x;
-    if (blockIdx.x * kThreads >= total) return;
-    __shared__ __align__(16) float sq[kRows][D];
-    __shared__ float s_lse[kRows];
-    __shared__ int s_node[kMaxDraft];
-    const float scale = kLog2e * rsqrtf((float)D);
-    if (threadIdx.x < n) {
-        int node = path[(size_t)b * path_stride + threadIdx.x];
+    cg::cluster_group cluster = cg::this_cluster();
+    const int rank = CL == 1 ? 0 : (int)cluster.block_rank();
+    Path p;
+    p.unit = blockIdx.y; p.b = p.unit / cv.Hkv; p.kh = p.unit % cv.Hkv; p.G = cv.Hq / cv.Hkv; p.n = lens.n[p.b];
+    if (p.n == 0) return;  // the whole cluster shares the unit
+    p.N = cv.n_seen[p.unit];
+    p.st = unit_state(p.N, cv);
+    p.total = p.st.L + p.n;
+    p.node = s_node;
+    if (threadIdx.x < p.n) {
+        int node = path[(size_t)p.b * path_stride + threadIdx.x];
         if (node < 0 || node >= dv.stride) { node = 0; atomicOr(&cv.stats->error, kErrBadIndex); }
         s_node[threadIdx.x] = node;
     }
     __syncthreads();
-    const int j = lam - st.L;
-    const T* krow = nullptr;
-    if (lam < st.L) krow = reinterpret_cast<const T*>(cv.K) + ((size_t)unit * cv.R + phys_row(lam, st)) * D;
-    else if (lam < total) krow = reinterpret_cast<const T*>(dv.k) + (((size_t)b * dv.stride + s_node[j]) * cv.Hkv + kh) * D;
-    float sum = 0.f;
-    for (int r0 = 0; r0 < n * G; r0 += kRows) {
-        __syncthreads();
-        for (int e = threadIdx.x; e < kRows * (D / 2); e += kThreads) {   // queries: encoded at their slot, scaled
-            const int r = r0 + e / (D / 2), c = e % (D / 2);
-            float x = 0.f, y = 0.f;
-            if (r < n * G) {
-                const T* row = reinterpret_cast<const T*>(dv.q) + (((size_t)b * dv.stride + s_node[r / G]) * cv.Hq + kh * G + r % G) * D;
-                x = Elem<T>::to_float(row[c]); y = Elem<T>::to_float(row[c + D / 2]);
-                if (cv.rope_cos) {
-                    const size_t at = (size_t)(st.L + r / G) * (D / 2) + c;
-                    const float cs = __ldg(cv.rope_cos + at), sn = __ldg(cv.rope_sin + at), x1 = x, x2 = y;
-                    x = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
-                    y = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
-                }
-                if (c == 0) s_lse[r - r0] = lse[((size_t)b * dv.stride + s_node[r / G]) * cv.Hq + kh * G + r % G] * kLog2e;
-            }
-            sq[r - r0][c] = x * scale; sq[r - r0][c + D / 2] = y * scale;
-        }
-        __syncthreads();
-        if (lam < total) {
-            float a[kRows];
-#pragma unroll
-            for (int r = 0; r < kRows; ++r) a[r] = 0.f;
-            for_key_row<T, D>(krow, cv, lam, [&](int c, const float (&x)[VEC]) {
-#pragma unroll
-                for (int r = 0; r < kRows; ++r) {
-#pragma unroll
-                    for (int e = 0; e < VEC; e += 4) {
-                        const float4 q4 = *reinterpret_cast<const float4*>(&sq[r][c + e]);
-                        a[r] = fmaf(q4.x, x[e], fmaf(q4.y, x[e + 1], fmaf(q4.z, x[e + 2], fmaf(q4.w, x[e + 3], a[r]))));
-                    }
-                }
-            });
-#pragma unroll
-            for (int r = 0; r < kRows; ++r)
-                if (r0 + r < n * G && (r0 + r) / G >= j) sum += exp2f(a[r] - s_lse[r]);
-        }
-    }
-    if (lam < total) {
-        ps.colsum[(size_t)unit * ps.QT * ps.n_max + lam] = sum;
-        if (j >= 0) {   // append
-            const size_t row = (size_t)unit * cv.R + st.L + st.i + j;
-            const T* vrow = reinterpret_cast<const T*>(dv.v) + (((size_t)b * dv.stride + s_node[j]) * cv.Hkv + kh) * D;
-            for (int e = 0; e < D / VEC; ++e) {
-                reinterpret_cast<uint4*>(cv.K)[row * (D / VEC) + e] = reinterpret_cast<const uint4*>(krow)[e];
-                reinterpret_cast<uint4*>(cv.V)[row * (D / VEC) + e] = reinterpret_cast<const uint4*>(vrow)[e];
-            }
-            cv.pos[row] = N + j;
-            cv.S[row] = 0.f;
-        }
-    }
+    if constexpr (sizeof(T) == 2) scores_bf16<D, ROPE>(cv, dv, p, lse, rank, CL, smem, rows8);
+    else scores_f32<D>(cv, dv, p, lse, rank, CL, smem);
+    auto unit_sync = [&]() { if (CL == 1) __syncthreads(); else cluster.sync(); };
+    unit_sync();  // every score and every appended row of the unit is in place; every block has read n_seen
+    if (rank == 0 && threadIdx.x == 0) cv.n_seen[p.unit] = p.N + p.n;
+    evict_unit<T, CL, kThreads>(cv, p.unit, rank, p.N, p.n, unit_sync);
 }
 
-template <typename T, int D>
-cudaError_t launch_t(const CacheView& cv, const PrefillScratch& ps, const DraftView& dv, const float* lse, const int32_t* path, int path_stride,
-                     const DraftLens& lens, int max_n, cudaStream_t s) {
-    return launch_pdl(accept_scores_kernel<T, D>, dim3((cv.c + max_n + kThreads - 1) / kThreads, cv.B * cv.Hkv), dim3(kThreads), 0, s, cv, ps, dv,
-                      lse, path, path_stride, lens);
+template <typename T, int D, int CL, bool ROPE>
+cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse, const int32_t* path, int path_stride, const DraftLens& lens,
+                     int max_n, cudaStream_t s) {
+    auto kern = accept_kernel<T, D, CL, ROPE>;
+    const int rows8 = (max_n * (cv.Hq / cv.Hkv) + 7) / 8 * 8;
+    const size_t smem = sizeof(T) == 2 ? (size_t)rows8 * (q_pitch<D>() + 4) : (size_t)kStage32 * (D + 1) * 4;
+    if (smem > 48 * 1024) {
+        static bool smem_set[64] = {};  // per device: the opt-in is needed once (to the longest path of the widest group)
+        int dev = 0;
+        cudaGetDevice(&dev);
+        dev &= 63;
+        if (!smem_set[dev]) {
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDraft * 8 * (q_pitch<D>() + 4));
+            if (e != cudaSuccess) return e;
+            smem_set[dev] = true;
+        }
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(CL, cv.B * cv.Hkv);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = CL;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = CL > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lse, path, path_stride, lens, rows8);
+}
+
+// Blocks per unit: until the machine holds two per SM, while a warp still finds keys to take.
+template <typename T, int D, bool ROPE>
+cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const float* lse, const int32_t* path, int path_stride, const DraftLens& lens,
+                     int max_n, int sms, cudaStream_t s) {
+    const long units = (long)cv.B * cv.Hkv;
+    const int keys = sizeof(T) == 2 ? kWarps * 16 : kThreads;
+    int cl = 1;
+    while (cl < 8 && units * cl < 2L * sms && cv.c / (2 * cl) >= keys) cl *= 2;
+    switch (cl) {
+        case 1: return launch_c<T, D, 1, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
+        case 2: return launch_c<T, D, 2, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
+        case 4: return launch_c<T, D, 4, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
+        default: return launch_c<T, D, 8, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
+    }
 }
 
 }  // namespace
 
-cudaError_t launch_accept_scores(const CacheView& cv, treekv_dtype dt, const PrefillScratch& ps, const DraftView& dv,
-                                 const float* lse, const int32_t* path, int path_stride, const DraftLens& lens, int max_n,
-                                 cudaStream_t stream) {
+cudaError_t launch_accept(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const float* lse, const int32_t* path,
+                          int path_stride, const DraftLens& lens, int max_n, int sms, cudaStream_t s) {
+    using T = __nv_bfloat16;
     if (dt == TREEKV_F32)
-        return cv.d == 64 ? launch_t<float, 64>(cv, ps, dv, lse, path, path_stride, lens, max_n, stream)
-                          : launch_t<float, 128>(cv, ps, dv, lse, path, path_stride, lens, max_n, stream);
-    return cv.d == 64 ? launch_t<__nv_bfloat16, 64>(cv, ps, dv, lse, path, path_stride, lens, max_n, stream)
-                      : launch_t<__nv_bfloat16, 128>(cv, ps, dv, lse, path, path_stride, lens, max_n, stream);
+        return cv.d == 64 ? launch_t<float, 64, false>(cv, dv, lse, path, path_stride, lens, max_n, sms, s)
+                          : launch_t<float, 128, false>(cv, dv, lse, path, path_stride, lens, max_n, sms, s);
+    if (cv.rope_cos)
+        return cv.d == 64 ? launch_t<T, 64, true>(cv, dv, lse, path, path_stride, lens, max_n, sms, s)
+                          : launch_t<T, 128, true>(cv, dv, lse, path, path_stride, lens, max_n, sms, s);
+    return cv.d == 64 ? launch_t<T, 64, false>(cv, dv, lse, path, path_stride, lens, max_n, sms, s)
+                      : launch_t<T, 128, false>(cv, dv, lse, path, path_stride, lens, max_n, sms, s);
 }
 
 }  // namespace treekv

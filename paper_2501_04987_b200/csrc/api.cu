@@ -152,7 +152,7 @@ treekv_status treekv_create(treekv_ctx** out, int budget, int n_heads, int n_kv_
     ctx->ps.colsum = reinterpret_cast<float*>(base + L.colsum);
     // (rows in flight during compaction stay in registers: the context has no staging rows; PrefillScratch's
     //  staging pointers are only used by the entry point that brings its own scratch)
-    ctx->ps.QT = L.QT; ctx->ps.n_max = L.n_max; ctx->ps.max_chunk = max_chunk; ctx->ps.window = 0; ctx->ps.slices = 0;
+    ctx->ps.QT = L.QT; ctx->ps.n_max = L.n_max; ctx->ps.max_chunk = max_chunk; ctx->ps.window = 0;
     ctx->st_q = base + L.st_q; ctx->st_k = base + L.st_k; ctx->st_v = base + L.st_v; ctx->st_out = base + L.st_out;
     ctx->dt = dtype; ctx->max_chunk = max_chunk; ctx->G = n_heads / n_kv_heads;
     ctx->elem = dtype == TREEKV_F32 ? 4 : 2;

@@ -248,7 +248,6 @@ struct PrefillScratch {
     int max_chunk;
     int window;       // 0: every query row of the chunk adds to the column sums (Algorithm 1 per row); > 0: only the
                       // last `window` tokens of each sequence's chunk do (observation window of the one-shot prefill)
-    int slices;       // > 0: that many slices of colsum hold the chunk's sums; 0: one per tile of 128 query rows
 };
 constexpr int kQTileRows = 128;  // query rows (token x head-in-group) per prefill tile
 

@@ -102,16 +102,13 @@ treekv_status treekv_accept_path(treekv_ctx* ctx, const void* dev_q, const void*
     if (stride < 1 || stride > kMaxDraft || path_stride < 1) return TREEKV_ERR_INVALID_ARG;
     if (ctx->max_chunk == 0) return TREEKV_ERR_BAD_STATE;  // a decode-only context has no rows for more than one new token
     DraftLens lens;
-    ChunkLens chunk;
     memset(&lens, 0, sizeof(lens));
-    memset(&chunk, 0, sizeof(chunk));
     int max_n = 0;
     for (int b = 0; b < ctx->cv.B; ++b) {
         const int n = host_lens ? host_lens[b] : path_stride;
         if (n < 0 || n > path_stride || n > stride || n > ctx->max_chunk) return TREEKV_ERR_INVALID_ARG;
         if (ctx->n_seen[b] + n >= 0x7fffffff - 1) return TREEKV_ERR_BAD_STATE;
         lens.n[b] = (uint8_t)n;
-        chunk.m[b] = (uint16_t)n;
         if (n > max_n) max_n = n;
     }
     if (max_n == 0) return TREEKV_OK;
@@ -122,12 +119,9 @@ treekv_status treekv_accept_path(treekv_ctx* ctx, const void* dev_q, const void*
     cudaError_t e = join_eviction_stream(ctx, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     const DraftView dv = {dev_q, dev_k, dev_v, nullptr, stride};
-    PrefillScratch ps = ctx->ps;
-    ps.slices = 1;
-    e = launch_accept_scores(ctx->cv, ctx->dt, ps, dv, dev_lse, dev_path, path_stride, lens, max_n, s);
-    if (e == cudaSuccess) e = launch_chunk_update_evict(ctx->cv, ctx->dt, ps, chunk, false, s);
+    e = launch_accept(ctx->cv, ctx->dt, dv, dev_lse, dev_path, path_stride, lens, max_n, ctx->sm_count, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
-    ctx->launches += 2;
+    ctx->launches += 1;
     for (int b = 0; b < ctx->cv.B; ++b) {
         const int64_t before = ctx->n_seen[b];
         ctx->n_seen[b] += lens.n[b];

@@ -63,10 +63,8 @@ cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const Draft
 bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV);
 cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,
                              int max_n, void* out, float* lse, int sms, cudaStream_t stream);
-// S gains what the accepted rows give to every live row; the accepted tokens' rows are appended.  Column sums go to
-// slice 0 of ps.colsum.
-cudaError_t launch_accept_scores(const CacheView& cv, treekv_dtype dt, const PrefillScratch& ps, const DraftView& dv,
-                                 const float* lse, const int32_t* path, int path_stride, const DraftLens& lens, int max_n,
-                                 cudaStream_t stream);
+// the accepted path enters the cache: append, score update, evictions, token counters
+cudaError_t launch_accept(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const float* lse, const int32_t* path,
+                          int path_stride, const DraftLens& lens, int max_n, int sms, cudaStream_t stream);
 
 }  // namespace treekv

@@ -5,6 +5,7 @@
 
 #include "common.cuh"
 #include "ctx.cuh"
+#include "evict.cuh"
 
 namespace treekv {
 
@@ -319,14 +320,9 @@ cudaError_t launch_chunk_evict(const CacheView& cv, treekv_dtype dt, const Prefi
 // The three steps above in one launch: score update, every eviction segment of the chunk, n_seen += m.
 // A unit is owned by a cluster of CL thread blocks: four blocks of 512 threads when the kernel runs in the caller's
 // stream, where its latency counts (the barriers are cluster barriers), or one block of 1024 threads when it runs on
-// the context's eviction stream beside the next attention kernel, where a small footprint counts (block barriers).  Inside a segment the pairs are taken in rounds of
-// increasing pair index; a round first reads everything it moves into registers (decision, survivor's K and V
-// rows, its S and position), the cluster synchronises, then the round writes.  That is enough because the
-// destination row i+p of pair p can only be a source row of an earlier pair ((p-i)/2 < p) - read in this round
-// or a previous one - and never of a later pair; rows moved down after a wrap follow the same rule.  A new
-// segment starts after a further cluster barrier, since its pairs read rows the previous one wrote.
+// the context's eviction stream beside the next attention kernel, where a small footprint counts (block barriers).
+// The evictions themselves are evict_unit() in evict.cuh.
 constexpr int evict_threads(int cl) { return cl == 1 ? 1024 : 512; }
-constexpr int kEvictItemsPerWarp = 4;
 
 template <typename T, int kEvictCluster>
 __global__ void __launch_bounds__(evict_threads(kEvictCluster))
@@ -348,17 +344,12 @@ chunk_update_evict_kernel(CacheView cv, PrefillScratch ps, ChunkLens lens) {
     const int N = cv.n_seen[unit];
     const UnitState st = unit_state(N, cv);
     const int n = st.L + m;
-    const int N1 = N + m;
-    const int w0 = cv.w0[unit];
-    T* Kc = reinterpret_cast<T*>(cv.K) + (size_t)unit * cv.R * cv.d;
-    T* Vc = reinterpret_cast<T*>(cv.V) + (size_t)unit * cv.R * cv.d;
     float* Sc = cv.S + (size_t)unit * cv.R;
-    int32_t* Pc = cv.pos + (size_t)unit * cv.R;
 
     // ---- score update (Algorithm 1: S <- S + a, summed over the chunk's steps; group mean): tiles added in a
     //      fixed order so the result does not depend on scheduling
     {
-        const int qt = ps.slices > 0 ? ps.slices : (m * G + kQTileRows - 1) / kQTileRows;
+        const int qt = (m * G + kQTileRows - 1) / kQTileRows;
         const float inv_g = 1.0f / (float)G;
         for (int lam = rank * kEvictThreads + threadIdx.x; lam < n; lam += kEvictCluster * kEvictThreads) {
             const float* part = ps.colsum + (size_t)unit * ps.QT * ps.n_max + lam;
@@ -369,62 +360,10 @@ chunk_update_evict_kernel(CacheView cv, PrefillScratch ps, ChunkLens lens) {
         }
     }
     unit_sync();  // every S of the unit is final; every block has read n_seen
-    if (rank == 0 && threadIdx.x == 0) cv.n_seen[unit] = N1;
+    if (rank == 0 && threadIdx.x == 0) cv.n_seen[unit] = N + m;
 
     // ---- eviction segments (Algorithm 1's "length > c" branch repeated with the scores frozen)
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const int gwarp = rank * (kEvictThreads / 32) + warp;
-    constexpr int kWarps = kEvictCluster * kEvictThreads / 32;
-    constexpr int kRound = kWarps * kEvictItemsPerWarp;
-    const int chunks = cv.d * (int)sizeof(T) / 16;  // 16-byte pieces per row: at most 32
-    const int nseg = evict_segment(N, m, cv, 0).nseg;
-    for (int seg = 0; seg < nseg; ++seg) {
-        const EvictSegment sg = evict_segment(N, m, cv, seg);
-        const int items = sg.E + sg.rebase;
-        for (int r0 = 0; r0 < items; r0 += kRound) {
-            uint4 kr[kEvictItemsPerWarp], vr[kEvictItemsPerWarp];
-            float sr[kEvictItemsPerWarp];
-            int32_t pr[kEvictItemsPerWarp];
-#pragma unroll
-            for (int u = 0; u < kEvictItemsPerWarp; ++u) {
-                const int item = r0 + u * kWarps + gwarp;
-                if (item >= items) continue;
-                int src;
-                if (item < sg.E) {
-                    const int l = cv.ns + 2 * (sg.i + item), r = l + 1;
-                    int evict_right = 0;
-                    if (lane == 0) {
-                        bool near_tie = false;
-                        evict_right = pair_evicts_right(Sc[l], score_count(N1, Pc[l], w0), Sc[r], score_count(N1, Pc[r], w0),
-                                                        cv.rule, &near_tie) ? 1 : 0;
-                        if (near_tie) atomicAdd(&cv.stats->near_ties, 1ull);
-                    }
-                    evict_right = __shfl_sync(0xffffffffu, evict_right, 0);
-                    src = evict_right ? l : r;
-                } else {
-                    src = cv.ns + 2 * cv.cm + (item - sg.E);
-                }
-                if (lane < chunks) {
-                    kr[u] = reinterpret_cast<const uint4*>(Kc + (size_t)src * cv.d)[lane];
-                    vr[u] = reinterpret_cast<const uint4*>(Vc + (size_t)src * cv.d)[lane];
-                }
-                if (lane == 0) { sr[u] = Sc[src]; pr[u] = Pc[src]; }
-            }
-            unit_sync();  // everything this round moves has been read
-#pragma unroll
-            for (int u = 0; u < kEvictItemsPerWarp; ++u) {
-                const int item = r0 + u * kWarps + gwarp;
-                if (item >= items) continue;
-                const int dst = cv.ns + (item < sg.E ? sg.i + item : cv.cm + (item - sg.E));
-                if (lane < chunks) {
-                    reinterpret_cast<uint4*>(Kc + (size_t)dst * cv.d)[lane] = kr[u];
-                    reinterpret_cast<uint4*>(Vc + (size_t)dst * cv.d)[lane] = vr[u];
-                }
-                if (lane == 0) { Sc[dst] = sr[u]; Pc[dst] = pr[u]; }
-            }
-        }
-        if (seg + 1 < nseg) unit_sync();  // the next segment's pairs read rows this one wrote
-    }
+    evict_unit<T, kEvictCluster, kEvictThreads>(cv, unit, rank, N, m, unit_sync);
     }
 }
 
