@@ -9,6 +9,7 @@ from __future__ import annotations
 
 import ctypes as C
 import os
+from array import array as _array
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libtreekv.so")
@@ -106,11 +107,11 @@ def _load():
     lib.treekv_norm_rope.restype = i32
     lib.treekv_norm_rope.argtypes = [vp, vp, C.c_int64, vp, vp, C.c_float, vp, vp, i32, vp, vp, vp, vp, i32, vp]
     lib.treekv_verify_tree.restype = i32
-    lib.treekv_verify_tree.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.POINTER(C.c_int32), i32, vp]
+    lib.treekv_verify_tree.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, i32, vp]
     lib.treekv_accept_path.restype = i32
-    lib.treekv_accept_path.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, C.POINTER(C.c_int32), vp]
+    lib.treekv_accept_path.argtypes = [vp, vp, vp, vp, vp, i32, vp, i32, vp, vp]
     lib.treekv_fork_sequences.restype = i32
-    lib.treekv_fork_sequences.argtypes = [vp, C.POINTER(C.c_int32), vp]
+    lib.treekv_fork_sequences.argtypes = [vp, vp, vp]
     lib.treekv_selftest_fork_plan.restype = i32
     lib.treekv_selftest_fork_plan.argtypes = [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
     return lib
@@ -279,6 +280,10 @@ class TreeKV:
         if not torch.cuda.is_available():
             raise RuntimeError("TreeKV needs a CUDA device; there is no CPU fallback")
         self.device = torch.device(device if device is not None else "cuda:%d" % torch.cuda.current_device())
+        if self.device.index is None:
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        # handle of torch's current stream, without making a Stream object for every call where torch offers that
+        self._raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda i: torch.cuda.current_stream(i).cuda_stream)
         self.budget, self.n_heads, self.n_kv_heads, self.head_dim = budget, n_heads, n_kv_heads, head_dim
         self.batch, self.max_chunk = batch, max_chunk
         self.dtype_code = TREEKV_F32 if dtype in ("f32", "fp32", torch.float32) else TREEKV_BF16
@@ -294,7 +299,7 @@ class TreeKV:
         self._h = h
 
     def _stream(self):
-        return self.torch.cuda.current_stream(self.device).cuda_stream
+        return self._raw_stream(self.device.index)
 
     def close(self):
         h, self._h = getattr(self, "_h", None), None
@@ -365,84 +370,109 @@ class TreeKV:
                                          q.shape[1], self._stream()), "treekv_prefill_chunk_host")
         return out
 
+    # The calls of drafted decoding are short on the device: their checks are written for few interpreter steps, and tensors
+    # made here are not looked at again.
     def _lens(self, lens, what):
-        if lens is not None and len(lens) != self.batch:
+        """Address of the numbers as int32 (and what keeps them), None where there are none."""
+        if lens is None:
+            return None, None
+        if len(lens) != self.batch:
             raise ValueError("expected %d %s, got %d" % (self.batch, what, len(lens)))
-        return lens
+        kept = _array("i", lens)
+        return kept.buffer_info()[0], kept
 
-    def _int(self, x, dtype, shape, what):
-        if not (x.is_cuda and x.is_contiguous() and x.dtype == dtype and tuple(x.shape) == tuple(shape)):
-            raise ValueError("expected %s as a contiguous %s CUDA tensor of shape %s, got %s %s" %
-                             (what, dtype, tuple(shape), x.dtype, tuple(x.shape)))
+    def _want(self, x, dtype, shape, what):
+        if not (x.shape == shape and x.dtype is dtype and x.device == self.device and x.is_contiguous()):
+            raise ValueError("expected %s as a contiguous %s tensor of shape %s on %s, got %s %s on %s" %
+                             (what, dtype, shape, self.device, x.dtype, tuple(x.shape), x.device))
+        return x.data_ptr()
 
     def norm_rope(self, qkv, q_weight=None, k_weight=None, cos=None, sin=None, positions=None, eps=1e-6, q=None, k=None, v=None):
         """(q, k, v) of the tokens of a packed projection [tokens, (n_heads + 2 n_kv_heads) * head_dim], whose rows may lie
         in wider ones: every q and k head normalised (where its weight [head_dim] is given) and rotated to the token's
         position (where tables [slots, head_dim/2] are given)."""
-        t = self.torch
+        t, want, dt = self.torch, self._want, self.tdtype
         Hq, Hkv, d = self.n_heads, self.n_kv_heads, self.head_dim
-        if not (qkv.is_cuda and qkv.dim() == 2 and qkv.dtype == self.tdtype and qkv.shape[1] == (Hq + 2 * Hkv) * d
-                and (qkv.stride(1) == 1 or qkv.numel() == 0)):
-            raise ValueError("expected a %s CUDA tensor [tokens, %d] with adjacent columns, got %s %s" %
-                             (self.tdtype, (Hq + 2 * Hkv) * d, qkv.dtype, tuple(qkv.shape)))
+        row = (Hq + 2 * Hkv) * d
+        if not (qkv.dim() == 2 and qkv.dtype is dt and qkv.device == self.device and qkv.shape[1] == row and qkv.stride(1) == 1):
+            raise ValueError("expected a %s tensor [tokens, %d] with adjacent columns on %s, got %s %s on %s" %
+                             (dt, row, self.device, qkv.dtype, tuple(qkv.shape), qkv.device))
         n = qkv.shape[0]
-        for w in (q_weight, k_weight):
-            if w is not None:
-                self._chk(w, (d,))
-        if (cos is None) != (sin is None) or (cos is not None and positions is None):
-            raise ValueError("a rotation takes cos, sin and positions")
-        for x in (cos, sin):
-            if x is not None:
-                self._int(x, t.float32, (cos.shape[0], d // 2), "cos and sin")
+        wq = None if q_weight is None else want(q_weight, dt, (d,), "q_weight")
+        wk = None if k_weight is None else want(k_weight, dt, (d,), "k_weight")
+        pc = ps = pp = None
+        slots = 0
+        if cos is not None or sin is not None:
+            if cos is None or sin is None or positions is None:
+                raise ValueError("a rotation takes cos, sin and positions")
+            slots = cos.shape[0]
+            pc, ps = want(cos, t.float32, (slots, d // 2), "cos"), want(sin, t.float32, (slots, d // 2), "sin")
         if positions is not None:
-            self._int(positions, t.int32, (n,), "positions")
-        q = t.empty((n, Hq, d), dtype=self.tdtype, device=qkv.device) if q is None else q
-        k = t.empty((n, Hkv, d), dtype=self.tdtype, device=qkv.device) if k is None else k
-        v = t.empty((n, Hkv, d), dtype=self.tdtype, device=qkv.device) if v is None else v
-        self._chk(q, (n, Hq, d)); self._chk(k, (n, Hkv, d)); self._chk(v, (n, Hkv, d))
-        ptr = lambda x: None if x is None else x.data_ptr()
+            pp = want(positions, t.int32, (n,), "positions")
+        if q is None:
+            q = qkv.new_empty((n, Hq, d))
+            pq = q.data_ptr()
+        else:
+            pq = want(q, dt, (n, Hq, d), "q")
+        if k is None:
+            k = qkv.new_empty((n, Hkv, d))
+            pk = k.data_ptr()
+        else:
+            pk = want(k, dt, (n, Hkv, d), "k")
+        if v is None:
+            v = qkv.new_empty((n, Hkv, d))
+            pv = v.data_ptr()
+        else:
+            pv = want(v, dt, (n, Hkv, d), "v")
         # (torch reports any stride for the rows of a tensor of one row)
-        stride = qkv.stride(0) if n > 1 else (Hq + 2 * Hkv) * d
-        _check(treekv_norm_rope(self._h, qkv.data_ptr(), stride, ptr(q_weight), ptr(k_weight), eps, ptr(cos), ptr(sin),
-                                0 if cos is None else cos.shape[0], ptr(positions), q.data_ptr(), k.data_ptr(), v.data_ptr(), n,
-                                self._stream()), "treekv_norm_rope")
+        st = lib.treekv_norm_rope(self._h, qkv.data_ptr(), qkv.stride(0) if n > 1 else row, wq, wk, eps, pc, ps, slots, pp, pq, pk, pv,
+                                  n, self._stream())
+        if st:
+            _check(st, "treekv_norm_rope")
         return q, k, v
 
     def verify_tree(self, q, k, v, mask=None, lens=None, out=None, lse=None):
         """(out, lse) of drafted tokens [batch, stride, heads, head_dim] over the cache and the drafted tokens that each
         one's mask word (int64 [batch, stride], bit j = drafted token j) names; without masks a chain."""
-        t = self.torch
+        want, dt = self._want, self.tdtype
         B, Hq, Hkv, d = self.batch, self.n_heads, self.n_kv_heads, self.head_dim
         n = q.shape[1]
-        self._chk(q, (B, n, Hq, d)); self._chk(k, (B, n, Hkv, d)); self._chk(v, (B, n, Hkv, d))
-        if mask is not None:
-            self._int(mask, t.int64, (B, n), "mask")
+        pq, pk, pv = want(q, dt, (B, n, Hq, d), "q"), want(k, dt, (B, n, Hkv, d), "k"), want(v, dt, (B, n, Hkv, d), "v")
+        pm = None if mask is None else want(mask, self.torch.int64, (B, n), "mask")
         if out is None:
-            out = t.empty_like(q)
+            out = q.new_empty((B, n, Hq, d))
+            po = out.data_ptr()
+        else:
+            po = want(out, dt, (B, n, Hq, d), "out")
         if lse is None:
-            lse = t.empty((B, n, Hq), dtype=t.float32, device=q.device)
-        self._chk(out, (B, n, Hq, d))
-        self._int(lse, t.float32, (B, n, Hq), "lse")
-        _check(treekv_verify_tree(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), None if mask is None else mask.data_ptr(),
-                                  out.data_ptr(), lse.data_ptr(), self._lens(lens, "draft lengths"), n, self._stream()),
-               "treekv_verify_tree")
+            lse = q.new_empty((B, n, Hq), dtype=self.torch.float32)
+            pl = lse.data_ptr()
+        else:
+            pl = want(lse, self.torch.float32, (B, n, Hq), "lse")
+        pn, kept = self._lens(lens, "draft lengths")
+        st = lib.treekv_verify_tree(self._h, pq, pk, pv, pm, po, pl, pn, n, self._stream())
+        if st:
+            _check(st, "treekv_verify_tree")
         return out, lse
 
     def accept_path(self, q, k, v, lse, path, lens=None):
         """The drafted tokens path[b, :lens[b]] (int32) of every sequence enter the cache; q, k, v, lse as in verify_tree."""
-        t = self.torch
+        want, dt = self._want, self.tdtype
         B, Hq, Hkv, d = self.batch, self.n_heads, self.n_kv_heads, self.head_dim
-        n = q.shape[1]
-        self._chk(q, (B, n, Hq, d)); self._chk(k, (B, n, Hkv, d)); self._chk(v, (B, n, Hkv, d))
-        self._int(lse, t.float32, (B, n, Hq), "lse")
-        self._int(path, t.int32, (B, path.shape[1]), "path")
-        _check(treekv_accept_path(self._h, q.data_ptr(), k.data_ptr(), v.data_ptr(), lse.data_ptr(), n, path.data_ptr(),
-                                  path.shape[1], self._lens(lens, "accepted lengths"), self._stream()), "treekv_accept_path")
+        n, m = q.shape[1], path.shape[1]
+        pq, pk, pv = want(q, dt, (B, n, Hq, d), "q"), want(k, dt, (B, n, Hkv, d), "k"), want(v, dt, (B, n, Hkv, d), "v")
+        pl, pp = want(lse, self.torch.float32, (B, n, Hq), "lse"), want(path, self.torch.int32, (B, m), "path")
+        pn, kept = self._lens(lens, "accepted lengths")
+        st = lib.treekv_accept_path(self._h, pq, pk, pv, pl, n, pp, m, pn, self._stream())
+        if st:
+            _check(st, "treekv_accept_path")
 
     def fork_sequences(self, source):
         """Sequence b becomes what sequence source[b] was (b: stays, -1: emptied), all at once."""
-        _check(treekv_fork_sequences(self._h, self._lens([int(x) for x in source], "sources"), self._stream()),
-               "treekv_fork_sequences")
+        p, kept = self._lens(source, "sources")
+        st = lib.treekv_fork_sequences(self._h, p, self._stream())
+        if st:
+            _check(st, "treekv_fork_sequences")
 
     def retained_positions(self):
         t = self.torch
