@@ -79,6 +79,19 @@ __device__ inline Tiles my_tiles(const UnitState& st, int rank, int split) {
     t.draft = t.count > 0 && t.t0 + t.count == all;
     return t;
 }
+// Position in the ring of K and V tiles: load x (K of tile x / 2, V for odd x) is in slot x mod slots, in that slot's round
+// x / slots.  Counted up: a division per step would cost the one thread that feeds the tensor cores more than the step.
+struct Ring {
+    int x, slot, phase, slots;
+    __device__ Ring(int x0, int n) : x(x0), slot(x0), phase(0), slots(n) {}  // x0 < n
+    __device__ void next() { ++x; if (++slot == slots) { slot = 0; phase ^= 1; } }
+};
+// Shared-memory matrix descriptor as two words: the low one holds the address and the leading offset, and moves by bytes /
+// 16; the high one - stride 1024, the version, 128-byte swizzle - is the same for all tiles.
+constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
+__device__ inline uint64_t desc_of(uint32_t lo) { return (uint64_t)kDescHi << 32 | lo; }
+// (the address of a block in a cluster has its rank above the bits that a descriptor takes)
+__device__ inline uint32_t desc_lo(uint32_t saddr, uint32_t lead_bytes) { return ((saddr >> 4) & 0x3fffu) | (lead_bytes >> 4) << 16; }
 // cached tile j of the block: first slab row and rows that exist
 __device__ inline void cached_tile(const Tiles& t, int j, int& row0, int& valid) {
     const int x = t.t0 + j - (t.draft ? 1 : 0);
@@ -135,17 +148,17 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             for (int h = 0; h < HALVES; ++h)
                 tma_load_3d(sQ + h * q_rows * 128, &tmQ, 64 * h, kh * G, b * dv.stride + r0 / G, bar(Q_FULL));
             int issued = 0;
-            for (int x = t.draft ? 2 : 0; x < 2 * NT; ++x) {
-                const int slot = x % slots;
-                if (!mbar_wait(bar(EMPTY + slot), ((x / slots) & 1) ^ 1)) { ok = false; break; }
+            for (Ring r(t.draft ? 2 : 0, slots); r.x < 2 * NT; r.next()) {
+                if (!mbar_wait(bar(EMPTY + r.slot), r.phase ^ 1)) { ok = false; break; }
                 int row0, valid;
-                cached_tile(t, x >> 1, row0, valid);
+                cached_tile(t, r.x >> 1, row0, valid);
                 const int grow = unit * cv.R + row0;
-                const uint32_t dst = sRing + slot * SLOT;
-                mbar_arrive_expect_tx(bar(FULL + slot), SLOT);
-                const CUtensorMap* map = x & 1 ? &tmV : &tmK;
-                for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * VHALF, map, 64 * h, grow, bar(FULL + slot));
-                issued = x + 1;
+                const uint32_t dst = sRing + r.slot * SLOT;
+                mbar_arrive_expect_tx(bar(FULL + r.slot), SLOT);
+                const CUtensorMap* map = r.x & 1 ? &tmV : &tmK;
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) tma_load_2d(dst + h * VHALF, map, 64 * h, grow, bar(FULL + r.slot));
+                issued = r.x + 1;
             }
             // nothing may still be on its way into this block's memory when it ends, whatever gave up
             ok = mbar_wait(bar(Q_FULL), 0) && ok;
@@ -157,34 +170,38 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (lane == 0 && NT > 0) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(128, kKeys, 0, 0);  // both operands K-major (rows x channels)
             constexpr uint32_t idesc_o = umma_idesc_bf16(128, D, 0, 1);      // P from tensor memory, V MN-major
-            auto issue_s = [&](int j) {
-                const int x = 2 * j, slot = x % slots;
-                if (!(ok = ok && mbar_wait(bar(FULL + slot), (x / slots) & 1))) return;
+            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, VHALF), q_half = q_rows * 128 / 16;
+            Ring rk(0, slots), rv(1, slots);
+            auto issue_s = [&](int buf) {  // the next tile's logits
+                if (!(ok = ok && mbar_wait(bar(FULL + rk.slot), rk.phase))) return;
                 tc_fence_after();
-                const uint32_t sK = sRing + slot * SLOT;
+                const uint32_t lo = k_lo + rk.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16(tmem + 64 * (j & 1), umma_desc_sw128(sQ + (kk >> 2) * q_rows * 128 + (kk & 3) * 32, 16, 1024),
-                              umma_desc_sw128(sK + (kk >> 2) * VHALF + (kk & 3) * 32, 16, 1024), idesc_s, kk > 0);
-                umma_commit(bar(EMPTY + slot));
-                umma_commit(bar(S_FULL + (j & 1)));
+                    umma_bf16(tmem + 64 * buf, desc_of(q_lo + (kk >> 2) * q_half + (kk & 3) * 2),
+                              desc_of(lo + (kk >> 2) * (VHALF / 16) + (kk & 3) * 2), idesc_s, kk > 0);
+                umma_commit(bar(EMPTY + rk.slot));
+                umma_commit(bar(S_FULL + buf));
+                rk.next(); rk.next();
             };
             ok = mbar_wait(bar(Q_FULL), 0);
-            for (int j = 0; j < 2 && j < NT; ++j) issue_s(j);
+            issue_s(0);
+            if (NT > 1) issue_s(1);
             for (int j = 0; j < NT && ok; ++j) {
-                const int x = 2 * j + 1, slot = x % slots;
-                ok = mbar_wait(bar(P_FULL + (j & 1)), (j >> 1) & 1) && mbar_wait(bar(FULL + slot), (x / slots) & 1);
+                const int buf = j & 1;
+                ok = mbar_wait(bar(FULL + rv.slot), rv.phase) && mbar_wait(bar(P_FULL + buf), (j >> 1) & 1);
                 if (!ok) break;
                 tc_fence_after();
-                const uint32_t sV = sRing + slot * SLOT;
+                const uint32_t lo = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < kKeys / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes, 8 columns of packed P
-                    umma_bf16_ta(tmO, tmem + 64 * (j & 1) + 8 * kk, umma_desc_sw128(sV + kk * 2048, VHALF, 1024), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
-                umma_commit(bar(EMPTY + slot));
+                    umma_bf16_ta(tmO, tmem + 64 * buf + 8 * kk, desc_of(lo + kk * (2048 / 16)), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+                umma_commit(bar(EMPTY + rv.slot));
                 umma_commit(bar(PV_DONE));
-                if (j + 2 < NT) {  // S_{j+2} overwrites P_j
-                    if (!(ok = mbar_wait(bar(PV_DONE), j & 1))) break;
-                    issue_s(j + 2);
+                rv.next(); rv.next();
+                if (j + 2 < NT) {  // the logits of tile j + 2 overwrite P_j
+                    if (!(ok = mbar_wait(bar(PV_DONE), buf))) break;
+                    issue_s(buf);
                 }
             }
             // every MMA of this block has finished before its memory and tensor memory are given to anything else
