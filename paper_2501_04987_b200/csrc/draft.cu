@@ -86,7 +86,7 @@ treekv_status treekv_verify_tree(treekv_ctx* ctx, const void* dev_q, const void*
         e = ctx->has_tm64 ? launch_verify_tc(ctx->cv, ctx->tmK64, ctx->tmV64, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s)
                           : cudaErrorNotSupported;
     else
-        e = launch_verify_simt(ctx->cv, ctx->dt, dv, lens, max_n, dev_out, dev_lse, s);
+        e = launch_verify_simt(ctx->cv, ctx->dt, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     ctx->launches += 1;
     return TREEKV_OK;

@@ -27,6 +27,17 @@ __device__ inline uint64_t draft_sees(const DraftView& dv, int b, int i, int n) 
 // sees, itself not counted)
 __device__ inline int draft_depth(uint64_t sees) { return max(__popcll(sees) - 1, 0); }
 
+// a pair of pieces, VEC channels and their partners half a head away, encoded at the slot whose table entries these are
+template <typename T>
+__device__ inline void rope_pairs(float (&x)[Elem<T>::kVec], float (&y)[Elem<T>::kVec], const float* cos, const float* sin) {
+#pragma unroll
+    for (int e = 0; e < Elem<T>::kVec; ++e) {
+        const float cs = __ldg(cos + e), sn = __ldg(sin + e), x1 = x[e], x2 = y[e];
+        x[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
+        y[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
+    }
+}
+
 // One key row in fp32, `slot` >= 0: encoded at that slot (see rope_apply).  Piece c of VEC channels and its partner
 // c + half come together: f(channel, value) is called for both.
 template <typename T, int D, typename F>
@@ -36,16 +47,8 @@ __device__ inline void for_key_row(const T* row, const CacheView& cv, int slot, 
         float x[VEC], y[VEC];
         Elem<T>::unpack(ld_plain(row + c * VEC), x);
         Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
-        if (cv.rope_cos) {
-#pragma unroll
-            for (int e = 0; e < VEC; ++e) {
-                const float cs = __ldg(cv.rope_cos + (size_t)slot * (D / 2) + c * VEC + e);
-                const float sn = __ldg(cv.rope_sin + (size_t)slot * (D / 2) + c * VEC + e);
-                const float x1 = x[e], x2 = y[e];
-                x[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
-                y[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
-            }
-        }
+        if (cv.rope_cos)
+            rope_pairs<T>(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
         f(c * VEC, x);
         f(D / 2 + c * VEC, y);
     }
@@ -58,7 +61,7 @@ struct DraftLens {
 };
 
 cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
-                               void* out, float* lse, cudaStream_t stream);
+                               void* out, float* lse, int sms, cudaStream_t stream);
 // bf16, no in-cache positions; tmK, tmV: maps over the slabs in boxes of the kernel's key tile (make_verify_maps)
 bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV);
 cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,

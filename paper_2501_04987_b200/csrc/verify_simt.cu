@@ -1,163 +1,340 @@
-// Attention of a tree of drafted tokens over the cache on CUDA cores: fp32 contexts, and every case the tensor-core
-// kernel leaves.
+// Attention of a tree of drafted tokens over the cache on CUDA cores: fp32 contexts, and bf16 ones with in-cache positions.
 //
 // Row r = token * G + head-in-group of one unit (sequence, KV head) attends to every cached row and to the drafted
 // tokens its mask names: out = softmax(q k / sqrt d) v in one pass over the keys with a running maximum and sum, all
-// fp32.  A block owns 16 rows and walks key tiles of 64: a thread takes one key against four rows (the key row is
-// streamed once per four rows, the queries come from shared memory as broadcasts), then one channel of the output
-// against its share of the rows.
+// fp32.  A block owns 32 rows and walks key tiles of 64 in shared memory.  A thread owns four rows (with the fifteen others
+// of its half-warp) and takes four keys of each tile for the logits, D / 16 channels for the output: 64 multiply-adds for
+// eight 16-byte reads of shared memory, most of them broadcasts, so the arithmetic is what bounds it once there are enough
+// rows.  A row's weights never leave its half-warp.  The next K tile is on its way while the weights meet V, the next V tile
+// while the logits are made.  With few units the keys of a unit are dealt to a cluster of blocks, which join their partial
+// results in shared memory.
 #include "draft.cuh"
+#include "tma.cuh"
 
 namespace treekv {
 
 namespace {
 
-constexpr int kThreads = 256;
-constexpr int kRows = 16, kKeys = 64;
+constexpr int kThreads = 128;
+constexpr int kRows = 32, kKeys = 64;
+constexpr int kMaxSplit = 8;
+
+template <int D> constexpr int k_pitch() { return D + 4; }  // floats: sixteen keys' 16-byte reads meet no conflict
+template <int D> constexpr size_t smem_bytes() {
+    return sizeof(float) * ((size_t)kRows * k_pitch<D>() + (size_t)kKeys * k_pitch<D>() + (size_t)kKeys * D + (size_t)kRows * (kKeys + 4));
+}
+
+__device__ inline void cp_async_16(float* dst, const void* src) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+}
+__device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
 template <typename T, int D>
-__global__ void __launch_bounds__(kThreads)
-verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ out, float* __restrict__ lse) {
-    constexpr int VEC = Elem<T>::kVec, CG = kThreads / D, RPT = kRows / CG;  // channel groups; rows of a thread's channel
+__global__ void __launch_bounds__(kThreads, 2)
+verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ out, float* __restrict__ lse, int split) {
+    constexpr int VEC = Elem<T>::kVec, HALF = D / 2 / VEC, KP = k_pitch<D>(), PP = kKeys + 4, NC = D / 64;  // NC: float4s of a thread's channels
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.y, b = unit / cv.Hkv, kh = unit % cv.Hkv;
-    const int n = lens.n[b], G = cv.Hq / cv.Hkv, r0 = blockIdx.x * kRows, rows = min(kRows, n * G - r0);
-    if (rows <= 0) return;
+    const int unit = blockIdx.z, b = unit / cv.Hkv, kh = unit % cv.Hkv, rank = blockIdx.x;
+    const int n = lens.n[b], G = cv.Hq / cv.Hkv, r0 = blockIdx.y * kRows, rows = min(kRows, n * G - r0);
+    if (rows <= 0) return;  // the whole cluster
     const UnitState st = unit_state(cv.n_seen[unit], cv);
-    const int total = st.L + n;
+    const int total = st.L + n, per = ((total + split - 1) / split + kKeys - 1) / kKeys * kKeys;
+    const int lo = min(rank * per, total), hi = min(lo + per, total);  // this block's live indices
     const T* Kc = reinterpret_cast<const T*>(cv.K) + (size_t)unit * cv.R * D;
     const T* Vc = reinterpret_cast<const T*>(cv.V) + (size_t)unit * cv.R * D;
     const T* kd = reinterpret_cast<const T*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
     const T* vd = reinterpret_cast<const T*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
     const size_t dstep = (size_t)cv.Hkv * D;
 
-    __shared__ __align__(16) float sq[kRows][D];
-    __shared__ float sp[kRows][kKeys + 1];
-    __shared__ float s_max[kRows], s_sum[kRows], s_fix[kRows];
+    extern __shared__ __align__(16) float smem[];
+    float* sq = smem;                    // [kRows][KP]
+    float* sk = sq + kRows * KP;         // [kKeys][KP]
+    float* sv = sk + kKeys * KP;         // [kKeys][D]
+    float* sp = sv + kKeys * D;          // [kRows][PP]
     __shared__ uint64_t s_sees[kRows];
+    __shared__ unsigned int s_bad[2];    // drafted tokens of this block's keys with a value that is not finite
     const int tid = threadIdx.x;
+    const bool rope = cv.rope_cos != nullptr;
     const float scale = kLog2e * rsqrtf((float)D);
 
-    if (tid < kRows) {
-        s_sees[tid] = tid < rows ? draft_sees(dv, b, (r0 + tid) / G, n) : 0ull;
-        s_max[tid] = -INFINITY; s_sum[tid] = 0.f;
-    }
+    if (tid < kRows) s_sees[tid] = tid < rows ? draft_sees(dv, b, (r0 + tid) / G, n) : 0ull;
+    if (tid < 2) s_bad[tid] = 0u;
+
+    auto row_of = [&](const T* cache, const T* draft, int lam) { return lam < st.L ? cache + (size_t)phys_row(lam, st) * D : draft + (size_t)(lam - st.L) * dstep; };
+    // K tile at k0: fp32 keys straight from memory; bf16 ones, or encoded at their slots, through registers
+    auto load_k = [&](int k0) {
+        const int kn = min(kKeys, hi - k0);
+        if (sizeof(T) == 4 && !rope) {
+            for (int e = tid; e < kn * (D / 4); e += kThreads) {
+                const int r = e / (D / 4), c = e % (D / 4);
+                cp_async_16(sk + r * KP + c * 4, reinterpret_cast<const float*>(row_of(Kc, kd, k0 + r)) + c * 4);
+            }
+        } else {
+            for (int e = tid; e < kn * HALF; e += kThreads) {
+                const int r = e / HALF, c = e % HALF, lam = k0 + r;
+                const T* row = row_of(Kc, kd, lam);
+                float x[VEC], y[VEC];
+                Elem<T>::unpack(ld_plain(row + c * VEC), x);
+                Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
+                if (rope) {
+                    const int slot = lam < st.L ? lam : st.L + draft_depth(draft_sees(dv, b, lam - st.L, n));
+                    rope_pairs<T>(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
+                }
+#pragma unroll
+                for (int u = 0; u < VEC; u += 4) {
+                    *reinterpret_cast<float4*>(sk + r * KP + c * VEC + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
+                    *reinterpret_cast<float4*>(sk + r * KP + D / 2 + c * VEC + u) = make_float4(y[u], y[u + 1], y[u + 2], y[u + 3]);
+                }
+            }
+        }
+        cp_async_commit();
+    };
+    // V tile; a drafted value that is not finite is left out here - a weight of zero would spread it - and added at the end
+    auto load_v = [&](int k0) {
+        const int kn = min(kKeys, hi - k0);
+        for (int e = tid; e < kKeys * (D / VEC); e += kThreads) {
+            const int r = e / (D / VEC), c = e % (D / VEC), lam = k0 + r;
+            float* dst = sv + r * D + c * VEC;
+            if (sizeof(T) == 4 && r < kn && lam < st.L) {
+                cp_async_16(dst, reinterpret_cast<const float*>(Vc) + (size_t)phys_row(lam, st) * D + c * VEC);
+                continue;
+            }
+            float x[VEC];
+#pragma unroll
+            for (int u = 0; u < VEC; ++u) x[u] = 0.f;
+            if (r < kn) {
+                Elem<T>::unpack(ld_plain(row_of(Vc, vd, lam) + c * VEC), x);
+                if (lam >= st.L) {
+#pragma unroll
+                    for (int u = 0; u < VEC; ++u)
+                        if (!(fabsf(x[u]) < INFINITY)) { x[u] = 0.f; atomicOr(&s_bad[(lam - st.L) >> 5], 1u << ((lam - st.L) & 31)); }
+                }
+            }
+#pragma unroll
+            for (int u = 0; u < VEC; u += 4) *reinterpret_cast<float4*>(dst + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
+        }
+        cp_async_commit();
+    };
+
     __syncthreads();
-    if (tid < kRows * (D / 2 / VEC)) {   // queries: encoded at their slot, scaled
-        const int r = tid / (D / 2 / VEC), c = tid % (D / 2 / VEC);
+    if (lo < hi) { load_k(lo); load_v(lo); }
+    for (int e = tid; e < kRows * HALF; e += kThreads) {   // queries: encoded at their slot, scaled
+        const int r = e / HALF, c = e % HALF;
         float x[VEC], y[VEC];
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { x[e] = 0.f; y[e] = 0.f; }
+        for (int u = 0; u < VEC; ++u) { x[u] = 0.f; y[u] = 0.f; }
         if (r < rows) {
-            const int t = (r0 + r) / G, h = (r0 + r) % G;
-            const T* row = reinterpret_cast<const T*>(dv.q) + (((size_t)b * dv.stride + t) * cv.Hq + kh * G + h) * D;
+            const T* row = reinterpret_cast<const T*>(dv.q) + (((size_t)b * dv.stride + (r0 + r) / G) * cv.Hq + kh * G + (r0 + r) % G) * D;
             Elem<T>::unpack(ld_plain(row + c * VEC), x);
             Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
-            if (cv.rope_cos) {
+            if (rope) {
                 const size_t at = (size_t)(st.L + draft_depth(s_sees[r])) * (D / 2) + c * VEC;
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    const float cs = __ldg(cv.rope_cos + at + e), sn = __ldg(cv.rope_sin + at + e), x1 = x[e], x2 = y[e];
-                    x[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
-                    y[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
-                }
+                rope_pairs<T>(x, y, cv.rope_cos + at, cv.rope_sin + at);
             }
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) { sq[r][c * VEC + e] = x[e] * scale; sq[r][D / 2 + c * VEC + e] = y[e] * scale; }
+        for (int u = 0; u < VEC; ++u) { sq[r * KP + c * VEC + u] = x[u] * scale; sq[r * KP + D / 2 + c * VEC + u] = y[u] * scale; }
     }
-    __syncthreads();
 
-    const int key = tid & (kKeys - 1), rg = tid / kKeys * 4;   // this thread's key of a tile and its four rows
-    const int ch = tid % D, cg = tid / D * RPT;                // its channel and that channel's first row
-    float o[RPT];
+    const int rg = tid / 16 * 4, l16 = tid % 16;   // this thread's four rows; its keys l16 + 16 i, its channels 4 l16 + 64 i
+    const bool live = rg < rows;                   // of the half-warp
+    const uint32_t mine = 0xffffu << (threadIdx.x & 16);  // its lanes
+    float m[4], l[4];
+    float4 o[4][NC];
 #pragma unroll
-    for (int r = 0; r < RPT; ++r) o[r] = 0.f;
-    for (int k0 = 0; k0 < total; k0 += kKeys) {
-        const int lam = k0 + key;
-        float a[4] = {0.f, 0.f, 0.f, 0.f};
-        if (lam < total) {
-            const int j = lam - st.L;  // >= 0: a drafted token
-            const T* row = j < 0 ? Kc + (size_t)phys_row(lam, st) * D : kd + (size_t)j * dstep;
-            const int slot = !cv.rope_cos ? 0 : j < 0 ? lam : st.L + draft_depth(draft_sees(dv, b, j, n));
-            for_key_row<T, D>(row, cv, slot, [&](int c, const float (&x)[VEC]) {
+    for (int r = 0; r < 4; ++r) {
+        m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
-                for (int r = 0; r < 4; ++r) {
+        for (int c = 0; c < NC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+    for (int k0 = lo; k0 < hi; k0 += kKeys) {
+        cp_async_wait<1>();   // K has arrived (V may still be on its way)
+        __syncthreads();
+        if (live) {
+            float a[4][4];
 #pragma unroll
-                    for (int e = 0; e < VEC; e += 4) {
-                        const float4 q4 = *reinterpret_cast<const float4*>(&sq[rg + r][c + e]);
-                        a[r] = fmaf(q4.x, x[e], fmaf(q4.y, x[e + 1], fmaf(q4.z, x[e + 2], fmaf(q4.w, x[e + 3], a[r]))));
+            for (int r = 0; r < 4; ++r)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a[r][k] = 0.f;
+#pragma unroll 4
+            for (int c = 0; c < D; c += 4) {
+                float4 q4[4], k4[4];
+#pragma unroll
+                for (int r = 0; r < 4; ++r) q4[r] = *reinterpret_cast<const float4*>(sq + (rg + r) * KP + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) k4[k] = *reinterpret_cast<const float4*>(sk + (l16 + 16 * k) * KP + c);
+#pragma unroll
+                for (int r = 0; r < 4; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k)
+                        a[r][k] = fmaf(q4[r].x, k4[k].x, fmaf(q4[r].y, k4[k].y, fmaf(q4[r].z, k4[k].z, fmaf(q4[r].w, k4[k].w, a[r][k]))));
+            }
+            const bool all_seen = k0 + kKeys <= min(hi, st.L);
+#pragma unroll
+            for (int r = 0; r < 4; ++r) {
+                if (!all_seen) {
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const int lam = k0 + l16 + 16 * k, j = lam - st.L;
+                        if (lam >= hi || (j >= 0 && !(s_sees[rg + r] >> j & 1))) a[r][k] = -INFINITY;
                     }
                 }
-            });
+                float mx = fmaxf(fmaxf(a[r][0], a[r][1]), fmaxf(a[r][2], a[r][3]));
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sp[rg + r][key] = j < 0 || (s_sees[rg + r] >> j & 1) ? a[r] : -INFINITY;
-        } else {
+                for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(mine, mx, off, 16));
+                const float now = fmaxf(m[r], mx), ref = now == -INFINITY ? 0.f : now, fix = exp2f(m[r] - ref);
+                m[r] = now;
+                float sum = 0.f;
 #pragma unroll
-            for (int r = 0; r < 4; ++r) sp[rg + r][key] = -INFINITY;
-        }
-        __syncthreads();
-        {   // running maximum and sum: sixteen threads per row
-            const int r = tid / 16, l = tid % 16;
-            float x[kKeys / 16], mx = -INFINITY;
+                for (int k = 0; k < 4; ++k) {
+                    const float p = exp2f(a[r][k] - ref);
+                    sp[(rg + r) * PP + l16 + 16 * k] = p;
+                    sum += p;
+                }
+                l[r] = l[r] * fix + sum;  // this thread's keys only
 #pragma unroll
-            for (int u = 0; u < kKeys / 16; ++u) { x[u] = sp[r][l + 16 * u]; mx = fmaxf(mx, x[u]); }
-#pragma unroll
-            for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(0xffffffffu, mx, off));
-            const float before = s_max[r], now = fmaxf(before, mx), ref = now == -INFINITY ? 0.f : now;
-            float sum = 0.f;
-#pragma unroll
-            for (int u = 0; u < kKeys / 16; ++u) { const float p = exp2f(x[u] - ref); sp[r][l + 16 * u] = p; sum += p; }
-#pragma unroll
-            for (int off = 8; off > 0; off >>= 1) sum += __shfl_xor_sync(0xffffffffu, sum, off);
-            __syncwarp();
-            if (l == 0) {
-                const float fix = exp2f(before - ref);  // 0 before the first visible key
-                s_fix[r] = fix; s_max[r] = now; s_sum[r] = s_sum[r] * fix + sum;
+                for (int c = 0; c < NC; ++c) { o[r][c].x *= fix; o[r][c].y *= fix; o[r][c].z *= fix; o[r][c].w *= fix; }
             }
         }
-        __syncthreads();
+        cp_async_wait<0>();   // V has arrived
+        __syncthreads();      // and nobody reads this K tile any more
+        if (k0 + kKeys < hi) load_k(k0 + kKeys);
+        if (live) {
+#pragma unroll 2
+            for (int k = 0; k < kKeys; k += 4) {
+                float4 p4[4];
 #pragma unroll
-        for (int r = 0; r < RPT; ++r) o[r] *= s_fix[cg + r];
-        const int kn = min(kKeys, total - k0);
-        for (int x = 0; x < kn; ++x) {
-            const int l2 = k0 + x, j = l2 - st.L;
-            const float val = Elem<T>::to_float(j < 0 ? Vc[(size_t)phys_row(l2, st) * D + ch] : vd[(size_t)j * dstep + ch]);
-            // a drafted token that a row does not see takes no part, whatever its value holds
+                for (int r = 0; r < 4; ++r) p4[r] = *reinterpret_cast<const float4*>(sp + (rg + r) * PP + k);
 #pragma unroll
-            for (int r = 0; r < RPT; ++r)
-                if (j < 0 || (s_sees[cg + r] >> j & 1)) o[r] = fmaf(sp[cg + r][x], val, o[r]);
+                for (int u = 0; u < 4; ++u) {
+#pragma unroll
+                    for (int c = 0; c < NC; ++c) {
+                        const float4 v4 = *reinterpret_cast<const float4*>(sv + (k + u) * D + 64 * c + 4 * l16);
+#pragma unroll
+                        for (int r = 0; r < 4; ++r) {
+                            const float p = u == 0 ? p4[r].x : u == 1 ? p4[r].y : u == 2 ? p4[r].z : p4[r].w;
+                            o[r][c].x = fmaf(p, v4.x, o[r][c].x); o[r][c].y = fmaf(p, v4.y, o[r][c].y);
+                            o[r][c].z = fmaf(p, v4.z, o[r][c].z); o[r][c].w = fmaf(p, v4.w, o[r][c].w);
+                        }
+                    }
+                }
+            }
         }
-        __syncthreads();
+        __syncthreads();      // nobody reads this V tile any more
+        if (k0 + kKeys < hi) load_v(k0 + kKeys);
     }
 #pragma unroll
-    for (int r = 0; r < RPT; ++r) {
-        if (cg + r < rows) {
-            const int t = (r0 + cg + r) / G, h = (r0 + cg + r) % G;
-            const float sum = s_sum[cg + r];
-            const size_t at = ((size_t)b * dv.stride + t) * cv.Hq + kh * G + h;
-            out[at * D + ch] = Elem<T>::from_float(sum == 0.f ? 0.f : o[r] / sum);  // sum = 0: nothing was visible
-            if (lse && ch == 0) lse[at] = sum == 0.f ? -INFINITY : (s_max[cg + r] + log2f(sum)) * (1.0f / kLog2e);
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int off = 8; off > 0; off >>= 1) l[r] += __shfl_xor_sync(mine, l[r], off, 16);
+
+    uint64_t bad = (uint64_t)s_bad[0] | (uint64_t)s_bad[1] << 32;
+    auto finish = [&](int row, int ch, float4 x, float M, float L) {  // four channels of one row, joined
+        const int tok = (r0 + row) / G, h = (r0 + row) % G;
+        const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
+        float f[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+        for (int u = 0; u < 4; ++u) f[u] = L == 0.f ? 0.f : f[u] / L;  // L = 0: nothing was visible
+        for (uint64_t left = bad & s_sees[row]; left; left &= left - 1) {
+            const T* vr = vd + (size_t)(__ffsll((long long)left) - 1) * dstep + ch;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) { const float y = Elem<T>::to_float(vr[u]); if (!(fabsf(y) < INFINITY)) f[u] += y; }
         }
+        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out + at * D + ch) = make_float4(f[0], f[1], f[2], f[3]);
+        else *reinterpret_cast<uint2*>(out + at * D + ch) = make_uint2(rope_pack_bf16(f[0], f[1]), rope_pack_bf16(f[2], f[3]));
+        if (lse && ch == 0) lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * (1.0f / kLog2e);
+    };
+    if (split == 1) {
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+#pragma unroll
+            for (int c = 0; c < NC; ++c)
+                if (rg + r < rows) finish(rg + r, 64 * c + 4 * l16, o[r][c], m[r], l[r]);
+        return;
+    }
+    // ---- the cluster's parts meet: a block joins rpo rows, and gets m, l and O of those rows from every block
+    constexpr int PITCH = D + 4;
+    const int rpo = (rows + split - 1) / split;
+    __shared__ __align__(8) float s_bad_of[kMaxSplit][2];
+    const uint32_t sPart = smem_addr_u32(smem), sStat = sPart + split * rpo * PITCH * 4;
+    __syncwarp();
+    cluster_sync_all();   // every block is done with its tiles
+#pragma unroll
+    for (int r = 0; r < 4; ++r) {
+        const int row = rg + r;
+        if (row < rows) {
+            const int owner = row / rpo, at = rank * rpo + row % rpo;
+            const uint32_t dst = map_to_cta(sPart, owner) + at * PITCH * 4;
+#pragma unroll
+            for (int c = 0; c < NC; ++c) st_remote_v4(dst + (64 * c + 4 * l16) * 4, o[r][c].x, o[r][c].y, o[r][c].z, o[r][c].w);
+            if (l16 == 0) st_remote_v2(map_to_cta(sStat, owner) + at * 8, m[r], l[r]);
+        }
+    }
+    if (tid < split) st_remote_v2(map_to_cta(smem_addr_u32(&s_bad_of[rank][0]), tid), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
+    __syncwarp();
+    cluster_sync_all();
+    bad = 0ull;
+    for (int s = 0; s < split; ++s) bad |= (uint64_t)__float_as_uint(s_bad_of[s][0]) | (uint64_t)__float_as_uint(s_bad_of[s][1]) << 32;
+    const float* stat = smem + split * rpo * PITCH;
+    for (int e = tid; e < rpo * (D / 4); e += kThreads) {
+        const int rl = e / (D / 4), c = e % (D / 4);
+        if (rank * rpo + rl >= rows) continue;
+        float M = -INFINITY, L = 0.f;
+        for (int s = 0; s < split; ++s) M = fmaxf(M, stat[(s * rpo + rl) * 2]);
+        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int s = 0; s < split; ++s) {
+            const float ms = stat[(s * rpo + rl) * 2], f = ms == -INFINITY ? 0.f : exp2f(ms - M);
+            L += stat[(s * rpo + rl) * 2 + 1] * f;
+            const float4 y = *reinterpret_cast<const float4*>(smem + (s * rpo + rl) * PITCH + 4 * c);
+            x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
+        }
+        finish(rank * rpo + rl, 4 * c, x, M, L);
     }
 }
 
 template <typename T, int D>
-cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, cudaStream_t s) {
-    const int G = cv.Hq / cv.Hkv;
-    return launch_pdl(verify_simt_kernel<T, D>, dim3((max_n * G + kRows - 1) / kRows, cv.B * cv.Hkv), dim3(kThreads), 0, s, cv, dv, lens,
-                      reinterpret_cast<T*>(out), lse);
+cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
+    const int G = cv.Hq / cv.Hkv, tiles_r = (max_n * G + kRows - 1) / kRows, keys = cv.c + max_n;
+    // Blocks of a cluster: until the machine holds two per SM, while each still has a tile of keys
+    int split = 1;
+    while (split < kMaxSplit && (long)cv.B * cv.Hkv * tiles_r * split < 2L * sms && keys > split * kKeys) split *= 2;
+    auto kern = verify_simt_kernel<T, D>;
+    static bool smem_set[64] = {};  // per device: the opt-in is needed once
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    if (!smem_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
+        if (e != cudaSuccess) return e;
+        smem_set[dev] = true;
+    }
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(split, tiles_r, cv.B * cv.Hkv);
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem_bytes<D>();
+    cfg.stream = s;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<T*>(out), lse, split);
 }
 
 }  // namespace
 
 cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
-                               void* out, float* lse, cudaStream_t stream) {
+                               void* out, float* lse, int sms, cudaStream_t stream) {
     if (dt == TREEKV_F32)
-        return cv.d == 64 ? launch_t<float, 64>(cv, dv, lens, max_n, out, lse, stream) : launch_t<float, 128>(cv, dv, lens, max_n, out, lse, stream);
-    return cv.d == 64 ? launch_t<__nv_bfloat16, 64>(cv, dv, lens, max_n, out, lse, stream)
-                      : launch_t<__nv_bfloat16, 128>(cv, dv, lens, max_n, out, lse, stream);
+        return cv.d == 64 ? launch_t<float, 64>(cv, dv, lens, max_n, out, lse, sms, stream) : launch_t<float, 128>(cv, dv, lens, max_n, out, lse, sms, stream);
+    return cv.d == 64 ? launch_t<__nv_bfloat16, 64>(cv, dv, lens, max_n, out, lse, sms, stream)
+                      : launch_t<__nv_bfloat16, 128>(cv, dv, lens, max_n, out, lse, sms, stream);
 }
 
 }  // namespace treekv

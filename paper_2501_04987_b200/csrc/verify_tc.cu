@@ -83,7 +83,7 @@ __device__ inline Tiles my_tiles(const UnitState& st, int rank, int split) {
 // x / slots.  Counted up: a division per step would cost the one thread that feeds the tensor cores more than the step.
 struct Ring {
     int x, slot, phase, slots;
-    __device__ Ring(int x0, int n) : x(x0), slot(x0), phase(0), slots(n) {}  // x0 < n
+    __device__ Ring(int x0, int n) : x(x0), slot(x0), phase(0), slots(n) {}  // x0 < n: 0, 1 or 2 of at least 4
     __device__ void next() { ++x; if (++slot == slots) { slot = 0; phase ^= 1; } }
 };
 // Shared-memory matrix descriptor as two words: the low one holds the address and the leading offset, and moves by bytes /
