@@ -5,20 +5,22 @@
 // itself): no second softmax pass and no values are needed, so the keys are read once and that is what bounds it.
 //
 // A cluster of blocks owns a unit (sequence, KV head).  bf16: a warp takes 16 keys at a time as the rows of mma.m16n8k16,
-// the path's queries, 8 at a time, as its columns.  The contraction runs over channels in any order, so a lane loads its
-// key fragments straight from memory as 16-byte pieces (channels 32u + 8t.. of rows g and g + 8) and the queries' the same
-// way from shared memory: no transposition, no shared-memory pass of the keys, and the next 16 keys are on their way
-// while these are used.  fp32: a thread per key, queries broadcast from shared memory.
+// the path's queries, 8 at a time, as its columns.  The contraction runs over channels in any order, so a lane's fragments
+// are 16-byte pieces of the rows (channels 32u + 8t.. of keys g and g + 8, of query g): no transposition.  A warp has a
+// ring of its own in shared memory, filled by bulk copies - 16 keys are 4 KB in one piece, or two at the ends of the cached
+// segments - and no other warp to wait for.  fp32: a thread per key, queries broadcast from shared memory.
 #include <cooperative_groups.h>
 
 #include "draft.cuh"
 #include "evict.cuh"
+#include "tma.cuh"
 
 namespace treekv {
 
 namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
+constexpr int kMaxDepth = 3;  // tiles of 16 keys a warp has on their way
 constexpr int kStage32 = 32;  // fp32: query rows in shared memory at a time
 
 __device__ inline float ex2(float x) {
@@ -55,36 +57,41 @@ __device__ inline size_t draft_row(const CacheView& cv, const DraftView& dv, con
 // rows, four pieces) meet no conflict
 template <int D> constexpr int q_pitch() { return D * 2 + 64; }
 
+// One contiguous piece of global memory into shared memory, completion as bytes on the mbarrier
+__device__ inline void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
+    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];"
+                 ::"r"(dst), "l"(src), "r"(bytes), "r"(bar) : "memory");
+}
+
 template <int D, bool ROPE>
 __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, const Path& p, const float* __restrict__ lse, int rank, int nblocks,
-                                   unsigned char* smem, int rows8) {
+                                   unsigned char* smem, int rows8, int depth, uint64_t (*bars)[kMaxDepth]) {
     using T = __nv_bfloat16;
-    constexpr int NU = D / 32, PITCH = q_pitch<D>();
+    constexpr int NU = D / 32, PITCH = q_pitch<D>(), ROWB = D * 2, TILE = 16 * ROWB;
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, g = lane >> 2, t = lane & 3;
     const int rows = p.n * p.G, tiles_r = (rows + 7) / 8, lg = __ffs(p.G) - 1;
-    float* s_lse = reinterpret_cast<float*>(smem + (size_t)rows8 * PITCH);
+    unsigned char* ring = smem + (size_t)warp * depth * TILE;
+    unsigned char* sq = smem + (size_t)kWarps * depth * TILE;
+    float* s_lse = reinterpret_cast<float*>(sq + (size_t)rows8 * PITCH);
     const float scale = kLog2e * rsqrtf((float)D);
-    const int ntiles = (p.total + 15) / 16, step = nblocks * kWarps;
+    const int ntiles = (p.total + 15) / 16, step = nblocks * kWarps, first = rank * kWarps + warp;
+    const T* Kc = reinterpret_cast<const T*>(cv.K) + (size_t)p.unit * cv.R * D;
 
-    uint4 kf[2][NU], kn[2][NU];
-    float s_old = 0.f, s_next = 0.f;
-    auto fetch = [&](int tile) {  // keys g and g + 8 of the tile; lane t = 0 / 1 also their scores
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-            const int lam = tile * 16 + g + 8 * h;
-            if (lam < p.total) {
-                const T* row = key_row<T, D>(cv, dv, p, lam);
-#pragma unroll
-                for (int u = 0; u < NU; ++u) kn[h][u] = ld_stream(row + 32 * u + 8 * t);
-                if (t == h) s_next = lam < p.st.L ? cv.S[(size_t)p.unit * cv.R + phys_row(lam, p.st)] : 0.f;
-            } else {
-#pragma unroll
-                for (int u = 0; u < NU; ++u) kn[h][u] = make_uint4(0, 0, 0, 0);
-            }
-        }
+    auto issue = [&](int tile, int stage) {  // one lane: the tile's rows, in as few pieces as they lie
+        const uint32_t bar = smem_addr_u32(&bars[warp][stage]), dst = smem_addr_u32(ring + stage * TILE);
+        const int lo = tile * 16, hi = min(lo + 16, p.total), mid = min(hi, p.st.L), cut = min(mid, max(lo, p.st.a));
+        mbar_arrive_expect_tx(bar, (uint32_t)(hi - lo) * ROWB);
+        if (cut > lo) bulk_load(dst, Kc + (size_t)lo * D, (uint32_t)(cut - lo) * ROWB, bar);
+        if (mid > cut) bulk_load(dst + (cut - lo) * ROWB, Kc + (size_t)(cut + p.st.i) * D, (uint32_t)(mid - cut) * ROWB, bar);
+        for (int lam = max(lo, p.st.L); lam < hi; ++lam)
+            bulk_load(dst + (lam - lo) * ROWB, reinterpret_cast<const T*>(dv.k) + draft_row<T, D>(cv, dv, p, lam - p.st.L), ROWB, bar);
     };
-    const int first = rank * kWarps + warp;
-    if (first < ntiles) fetch(first);
+    if (lane == 0) {
+        for (int x = 0; x < depth; ++x) mbar_init(smem_addr_u32(&bars[warp][x]), 1);
+        mbar_fence_init();
+        for (int x = 0; x < depth; ++x)
+            if (first + x * step < ntiles) issue(first + x * step, x);
+    }
 
     // ---- the path's queries (encoded at their slots with in-cache positions) and their log-sum-exps
     for (int e = tid; e < tiles_r * 8 * (D / 16); e += kThreads) {
@@ -99,25 +106,41 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
         } else if (c == 0) {
             s_lse[r] = INFINITY;  // weight 0
         }
-        *reinterpret_cast<uint4*>(smem + r * PITCH + c * 16) = lo;
-        *reinterpret_cast<uint4*>(smem + r * PITCH + (c + D / 16) * 16) = hi;
+        *reinterpret_cast<uint4*>(sq + r * PITCH + c * 16) = lo;
+        *reinterpret_cast<uint4*>(sq + r * PITCH + (c + D / 16) * 16) = hi;
     }
     __syncthreads();
 
+    bool ok = true;
+    int stage = 0, phase = 0;
     for (int tile = first; tile < ntiles; tile += step) {
+        const int lam0 = tile * 16, mine = lam0 + g + 8 * (t & 1);  // the key whose score this lane (t < 2) writes
+        const size_t mine_row = (size_t)p.unit * cv.R + (mine < p.st.L ? phys_row(mine, p.st) : mine + p.st.i);
+        const float s_old = t < 2 && mine < p.st.L ? cv.S[mine_row] : 0.f;
+        ok = ok && mbar_wait(smem_addr_u32(&bars[warp][stage]), phase);
+        uint4 kf[2][NU];
 #pragma unroll
-        for (int h = 0; h < 2; ++h)
+        for (int h = 0; h < 2; ++h) {  // rows two apart lie on the same banks: odd ones take their pieces in the other order
+            const unsigned char* row = ring + stage * TILE + (g + 8 * h) * ROWB + t * 16;
 #pragma unroll
-            for (int u = 0; u < NU; ++u) kf[h][u] = kn[h][u];
-        s_old = s_next;
-        if (tile + step < ntiles) fetch(tile + step);
-        const int lam0 = tile * 16;
+            for (int u = 0; u < NU; u += 2) {
+                const uint4 x = *reinterpret_cast<const uint4*>(row + (u + (g & 1)) * 64), y = *reinterpret_cast<const uint4*>(row + (u + 1 - (g & 1)) * 64);
+                kf[h][u] = g & 1 ? y : x;
+                kf[h][u + 1] = g & 1 ? x : y;
+            }
+        }
+        __syncwarp();
+        if (lane == 0 && tile + depth * step < ntiles) issue(tile + depth * step, stage);
+        if (++stage == depth) { stage = 0; phase ^= 1; }
         const bool has_new = lam0 + 16 > p.st.L;
-        if (has_new) {  // append: the lane's pieces of the key row, as they came
+        if (has_new) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const int j = lam0 + g + 8 * h - p.st.L;
-                if (j >= 0 && j < p.n) {
+                const int lam = lam0 + g + 8 * h, j = lam - p.st.L;
+                if (lam >= p.total) {  // no key: what lies in its place of the ring is of no account
+#pragma unroll
+                    for (int u = 0; u < NU; ++u) kf[h][u] = make_uint4(0, 0, 0, 0);
+                } else if (j >= 0) {   // append: the lane's pieces of the key row, as they came
                     const size_t row = ((size_t)p.unit * cv.R + p.st.L + p.st.i + j) * D;
                     const T* v = reinterpret_cast<const T*>(dv.v) + draft_row<T, D>(cv, dv, p, j);
 #pragma unroll
@@ -142,7 +165,7 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
         const int j0 = lam0 + g - p.st.L;
         for (int rt = 0; rt < tiles_r; ++rt) {
             float c[4] = {0.f, 0.f, 0.f, 0.f};
-            const unsigned char* qrow = smem + (rt * 8 + g) * PITCH + t * 16;
+            const unsigned char* qrow = sq + (rt * 8 + g) * PITCH + t * 16;
 #pragma unroll
             for (int u = 0; u < NU; ++u) {
                 const uint4 q = *reinterpret_cast<const uint4*>(qrow + u * 64);
@@ -163,15 +186,12 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
         }
         sum0 += __shfl_xor_sync(0xffffffffu, sum0, 1); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 1);
         sum0 += __shfl_xor_sync(0xffffffffu, sum0, 2); sum1 += __shfl_xor_sync(0xffffffffu, sum1, 2);
-        if (t < 2) {
-            const int lam = lam0 + g + 8 * t;
-            if (lam < p.total) {
-                const size_t row = (size_t)p.unit * cv.R + (lam < p.st.L ? phys_row(lam, p.st) : lam + p.st.i);
-                cv.S[row] = s_old + (t ? sum1 : sum0) * (1.0f / (float)p.G);
-                if (lam >= p.st.L) cv.pos[row] = p.N + lam - p.st.L;
-            }
+        if (t < 2 && mine < p.total) {
+            cv.S[mine_row] = s_old + (t ? sum1 : sum0) * (1.0f / (float)p.G);
+            if (mine >= p.st.L) cv.pos[mine_row] = p.N + mine - p.st.L;
         }
     }
+    if (!ok && lane == 0) atomicOr(&cv.stats->error, 4u);
 }
 
 template <int D>
@@ -242,9 +262,10 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
 template <typename T, int D, int CL, bool ROPE>
 __global__ void __launch_bounds__(kThreads, 2)
 accept_kernel(CacheView cv, DraftView dv, const float* __restrict__ lse, const int32_t* __restrict__ path, int path_stride, DraftLens lens,
-              int rows8) {
+              int rows8, int depth) {
     namespace cg = cooperative_groups;
-    extern __shared__ __align__(16) unsigned char smem[];
+    extern __shared__ __align__(128) unsigned char smem[];
+    __shared__ __align__(8) uint64_t bars[kWarps][kMaxDepth];
     __shared__ int s_node[kMaxDraft];
     pdl_trigger();
     pdl_wait();
@@ -263,7 +284,7 @@ accept_kernel(CacheView cv, DraftView dv, const float* __restrict__ lse, const i
         s_node[threadIdx.x] = node;
     }
     __syncthreads();
-    if constexpr (sizeof(T) == 2) scores_bf16<D, ROPE>(cv, dv, p, lse, rank, CL, smem, rows8);
+    if constexpr (sizeof(T) == 2) scores_bf16<D, ROPE>(cv, dv, p, lse, rank, CL, smem, rows8, depth, bars);
     else scores_f32<D>(cv, dv, p, lse, rank, CL, smem);
     auto unit_sync = [&]() { if (CL == 1) __syncthreads(); else cluster.sync(); };
     unit_sync();  // every score and every appended row of the unit is in place; every block has read n_seen
@@ -276,14 +297,20 @@ cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse,
                      int max_n, cudaStream_t s) {
     auto kern = accept_kernel<T, D, CL, ROPE>;
     const int rows8 = (max_n * (cv.Hq / cv.Hkv) + 7) / 8 * 8;
-    const size_t smem = sizeof(T) == 2 ? (size_t)rows8 * (q_pitch<D>() + 4) : (size_t)kStage32 * (D + 1) * 4;
+    // Two blocks per SM while the queries leave room for it beside rings of two tiles per warp; the widest ones (512 rows)
+    // leave one tile per warp in the one block that then fits.
+    constexpr size_t kTile = 16 * D * 2, kRing = kWarps * kTile, kHalfSm = 112 * 1024, kSm = 226 * 1024;
+    const size_t queries = (size_t)rows8 * (q_pitch<D>() + 4);
+    const size_t room = (queries + 2 * kRing <= kHalfSm ? kHalfSm : kSm) - queries;
+    const int depth = (int)(room / kRing < kMaxDepth ? room / kRing : kMaxDepth);
+    const size_t smem = sizeof(T) == 2 ? queries + depth * kRing : (size_t)kStage32 * (D + 1) * 4;
     if (smem > 48 * 1024) {
-        static bool smem_set[64] = {};  // per device: the opt-in is needed once (to the longest path of the widest group)
+        static bool smem_set[64] = {};  // per device: the opt-in is needed once
         int dev = 0;
         cudaGetDevice(&dev);
         dev &= 63;
         if (!smem_set[dev]) {
-            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kMaxDraft * 8 * (q_pitch<D>() + 4));
+            const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSm);
             if (e != cudaSuccess) return e;
             smem_set[dev] = true;
         }
@@ -302,7 +329,7 @@ cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse,
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = CL > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lse, path, path_stride, lens, rows8);
+    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lse, path, path_stride, lens, rows8, depth);
 }
 
 // Blocks per unit: until the machine holds two per SM, while a warp still finds keys to take.
