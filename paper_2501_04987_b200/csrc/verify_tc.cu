@@ -99,6 +99,17 @@ __device__ inline void cached_tile(const Tiles& t, int j, int& row0, int& valid)
     else { const int lam = t.a + (x - t.nA) * kKeys; row0 = lam + t.i; valid = min(kKeys, t.L - lam); }
 }
 
+// values of drafted token j that are not finite, channels [ch, ch + N): taken out of the tile, they go straight into the sum
+template <int N, int D>
+__device__ inline void add_not_finite(float (&x)[N], const CacheView& cv, const DraftView& dv, int b, int kh, int j, int ch) {
+    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(dv.v) + (((size_t)b * dv.stride + j) * cv.Hkv + kh) * D + ch;
+#pragma unroll
+    for (int e = 0; e < N; ++e) {
+        const float y = __bfloat162float(v[e]);
+        if (!(fabsf(y) < INFINITY)) x[e] += y;
+    }
+}
+
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
 verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
@@ -268,7 +279,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
                 for (int e = 1; e < 32; ++e) { mx0 = fmaxf(mx0, __uint_as_float(s0[e])); mx1 = fmaxf(mx1, __uint_as_float(s1[e])); }
                 const float mx = fmaxf(mx0, mx1) * sc2;
-                const bool grow = mx > m_ref + kSlack;  // also from minus infinity to anything
+                const bool grow = mx > m_ref + kSlack && row < rows;  // also from minus infinity to anything
                 if (__any_sync(0xffffffffu, grow)) {
                     const float f = grow ? ex2(m_ref - mx) : 1.f;
                     if (grow) { m_ref = mx; l_run *= f; }
@@ -322,10 +333,45 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     }
     __syncwarp();
 
+    if (split == 1) {
+        // ---- a thread's row is complete: out it goes, 64 bytes at a time
+        if (warp >= 2) {
+            const int quarter = warp & 3, row = quarter * 32 + lane;
+            if (quarter * 32 < rows) {
+                const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+                const int tok = min((r0 + row) / G, n - 1), h = (r0 + row) % G;
+                const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
+                const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;  // 0: the row sees nothing
+                const uint64_t bad = ((uint64_t)s_bad[0] | (uint64_t)s_bad[1] << 32) & (row < rows ? draft_sees(dv, b, tok, n) : 0ull);
+#pragma unroll
+                for (int cg = 0; cg < D / 32; ++cg) {
+                    uint32_t o[32];
+                    tmem_ld32(tmO + lane_off + cg * 32, o);
+                    tmem_ld_wait_for(o);
+                    if (row < rows) {
+                        float x[32];
+#pragma unroll
+                        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(o[e]) * inv;
+                        for (uint64_t left = bad; left; left &= left - 1) add_not_finite<32, D>(x, cv, dv, b, kh, __ffsll((long long)left) - 1, cg * 32);
+                        uint4* dst = reinterpret_cast<uint4*>(out + at * D + cg * 32);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            dst[e] = make_uint4(rope_pack_bf16(x[8 * e], x[8 * e + 1]), rope_pack_bf16(x[8 * e + 2], x[8 * e + 3]),
+                                                rope_pack_bf16(x[8 * e + 4], x[8 * e + 5]), rope_pack_bf16(x[8 * e + 6], x[8 * e + 7]));
+                    }
+                }
+                if (lse && row < rows) lse[at] = l_run == 0.f ? -INFINITY : (m_ref + log2f(l_run)) * (1.0f / kLog2e);
+                tc_fence_before();
+            }
+        }
+        __syncthreads();
+        if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
+        return;
+    }
     // ---- the cluster's partial results meet: a block joins rpo rows, and gets from every block m, l and O of those rows
     const int rpo = (rows + split - 1) / split;
     const uint32_t sPart = base, sStat = base + split * rpo * PITCH * 4;  // [split][rpo][PITCH], [split][rpo][2]
-    if (split > 1) cluster_sync_all(); else __syncthreads();              // (1) every block's tiles are consumed
+    cluster_sync_all();  // (1) every block's tiles are consumed
     if (warp >= 2) {
         const int quarter = warp & 3, row = quarter * 32 + lane;
         const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
@@ -351,7 +397,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             st_remote_v2(map_to_cta(smem_addr_u32(s_bad_all), tid - 64), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
     }
     __syncwarp();
-    if (split > 1) cluster_sync_all(); else __syncthreads();  // (2) all parts have arrived
+    cluster_sync_all();  // (2) all parts have arrived
     {
         const float* part = reinterpret_cast<const float*>(base_ptr);
         const float* stat = part + split * rpo * PITCH;
@@ -378,17 +424,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const int tok = (r0 + row) / G, h = (r0 + row) % G;
 #pragma unroll
             for (int u = 0; u < 8; ++u) o[u] *= inv;
-            if (bad) {
-                for (uint64_t left = bad & draft_sees(dv, b, tok, n); left; left &= left - 1) {
-                    const int d = __ffsll((long long)left) - 1;
-                    const __nv_bfloat16* vr = reinterpret_cast<const __nv_bfloat16*>(dv.v) + (((size_t)b * dv.stride + d) * cv.Hkv + kh) * D + c * 8;
-#pragma unroll
-                    for (int u = 0; u < 8; ++u) {
-                        const float x = __bfloat162float(vr[u]);
-                        if (!(fabsf(x) < INFINITY)) o[u] += x;
-                    }
-                }
-            }
+            if (bad)
+                for (uint64_t left = bad & draft_sees(dv, b, tok, n); left; left &= left - 1)
+                    add_not_finite<8, D>(o, cv, dv, b, kh, __ffsll((long long)left) - 1, c * 8);
             const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
             *reinterpret_cast<uint4*>(out + at * D + c * 8) =
                 make_uint4(rope_pack_bf16(o[0], o[1]), rope_pack_bf16(o[2], o[3]), rope_pack_bf16(o[4], o[5]), rope_pack_bf16(o[6], o[7]));
