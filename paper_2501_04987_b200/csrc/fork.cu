@@ -13,10 +13,10 @@ namespace treekv {
 namespace {
 
 constexpr int kForkThreads = 256;
-constexpr int kForkUnroll = 4;  // rows of a thread per block
+constexpr int kForkUnroll = 2;  // rows of a thread: more of them cost the occupancy that hides the latency of a component's chain
 
-template <int D16, int MAXB>
-__global__ void __launch_bounds__(kForkThreads) fork_kernel(CacheView cv, ForkPlan<MAXB> plan) {
+template <int D16, int MAXB, bool RINGS>
+__global__ void __launch_bounds__(kForkThreads, RINGS ? 4 : 5) fork_kernel(CacheView cv, ForkPlan<MAXB> plan) {
     constexpr int RPB = kForkThreads / D16;     // rows of a block per unrolled step
     constexpr int ROWS = RPB * kForkUnroll;     // rows of a block
     pdl_trigger();
@@ -27,39 +27,38 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(CacheView cv, ForkPl
     uint4* V = reinterpret_cast<uint4*>(cv.V);
     auto unit = [&](int b) { return (size_t)(b * cv.Hkv + kh); };
 
-    // ---- K and V
-    uint4 k[kForkUnroll], v[kForkUnroll], ks[kForkUnroll], vs[kForkUnroll];
+    // ---- K and V.  Geometry and content stay from one operation to the next as long as the source does.
+    uint4 k[kForkUnroll], v[kForkUnroll], ks[RINGS ? kForkUnroll : 1], vs[RINGS ? kForkUnroll : 1];
+    bool live[kForkUnroll];
+    int held = -1;
     for (int o = first; o < last; ++o) {
         const int src = plan.src[o], dst = plan.dst[o];
         if (src == kForkEmpty) continue;
-        const UnitState st = unit_state(plan.seen[o], cv);
-        const int end = st.L + st.i;
-        if (r0 >= end) continue;
-        const bool fresh = src != kForkKept && (o == first || plan.src[o - 1] != src);
+        if (src != held) {
+            held = src;
+            const UnitState st = unit_state(plan.seen[o], cv);
+            const uint4* Ks = K + unit(src) * cv.R * D16 + piece;
+            const uint4* Vs = V + unit(src) * cv.R * D16 + piece;
 #pragma unroll
-        for (int u = 0; u < kForkUnroll; ++u) {
-            const int r = rt + u * RPB;
-            if (r < st.a || (r >= st.a + st.i && r < end)) {
-                if (fresh) {
-                    const size_t at = (unit(src) * cv.R + r) * D16 + piece;
-                    k[u] = ld_stream(K + at);
-                    v[u] = ld_stream(V + at);
+            for (int u = 0; u < kForkUnroll; ++u) {
+                const int r = rt + u * RPB;
+                live[u] = r < st.a || (r >= st.a + st.i && r < st.L + st.i);
+                if (live[u]) {
+                    if (RINGS && src == kForkKept) { k[u] = ks[RINGS ? u : 0]; v[u] = vs[RINGS ? u : 0]; }
+                    else { k[u] = ld_stream(Ks + (size_t)r * D16); v[u] = ld_stream(Vs + (size_t)r * D16); }
                 }
             }
         }
+        if (RINGS && dst == kForkKept) {
 #pragma unroll
-        for (int u = 0; u < kForkUnroll; ++u) {
-            const int r = rt + u * RPB;
-            if (r < st.a || (r >= st.a + st.i && r < end)) {
-                if (dst == kForkKept) {
-                    ks[u] = k[u]; vs[u] = v[u];
-                } else {
-                    const size_t at = (unit(dst) * cv.R + r) * D16 + piece;
-                    K[at] = src == kForkKept ? ks[u] : k[u];
-                    V[at] = src == kForkKept ? vs[u] : v[u];
-                }
-            }
+            for (int u = 0; u < kForkUnroll; ++u) { ks[RINGS ? u : 0] = k[u]; vs[RINGS ? u : 0] = v[u]; }
+            continue;
         }
+        uint4* Kd = K + (unit(dst) * cv.R + rt) * D16 + piece;
+        uint4* Vd = V + (unit(dst) * cv.R + rt) * D16 + piece;
+#pragma unroll
+        for (int u = 0; u < kForkUnroll; ++u)
+            if (live[u]) { Kd[u * RPB * D16] = k[u]; Vd[u * RPB * D16] = v[u]; }
     }
     // ---- S, stream positions, and the sequence's own counters
     if (threadIdx.x < ROWS) {
@@ -82,7 +81,7 @@ __global__ void __launch_bounds__(kForkThreads) fork_kernel(CacheView cv, ForkPl
     }
 }
 
-template <int D16, int MAXB>
+template <int D16, int MAXB, bool RINGS>
 cudaError_t launch_fork_b(const CacheView& cv, const ForkPlanHost& p, cudaStream_t stream) {
     ForkPlan<MAXB> plan;
     int rows = 1;
@@ -93,13 +92,16 @@ cudaError_t launch_fork_b(const CacheView& cv, const ForkPlanHost& p, cudaStream
     }
     for (int c = 0; c <= p.n_comps; ++c) plan.start[c] = p.start[c];
     constexpr int ROWS = kForkThreads / D16 * kForkUnroll;
-    return launch_pdl(fork_kernel<D16, MAXB>, dim3((rows + ROWS - 1) / ROWS, cv.Hkv, p.n_comps), dim3(kForkThreads), 0, stream, cv, plan);
+    return launch_pdl(fork_kernel<D16, MAXB, RINGS>, dim3((rows + ROWS - 1) / ROWS, cv.Hkv, p.n_comps), dim3(kForkThreads), 0, stream, cv, plan);
 }
 
 template <int D16>
 cudaError_t launch_fork_t(const CacheView& cv, const ForkPlanHost& p, cudaStream_t stream) {
-    // the plan travels as a kernel parameter: a small one for the usual batch
-    return p.n_ops <= 64 ? launch_fork_b<D16, 64>(cv, p, stream) : launch_fork_b<D16, kForkMaxOps>(cv, p, stream);
+    // The plan travels as a kernel parameter: a small one for the usual batch.  Without rings a thread keeps no second value.
+    bool rings = false;
+    for (int o = 0; o < p.n_ops; ++o) rings = rings || p.dst[o] == kForkKept;
+    if (p.n_ops <= 64) return rings ? launch_fork_b<D16, 64, true>(cv, p, stream) : launch_fork_b<D16, 64, false>(cv, p, stream);
+    return rings ? launch_fork_b<D16, kForkMaxOps, true>(cv, p, stream) : launch_fork_b<D16, kForkMaxOps, false>(cv, p, stream);
 }
 
 }  // namespace
