@@ -346,7 +346,7 @@ struct NormRope {
     float eps;
     int slots, tokens, Hq, Hkv;
 };
-cudaError_t launch_norm_rope(const NormRope& a, treekv_dtype dt, int D, DevStats* stats, cudaStream_t stream);
+cudaError_t launch_norm_rope(const NormRope& a, treekv_dtype dt, int D, DevStats* stats, int sms, cudaStream_t stream);
 
 // Copies between the sequences of a batch (fork.cu): operations of each connected component of the copy graph in an
 // order in which no sequence is overwritten before all its copies have been taken.

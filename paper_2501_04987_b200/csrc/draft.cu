@@ -52,7 +52,7 @@ treekv_status treekv_norm_rope(treekv_ctx* ctx, const void* dev_qkv, int64_t row
     a.qkv = dev_qkv; a.row_stride = row_stride; a.wq = dev_q_weight; a.wk = dev_k_weight;
     a.cos = dev_cos; a.sin = dev_sin; a.pos = dev_pos; a.q = dev_q; a.k = dev_k; a.v = dev_v;
     a.eps = eps; a.slots = slots; a.tokens = tokens; a.Hq = ctx->cv.Hq; a.Hkv = ctx->cv.Hkv;
-    const cudaError_t e = launch_norm_rope(a, ctx->dt, d, ctx->cv.stats, static_cast<cudaStream_t>(stream));
+    const cudaError_t e = launch_norm_rope(a, ctx->dt, d, ctx->cv.stats, ctx->sm_count, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     ctx->launches += 1;
     return TREEKV_OK;
