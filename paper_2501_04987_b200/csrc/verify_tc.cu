@@ -20,12 +20,13 @@
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
 #include <algorithm>
 
-#include "draft.cuh"
-#include "tma.cuh"
+#include "verify_tc.cuh"
 
 namespace treekv {
 
 namespace {
+
+using namespace vtc;
 
 constexpr int kThreads = 192;
 constexpr int kKeys = 64;                  // keys of a tile
@@ -34,88 +35,16 @@ constexpr int kMaxSlots = 8;
 constexpr uint32_t kTmemCols = 256;        // S 64, S 64, O 128: two blocks share an SM's 512 columns
 constexpr size_t kSmemMin = 80 * 1024;     // never a third block on an SM: it would wait for tensor memory inside a cluster
 constexpr size_t kSmemMax = 112 * 1024;
-constexpr float kSlack = 8.f;              // log2 by which a row's maximum may outgrow its reference
+static_assert(kKeys == kMaxDraft, "the drafted tokens are one tile");
 
 enum Bar { Q_FULL = 0, S_FULL = 1, P_FULL = 3, PV_DONE = 5, FULL = 6, EMPTY = FULL + kMaxSlots, N_BARS = EMPTY + kMaxSlots };
-
-__device__ inline float ex2(float x) {
-    float y;
-    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
-    return y;
-}
-// D[tmem] (+)= A[tmem] * B[smem desc]
-__device__ inline void umma_bf16_ta(uint32_t d_tmem, uint32_t a_tmem, uint64_t b_desc, uint32_t idesc, uint32_t accumulate) {
-    asm volatile(
-        "{\n\t.reg .pred p;\n\t"
-        "setp.ne.b32 p, %4, 0;\n\t"
-        "tcgen05.mma.cta_group::1.kind::f16 [%0], [%1], %2, %3, {%5, %6, %7, %8}, p;\n\t}"
-        ::"r"(d_tmem), "r"(a_tmem), "l"(b_desc), "r"(idesc), "r"(accumulate), "r"(0u), "r"(0u), "r"(0u), "r"(0u) : "memory");
-}
-__device__ inline void tmem_st32(uint32_t taddr, const uint32_t (&r)[32]) {
-    asm volatile(
-        "tcgen05.st.sync.aligned.32x32b.x32.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16,"
-        "%17,%18,%19,%20,%21,%22,%23,%24,%25,%26,%27,%28,%29,%30,%31,%32};"
-        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
-          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]),
-          "r"(r[16]), "r"(r[17]), "r"(r[18]), "r"(r[19]), "r"(r[20]), "r"(r[21]), "r"(r[22]), "r"(r[23]),
-          "r"(r[24]), "r"(r[25]), "r"(r[26]), "r"(r[27]), "r"(r[28]), "r"(r[29]), "r"(r[30]), "r"(r[31]) : "memory");
-}
-__device__ inline void tmem_st_wait() { asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory"); }
-
-// A block's key tiles: cached rows in two segments (rows = index below the split point a, index + i behind it), then the
-// drafted tokens as the last tile of the unit.  The block that owns that one takes it first.
-struct Tiles {
-    int a, i, L, nA, nB, t0, count;
-    bool draft;  // this block's tile 0 is the drafted one
-};
-__device__ inline Tiles my_tiles(const UnitState& st, int rank, int split) {
-    Tiles t;
-    t.a = min(st.a, st.L); t.i = st.i; t.L = st.L;
-    t.nA = (t.a + kKeys - 1) / kKeys;
-    t.nB = (st.L - t.a + kKeys - 1) / kKeys;
-    const int all = t.nA + t.nB + 1, per = (all + split - 1) / split;
-    t.t0 = min(rank * per, all);
-    t.count = min(per, all - t.t0);
-    t.draft = t.count > 0 && t.t0 + t.count == all;
-    return t;
-}
-// Position in the ring of K and V tiles: load x (K of tile x / 2, V for odd x) is in slot x mod slots, in that slot's round
-// x / slots.  Counted up: a division per step would cost the one thread that feeds the tensor cores more than the step.
-struct Ring {
-    int x, slot, phase, slots;
-    __device__ Ring(int x0, int n) : x(x0), slot(x0), phase(0), slots(n) {}  // x0 < n: 0, 1 or 2 of at least 4
-    __device__ void next() { ++x; if (++slot == slots) { slot = 0; phase ^= 1; } }
-};
-// Shared-memory matrix descriptor as two words: the low one holds the address and the leading offset, and moves by bytes /
-// 16; the high one - stride 1024, the version, 128-byte swizzle - is the same for all tiles.
-constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
-__device__ inline uint64_t desc_of(uint32_t lo) { return (uint64_t)kDescHi << 32 | lo; }
-// (the address of a block in a cluster has its rank above the bits that a descriptor takes)
-__device__ inline uint32_t desc_lo(uint32_t saddr, uint32_t lead_bytes) { return ((saddr >> 4) & 0x3fffu) | (lead_bytes >> 4) << 16; }
-// cached tile j of the block: first slab row and rows that exist
-__device__ inline void cached_tile(const Tiles& t, int j, int& row0, int& valid) {
-    const int x = t.t0 + j - (t.draft ? 1 : 0);
-    if (x < t.nA) { row0 = x * kKeys; valid = min(kKeys, t.a - row0); }
-    else { const int lam = t.a + (x - t.nA) * kKeys; row0 = lam + t.i; valid = min(kKeys, t.L - lam); }
-}
-
-// values of drafted token j that are not finite, channels [ch, ch + N): taken out of the tile, they go straight into the sum
-template <int N, int D>
-__device__ inline void add_not_finite(float (&x)[N], const CacheView& cv, const DraftView& dv, int b, int kh, int j, int ch) {
-    const __nv_bfloat16* v = reinterpret_cast<const __nv_bfloat16*>(dv.v) + (((size_t)b * dv.stride + j) * cv.Hkv + kh) * D + ch;
-#pragma unroll
-    for (int e = 0; e < N; ++e) {
-        const float y = __bfloat162float(v[e]);
-        if (!(fabsf(y) < INFINITY)) x[e] += y;
-    }
-}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
 verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  CacheView cv, DraftView dv, DraftLens lens, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
                  int q_rows, int q_bytes, int slots, int split) {
-    constexpr int HALVES = D / 64, SLOT = kKeys * D * 2, VHALF = kKeys * 128, PITCH = D + 4;
+    constexpr int HALVES = D / 64, SLOT = kKeys * D * 2, VHALF = kKeys * 128;
     const int unit = blockIdx.z, b = unit / cv.Hkv, kh = unit % cv.Hkv, rank = blockIdx.x;
     const int G = cv.Hq / cv.Hkv, n = lens.n[b], r0 = blockIdx.y * 128, rows = min(128, n * G - r0);
     pdl_trigger();
@@ -147,7 +76,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t tmem = tmem_slot, tmO = tmem + 128;  // S / P of tile j at column 64 (j & 1)
     pdl_wait();
     const UnitState st = unit_state(cv.n_seen[unit], cv);
-    const Tiles t = my_tiles(st, rank, split);
+    const Tiles t = my_tiles<kKeys>(st, rank, split);
     const int NT = t.count;
 
     bool ok = true;
@@ -162,7 +91,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             for (Ring r(t.draft ? 2 : 0, slots); r.x < 2 * NT; r.next()) {
                 if (!mbar_wait(bar(EMPTY + r.slot), r.phase ^ 1)) { ok = false; break; }
                 int row0, valid;
-                cached_tile(t, r.x >> 1, row0, valid);
+                cached_tile<kKeys>(t, r.x >> 1, row0, valid);
                 const int grow = unit * cv.R + row0;
                 const uint32_t dst = sRing + r.slot * SLOT;
                 mbar_arrive_expect_tx(bar(FULL + r.slot), SLOT);
@@ -229,27 +158,8 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         if (t.draft) {
             if (row < rows) sees = draft_sees(dv, b, (r0 + row) / G, n);
             // the drafted tokens' K and V into ring loads 0 and 1
-            const uint4* ks = reinterpret_cast<const uint4*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * (D / 8);
-            const uint4* vs = reinterpret_cast<const uint4*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * (D / 8);
             unsigned char* ring = base_ptr + HALVES * q_rows * 128;
-            for (int e = st_tid; e < kKeys * (D / 8); e += 128) {
-                const int r = e / (D / 8), c = e % (D / 8);
-                uint4 kx = make_uint4(0, 0, 0, 0), vx = kx;
-                if (r < n) {
-                    kx = ks[(size_t)r * cv.Hkv * (D / 8) + c];
-                    vx = vs[(size_t)r * cv.Hkv * (D / 8) + c];
-                    uint32_t* w = &vx.x;
-#pragma unroll
-                    for (int u = 0; u < 4; ++u) {
-                        const uint32_t lo = (w[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (w[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                        if (lo | hi) { w[u] &= ~(lo | hi); atomicOr(&s_bad[r >> 5], 1u << (r & 31)); }
-                    }
-                }
-                const int off = (c >> 3) * VHALF + r * 128 + (((c & 7) ^ (r & 7)) << 4);
-                *reinterpret_cast<uint4*>(ring + off) = kx;
-                *reinterpret_cast<uint4*>(ring + SLOT + off) = vx;
-            }
-            fence_proxy_async_smem();
+            stage_draft<D>(cv, dv, b, kh, n, ring, ring + SLOT, VHALF, s_bad, st_tid, 128);
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (st_tid == 0) { mbar_arrive(bar(FULL)); mbar_arrive(bar(FULL + 1)); }
         }
@@ -257,7 +167,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const uint32_t tmS = tmem + 64 * (j & 1) + lane_off;
             const bool draft = t.draft && j == 0;
             int row0 = 0, valid = kKeys;
-            if (!draft) cached_tile(t, j, row0, valid);
+            if (!draft) cached_tile<kKeys>(t, j, row0, valid);
             if (!mbar_wait(bar(S_FULL + (j & 1)), (j >> 1) & 1)) { ok = false; break; }
             tc_fence_after();
             if (live) {
@@ -312,16 +222,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 tmem_st_wait();
             }
             if (!draft && valid < kKeys) {
-                // rows of the slab that hold no token of this unit may hold anything: their weight is zero, their values
-                // must not be NaN
                 const int x = 2 * j + 1, slot = x % slots;
                 if (!mbar_wait(bar(FULL + slot), (x / slots) & 1)) { ok = false; break; }
-                unsigned char* v = base_ptr + HALVES * q_rows * 128 + slot * SLOT;
-                for (int e = st_tid; e < (kKeys - valid) * (D / 8); e += 128) {
-                    const int r = valid + e / (D / 8), c = e % (D / 8);
-                    *reinterpret_cast<uint4*>(v + (c >> 3) * VHALF + r * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
-                }
-                fence_proxy_async_smem();
+                clear_rows<D, kKeys>(base_ptr + HALVES * q_rows * 128 + slot * SLOT, valid, st_tid, 128);
             }
             tc_fence_before();
             __syncwarp();
@@ -333,120 +236,26 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     }
     __syncwarp();
 
+    const uint64_t bad_here = (uint64_t)s_bad[0] | (uint64_t)s_bad[1] << 32;
+    const int quarter = warp & 3, row = quarter * 32 + lane;
+    const bool has_rows = warp >= 2 && quarter * 32 < rows;  // of the warp
+    const uint32_t tmOq = tmO + ((uint32_t)(quarter * 32) << 16);
     if (split == 1) {
-        // ---- a thread's row is complete: out it goes, 64 bytes at a time
-        if (warp >= 2) {
-            const int quarter = warp & 3, row = quarter * 32 + lane;
-            if (quarter * 32 < rows) {
-                const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-                const int tok = min((r0 + row) / G, n - 1), h = (r0 + row) % G;
-                const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
-                const float inv = l_run == 0.f ? 0.f : 1.0f / l_run;  // 0: the row sees nothing
-                const uint64_t bad = ((uint64_t)s_bad[0] | (uint64_t)s_bad[1] << 32) & (row < rows ? draft_sees(dv, b, tok, n) : 0ull);
-#pragma unroll
-                for (int cg = 0; cg < D / 32; ++cg) {
-                    uint32_t o[32];
-                    tmem_ld32(tmO + lane_off + cg * 32, o);
-                    tmem_ld_wait_for(o);
-                    if (row < rows) {
-                        float x[32];
-#pragma unroll
-                        for (int e = 0; e < 32; ++e) x[e] = __uint_as_float(o[e]) * inv;
-                        for (uint64_t left = bad; left; left &= left - 1) add_not_finite<32, D>(x, cv, dv, b, kh, __ffsll((long long)left) - 1, cg * 32);
-                        uint4* dst = reinterpret_cast<uint4*>(out + at * D + cg * 32);
-#pragma unroll
-                        for (int e = 0; e < 4; ++e)
-                            dst[e] = make_uint4(rope_pack_bf16(x[8 * e], x[8 * e + 1]), rope_pack_bf16(x[8 * e + 2], x[8 * e + 3]),
-                                                rope_pack_bf16(x[8 * e + 4], x[8 * e + 5]), rope_pack_bf16(x[8 * e + 6], x[8 * e + 7]));
-                    }
-                }
-                if (lse && row < rows) lse[at] = l_run == 0.f ? -INFINITY : (m_ref + log2f(l_run)) * (1.0f / kLog2e);
-                tc_fence_before();
-            }
-        }
-        __syncthreads();
-        if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
-        return;
-    }
-    // ---- the cluster's partial results meet: a block joins rpo rows, and gets from every block m, l and O of those rows
-    const int rpo = (rows + split - 1) / split;
-    const uint32_t sPart = base, sStat = base + split * rpo * PITCH * 4;  // [split][rpo][PITCH], [split][rpo][2]
-    cluster_sync_all();  // (1) every block's tiles are consumed
-    if (warp >= 2) {
-        const int quarter = warp & 3, row = quarter * 32 + lane;
-        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
-        if (quarter * 32 < rows) {
-            const int owner = row / rpo, at = rank * rpo + row % rpo;
-            const uint32_t dst = map_to_cta(sPart, min(owner, split - 1)) + at * PITCH * 4;
-#pragma unroll
-            for (int cg = 0; cg < D / 32; ++cg) {
-                uint32_t o[32];
-                if (NT > 0) { tmem_ld32(tmO + lane_off + cg * 32, o); tmem_ld_wait_for(o); }
-                if (row < rows) {
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const bool z = NT == 0;
-                        st_remote_v4(dst + (cg * 32 + e) * 4, z ? 0.f : __uint_as_float(o[e]), z ? 0.f : __uint_as_float(o[e + 1]),
-                                     z ? 0.f : __uint_as_float(o[e + 2]), z ? 0.f : __uint_as_float(o[e + 3]));
-                    }
-                }
-            }
-            if (row < rows) st_remote_v2(map_to_cta(sStat, min(owner, split - 1)) + at * 8, m_ref, l_run);
-        }
-        if (t.draft && tid - 64 < split)
+        if (has_rows) store_row<D>(cv, dv, b, kh, n, r0 + row, row < rows, tmOq, m_ref, l_run, bad_here, out, lse);
+    } else {
+        const int rpo = (rows + split - 1) / split;
+        cluster_sync_all();  // every block's tiles are consumed: shared memory takes the parts
+        if (has_rows) send_row<D>(base, split, rpo, rank, row, row < rows, NT > 0, tmOq, m_ref, l_run);
+        if (t.draft && warp >= 2 && tid - 64 < split)
             st_remote_v2(map_to_cta(smem_addr_u32(s_bad_all), tid - 64), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
-    }
-    __syncwarp();
-    cluster_sync_all();  // (2) all parts have arrived
-    {
-        const float* part = reinterpret_cast<const float*>(base_ptr);
-        const float* stat = part + split * rpo * PITCH;
+        __syncwarp();
+        cluster_sync_all();  // all parts have arrived
         const uint64_t bad = (uint64_t)__float_as_uint(s_bad_all[0]) | (uint64_t)__float_as_uint(s_bad_all[1]) << 32;
-        constexpr int LPR = D / 8;  // threads per row, eight channels each
-        for (int e = tid; e < rpo * LPR; e += kThreads) {
-            const int rl = e / LPR, c = e % LPR, row = rank * rpo + rl;
-            if (row >= rows) continue;
-            float M = -INFINITY;
-            for (int s = 0; s < split; ++s) M = fmaxf(M, stat[(s * rpo + rl) * 2]);
-            float l = 0.f, o[8];
-#pragma unroll
-            for (int u = 0; u < 8; ++u) o[u] = 0.f;
-            for (int s = 0; s < split; ++s) {
-                const float ms = stat[(s * rpo + rl) * 2];
-                const float f = ms == -INFINITY ? 0.f : ex2(ms - M);
-                l += stat[(s * rpo + rl) * 2 + 1] * f;
-                const float4 x = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8);
-                const float4 y = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8 + 4);
-                o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
-                o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
-            }
-            const float inv = l == 0.f ? 0.f : 1.0f / l;  // l = 0: the row sees nothing
-            const int tok = (r0 + row) / G, h = (r0 + row) % G;
-#pragma unroll
-            for (int u = 0; u < 8; ++u) o[u] *= inv;
-            if (bad)
-                for (uint64_t left = bad & draft_sees(dv, b, tok, n); left; left &= left - 1)
-                    add_not_finite<8, D>(o, cv, dv, b, kh, __ffsll((long long)left) - 1, c * 8);
-            const size_t at = ((size_t)b * dv.stride + tok) * cv.Hq + kh * G + h;
-            *reinterpret_cast<uint4*>(out + at * D + c * 8) =
-                make_uint4(rope_pack_bf16(o[0], o[1]), rope_pack_bf16(o[2], o[3]), rope_pack_bf16(o[4], o[5]), rope_pack_bf16(o[6], o[7]));
-            if (lse && c == 0) lse[at] = l == 0.f ? -INFINITY : (M + log2f(l)) * (1.0f / kLog2e);
-        }
+        join_rows<D>(cv, dv, b, kh, n, r0, rows, reinterpret_cast<const float*>(base_ptr), split, rpo, rank, bad, out, lse, tid, kThreads);
     }
+    tc_fence_before();
     __syncthreads();
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
-}
-
-// Blocks of a cluster (key splits): the machine holds two blocks per SM; a split costs every block its start and end,
-// worth about four tiles, once more.
-int pick_split(long blocks, int tiles, int sms) {
-    int best = 1;
-    long least = -1;
-    for (int s = 1; s <= kMaxSplit; s *= 2) {
-        const long waves = (blocks * s + 2L * sms - 1) / (2L * sms), cost = waves * ((tiles + s - 1) / s + 4);
-        if (least < 0 || cost < least) { least = cost; best = s; }
-    }
-    return best;
 }
 
 template <int D>
@@ -454,10 +263,7 @@ cudaError_t launch_t(const CacheView& cv, const CUtensorMap& tmK, const CUtensor
                      void* out, float* lse, int sms, cudaStream_t stream) {
     const int G = cv.Hq / cv.Hkv, box = std::min(128 / G, dv.stride);
     CUtensorMap tmQ;
-    const uint64_t dims[3] = {(uint64_t)D, (uint64_t)cv.Hq, (uint64_t)cv.B * dv.stride};
-    const uint64_t strides[2] = {(uint64_t)D * 2, (uint64_t)cv.Hq * D * 2};
-    const uint32_t boxes[3] = {64u, (uint32_t)G, (uint32_t)box};
-    if (!make_tensor_map_bf16(&tmQ, dv.q, 3, dims, strides, boxes)) return cudaErrorInvalidValue;
+    if (!make_q_map(&tmQ, cv, dv, box)) return cudaErrorInvalidValue;
     const int q_rows = box * G <= 32 ? 32 : box * G <= 64 ? 64 : 128;
     const size_t q_area = (size_t)(D / 64) * q_rows * 128, slot = (size_t)kKeys * D * 2;
     const int slots = (int)std::min<size_t>(kMaxSlots, (kSmemMax - 1024 - q_area) / slot);
@@ -475,7 +281,7 @@ cudaError_t launch_t(const CacheView& cv, const CUtensorMap& tmK, const CUtensor
         smem_set[dev] = true;
     }
     const int tiles_r = (max_n * G + 127) / 128;
-    const int split = pick_split((long)cv.B * cv.Hkv * tiles_r, (cv.c + kKeys - 1) / kKeys + 2, sms);
+    const int split = pick_split((long)cv.B * cv.Hkv * tiles_r, (cv.c + kKeys - 1) / kKeys + 2, 2L * sms, 4, kMaxSplit);
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(split, tiles_r, cv.B * cv.Hkv);
     cfg.blockDim = dim3(kThreads);
