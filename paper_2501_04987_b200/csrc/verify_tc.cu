@@ -37,7 +37,10 @@ constexpr size_t kSmemMin = 80 * 1024;     // never a third block on an SM: it w
 constexpr size_t kSmemMax = 112 * 1024;
 static_assert(kKeys == kMaxDraft, "the drafted tokens are one tile");
 
-enum Bar { Q_FULL = 0, S_FULL = 1, P_FULL = 3, PV_DONE = 5, FULL = 6, EMPTY = FULL + kMaxSlots, N_BARS = EMPTY + kMaxSlots };
+// FULL: a slot's tile has arrived.  USED: the MMAs that read it are done - for a K tile that also says that its logits are
+// there, for a V tile that its share of O is in: one commit and one barrier for both (a commit holds the issuing thread
+// for some 80 cycles).
+enum Bar { Q_FULL = 0, P_FULL = 1, FULL = 3, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -63,9 +66,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
 
     if (tid == 0) {
-        mbar_init(bar(Q_FULL), 1); mbar_init(bar(PV_DONE), 1);
-        for (int s = 0; s < 2; ++s) { mbar_init(bar(S_FULL + s), 1); mbar_init(bar(P_FULL + s), 4); }
-        for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(EMPTY + s), 1); }
+        mbar_init(bar(Q_FULL), 1);
+        for (int s = 0; s < 2; ++s) mbar_init(bar(P_FULL + s), 4);
+        for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(USED + s), 1); }
         s_bad[0] = s_bad[1] = 0u;
         mbar_fence_init();
     }
@@ -89,7 +92,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 tma_load_3d(sQ + h * q_rows * 128, &tmQ, 64 * h, kh * G, b * dv.stride + r0 / G, bar(Q_FULL));
             int issued = 0;
             for (Ring r(t.draft ? 2 : 0, slots); r.x < 2 * NT; r.next()) {
-                if (!mbar_wait(bar(EMPTY + r.slot), r.phase ^ 1)) { ok = false; break; }
+                if (!mbar_wait(bar(USED + r.slot), r.phase ^ 1)) { ok = false; break; }
                 int row0, valid;
                 cached_tile<kKeys>(t, r.x >> 1, row0, valid);
                 const int grow = unit * cv.R + row0;
@@ -113,39 +116,37 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, VHALF), q_half = q_rows * 128 / 16;
             Ring rk(0, slots), rv(1, slots);
             auto issue_s = [&](int buf) {  // the next tile's logits
-                if (!(ok = ok && mbar_wait(bar(FULL + rk.slot), rk.phase))) return;
                 tc_fence_after();
                 const uint32_t lo = k_lo + rk.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
                     umma_bf16(tmem + 64 * buf, desc_of(q_lo + (kk >> 2) * q_half + (kk & 3) * 2),
                               desc_of(lo + (kk >> 2) * (VHALF / 16) + (kk & 3) * 2), idesc_s, kk > 0);
-                umma_commit(bar(EMPTY + rk.slot));
-                umma_commit(bar(S_FULL + buf));
+                umma_commit(bar(USED + rk.slot));
                 rk.next(); rk.next();
             };
-            ok = mbar_wait(bar(Q_FULL), 0);
-            issue_s(0);
-            if (NT > 1) issue_s(1);
+            ok = mbar_wait2(bar(Q_FULL), 0, bar(FULL + rk.slot), rk.phase);
+            if (ok) issue_s(0);
+            if (ok && NT > 1 && (ok = mbar_wait(bar(FULL + rk.slot), rk.phase))) issue_s(1);
+            int last = 0, last_phase = 0;
             for (int j = 0; j < NT && ok; ++j) {
                 const int buf = j & 1;
-                ok = mbar_wait(bar(FULL + rv.slot), rv.phase) && mbar_wait(bar(P_FULL + buf), (j >> 1) & 1);
-                if (!ok) break;
+                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + buf), (j >> 1) & 1))) break;
                 tc_fence_after();
                 const uint32_t lo = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < kKeys / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes, 8 columns of packed P
                     umma_bf16_ta(tmO, tmem + 64 * buf + 8 * kk, desc_of(lo + kk * (2048 / 16)), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
-                umma_commit(bar(EMPTY + rv.slot));
-                umma_commit(bar(PV_DONE));
+                last = rv.slot; last_phase = rv.phase;
+                umma_commit(bar(USED + last));
                 rv.next(); rv.next();
                 if (j + 2 < NT) {  // the logits of tile j + 2 overwrite P_j
-                    if (!(ok = mbar_wait(bar(PV_DONE), buf))) break;
+                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(USED + last), last_phase))) break;
                     issue_s(buf);
                 }
             }
             // every MMA of this block has finished before its memory and tensor memory are given to anything else
-            if (ok) ok = mbar_wait(bar(PV_DONE), (NT - 1) & 1);
+            if (ok) ok = mbar_wait(bar(USED + last), last_phase);
             if (!ok) atomicOr(&cv.stats->error, 8u);
         }
     } else {
@@ -163,12 +164,14 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (st_tid == 0) { mbar_arrive(bar(FULL)); mbar_arrive(bar(FULL + 1)); }
         }
+        Ring rk(0, slots), rv(1, slots);  // this tile's K and V
+        int done = 0, done_phase = 0;     // V of the tile before
         for (int j = 0; j < NT && ok; ++j) {
             const uint32_t tmS = tmem + 64 * (j & 1) + lane_off;
             const bool draft = t.draft && j == 0;
             int row0 = 0, valid = kKeys;
             if (!draft) cached_tile<kKeys>(t, j, row0, valid);
-            if (!mbar_wait(bar(S_FULL + (j & 1)), (j >> 1) & 1)) { ok = false; break; }
+            if (!mbar_wait(bar(USED + rk.slot), rk.phase)) { ok = false; break; }
             tc_fence_after();
             if (live) {
                 uint32_t s0[32], s1[32];
@@ -194,7 +197,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     const float f = grow ? ex2(m_ref - mx) : 1.f;
                     if (grow) { m_ref = mx; l_run *= f; }
                     if (j > 0) {
-                        if (!mbar_wait(bar(PV_DONE), (j - 1) & 1)) ok = false;
+                        if (!mbar_wait(bar(USED + done), done_phase)) ok = false;
                         tc_fence_after();
 #pragma unroll
                         for (int cg = 0; cg < D / 32; ++cg) {
@@ -222,15 +225,16 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 tmem_st_wait();
             }
             if (!draft && valid < kKeys) {
-                const int x = 2 * j + 1, slot = x % slots;
-                if (!mbar_wait(bar(FULL + slot), (x / slots) & 1)) { ok = false; break; }
-                clear_rows<D, kKeys>(base_ptr + HALVES * q_rows * 128 + slot * SLOT, valid, st_tid, 128);
+                if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
+                clear_rows<D, kKeys>(base_ptr + HALVES * q_rows * 128 + rv.slot * SLOT, valid, st_tid, 128);
             }
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(P_FULL + (j & 1)));
+            done = rv.slot; done_phase = rv.phase;
+            rk.next(); rk.next(); rv.next(); rv.next();
         }
-        if (ok && NT > 0) ok = mbar_wait(bar(PV_DONE), (NT - 1) & 1);
+        if (ok && NT > 0) ok = mbar_wait(bar(USED + done), done_phase);
         if (!ok && lane == 0) atomicOr(&cv.stats->error, 16u);
         tc_fence_after();
     }

@@ -68,6 +68,20 @@ struct Ring {
     __device__ void next() { ++x; if (++slot == slots) { slot = 0; phase ^= 1; } }
 };
 
+// Two barriers at once, bounded: one check of a barrier takes about 160 cycles even when there is nothing to wait for, and
+// the two overlap.
+__device__ inline bool mbar_wait2(uint32_t bar_a, uint32_t par_a, uint32_t bar_b, uint32_t par_b) {
+    uint32_t a, b;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 p, [%2], %3;\n\t"
+        "mbarrier.try_wait.parity.shared::cta.b64 q, [%4], %5;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t"
+        "selp.u32 %1, 1, 0, q;\n\t}"
+        : "=r"(a), "=r"(b) : "r"(bar_a), "r"(par_a), "r"(bar_b), "r"(par_b) : "memory");
+    return (a || mbar_wait(bar_a, par_a)) && (b || mbar_wait(bar_b, par_b));
+}
+
 // Shared-memory matrix descriptor as two words: the low one holds the address and the leading offset, and moves by bytes /
 // 16; the high one - stride 1024, the version, 128-byte swizzle - is the same for all tiles.
 constexpr uint32_t kDescHi = (1024u >> 4) | 1u << 14 | 2u << 29;
