@@ -56,8 +56,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     __shared__ uint32_t tmem_slot;
-    __shared__ uint32_t s_bad[2];       // drafted tokens with a value that is not finite (this block staged them)
-    __shared__ __align__(8) float s_bad_all[2];  // the same, from the block that did
+    __shared__ __align__(8) uint32_t s_bad[2];       // drafted tokens with a value that is not finite (this block staged them)
     const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* base_ptr = smem_raw + (base - smem_addr_u32(smem_raw));
     const uint32_t sQ = base, sRing = base + HALVES * q_rows * 128;
@@ -247,15 +246,18 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (split == 1) {
         if (has_rows) store_row<D>(cv, dv, b, kh, n, r0 + row, row < rows, tmOq, m_ref, l_run, bad_here, out, lse);
     } else {
-        const int rpo = (rows + split - 1) / split;
-        cluster_sync_all();  // every block's tiles are consumed: shared memory takes the parts
-        if (has_rows) send_row<D>(base, split, rpo, rank, row, row < rows, NT > 0, tmOq, m_ref, l_run);
-        if (t.draft && warp >= 2 && tid - 64 < split)
-            st_remote_v2(map_to_cta(smem_addr_u32(s_bad_all), tid - 64), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
+        __syncthreads();  // this block's tiles are consumed: its shared memory takes its part
+        if (has_rows) keep_row<D>(reinterpret_cast<float*>(base_ptr), row, row < rows, NT > 0, tmOq, m_ref, l_run);
         __syncwarp();
-        cluster_sync_all();  // all parts have arrived
-        const uint64_t bad = (uint64_t)__float_as_uint(s_bad_all[0]) | (uint64_t)__float_as_uint(s_bad_all[1]) << 32;
-        join_rows<D>(cv, dv, b, kh, n, r0, rows, reinterpret_cast<const float*>(base_ptr), split, rpo, rank, bad, out, lse, tid, kThreads);
+        cluster_sync_all();  // all parts are there
+        const int all = t.nA + t.nB + 1, drafted = (all - 1) / ((all + split - 1) / split);  // the block with the drafted tile
+        const float2 bad2 = ld_remote_v2(map_to_cta(smem_addr_u32(s_bad), drafted));
+        const uint64_t bad = (uint64_t)__float_as_uint(bad2.x) | (uint64_t)__float_as_uint(bad2.y) << 32;
+        if (split == 8) join_rows<D, 8>(cv, dv, b, kh, n, r0, rows, base, rank, bad, out, lse, tid, kThreads);
+        else if (split == 4) join_rows<D, 4>(cv, dv, b, kh, n, r0, rows, base, rank, bad, out, lse, tid, kThreads);
+        else join_rows<D, 2>(cv, dv, b, kh, n, r0, rows, base, rank, bad, out, lse, tid, kThreads);
+        __syncwarp();
+        cluster_sync_all();  // nobody leaves while its part may be read
     }
     tc_fence_before();
     __syncthreads();

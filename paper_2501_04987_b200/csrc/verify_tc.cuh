@@ -167,13 +167,22 @@ __device__ inline void store_row(const CacheView& cv, const DraftView& dv, int b
 }
 
 // ---- Keys of a unit dealt to a cluster: every block has m, l and O of all its rows (the first is r0 of the unit) at its own
-// reference.  Block q joins rows [q rpo, (q + 1) rpo); the others' parts come to it through shared memory:
-// [split][rpo][D + 4] floats at `part`, then [split][rpo][2].
+// reference, and leaves them in its shared memory: [128][D + 4] floats, then [128][2].  Block q joins rows [q rpo, (q + 1) rpo),
+// reading the others' parts there (stores into the owner's memory took twice as long: 96 rows of eight blocks 4300 cycles).
+__device__ inline float4 ld_remote_v4(uint32_t caddr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(caddr) : "memory");
+    return v;
+}
+__device__ inline float2 ld_remote_v2(uint32_t caddr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(caddr) : "memory");
+    return v;
+}
+constexpr int kPartRows = 128;
 template <int D>
-__device__ inline void send_row(uint32_t part, int split, int rpo, int rank, int row, bool real, bool any, uint32_t tm, float m, float l) {
+__device__ inline void keep_row(float* part, int row, bool real, bool any, uint32_t tm, float m, float l) {
     constexpr int PITCH = D + 4;
-    const int owner = min(row / rpo, split - 1), at = rank * rpo + row % rpo;
-    const uint32_t dst = map_to_cta(part, owner) + at * PITCH * 4;
 #pragma unroll
     for (int cg = 0; cg < D / 32; ++cg) {
         uint32_t o[32];
@@ -181,34 +190,49 @@ __device__ inline void send_row(uint32_t part, int split, int rpo, int rank, int
         if (real) {
 #pragma unroll
             for (int e = 0; e < 32; e += 4)
-                st_remote_v4(dst + (cg * 32 + e) * 4, any ? __uint_as_float(o[e]) : 0.f, any ? __uint_as_float(o[e + 1]) : 0.f,
-                             any ? __uint_as_float(o[e + 2]) : 0.f, any ? __uint_as_float(o[e + 3]) : 0.f);
+                *reinterpret_cast<float4*>(part + row * PITCH + cg * 32 + e) =
+                    any ? make_float4(__uint_as_float(o[e]), __uint_as_float(o[e + 1]), __uint_as_float(o[e + 2]), __uint_as_float(o[e + 3]))
+                        : make_float4(0.f, 0.f, 0.f, 0.f);
         }
     }
-    if (real) st_remote_v2(map_to_cta(part + split * rpo * PITCH * 4, owner) + at * 8, m, l);
+    if (real) *reinterpret_cast<float2*>(part + kPartRows * PITCH + row * 2) = make_float2(m, l);
 }
-template <int D>
-__device__ inline void join_rows(const CacheView& cv, const DraftView& dv, int b, int kh, int n, int r0, int rows, const float* part, int split,
-                                 int rpo, int rank, uint64_t bad, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, int t, int nthr) {
+template <int D, int SPLIT>
+__device__ inline void join_rows(const CacheView& cv, const DraftView& dv, int b, int kh, int n, int r0, int rows, uint32_t part, int rank,
+                                 uint64_t bad, __nv_bfloat16* __restrict__ out, float* __restrict__ lse, int t, int nthr) {
     constexpr int PITCH = D + 4, LPR = D / 8;  // threads per row, eight channels each
-    const int G = cv.Hq / cv.Hkv;
-    const float* stat = part + split * rpo * PITCH;
+    const int G = cv.Hq / cv.Hkv, rpo = (rows + SPLIT - 1) / SPLIT;
+    uint32_t peer[SPLIT];
+#pragma unroll
+    for (int s = 0; s < SPLIT; ++s) peer[s] = map_to_cta(part, s);
     for (int e = t; e < rpo * LPR; e += nthr) {
         const int rl = e / LPR, c = e % LPR, row = rank * rpo + rl;
         if (row >= rows) continue;
+        float2 stat[SPLIT];
         float M = -INFINITY;
-        for (int s = 0; s < split; ++s) M = fmaxf(M, stat[(s * rpo + rl) * 2]);
+#pragma unroll
+        for (int s = 0; s < SPLIT; ++s) stat[s] = ld_remote_v2(peer[s] + (kPartRows * PITCH + row * 2) * 4);
+#pragma unroll
+        for (int s = 0; s < SPLIT; ++s) M = fmaxf(M, stat[s].x);
         float l = 0.f, o[8];
 #pragma unroll
         for (int u = 0; u < 8; ++u) o[u] = 0.f;
-        for (int s = 0; s < split; ++s) {
-            const float ms = stat[(s * rpo + rl) * 2];
-            const float f = ms == -INFINITY ? 0.f : ex2(ms - M);
-            l += stat[(s * rpo + rl) * 2 + 1] * f;
-            const float4 x = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8);
-            const float4 y = *reinterpret_cast<const float4*>(part + (s * rpo + rl) * PITCH + c * 8 + 4);
-            o[0] += x.x * f; o[1] += x.y * f; o[2] += x.z * f; o[3] += x.w * f;
-            o[4] += y.x * f; o[5] += y.y * f; o[6] += y.z * f; o[7] += y.w * f;
+#pragma unroll
+        for (int s0 = 0; s0 < SPLIT; s0 += 4) {
+            constexpr int W = SPLIT < 4 ? SPLIT : 4;  // parts on their way at a time
+            float4 x[W], y[W];
+#pragma unroll
+            for (int s = 0; s < W; ++s) {
+                x[s] = ld_remote_v4(peer[s0 + s] + (row * PITCH + c * 8) * 4);
+                y[s] = ld_remote_v4(peer[s0 + s] + (row * PITCH + c * 8 + 4) * 4);
+            }
+#pragma unroll
+            for (int s = 0; s < W; ++s) {
+                const float ms = stat[s0 + s].x, f = ms == -INFINITY ? 0.f : ex2(ms - M);
+                l += stat[s0 + s].y * f;
+                o[0] += x[s].x * f; o[1] += x[s].y * f; o[2] += x[s].z * f; o[3] += x[s].w * f;
+                o[4] += y[s].x * f; o[5] += y[s].y * f; o[6] += y[s].z * f; o[7] += y[s].w * f;
+            }
         }
         const float inv = l == 0.f ? 0.f : 1.0f / l;  // l = 0: the row sees nothing
         const int tok = (r0 + row) / G, h = (r0 + row) % G;
