@@ -8,7 +8,8 @@
 // the path's queries, 8 at a time, as its columns.  The contraction runs over channels in any order, so a lane's fragments
 // are 16-byte pieces of the rows (channels 32u + 8t.. of keys g and g + 8, of query g): no transposition.  A warp has a
 // ring of its own in shared memory, filled by bulk copies - 16 keys are 4 KB in one piece, or two at the ends of the cached
-// segments - and no other warp to wait for.  fp32: a thread per key, queries broadcast from shared memory.
+// segments - and no other warp to wait for.  fp32: tiles of 64 keys and 32 query rows in shared memory, a thread two rows
+// against four keys.
 #include <cooperative_groups.h>
 
 #include "draft.cuh"
@@ -21,7 +22,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxDepth = 3;  // tiles of 16 keys a warp has on their way
-constexpr int kStage32 = 32;  // fp32: query rows in shared memory at a time
+constexpr int kRows32 = 32, kKeys32 = 64;  // fp32: query rows and keys in shared memory at a time
 
 __device__ inline float ex2(float x) {
     float y;
@@ -194,67 +195,129 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
     if (!ok && lane == 0) atomicOr(&cv.stats->error, 4u);
 }
 
+// fp32, shared memory: [kRows32][D + 4] queries, two tiles [kKeys32][D + 4] of keys, [16][kKeys32] partial sums, [kRows32]
+// log-sum-exps, [keys of the block] sums
+template <int D> constexpr size_t f32_smem_floats(int keys) {
+    return (size_t)(kRows32 + 2 * kKeys32) * (D + 4) + 16 * kKeys32 + kRows32 + keys;
+}
 template <int D>
 __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, const Path& p, const float* __restrict__ lse, int rank, int nblocks,
                                   unsigned char* smem) {
-    float* sq = reinterpret_cast<float*>(smem);  // [kStage32][D]
-    float* s_lse = sq + kStage32 * D;
+    constexpr int PITCH = D + 4;
+    float* sq = reinterpret_cast<float*>(smem);
+    float* sk = sq + kRows32 * PITCH;                // [2][kKeys32][PITCH]
+    float* red = sk + 2 * kKeys32 * PITCH;           // [16][kKeys32]
+    float* s_lse = red + 16 * kKeys32;
+    float* sums = s_lse + kRows32;
     const int rows = p.n * p.G, tid = threadIdx.x, lg = __ffs(p.G) - 1;
+    const int per = (p.total + nblocks - 1) / nblocks, lo = min(rank * per, p.total), hi = min(lo + per, p.total);
     const float scale = kLog2e * rsqrtf((float)D);
-    for (int base = rank * kThreads; base < p.total; base += nblocks * kThreads) {
-        const int lam = base + tid, j = lam - p.st.L;
-        const float* krow = lam < p.total ? key_row<float, D>(cv, dv, p, lam) : nullptr;
-        float sum = 0.f;
-        for (int r0 = 0; r0 < rows; r0 += kStage32) {
-            __syncthreads();
-            for (int e = tid; e < kStage32 * (D / 2); e += kThreads) {  // queries: encoded at their slots, scaled
-                const int r = r0 + e / (D / 2), c = e % (D / 2);
-                float x = 0.f, y = 0.f;
-                if (r < rows) {
-                    const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
-                    const float* row = reinterpret_cast<const float*>(dv.q) + at * D;
-                    x = row[c]; y = row[c + D / 2];
-                    if (cv.rope_cos) {
-                        const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c;
-                        const float cs = __ldg(cv.rope_cos + tab), sn = __ldg(cv.rope_sin + tab), x1 = x, x2 = y;
-                        x = __fmaf_rn(x1, cs, -__fmul_rn(x2, sn));
-                        y = __fmaf_rn(x2, cs, __fmul_rn(x1, sn));
-                    }
-                    if (c == 0) s_lse[r - r0] = lse[at] * kLog2e;
-                }
-                sq[(r - r0) * D + c] = x * scale; sq[(r - r0) * D + c + D / 2] = y * scale;
+    const int r0 = tid / 16 * 2, l16 = tid % 16;     // this thread's two rows; its keys l16 + 16 i
+    auto load_k = [&](int k0, int buf) {
+        float* dst = sk + buf * kKeys32 * PITCH;
+        const int kn = min(kKeys32, hi - k0);
+        if (!cv.rope_cos) {
+            for (int e = tid; e < kn * (D / 4); e += kThreads) {
+                const int r = e / (D / 4), c = e % (D / 4);
+                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr_u32(dst + r * PITCH + c * 4)),
+                             "l"(key_row<float, D>(cv, dv, p, k0 + r) + c * 4) : "memory");
             }
-            __syncthreads();
-            if (lam < p.total) {
-                for (int r8 = 0; r8 < kStage32 && r0 + r8 < rows; r8 += 8) {
-                    float a[8];
-#pragma unroll
-                    for (int r = 0; r < 8; ++r) a[r] = 0.f;
-                    for_key_row<float, D>(krow, cv, lam, [&](int c, const float (&x)[4]) {
-#pragma unroll
-                        for (int r = 0; r < 8; ++r) {
-                            const float4 q4 = *reinterpret_cast<const float4*>(sq + (r8 + r) * D + c);
-                            a[r] = fmaf(q4.x, x[0], fmaf(q4.y, x[1], fmaf(q4.z, x[2], fmaf(q4.w, x[3], a[r]))));
-                        }
-                    });
-#pragma unroll
-                    for (int r = 0; r < 8; ++r)
-                        if (r0 + r8 + r < rows && ((r0 + r8 + r) >> lg) >= j) sum += exp2f(a[r] - s_lse[r8 + r]);
-                }
+        } else {
+            for (int e = tid; e < kn * (D / 8); e += kThreads) {
+                const int r = e / (D / 8), c = e % (D / 8);
+                const float* row = key_row<float, D>(cv, dv, p, k0 + r);
+                float x[4], y[4];
+                Elem<float>::unpack(ld_plain(row + c * 4), x);
+                Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
+                const size_t at = (size_t)(k0 + r) * (D / 2) + c * 4;
+                rope_pairs<float>(x, y, cv.rope_cos + at, cv.rope_sin + at);
+                *reinterpret_cast<float4*>(dst + r * PITCH + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(dst + r * PITCH + D / 2 + c * 4) = make_float4(y[0], y[1], y[2], y[3]);
             }
         }
-        if (lam < p.total) {
-            const size_t row = (size_t)p.unit * cv.R + (j < 0 ? phys_row(lam, p.st) : lam + p.st.i);
-            cv.S[row] = (j < 0 ? cv.S[row] : 0.f) + sum * (1.0f / (float)p.G);
-            if (j >= 0) {  // append
-                const uint4* ks = reinterpret_cast<const uint4*>(krow);
-                const uint4* vs = reinterpret_cast<const uint4*>(reinterpret_cast<const float*>(dv.v) + draft_row<float, D>(cv, dv, p, j));
-                for (int e = 0; e < D / 4; ++e) {
-                    reinterpret_cast<uint4*>(cv.K)[row * (D / 4) + e] = ks[e];
-                    reinterpret_cast<uint4*>(cv.V)[row * (D / 4) + e] = vs[e];
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    for (int e = tid; e < hi - lo; e += kThreads) sums[e] = 0.f;
+    for (int c0 = 0; c0 < rows; c0 += kRows32) {     // 32 rows at a time over this block's keys
+        __syncthreads();
+        if (lo < hi) load_k(lo, 0);
+        for (int e = tid; e < kRows32 * (D / 8); e += kThreads) {  // queries: encoded at their slots, scaled
+            const int r = c0 + e / (D / 8), c = e % (D / 8);
+            float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
+            if (r < rows) {
+                const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
+                const float* row = reinterpret_cast<const float*>(dv.q) + at * D;
+                Elem<float>::unpack(ld_plain(row + c * 4), x);
+                Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
+                if (cv.rope_cos) {
+                    const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 4;
+                    rope_pairs<float>(x, y, cv.rope_cos + tab, cv.rope_sin + tab);
                 }
-                cv.pos[row] = p.N + j;
+                if (c == 0) s_lse[r - c0] = lse[at] * kLog2e;
+            } else if (c == 0) {
+                s_lse[r - c0] = INFINITY;  // weight 0
             }
+            float* dst = sq + (r - c0) * PITCH + c * 4;
+            *reinterpret_cast<float4*>(dst) = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
+            *reinterpret_cast<float4*>(dst + D / 2) = make_float4(y[0] * scale, y[1] * scale, y[2] * scale, y[3] * scale);
+        }
+        const bool live = c0 + r0 < rows;
+        int buf = 0;
+        for (int k0 = lo; k0 < hi; k0 += kKeys32, buf ^= 1) {
+            if (k0 + kKeys32 < hi) {
+                load_k(k0 + kKeys32, buf ^ 1);
+                asm volatile("cp.async.wait_group 1;" ::: "memory");
+            } else {
+                asm volatile("cp.async.wait_group 0;" ::: "memory");
+            }
+            __syncthreads();
+            float part[4] = {0.f, 0.f, 0.f, 0.f};
+            if (live) {
+                const float* kt = sk + buf * kKeys32 * PITCH + l16 * PITCH;
+                const float* qt = sq + r0 * PITCH;
+                float a[2][4] = {};
+#pragma unroll 4
+                for (int c = 0; c < D; c += 4) {
+                    const float4 q0 = *reinterpret_cast<const float4*>(qt + c), q1 = *reinterpret_cast<const float4*>(qt + PITCH + c);
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) {
+                        const float4 x = *reinterpret_cast<const float4*>(kt + 16 * k * PITCH + c);
+                        a[0][k] = fmaf(q0.x, x.x, fmaf(q0.y, x.y, fmaf(q0.z, x.z, fmaf(q0.w, x.w, a[0][k]))));
+                        a[1][k] = fmaf(q1.x, x.x, fmaf(q1.y, x.y, fmaf(q1.z, x.z, fmaf(q1.w, x.w, a[1][k]))));
+                    }
+                }
+#pragma unroll
+                for (int k = 0; k < 4; ++k) {
+                    const int j = k0 + l16 + 16 * k - p.st.L;  // a path token is seen from itself on
+#pragma unroll
+                    for (int r = 0; r < 2; ++r)
+                        if (((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k] - s_lse[r0 + r]);
+                }
+            }
+#pragma unroll
+            for (int k = 0; k < 4; ++k) red[(tid / 16) * kKeys32 + l16 + 16 * k] = part[k];
+            __syncthreads();  // the tile's shares are there, and nobody reads its keys any more
+            if (tid < kKeys32 && k0 + tid < hi) {
+                float x = 0.f;
+#pragma unroll
+                for (int g = 0; g < 16; ++g) x += red[g * kKeys32 + tid];
+                sums[k0 - lo + tid] += x;
+            }
+        }
+    }
+    __syncthreads();
+    for (int e = tid; e < hi - lo; e += kThreads) {
+        const int lam = lo + e;
+        const size_t row = (size_t)p.unit * cv.R + (lam < p.st.L ? phys_row(lam, p.st) : lam + p.st.i);
+        cv.S[row] = (lam < p.st.L ? cv.S[row] : 0.f) + sums[e] * (1.0f / (float)p.G);
+        if (lam >= p.st.L) cv.pos[row] = p.N + lam - p.st.L;
+    }
+    for (int e = tid; e < p.n * (D / 4); e += kThreads) {  // append
+        const int j = e / (D / 4), c = e % (D / 4), lam = p.st.L + j;
+        if (lam >= lo && lam < hi) {
+            const size_t row = ((size_t)p.unit * cv.R + lam + p.st.i) * (D / 4) + c, src = draft_row<float, D>(cv, dv, p, j) / 4 + c;
+            reinterpret_cast<uint4*>(cv.K)[row] = reinterpret_cast<const uint4*>(dv.k)[src];
+            reinterpret_cast<uint4*>(cv.V)[row] = reinterpret_cast<const uint4*>(dv.v)[src];
         }
     }
 }
@@ -303,7 +366,7 @@ cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse,
     const size_t queries = (size_t)rows8 * (q_pitch<D>() + 4);
     const size_t room = (queries + 2 * kRing <= kHalfSm ? kHalfSm : kSm) - queries;
     const int depth = (int)(room / kRing < kMaxDepth ? room / kRing : kMaxDepth);
-    const size_t smem = sizeof(T) == 2 ? queries + depth * kRing : (size_t)kStage32 * (D + 1) * 4;
+    const size_t smem = sizeof(T) == 2 ? queries + depth * kRing : f32_smem_floats<D>((cv.c + max_n + CL - 1) / CL) * 4;
     if (smem > 48 * 1024) {
         static bool smem_set[64] = {};  // per device: the opt-in is needed once
         int dev = 0;
@@ -339,9 +402,11 @@ template <typename T, int D, bool ROPE>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const float* lse, const int32_t* path, int path_stride, const DraftLens& lens,
                      int max_n, int sms, cudaStream_t s) {
     const long units = (long)cv.B * cv.Hkv;
-    const int keys = sizeof(T) == 2 ? kWarps * 16 : kThreads;
+    const int keys = sizeof(T) == 2 ? kWarps * 16 : 2 * kKeys32;
     int cl = 1;
     while (cl < 8 && units * cl < sms && cv.c / (2 * cl) >= keys) cl *= 2;
+    // (fp32: a block keeps its keys' sums in shared memory, and two blocks share an SM's)
+    while (sizeof(T) == 4 && cl < 8 && f32_smem_floats<D>((cv.c + max_n + cl - 1) / cl) * 4 > 112 * 1024) cl *= 2;
     switch (cl) {
         case 1: return launch_c<T, D, 1, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
         case 2: return launch_c<T, D, 2, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);

@@ -2,10 +2,10 @@
 //
 // Row r = token * G + head-in-group of one unit (sequence, KV head) attends to every cached row and to the drafted
 // tokens its mask names: out = softmax(q k / sqrt d) v in one pass over the keys with a running maximum and sum, all
-// fp32.  A block owns 32 rows and walks key tiles of 64 in shared memory.  A thread owns four rows (with the fifteen others
-// of its half-warp) and takes four keys of each tile for the logits, D / 16 channels for the output: 64 multiply-adds for
-// eight 16-byte reads of shared memory, most of them broadcasts, so the arithmetic is what bounds it once there are enough
-// rows.  A row's weights never leave its half-warp.  The next K tile is on its way while the weights meet V, the next V tile
+// fp32.  A block owns 8 RT rows and walks key tiles of 64 in shared memory.  A thread owns RT rows (with the fifteen others
+// of its half-warp) and takes four keys of each tile for the logits, D / 16 channels for the output: with four rows 64
+// multiply-adds for eight 16-byte reads of shared memory, most of them broadcasts, so the arithmetic is what bounds it once
+// there are enough rows.  RT follows the call's rows: every thread has some, and the keys are read by as few blocks as can be.  A row's weights never leave its half-warp.  The next K tile is on its way while the weights meet V, the next V tile
 // while the logits are made.  With few units the keys of a unit are dealt to a cluster of blocks, which join their partial
 // results in shared memory.
 #include "draft.cuh"
@@ -16,12 +16,12 @@ namespace treekv {
 namespace {
 
 constexpr int kThreads = 128;
-constexpr int kRows = 32, kKeys = 64;
+constexpr int kKeys = 64;
 constexpr int kMaxSplit = 8;
 
 template <int D> constexpr int k_pitch() { return D + 4; }  // floats: sixteen keys' 16-byte reads meet no conflict
-template <int D> constexpr size_t smem_bytes() {
-    return sizeof(float) * ((size_t)kRows * k_pitch<D>() + (size_t)kKeys * k_pitch<D>() + (size_t)kKeys * D + (size_t)kRows * (kKeys + 4));
+template <int D, int RT> constexpr size_t smem_bytes() {
+    return sizeof(float) * ((size_t)(8 * RT + kKeys) * k_pitch<D>() + (size_t)kKeys * D + (size_t)8 * RT * (kKeys + 4));
 }
 
 __device__ inline void cp_async_16(float* dst, const void* src) {
@@ -30,9 +30,10 @@ __device__ inline void cp_async_16(float* dst, const void* src) {
 __device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename T, int D>
+template <typename T, int D, int RT>
 __global__ void __launch_bounds__(kThreads, 2)
 verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ out, float* __restrict__ lse, int split) {
+    constexpr int kRows = 8 * RT;
     constexpr int VEC = Elem<T>::kVec, HALF = D / 2 / VEC, KP = k_pitch<D>(), PP = kKeys + 4, NC = D / 64;  // NC: float4s of a thread's channels
     pdl_trigger();
     pdl_wait();
@@ -138,13 +139,13 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         for (int u = 0; u < VEC; ++u) { sq[r * KP + c * VEC + u] = x[u] * scale; sq[r * KP + D / 2 + c * VEC + u] = y[u] * scale; }
     }
 
-    const int rg = tid / 16 * 4, l16 = tid % 16;   // this thread's four rows; its keys l16 + 16 i, its channels 4 l16 + 64 i
+    const int rg = tid / 16 * RT, l16 = tid % 16;  // this thread's rows; its keys l16 + 16 i, its channels 4 l16 + 64 i
     const bool live = rg < rows;                   // of the half-warp
     const uint32_t mine = 0xffffu << (threadIdx.x & 16);  // its lanes
-    float m[4], l[4];
-    float4 o[4][NC];
+    float m[RT], l[RT];
+    float4 o[RT][NC];
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
         for (int c = 0; c < NC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -153,27 +154,27 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         cp_async_wait<1>();   // K has arrived (V may still be on its way)
         __syncthreads();
         if (live) {
-            float a[4][4];
+            float a[RT][4];
 #pragma unroll
-            for (int r = 0; r < 4; ++r)
+            for (int r = 0; r < RT; ++r)
 #pragma unroll
                 for (int k = 0; k < 4; ++k) a[r][k] = 0.f;
 #pragma unroll 4
             for (int c = 0; c < D; c += 4) {
-                float4 q4[4], k4[4];
+                float4 q4[RT], k4[4];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) q4[r] = *reinterpret_cast<const float4*>(sq + (rg + r) * KP + c);
+                for (int r = 0; r < RT; ++r) q4[r] = *reinterpret_cast<const float4*>(sq + (rg + r) * KP + c);
 #pragma unroll
                 for (int k = 0; k < 4; ++k) k4[k] = *reinterpret_cast<const float4*>(sk + (l16 + 16 * k) * KP + c);
 #pragma unroll
-                for (int r = 0; r < 4; ++r)
+                for (int r = 0; r < RT; ++r)
 #pragma unroll
                     for (int k = 0; k < 4; ++k)
                         a[r][k] = fmaf(q4[r].x, k4[k].x, fmaf(q4[r].y, k4[k].y, fmaf(q4[r].z, k4[k].z, fmaf(q4[r].w, k4[k].w, a[r][k]))));
             }
             const bool all_seen = k0 + kKeys <= min(hi, st.L);
 #pragma unroll
-            for (int r = 0; r < 4; ++r) {
+            for (int r = 0; r < RT; ++r) {
                 if (!all_seen) {
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
@@ -204,16 +205,16 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         if (live) {
 #pragma unroll 2
             for (int k = 0; k < kKeys; k += 4) {
-                float4 p4[4];
+                float4 p4[RT];
 #pragma unroll
-                for (int r = 0; r < 4; ++r) p4[r] = *reinterpret_cast<const float4*>(sp + (rg + r) * PP + k);
+                for (int r = 0; r < RT; ++r) p4[r] = *reinterpret_cast<const float4*>(sp + (rg + r) * PP + k);
 #pragma unroll
                 for (int u = 0; u < 4; ++u) {
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
                         const float4 v4 = *reinterpret_cast<const float4*>(sv + (k + u) * D + 64 * c + 4 * l16);
 #pragma unroll
-                        for (int r = 0; r < 4; ++r) {
+                        for (int r = 0; r < RT; ++r) {
                             const float p = u == 0 ? p4[r].x : u == 1 ? p4[r].y : u == 2 ? p4[r].z : p4[r].w;
                             o[r][c].x = fmaf(p, v4.x, o[r][c].x); o[r][c].y = fmaf(p, v4.y, o[r][c].y);
                             o[r][c].z = fmaf(p, v4.z, o[r][c].z); o[r][c].w = fmaf(p, v4.w, o[r][c].w);
@@ -226,7 +227,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         if (k0 + kKeys < hi) load_v(k0 + kKeys);
     }
 #pragma unroll
-    for (int r = 0; r < 4; ++r)
+    for (int r = 0; r < RT; ++r)
 #pragma unroll
         for (int off = 8; off > 0; off >>= 1) l[r] += __shfl_xor_sync(mine, l[r], off, 16);
 
@@ -248,7 +249,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     };
     if (split == 1) {
 #pragma unroll
-        for (int r = 0; r < 4; ++r)
+        for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
                 if (rg + r < rows) finish(rg + r, 64 * c + 4 * l16, o[r][c], m[r], l[r]);
@@ -262,7 +263,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     __syncwarp();
     cluster_sync_all();   // every block is done with its tiles
 #pragma unroll
-    for (int r = 0; r < 4; ++r) {
+    for (int r = 0; r < RT; ++r) {
         const int row = rg + r;
         if (row < rows) {
             const int owner = row / rpo, at = rank * rpo + row % rpo;
@@ -294,26 +295,26 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     }
 }
 
-template <typename T, int D>
-cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
-    const int G = cv.Hq / cv.Hkv, tiles_r = (max_n * G + kRows - 1) / kRows, keys = cv.c + max_n;
+template <typename T, int D, int RT>
+cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
+    const int G = cv.Hq / cv.Hkv, tiles_r = (max_n * G + 8 * RT - 1) / (8 * RT), keys = cv.c + max_n;
     // Blocks of a cluster: until the machine holds two per SM, while each still has a tile of keys
     int split = 1;
     while (split < kMaxSplit && (long)cv.B * cv.Hkv * tiles_r * split < 2L * sms && keys > split * kKeys) split *= 2;
-    auto kern = verify_simt_kernel<T, D>;
+    auto kern = verify_simt_kernel<T, D, RT>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
     dev &= 63;
     if (!smem_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D>());
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, RT>());
         if (e != cudaSuccess) return e;
         smem_set[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(split, tiles_r, cv.B * cv.Hkv);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem_bytes<D>();
+    cfg.dynamicSmemBytes = smem_bytes<D, RT>();
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
@@ -325,6 +326,21 @@ cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& 
     cfg.attrs = attr;
     cfg.numAttrs = split > 1 ? 2 : 1;
     return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<T*>(out), lse, split);
+}
+
+// Rows per thread: the fewest tiles of at most 48 rows (D = 128: two blocks' shared memory fills an SM) or 64, and those even.
+template <typename T, int D>
+cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
+    const int groups = (max_n * (cv.Hq / cv.Hkv) + 7) / 8, most = D == 128 ? 6 : 8, tiles = (groups + most - 1) / most;
+    switch ((groups + tiles - 1) / tiles) {
+        case 1: return launch_rt<T, D, 1>(cv, dv, lens, max_n, out, lse, sms, s);
+        case 2: return launch_rt<T, D, 2>(cv, dv, lens, max_n, out, lse, sms, s);
+        case 3: return launch_rt<T, D, 3>(cv, dv, lens, max_n, out, lse, sms, s);
+        case 4: return launch_rt<T, D, 4>(cv, dv, lens, max_n, out, lse, sms, s);
+        case 5: return launch_rt<T, D, 5>(cv, dv, lens, max_n, out, lse, sms, s);
+        case 6: return launch_rt<T, D, 6>(cv, dv, lens, max_n, out, lse, sms, s);
+        default: return launch_rt<T, D, D == 128 ? 6 : 8>(cv, dv, lens, max_n, out, lse, sms, s);
+    }
 }
 
 }  // namespace
