@@ -275,15 +275,15 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
             if (live) {
                 const float* kt = sk + buf * kKeys32 * PITCH + l16 * PITCH;
                 const float* qt = sq + r0 * PITCH;
-                float a[2][4] = {};
+                float2 a[2][4] = {};  // even and odd channels
 #pragma unroll 4
                 for (int c = 0; c < D; c += 4) {
-                    const float4 q0 = *reinterpret_cast<const float4*>(qt + c), q1 = *reinterpret_cast<const float4*>(qt + PITCH + c);
+                    const Float22 q0 = *reinterpret_cast<const Float22*>(qt + c), q1 = *reinterpret_cast<const Float22*>(qt + PITCH + c);
 #pragma unroll
                     for (int k = 0; k < 4; ++k) {
-                        const float4 x = *reinterpret_cast<const float4*>(kt + 16 * k * PITCH + c);
-                        a[0][k] = fmaf(q0.x, x.x, fmaf(q0.y, x.y, fmaf(q0.z, x.z, fmaf(q0.w, x.w, a[0][k]))));
-                        a[1][k] = fmaf(q1.x, x.x, fmaf(q1.y, x.y, fmaf(q1.z, x.z, fmaf(q1.w, x.w, a[1][k]))));
+                        const Float22 x = *reinterpret_cast<const Float22*>(kt + 16 * k * PITCH + c);
+                        a[0][k] = fma2(q0.hi, x.hi, fma2(q0.lo, x.lo, a[0][k]));
+                        a[1][k] = fma2(q1.hi, x.hi, fma2(q1.lo, x.lo, a[1][k]));
                     }
                 }
 #pragma unroll
@@ -291,7 +291,7 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
                     const int j = k0 + l16 + 16 * k - p.st.L;  // a path token is seen from itself on
 #pragma unroll
                     for (int r = 0; r < 2; ++r)
-                        if (((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k] - s_lse[r0 + r]);
+                        if (((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k].x + a[r][k].y - s_lse[r0 + r]);
                 }
             }
 #pragma unroll

@@ -38,21 +38,15 @@ __device__ inline void rope_pairs(float (&x)[Elem<T>::kVec], float (&y)[Elem<T>:
     }
 }
 
-// One key row in fp32, `slot` >= 0: encoded at that slot (see rope_apply).  Piece c of VEC channels and its partner
-// c + half come together: f(channel, value) is called for both.
-template <typename T, int D, typename F>
-__device__ inline void for_key_row(const T* row, const CacheView& cv, int slot, F&& f) {
-    constexpr int VEC = Elem<T>::kVec, HALF = D / 2 / VEC;
-    for (int c = 0; c < HALF; ++c) {
-        float x[VEC], y[VEC];
-        Elem<T>::unpack(ld_plain(row + c * VEC), x);
-        Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
-        if (cv.rope_cos)
-            rope_pairs<T>(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
-        f(c * VEC, x);
-        f(D / 2 + c * VEC, y);
-    }
+// two fp32 multiply-adds in one instruction: (a.x b.x + c.x, a.y b.y + c.y)
+__device__ inline float2 fma2(float2 a, float2 b, float2 c) {
+    float2 d;
+    asm("fma.rn.f32x2 %0, %1, %2, %3;"
+        : "=l"(reinterpret_cast<unsigned long long&>(d))
+        : "l"(reinterpret_cast<unsigned long long&>(a)), "l"(reinterpret_cast<unsigned long long&>(b)), "l"(reinterpret_cast<unsigned long long&>(c)));
+    return d;
 }
+struct alignas(16) Float22 { float2 lo, hi; };  // four floats as the two pairs fma2() takes
 #endif
 
 // draft lengths of a verify call, accepted lengths of an accept call: 0..64

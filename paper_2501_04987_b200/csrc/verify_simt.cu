@@ -143,35 +143,39 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     const bool live = rg < rows;                   // of the half-warp
     const uint32_t mine = 0xffffu << (threadIdx.x & 16);  // its lanes
     float m[RT], l[RT];
-    float4 o[RT][NC];
+    Float22 o[RT][NC];
 #pragma unroll
     for (int r = 0; r < RT; ++r) {
         m[r] = -INFINITY; l[r] = 0.f;
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[r][c] = make_float4(0.f, 0.f, 0.f, 0.f);
+        for (int c = 0; c < NC; ++c) o[r][c].lo = o[r][c].hi = make_float2(0.f, 0.f);
     }
     for (int k0 = lo; k0 < hi; k0 += kKeys) {
         cp_async_wait<1>();   // K has arrived (V may still be on its way)
         __syncthreads();
         if (live) {
+            float2 a2[RT][4];  // even and odd channels
+#pragma unroll
+            for (int r = 0; r < RT; ++r)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) a2[r][k] = make_float2(0.f, 0.f);
+#pragma unroll 4
+            for (int c = 0; c < D; c += 4) {
+                Float22 q4[RT], k4[4];
+#pragma unroll
+                for (int r = 0; r < RT; ++r) q4[r] = *reinterpret_cast<const Float22*>(sq + (rg + r) * KP + c);
+#pragma unroll
+                for (int k = 0; k < 4; ++k) k4[k] = *reinterpret_cast<const Float22*>(sk + (l16 + 16 * k) * KP + c);
+#pragma unroll
+                for (int r = 0; r < RT; ++r)
+#pragma unroll
+                    for (int k = 0; k < 4; ++k) a2[r][k] = fma2(q4[r].hi, k4[k].hi, fma2(q4[r].lo, k4[k].lo, a2[r][k]));
+            }
             float a[RT][4];
 #pragma unroll
             for (int r = 0; r < RT; ++r)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) a[r][k] = 0.f;
-#pragma unroll 4
-            for (int c = 0; c < D; c += 4) {
-                float4 q4[RT], k4[4];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) q4[r] = *reinterpret_cast<const float4*>(sq + (rg + r) * KP + c);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) k4[k] = *reinterpret_cast<const float4*>(sk + (l16 + 16 * k) * KP + c);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k)
-                        a[r][k] = fmaf(q4[r].x, k4[k].x, fmaf(q4[r].y, k4[k].y, fmaf(q4[r].z, k4[k].z, fmaf(q4[r].w, k4[k].w, a[r][k]))));
-            }
+                for (int k = 0; k < 4; ++k) a[r][k] = a2[r][k].x + a2[r][k].y;
             const bool all_seen = k0 + kKeys <= min(hi, st.L);
 #pragma unroll
             for (int r = 0; r < RT; ++r) {
@@ -196,7 +200,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
                 }
                 l[r] = l[r] * fix + sum;  // this thread's keys only
 #pragma unroll
-                for (int c = 0; c < NC; ++c) { o[r][c].x *= fix; o[r][c].y *= fix; o[r][c].z *= fix; o[r][c].w *= fix; }
+                for (int c = 0; c < NC; ++c) { o[r][c].lo.x *= fix; o[r][c].lo.y *= fix; o[r][c].hi.x *= fix; o[r][c].hi.y *= fix; }
             }
         }
         cp_async_wait<0>();   // V has arrived
@@ -212,12 +216,13 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
                 for (int u = 0; u < 4; ++u) {
 #pragma unroll
                     for (int c = 0; c < NC; ++c) {
-                        const float4 v4 = *reinterpret_cast<const float4*>(sv + (k + u) * D + 64 * c + 4 * l16);
+                        const Float22 v4 = *reinterpret_cast<const Float22*>(sv + (k + u) * D + 64 * c + 4 * l16);
 #pragma unroll
                         for (int r = 0; r < RT; ++r) {
                             const float p = u == 0 ? p4[r].x : u == 1 ? p4[r].y : u == 2 ? p4[r].z : p4[r].w;
-                            o[r][c].x = fmaf(p, v4.x, o[r][c].x); o[r][c].y = fmaf(p, v4.y, o[r][c].y);
-                            o[r][c].z = fmaf(p, v4.z, o[r][c].z); o[r][c].w = fmaf(p, v4.w, o[r][c].w);
+                            const float2 pp = make_float2(p, p);
+                            o[r][c].lo = fma2(pp, v4.lo, o[r][c].lo);
+                            o[r][c].hi = fma2(pp, v4.hi, o[r][c].hi);
                         }
                     }
                 }
@@ -252,7 +257,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         for (int r = 0; r < RT; ++r)
 #pragma unroll
             for (int c = 0; c < NC; ++c)
-                if (rg + r < rows) finish(rg + r, 64 * c + 4 * l16, o[r][c], m[r], l[r]);
+                if (rg + r < rows) finish(rg + r, 64 * c + 4 * l16, make_float4(o[r][c].lo.x, o[r][c].lo.y, o[r][c].hi.x, o[r][c].hi.y), m[r], l[r]);
         return;
     }
     // ---- the cluster's parts meet: a block joins rpo rows, and gets m, l and O of those rows from every block
@@ -269,7 +274,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
             const int owner = row / rpo, at = rank * rpo + row % rpo;
             const uint32_t dst = map_to_cta(sPart, owner) + at * PITCH * 4;
 #pragma unroll
-            for (int c = 0; c < NC; ++c) st_remote_v4(dst + (64 * c + 4 * l16) * 4, o[r][c].x, o[r][c].y, o[r][c].z, o[r][c].w);
+            for (int c = 0; c < NC; ++c) st_remote_v4(dst + (64 * c + 4 * l16) * 4, o[r][c].lo.x, o[r][c].lo.y, o[r][c].hi.x, o[r][c].hi.y);
             if (l16 == 0) st_remote_v2(map_to_cta(sStat, owner) + at * 8, m[r], l[r]);
         }
     }
@@ -296,11 +301,7 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
 }
 
 template <typename T, int D, int RT>
-cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
-    const int G = cv.Hq / cv.Hkv, tiles_r = (max_n * G + 8 * RT - 1) / (8 * RT), keys = cv.c + max_n;
-    // Blocks of a cluster: until the machine holds two per SM, while each still has a tile of keys
-    int split = 1;
-    while (split < kMaxSplit && (long)cv.B * cv.Hkv * tiles_r * split < 2L * sms && keys > split * kKeys) split *= 2;
+cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int tiles_r, int split, void* out, float* lse, cudaStream_t s) {
     auto kern = verify_simt_kernel<T, D, RT>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
@@ -328,18 +329,34 @@ cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens&
     return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<T*>(out), lse, split);
 }
 
-// Rows per thread: the fewest tiles of at most 48 rows (D = 128: two blocks' shared memory fills an SM) or 64, and those even.
+// Rows per thread and blocks per cluster, by the time they should take: waves of two blocks per SM, each as long as its key
+// tiles, a tile as long as a thread's rows and a part that does not grow with them - the rows count once where a block has
+// its SM to itself, twice where two share it.  Up to 48 rows a tile with D = 128, so that two blocks' shared memory still
+// fits an SM.
 template <typename T, int D>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
-    const int groups = (max_n * (cv.Hq / cv.Hkv) + 7) / 8, most = D == 128 ? 6 : 8, tiles = (groups + most - 1) / most;
-    switch ((groups + tiles - 1) / tiles) {
-        case 1: return launch_rt<T, D, 1>(cv, dv, lens, max_n, out, lse, sms, s);
-        case 2: return launch_rt<T, D, 2>(cv, dv, lens, max_n, out, lse, sms, s);
-        case 3: return launch_rt<T, D, 3>(cv, dv, lens, max_n, out, lse, sms, s);
-        case 4: return launch_rt<T, D, 4>(cv, dv, lens, max_n, out, lse, sms, s);
-        case 5: return launch_rt<T, D, 5>(cv, dv, lens, max_n, out, lse, sms, s);
-        case 6: return launch_rt<T, D, 6>(cv, dv, lens, max_n, out, lse, sms, s);
-        default: return launch_rt<T, D, D == 128 ? 6 : 8>(cv, dv, lens, max_n, out, lse, sms, s);
+    const int G = cv.Hq / cv.Hkv, keys = cv.c + max_n;
+    int rt = 1, split = 1;
+    long least = -1;
+    for (int r = 1; r <= (D == 128 ? 6 : 8); r += r == 6 ? 2 : 1) {
+        long tiles = 0;
+        for (int b = 0; b < cv.B; ++b) tiles += (lens.n[b] * G + 8 * r - 1) / (8 * r);
+        for (int x = 1; x <= kMaxSplit; x *= 2) {
+            if (x > 1 && keys <= (x / 2) * kKeys) break;
+            const long blocks = tiles * cv.Hkv * x, steps = (keys + x * kKeys - 1) / (x * kKeys) + 1;
+            const long cost = blocks <= sms ? steps * (3 + r) : (blocks + 2L * sms - 1) / (2L * sms) * steps * (3 + 2 * r);
+            if (least < 0 || cost < least) { least = cost; rt = r; split = x; }
+        }
+    }
+    const int tiles = (max_n * G + 8 * rt - 1) / (8 * rt);
+    switch (rt) {
+        case 1: return launch_rt<T, D, 1>(cv, dv, lens, tiles, split, out, lse, s);
+        case 2: return launch_rt<T, D, 2>(cv, dv, lens, tiles, split, out, lse, s);
+        case 3: return launch_rt<T, D, 3>(cv, dv, lens, tiles, split, out, lse, s);
+        case 4: return launch_rt<T, D, 4>(cv, dv, lens, tiles, split, out, lse, s);
+        case 5: return launch_rt<T, D, 5>(cv, dv, lens, tiles, split, out, lse, s);
+        case 6: return launch_rt<T, D, 6>(cv, dv, lens, tiles, split, out, lse, s);
+        default: return launch_rt<T, D, D == 128 ? 6 : 8>(cv, dv, lens, tiles, split, out, lse, s);
     }
 }
 
