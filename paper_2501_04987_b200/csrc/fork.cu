@@ -60,23 +60,47 @@ __global__ void __launch_bounds__(kForkThreads, RINGS ? 4 : 5) fork_kernel(Cache
         for (int u = 0; u < kForkUnroll; ++u)
             if (live[u]) { Kd[u * RPB * D16] = k[u]; Vd[u * RPB * D16] = v[u]; }
     }
-    // ---- S, stream positions, and the sequence's own counters
+    // ---- S, stream positions, and the sequence's own counters: a thread per row.  Few blocks have this to do and a component
+    // may be a long chain of sources, each a trip to memory: four sources are read before their copies are written (a source
+    // is never a copy that this call has written, so no load has a store to wait for).
     if (threadIdx.x < ROWS) {
         const int r = r0 + threadIdx.x;
-        float s = 0.f, s_kept = 0.f;
-        int p = 0, p_kept = 0, w0 = 0, w0_kept = 0;
-        for (int o = first; o < last; ++o) {
-            const int src = plan.src[o], dst = plan.dst[o];
+        float s_kept = 0.f, sc[4];
+        int p_kept = 0, w_kept = 0, ps[4], ws[4];
+        bool lv[4];
+        auto fetch1 = [&](int o, float& sx, int& px, int& wx) { 
+            const int src = plan.src[o];
             const UnitState st = unit_state(plan.seen[o], cv);
-            const bool live = r < st.a || (r >= st.a + st.i && r < st.L + st.i);
-            if (src == kForkKept) { s = s_kept; p = p_kept; w0 = w0_kept; }
-            else if (src != kForkEmpty) {
-                if (live) { s = cv.S[unit(src) * cv.R + r]; p = cv.pos[unit(src) * cv.R + r]; }
-                if (r == 0) w0 = cv.w0[unit(src)];
-            } else w0 = 0;
-            if (dst == kForkKept) { s_kept = s; p_kept = p; w0_kept = w0; continue; }
-            if (live && src != kForkEmpty) { cv.S[unit(dst) * cv.R + r] = s; cv.pos[unit(dst) * cv.R + r] = p; }
-            if (r == 0) { cv.n_seen[unit(dst)] = plan.seen[o]; cv.w0[unit(dst)] = w0; }
+            const bool has = r < st.a || (r >= st.a + st.i && r < st.L + st.i);
+            if (src < kForkEmpty) {
+                if (has) { sx = cv.S[unit(src) * cv.R + r]; px = cv.pos[unit(src) * cv.R + r]; }
+                if (r == 0) wx = cv.w0[unit(src)];
+            }
+            return has;
+        };
+        int o = first;
+        if (plan.dst[o] == kForkKept) { fetch1(o, s_kept, p_kept, w_kept); ++o; }
+        while (o < last) {
+            int from[5];
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                from[g] = o;
+                if (o < last) {
+                    const int src = plan.src[o];
+                    sc[g] = s_kept; ps[g] = p_kept; ws[g] = src == kForkEmpty ? 0 : w_kept;
+                    lv[g] = fetch1(o, sc[g], ps[g], ws[g]) && src != kForkEmpty;
+                    do ++o; while (o < last && plan.src[o] == src);
+                }
+            }
+            from[4] = o;
+#pragma unroll
+            for (int g = 0; g < 4; ++g) {
+                for (int x = from[g]; x < from[g + 1]; ++x) {
+                    const size_t to = unit(plan.dst[x]);
+                    if (lv[g]) { cv.S[to * cv.R + r] = sc[g]; cv.pos[to * cv.R + r] = ps[g]; }
+                    if (r == 0) { cv.n_seen[to] = plan.seen[x]; cv.w0[to] = ws[g]; }
+                }
+            }
         }
     }
 }
