@@ -489,10 +489,10 @@ class TreeKV:
         return sb
 
     def stats(self, check=True):
-        """Counters as a dict.  With check=False a device-side give-up (TREEKV_ERR_TIMEOUT) is reported through
-        'device_error' and 'status' instead of raising."""
+        """Counters as a dict.  With check=False what the device recorded - a give-up (TREEKV_ERR_TIMEOUT), an index out of
+        range (TREEKV_ERR_INVALID_ARG) - is reported through 'device_error' and 'status' instead of raising."""
         st, s = treekv_get_stats(self._h, self._stream())
-        if check or st not in (TREEKV_OK, 6):
+        if check or st not in (TREEKV_OK, 1, 6):
             _check(st, "treekv_get_stats")
         return {"status": st, "evictions": s.evictions, "near_ties": s.near_ties, "kernel_launches": s.kernel_launches,
                 "device_error": s.device_error, "last_cuda_error": s.last_cuda_error}

@@ -120,8 +120,10 @@ def test_norm_rope_padding_bad_positions_and_missing_v(gpu):
     pos[3] = 8
     q, k, v = kv.norm_rope(qkv, cos=cos, sin=sin, positions=pos, q=mark(hq), k=mark(hkv), v=mark(hkv))
     assert bool((q[3] == 7).all() and (k[3] == 7).all() and (v[3] == 7).all()) and torch.equal(q[8], q2[8])
-    status, s = gpu.treekv_get_stats(kv._h, kv._stream())
-    assert status == 1 and s.device_error == BAD_INDEX
+    with pytest.raises(gpu.TreeKVError):
+        kv.stats()
+    st = kv.stats(check=False)
+    assert st["status"] == 1 and st["device_error"] == BAD_INDEX
     kv.reset()
     assert kv.stats()["device_error"] == 0
 
@@ -433,6 +435,7 @@ def test_verify_in_a_graph_follows_the_cache(gpu):
     pos = torch.randint(0, 64, (36,), device="cuda", dtype=torch.int32)
     qn, kn, vn = torch.empty((36, 8, 128), device="cuda", dtype=kv.tdtype), *(torch.empty((36, 2, 128), device="cuda", dtype=kv.tdtype) for _ in range(2))
     out, lse = torch.empty_like(q), torch.empty((3, 12, 8), device="cuda")
+    path = torch.zeros((3, 1), dtype=torch.int32, device="cuda")
     stream = torch.cuda.Stream()
     graph = torch.cuda.CUDAGraph()
     with torch.cuda.stream(stream):
@@ -442,9 +445,10 @@ def test_verify_in_a_graph_follows_the_cache(gpu):
         with torch.cuda.graph(graph, stream=stream):
             kv.norm_rope(wide, cos=cos, sin=sin, positions=pos, q=qn, k=kn, v=vn)
             kv.verify_tree(q, k, v, mask=mask, out=out, lse=lse)
-            with pytest.raises(gpu.TreeKVError) as e:
-                kv.fork_sequences([0, 0, 0])
-            assert e.value.status == 2
+            for call in (lambda: kv.fork_sequences([0, 0, 0]), lambda: kv.accept_path(q, k, v, lse, path, [1, 0, 1])):
+                with pytest.raises(gpu.TreeKVError) as e:
+                    call()
+                assert e.value.status == 2
     torch.cuda.synchronize()
     for step in range(3):
         q.copy_(torch.randn_like(q)); wide.copy_(torch.randn_like(wide))
@@ -479,6 +483,7 @@ def _path_rows(B, T, lens, took, seed):
 @pytest.mark.parametrize("dtype,d,hq,hkv,budget,chunk,protect,rope,rule", [
     ("bf16", 128, 8, 2, 96, 32, None, False, 0), ("bf16", 128, 2, 2, 40, 16, None, False, 0), ("bf16", 128, 8, 1, 60, 16, (4, 20), False, 0),
     ("bf16", 64, 4, 2, 64, 16, None, False, 3), ("f32", 64, 4, 4, 50, 16, None, False, 0), ("f32", 128, 4, 1, 70, 64, (3, 9), True, 0),
+    ("bf16", 128, 2, 1, 2, 16, None, False, 0), ("f32", 64, 2, 2, 3, 8, None, False, 0), ("bf16", 64, 8, 1, 5, 64, (1, 2), False, 0),
     ("bf16", 128, 4, 1, 80, 16, None, True, 0), ("bf16", 64, 2, 2, 33, 16, None, True, 0), ("bf16", 128, 4, 2, 20, 16, None, False, 1)])
 def test_drafted_decoding_in_lock_step(gpu, dtype, d, hq, hkv, budget, chunk, protect, rope, rule):
     """Prefill, then drafted steps with decode steps between them, against the oracle, for which an accepted path is a chunk:
@@ -580,6 +585,95 @@ def test_accept_equals_a_chunk(gpu, dtype, d, hq, hkv):
     kv2.accept_path(q, k, v, lse, path, took)
     c, _ = kv2.export_state()
     assert torch.equal(a, c)
+
+
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 64, 2, 2), ("f32", 64, 4, 1)])
+def test_a_draft_of_one_is_a_decode_step(gpu, dtype, d, hq, hkv):
+    """One drafted token, accepted: the cache of a decode step, and its output."""
+    import torch
+
+    seen = [0, 5, 99, 100, 101, 250]
+    pair = [_filled(gpu, dtype, d, hq, hkv, 100, seen, 4, seed=51)[0] for _ in range(2)]
+    path = torch.zeros((6, 1), dtype=torch.int32, device="cuda")
+    for step in range(5):
+        q, k, v = _draft(pair[0], 1, 52 + step)
+        out, lse = pair[0].verify_tree(q, k, v)
+        pair[0].accept_path(q, k, v, lse, path)
+        want = pair[1].decode_step(q[:, 0].contiguous(), k[:, 0].contiguous(), v[:, 0].contiguous())
+        # two kernels' roundings around values of at most 5 (the output's, and the weights' where those go to bf16)
+        tol = 5 * 4 * HALF[dtype] if dtype == "bf16" else 5e-5
+        assert float((out[:, 0].double() - want.double()).abs().max()) <= tol
+        a, b = (x.retained_positions() for x in pair)
+        assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+        sa, sb = (x.scores() for x in pair)
+        assert float((sa - sb).abs().max()) <= 1e-5 * float(sb.abs().max())
+    assert [pair[0].tokens_seen(b) for b in range(6)] == [n + 5 for n in seen]
+
+
+def test_drafts_behind_a_pending_eviction(gpu):
+    """The eviction of a chunk on the context's own stream is waited for."""
+    import torch
+
+    pair = [_filled(gpu, "bf16", 128, 4, 2, 96, [96, 300, 20], 32, seed=60)[0] for _ in range(2)]
+    pair[0].set_option(gpu.OPT_EVICTION_STREAM, 1)
+    x = [torch.randn((3, 32, h, 128), device="cuda").to(pair[0].tdtype) for h in (4, 2, 2)]
+    q, k, v = _draft(pair[0], 9, 61)
+    rows, paths = _path_rows(3, 9, [9] * 3, [3, 4, 2], 62)
+    path = torch.tensor([(p + [0] * 4)[:4] for p in paths], dtype=torch.int32, device="cuda")
+    got = []
+    for kv in pair:
+        kv.prefill_chunk(*x)
+        out, lse = kv.verify_tree(q, k, v, mask=_mask_tensor(rows))
+        kv.prefill_chunk(*x)
+        kv.accept_path(q, k, v, lse, path, [3, 4, 2])
+        got.append((out, lse, kv.export_state()[0]))
+    assert all(torch.equal(a, b) for a, b in zip(*got))
+
+
+def test_offsets_beyond_32_bits(gpu):
+    """Slabs of more than 2^32 bytes: the last sequence's rows lie behind them."""
+    import torch
+
+    B, hkv, d, budget, T = 56, 8, 128, 20480, 20
+    kv = gpu.TreeKV(budget, hkv, hkv, d, "bf16", B, 8)
+    assert B * hkv * (2 * budget + 8) * d * 2 > 2 ** 32
+    image, _ = kv.export_state()
+    K, V, S, P, N = _image_parts(torch, kv, image)
+    seen = [0] * (B - 2) + [budget + 77, 3 * budget + 11]
+    g = torch.Generator(device="cuda").manual_seed(70)
+    for b in (B - 2, B - 1):
+        K[b] = torch.randn((hkv, budget, d), generator=g, device="cuda").to(kv.tdtype)
+        V[b] = torch.randn((hkv, budget, d), generator=g, device="cuda").to(kv.tdtype)
+        P[b] = torch.arange(seen[b] - budget, seen[b], device="cuda", dtype=torch.int32)
+        S[b] = torch.rand((hkv, budget), generator=g, device="cuda") + 0.5
+        N[b] = seen[b]
+    kv.import_state(image, seen)
+    keep = [x[B - 2:].clone() for x in (K, V, S, P)]
+    draft = _draft(kv, T, 71)
+    rows, paths = _path_rows(B, T, [0] * (B - 2) + [T, T], [0] * (B - 2) + [5, 6], 72)
+    lens = [0] * (B - 2) + [T, T]
+    out, lse = kv.verify_tree(*draft, mask=_mask_tensor(rows), lens=lens)
+    _check_verify(kv, (K, V), seen, draft, rows, lens, out, lse, heads=[0, 7])
+    path = torch.tensor([(p + [0] * 6)[:6] for p in paths], dtype=torch.int32, device="cuda")
+    kv.accept_path(*draft, lse, path, [0] * (B - 2) + [5, 6])
+    kv.fork_sequences([B - 1] + list(range(1, B - 1)) + [B - 2])
+    pos, cnt = kv.retained_positions()
+    assert bool((cnt[[0, B - 2, B - 1]] == budget).all()) and kv.tokens_seen(0) == seen[-1] + 6 and kv.tokens_seen(B - 1) == seen[-2] + 5
+    image, _ = kv.export_state()
+    K2, V2, S2, P2, _ = _image_parts(torch, kv, image)
+    where = {0: 1, B - 2: 0, B - 1: 0}        # sequence -> which of the two its content was
+    for b, x in where.items():
+        took = 6 if x else 5
+        for h in (0, 7):
+            # Algorithm 1 lets one of each of `took` adjacent pairs go: all other rows are the old ones, the path's behind them
+            old = {int(p): i for i, p in enumerate(keep[3][x, h].tolist())}
+            now = P2[b, h].tolist()
+            assert now[-took:] == list(range(seen[B - 2 + x], seen[B - 2 + x] + took)) and len(set(now)) == budget
+            idx = torch.tensor([old[p] for p in now[:-took]], device="cuda")
+            assert torch.equal(K2[b, h, :-took], keep[0][x, h, idx]) and torch.equal(V2[b, h, :-took], keep[1][x, h, idx])
+            nodes = torch.tensor(paths[B - 2 + x], device="cuda")
+            assert torch.equal(K2[b, h, -took:], draft[1][B - 2 + x, nodes, h]) and torch.equal(V2[b, h, -took:], draft[2][B - 2 + x, nodes, h])
+    assert kv.stats()["device_error"] == 0
 
 
 def test_accept_of_a_bad_path_and_refusals(gpu):
