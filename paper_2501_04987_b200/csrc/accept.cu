@@ -230,7 +230,7 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
                 Elem<float>::unpack(ld_plain(row + c * 4), x);
                 Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
                 const size_t at = (size_t)(k0 + r) * (D / 2) + c * 4;
-                rope_pairs<float>(x, y, cv.rope_cos + at, cv.rope_sin + at);
+                rope_pairs(x, y, cv.rope_cos + at, cv.rope_sin + at);
                 *reinterpret_cast<float4*>(dst + r * PITCH + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
                 *reinterpret_cast<float4*>(dst + r * PITCH + D / 2 + c * 4) = make_float4(y[0], y[1], y[2], y[3]);
             }
@@ -251,7 +251,7 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
                 Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
                 if (cv.rope_cos) {
                     const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 4;
-                    rope_pairs<float>(x, y, cv.rope_cos + tab, cv.rope_sin + tab);
+                    rope_pairs(x, y, cv.rope_cos + tab, cv.rope_sin + tab);
                 }
                 if (c == 0) s_lse[r - c0] = lse[at] * kLog2e;
             } else if (c == 0) {

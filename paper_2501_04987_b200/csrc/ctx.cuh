@@ -8,8 +8,8 @@ struct treekv_ctx {
     treekv::PrefillScratch ps;
     CUtensorMap tmK, tmV;  // 2-D maps over the K and V slabs (rows x head_dim), box 128 rows x 64 channels (bf16, d=128)
     CUtensorMap tmKrot;    // the same over k_rot, the slab of keys encoded at their cache slots (in-cache positions)
-    CUtensorMap tmK64, tmV64;  // the K and V slabs in boxes of 64 rows x 64 channels (bf16): attention of drafted trees
-    bool has_tm64;
+    CUtensorMap tmKv, tmVv;  // the K and V slabs in boxes of 64 rows x 64 channels (bf16): attention of drafted trees
+    bool has_tmv;
     void* k_rot;
     bool has_tma;
     treekv_dtype dt;

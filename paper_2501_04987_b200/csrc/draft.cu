@@ -82,11 +82,11 @@ treekv_status treekv_verify_tree(treekv_ctx* ctx, const void* dev_q, const void*
     cudaError_t e = join_eviction_stream(ctx, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     const DraftView dv = {dev_q, dev_k, dev_v, dev_mask, stride};
-    if (ctx->dt == TREEKV_BF16 && !ctx->cv.rope_cos)
-        e = ctx->has_tm64 ? launch_verify_tc(ctx->cv, ctx->tmK64, ctx->tmV64, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s)
-                          : cudaErrorNotSupported;
+    if (ctx->dt == TREEKV_BF16)
+        e = ctx->has_tmv ? launch_verify_tc(ctx->cv, ctx->tmKv, ctx->tmVv, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s)
+                         : cudaErrorNotSupported;
     else
-        e = launch_verify_simt(ctx->cv, ctx->dt, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s);
+        e = launch_verify_f32(ctx->cv, dv, lens, max_n, dev_out, dev_lse, ctx->sm_count, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     ctx->launches += 1;
     return TREEKV_OK;

@@ -27,14 +27,13 @@ __device__ inline uint64_t draft_sees(const DraftView& dv, int b, int i, int n) 
 // sees, itself not counted)
 __device__ inline int draft_depth(uint64_t sees) { return max(__popcll(sees) - 1, 0); }
 
-// a pair of pieces, VEC channels and their partners half a head away, encoded at the slot whose table entries these are
-template <typename T>
-__device__ inline void rope_pairs(float (&x)[Elem<T>::kVec], float (&y)[Elem<T>::kVec], const float* cos, const float* sin) {
+// fp32: four channels and their partners half a head away, encoded at the slot whose table entries these are
+__device__ inline void rope_pairs(float (&x)[4], float (&y)[4], const float* cos, const float* sin) {
 #pragma unroll
-    for (int e = 0; e < Elem<T>::kVec; ++e) {
+    for (int e = 0; e < 4; ++e) {
         const float cs = __ldg(cos + e), sn = __ldg(sin + e), x1 = x[e], x2 = y[e];
-        x[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x1, cs, -__fmul_rn(x2, sn))));
-        y[e] = Elem<T>::to_float(Elem<T>::from_float(__fmaf_rn(x2, cs, __fmul_rn(x1, sn))));
+        x[e] = __fmaf_rn(x1, cs, -__fmul_rn(x2, sn));
+        y[e] = __fmaf_rn(x2, cs, __fmul_rn(x1, sn));
     }
 }
 
@@ -54,9 +53,9 @@ struct DraftLens {
     uint8_t n[kMaxBatch];
 };
 
-cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
-                               void* out, float* lse, int sms, cudaStream_t stream);
-// bf16, no in-cache positions; tmK, tmV: maps over the slabs in boxes of the kernel's key tile (make_verify_maps)
+cudaError_t launch_verify_f32(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms,
+                              cudaStream_t stream);
+// bf16; tmK, tmV: maps over the slabs in boxes of the kernel's key tile (make_verify_maps)
 bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV);
 cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,
                              int max_n, void* out, float* lse, int sms, cudaStream_t stream);

@@ -1,4 +1,4 @@
-// Attention of a tree of drafted tokens over the cache on CUDA cores: fp32 contexts, and bf16 ones with in-cache positions.
+// Attention of a tree of drafted tokens over the cache on CUDA cores: fp32 contexts.
 //
 // Row r = token * G + head-in-group of one unit (sequence, KV head) attends to every cached row and to the drafted
 // tokens its mask names: out = softmax(q k / sqrt d) v in one pass over the keys with a running maximum and sum, all
@@ -30,11 +30,11 @@ __device__ inline void cp_async_16(float* dst, const void* src) {
 __device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <typename T, int D, int RT>
+template <int D, int RT>
 __global__ void __launch_bounds__(kThreads, 2)
-verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ out, float* __restrict__ lse, int split) {
+verify_f32_kernel(CacheView cv, DraftView dv, DraftLens lens, float* __restrict__ out, float* __restrict__ lse, int split) {
     constexpr int kRows = 8 * RT;
-    constexpr int VEC = Elem<T>::kVec, HALF = D / 2 / VEC, KP = k_pitch<D>(), PP = kKeys + 4, NC = D / 64;  // NC: float4s of a thread's channels
+    constexpr int VEC = 4, HALF = D / 2 / VEC, KP = k_pitch<D>(), PP = kKeys + 4, NC = D / 64;  // NC: float4s of a thread's channels
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.z, b = unit / cv.Hkv, kh = unit % cv.Hkv, rank = blockIdx.x;
@@ -43,10 +43,10 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     const UnitState st = unit_state(cv.n_seen[unit], cv);
     const int total = st.L + n, per = ((total + split - 1) / split + kKeys - 1) / kKeys * kKeys;
     const int lo = min(rank * per, total), hi = min(lo + per, total);  // this block's live indices
-    const T* Kc = reinterpret_cast<const T*>(cv.K) + (size_t)unit * cv.R * D;
-    const T* Vc = reinterpret_cast<const T*>(cv.V) + (size_t)unit * cv.R * D;
-    const T* kd = reinterpret_cast<const T*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
-    const T* vd = reinterpret_cast<const T*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
+    const float* Kc = reinterpret_cast<const float*>(cv.K) + (size_t)unit * cv.R * D;
+    const float* Vc = reinterpret_cast<const float*>(cv.V) + (size_t)unit * cv.R * D;
+    const float* kd = reinterpret_cast<const float*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
+    const float* vd = reinterpret_cast<const float*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
     const size_t dstep = (size_t)cv.Hkv * D;
 
     extern __shared__ __align__(16) float smem[];
@@ -63,11 +63,11 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     if (tid < kRows) s_sees[tid] = tid < rows ? draft_sees(dv, b, (r0 + tid) / G, n) : 0ull;
     if (tid < 2) s_bad[tid] = 0u;
 
-    auto row_of = [&](const T* cache, const T* draft, int lam) { return lam < st.L ? cache + (size_t)phys_row(lam, st) * D : draft + (size_t)(lam - st.L) * dstep; };
-    // K tile at k0: fp32 keys straight from memory; bf16 ones, or encoded at their slots, through registers
+    auto row_of = [&](const float* cache, const float* draft, int lam) { return lam < st.L ? cache + (size_t)phys_row(lam, st) * D : draft + (size_t)(lam - st.L) * dstep; };
+    // K tile at k0: straight from memory, or through registers where the keys are encoded at their slots
     auto load_k = [&](int k0) {
         const int kn = min(kKeys, hi - k0);
-        if (sizeof(T) == 4 && !rope) {
+        if (!rope) {
             for (int e = tid; e < kn * (D / 4); e += kThreads) {
                 const int r = e / (D / 4), c = e % (D / 4);
                 cp_async_16(sk + r * KP + c * 4, reinterpret_cast<const float*>(row_of(Kc, kd, k0 + r)) + c * 4);
@@ -75,19 +75,14 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         } else {
             for (int e = tid; e < kn * HALF; e += kThreads) {
                 const int r = e / HALF, c = e % HALF, lam = k0 + r;
-                const T* row = row_of(Kc, kd, lam);
+                const float* row = row_of(Kc, kd, lam);
                 float x[VEC], y[VEC];
-                Elem<T>::unpack(ld_plain(row + c * VEC), x);
-                Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
-                if (rope) {
-                    const int slot = lam < st.L ? lam : st.L + draft_depth(draft_sees(dv, b, lam - st.L, n));
-                    rope_pairs<T>(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
-                }
-#pragma unroll
-                for (int u = 0; u < VEC; u += 4) {
-                    *reinterpret_cast<float4*>(sk + r * KP + c * VEC + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
-                    *reinterpret_cast<float4*>(sk + r * KP + D / 2 + c * VEC + u) = make_float4(y[u], y[u + 1], y[u + 2], y[u + 3]);
-                }
+                Elem<float>::unpack(ld_plain(row + c * VEC), x);
+                Elem<float>::unpack(ld_plain(row + D / 2 + c * VEC), y);
+                const int slot = lam < st.L ? lam : st.L + draft_depth(draft_sees(dv, b, lam - st.L, n));
+                rope_pairs(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
+                *reinterpret_cast<float4*>(sk + r * KP + c * VEC) = make_float4(x[0], x[1], x[2], x[3]);
+                *reinterpret_cast<float4*>(sk + r * KP + D / 2 + c * VEC) = make_float4(y[0], y[1], y[2], y[3]);
             }
         }
         cp_async_commit();
@@ -98,23 +93,20 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
         for (int e = tid; e < kKeys * (D / VEC); e += kThreads) {
             const int r = e / (D / VEC), c = e % (D / VEC), lam = k0 + r;
             float* dst = sv + r * D + c * VEC;
-            if (sizeof(T) == 4 && r < kn && lam < st.L) {
+            if (r < kn && lam < st.L) {
                 cp_async_16(dst, reinterpret_cast<const float*>(Vc) + (size_t)phys_row(lam, st) * D + c * VEC);
                 continue;
             }
             float x[VEC];
 #pragma unroll
             for (int u = 0; u < VEC; ++u) x[u] = 0.f;
-            if (r < kn) {
-                Elem<T>::unpack(ld_plain(row_of(Vc, vd, lam) + c * VEC), x);
-                if (lam >= st.L) {
+            if (r < kn) {  // a drafted one
+                Elem<float>::unpack(ld_plain(vd + (size_t)(lam - st.L) * dstep + c * VEC), x);
 #pragma unroll
-                    for (int u = 0; u < VEC; ++u)
-                        if (!(fabsf(x[u]) < INFINITY)) { x[u] = 0.f; atomicOr(&s_bad[(lam - st.L) >> 5], 1u << ((lam - st.L) & 31)); }
-                }
+                for (int u = 0; u < VEC; ++u)
+                    if (!(fabsf(x[u]) < INFINITY)) { x[u] = 0.f; atomicOr(&s_bad[(lam - st.L) >> 5], 1u << ((lam - st.L) & 31)); }
             }
-#pragma unroll
-            for (int u = 0; u < VEC; u += 4) *reinterpret_cast<float4*>(dst + u) = make_float4(x[u], x[u + 1], x[u + 2], x[u + 3]);
+            *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
         }
         cp_async_commit();
     };
@@ -127,12 +119,12 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
 #pragma unroll
         for (int u = 0; u < VEC; ++u) { x[u] = 0.f; y[u] = 0.f; }
         if (r < rows) {
-            const T* row = reinterpret_cast<const T*>(dv.q) + (((size_t)b * dv.stride + (r0 + r) / G) * cv.Hq + kh * G + (r0 + r) % G) * D;
-            Elem<T>::unpack(ld_plain(row + c * VEC), x);
-            Elem<T>::unpack(ld_plain(row + D / 2 + c * VEC), y);
+            const float* row = reinterpret_cast<const float*>(dv.q) + (((size_t)b * dv.stride + (r0 + r) / G) * cv.Hq + kh * G + (r0 + r) % G) * D;
+            Elem<float>::unpack(ld_plain(row + c * VEC), x);
+            Elem<float>::unpack(ld_plain(row + D / 2 + c * VEC), y);
             if (rope) {
                 const size_t at = (size_t)(st.L + draft_depth(s_sees[r])) * (D / 2) + c * VEC;
-                rope_pairs<T>(x, y, cv.rope_cos + at, cv.rope_sin + at);
+                rope_pairs(x, y, cv.rope_cos + at, cv.rope_sin + at);
             }
         }
 #pragma unroll
@@ -244,12 +236,11 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
 #pragma unroll
         for (int u = 0; u < 4; ++u) f[u] = L == 0.f ? 0.f : f[u] / L;  // L = 0: nothing was visible
         for (uint64_t left = bad & s_sees[row]; left; left &= left - 1) {
-            const T* vr = vd + (size_t)(__ffsll((long long)left) - 1) * dstep + ch;
+            const float* vr = vd + (size_t)(__ffsll((long long)left) - 1) * dstep + ch;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) { const float y = Elem<T>::to_float(vr[u]); if (!(fabsf(y) < INFINITY)) f[u] += y; }
+            for (int u = 0; u < 4; ++u) { const float y = vr[u]; if (!(fabsf(y) < INFINITY)) f[u] += y; }
         }
-        if constexpr (sizeof(T) == 4) *reinterpret_cast<float4*>(out + at * D + ch) = make_float4(f[0], f[1], f[2], f[3]);
-        else *reinterpret_cast<uint2*>(out + at * D + ch) = make_uint2(rope_pack_bf16(f[0], f[1]), rope_pack_bf16(f[2], f[3]));
+        *reinterpret_cast<float4*>(out + at * D + ch) = make_float4(f[0], f[1], f[2], f[3]);
         if (lse && ch == 0) lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * (1.0f / kLog2e);
     };
     if (split == 1) {
@@ -300,9 +291,9 @@ verify_simt_kernel(CacheView cv, DraftView dv, DraftLens lens, T* __restrict__ o
     }
 }
 
-template <typename T, int D, int RT>
+template <int D, int RT>
 cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int tiles_r, int split, void* out, float* lse, cudaStream_t s) {
-    auto kern = verify_simt_kernel<T, D, RT>;
+    auto kern = verify_f32_kernel<D, RT>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
@@ -326,14 +317,14 @@ cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens&
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<T*>(out), lse, split);
+    return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<float*>(out), lse, split);
 }
 
 // Rows per thread and blocks per cluster, by the time they should take: waves of two blocks per SM, each as long as its key
 // tiles, a tile as long as a thread's rows and a part that does not grow with them - the rows count once where a block has
 // its SM to itself, twice where two share it.  Up to 48 rows a tile with D = 128, so that two blocks' shared memory still
 // fits an SM.
-template <typename T, int D>
+template <int D>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
     const int G = cv.Hq / cv.Hkv, keys = cv.c + max_n;
     int rt = 1, split = 1;
@@ -350,24 +341,21 @@ cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& 
     }
     const int tiles = (max_n * G + 8 * rt - 1) / (8 * rt);
     switch (rt) {
-        case 1: return launch_rt<T, D, 1>(cv, dv, lens, tiles, split, out, lse, s);
-        case 2: return launch_rt<T, D, 2>(cv, dv, lens, tiles, split, out, lse, s);
-        case 3: return launch_rt<T, D, 3>(cv, dv, lens, tiles, split, out, lse, s);
-        case 4: return launch_rt<T, D, 4>(cv, dv, lens, tiles, split, out, lse, s);
-        case 5: return launch_rt<T, D, 5>(cv, dv, lens, tiles, split, out, lse, s);
-        case 6: return launch_rt<T, D, 6>(cv, dv, lens, tiles, split, out, lse, s);
-        default: return launch_rt<T, D, D == 128 ? 6 : 8>(cv, dv, lens, tiles, split, out, lse, s);
+        case 1: return launch_rt<D, 1>(cv, dv, lens, tiles, split, out, lse, s);
+        case 2: return launch_rt<D, 2>(cv, dv, lens, tiles, split, out, lse, s);
+        case 3: return launch_rt<D, 3>(cv, dv, lens, tiles, split, out, lse, s);
+        case 4: return launch_rt<D, 4>(cv, dv, lens, tiles, split, out, lse, s);
+        case 5: return launch_rt<D, 5>(cv, dv, lens, tiles, split, out, lse, s);
+        case 6: return launch_rt<D, 6>(cv, dv, lens, tiles, split, out, lse, s);
+        default: return launch_rt<D, D == 128 ? 6 : 8>(cv, dv, lens, tiles, split, out, lse, s);
     }
 }
 
 }  // namespace
 
-cudaError_t launch_verify_simt(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const DraftLens& lens, int max_n,
-                               void* out, float* lse, int sms, cudaStream_t stream) {
-    if (dt == TREEKV_F32)
-        return cv.d == 64 ? launch_t<float, 64>(cv, dv, lens, max_n, out, lse, sms, stream) : launch_t<float, 128>(cv, dv, lens, max_n, out, lse, sms, stream);
-    return cv.d == 64 ? launch_t<__nv_bfloat16, 64>(cv, dv, lens, max_n, out, lse, sms, stream)
-                      : launch_t<__nv_bfloat16, 128>(cv, dv, lens, max_n, out, lse, sms, stream);
+cudaError_t launch_verify_f32(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms,
+                              cudaStream_t stream) {
+    return cv.d == 64 ? launch_t<64>(cv, dv, lens, max_n, out, lse, sms, stream) : launch_t<128>(cv, dv, lens, max_n, out, lse, sms, stream);
 }
 
 }  // namespace treekv

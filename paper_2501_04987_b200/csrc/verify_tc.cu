@@ -17,6 +17,9 @@
 // become zeros; a value that is not finite is taken out of the tile, where a weight of zero would spread it as NaN, and
 // added to the rows that see it at the end).
 //
+// In-cache positions (a variant of its own): the softmax warps encode each K tile in place at its cache slots, two tiles
+// ahead, and the queries and drafted keys at the slots where they will sit if accepted.
+//
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
 #include <algorithm>
 
@@ -40,9 +43,10 @@ static_assert(kKeys == kMaxDraft, "the drafted tokens are one tile");
 // FULL: a slot's tile has arrived.  USED: the MMAs that read it are done - for a K tile that also says that its logits are
 // there, for a V tile that its share of O is in: one commit and one barrier for both (a commit holds the issuing thread
 // for some 80 cycles).
-enum Bar { Q_FULL = 0, P_FULL = 1, FULL = 3, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
+// KEYED: (in-cache positions) the softmax warps have encoded the K tile of that parity, or - the last one - the queries.
+enum Bar { Q_FULL = 0, P_FULL = 1, KEYED = 3, FULL = 6, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
 
-template <int D>
+template <int D, bool ROPE>
 __global__ void __launch_bounds__(kThreads, 2)
 verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  CacheView cv, DraftView dv, DraftLens lens, __nv_bfloat16* __restrict__ out, float* __restrict__ lse,
@@ -67,6 +71,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (tid == 0) {
         mbar_init(bar(Q_FULL), 1);
         for (int s = 0; s < 2; ++s) mbar_init(bar(P_FULL + s), 4);
+        for (int s = 0; s < 3; ++s) mbar_init(bar(KEYED + s), 4);
         for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(USED + s), 1); }
         s_bad[0] = s_bad[1] = 0u;
         mbar_fence_init();
@@ -114,7 +119,10 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             constexpr uint32_t idesc_o = umma_idesc_bf16(128, D, 0, 1);      // P from tensor memory, V MN-major
             const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, VHALF), q_half = q_rows * 128 / 16;
             Ring rk(0, slots), rv(1, slots);
+            int js = 0;  // the next tile whose logits are issued
+            auto keyed = [&]() { return !ROPE || mbar_wait(bar(KEYED + (js & 1)), (js >> 1) & 1); };
             auto issue_s = [&](int buf) {  // the next tile's logits
+                ++js;
                 tc_fence_after();
                 const uint32_t lo = k_lo + rk.slot * (SLOT / 16);
 #pragma unroll
@@ -124,9 +132,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 umma_commit(bar(USED + rk.slot));
                 rk.next(); rk.next();
             };
-            ok = mbar_wait2(bar(Q_FULL), 0, bar(FULL + rk.slot), rk.phase);
+            ok = mbar_wait2(bar(Q_FULL), 0, bar(FULL + rk.slot), rk.phase) && (!ROPE || mbar_wait(bar(KEYED + 2), 0)) && keyed();
             if (ok) issue_s(0);
-            if (ok && NT > 1 && (ok = mbar_wait(bar(FULL + rk.slot), rk.phase))) issue_s(1);
+            if (ok && NT > 1 && (ok = mbar_wait(bar(FULL + rk.slot), rk.phase) && keyed())) issue_s(1);
             int last = 0, last_phase = 0;
             for (int j = 0; j < NT && ok; ++j) {
                 const int buf = j & 1;
@@ -140,7 +148,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 umma_commit(bar(USED + last));
                 rv.next(); rv.next();
                 if (j + 2 < NT) {  // the logits of tile j + 2 overwrite P_j
-                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(USED + last), last_phase))) break;
+                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(USED + last), last_phase) && keyed())) break;
                     issue_s(buf);
                 }
             }
@@ -162,6 +170,31 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             stage_draft<D>(cv, dv, b, kh, n, ring, ring + SLOT, VHALF, s_bad, st_tid, 128);
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (st_tid == 0) { mbar_arrive(bar(FULL)); mbar_arrive(bar(FULL + 1)); }
+        }
+        // in-cache positions: the queries where they will sit if accepted, a cached key at its slot (a drafted one at its own)
+        Ring ke(0, slots);
+        auto encode_keys = [&](int j) {
+            ok = ok && mbar_wait(bar(FULL + ke.slot), ke.phase);
+            unsigned char* tile = base_ptr + HALVES * q_rows * 128 + ke.slot * SLOT;
+            if (t.draft && j == 0) {
+                encode_rows<D>(cv, tile, kKeys, VHALF, st_tid, 128, [&](int r) { return r < n ? st.L + draft_depth(draft_sees(dv, b, r, n)) : -1; });
+            } else {
+                int row0, valid;
+                cached_tile<kKeys>(t, j, row0, valid);
+                const int slot0 = row0 < t.a ? row0 : row0 - t.i;
+                encode_rows<D>(cv, tile, kKeys, VHALF, st_tid, 128, [&](int r) { return r < valid ? slot0 + r : -1; });
+            }
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(KEYED + (j & 1)));
+            ke.next(); ke.next();
+        };
+        if (ROPE && NT > 0) {
+            ok = ok && mbar_wait(bar(Q_FULL), 0);
+            encode_rows<D>(cv, base_ptr, rows, q_rows * 128, st_tid, 128,
+                           [&](int r) { return st.L + draft_depth(draft_sees(dv, b, (r0 + r) / G, n)); });
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(KEYED + 2));
+            for (int j = 0; j < 2 && j < NT; ++j) encode_keys(j);
         }
         Ring rk(0, slots), rv(1, slots);  // this tile's K and V
         int done = 0, done_phase = 0;     // V of the tile before
@@ -230,6 +263,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             tc_fence_before();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(P_FULL + (j & 1)));
+            if (ROPE && j + 2 < NT) encode_keys(j + 2);
             done = rv.slot; done_phase = rv.phase;
             rk.next(); rk.next(); rv.next(); rv.next();
         }
@@ -264,7 +298,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
 }
 
-template <int D>
+template <int D, bool ROPE>
 cudaError_t launch_t(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens, int max_n,
                      void* out, float* lse, int sms, cudaStream_t stream) {
     const int G = cv.Hq / cv.Hkv, box = std::min(128 / G, dv.stride);
@@ -276,7 +310,7 @@ cudaError_t launch_t(const CacheView& cv, const CUtensorMap& tmK, const CUtensor
     // The queries' matrix operand is read as 128 rows.  With fewer loaded the others are what lies behind them in the ring:
     // such a row has a lane of its own, which nobody looks at.
     const size_t smem = std::max(kSmemMin, 1024 + q_area + slots * slot);
-    auto kern = verify_tc_kernel<D>;
+    auto kern = verify_tc_kernel<D, ROPE>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
@@ -317,8 +351,11 @@ bool make_verify_maps(const CacheView& cv, CUtensorMap* tmK, CUtensorMap* tmV) {
 
 cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const CUtensorMap& tmV, const DraftView& dv, const DraftLens& lens,
                              int max_n, void* out, float* lse, int sms, cudaStream_t stream) {
-    return cv.d == 64 ? launch_t<64>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream)
-                      : launch_t<128>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream);
+    if (cv.rope_cos)
+        return cv.d == 64 ? launch_t<64, true>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream)
+                          : launch_t<128, true>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream);
+    return cv.d == 64 ? launch_t<64, false>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream)
+                      : launch_t<128, false>(cv, tmK, tmV, dv, lens, max_n, out, lse, sms, stream);
 }
 
 }  // namespace treekv

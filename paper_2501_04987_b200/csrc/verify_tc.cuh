@@ -116,6 +116,22 @@ __device__ inline void stage_draft(const CacheView& cv, const DraftView& dv, int
     }
     fence_proxy_async_smem();
 }
+// In-cache positions: rows of a tile in shared memory (K, or the queries), encoded in place at slots slot(row) of the tables;
+// a negative slot leaves the row as it is.  Halves of 64 channels are `half` bytes apart.
+template <int D, typename Slot>
+__device__ inline void encode_rows(const CacheView& cv, unsigned char* tile, int rows, int half, int t, int nthr, Slot&& slot) {
+    constexpr int PAIRS = D / 16;  // 16-byte pieces c and c + PAIRS hold the partners
+    for (int e = t; e < rows * PAIRS; e += nthr) {
+        const int r = e / PAIRS, c = e % PAIRS, at = slot(r);
+        if (at < 0) continue;
+        auto piece = [&](int x) { return reinterpret_cast<uint4*>(tile + (x >> 3) * half + r * 128 + (((x & 7) ^ (r & 7)) << 4)); };
+        uint4 lo = *piece(c), hi = *piece(c + PAIRS);
+        rope_piece_pair(lo, hi, cv.rope_cos + (size_t)at * (D / 2) + c * 8, cv.rope_sin + (size_t)at * (D / 2) + c * 8);
+        *piece(c) = lo;
+        *piece(c + PAIRS) = hi;
+    }
+    fence_proxy_async_smem();
+}
 // Rows [valid, KEYS) of a V tile hold no token of this unit and may hold anything: their weight is zero, their values must
 // not be NaN.
 template <int D, int KEYS>

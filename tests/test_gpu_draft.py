@@ -370,11 +370,13 @@ def test_verify_with_values_that_must_not_spread(gpu, dtype, d, hq, hkv):
     assert kv.stats()["device_error"] == 0
 
 
-@pytest.mark.parametrize("dtype,d,hq,hkv,max_chunk", [("bf16", 128, 8, 2, 16), ("bf16", 128, 2, 2, 0), ("bf16", 64, 4, 2, 16), ("f32", 64, 4, 2, 0)])
-def test_verify_with_in_cache_positions(gpu, dtype, d, hq, hkv, max_chunk):
+@pytest.mark.parametrize("dtype,d,hq,hkv,max_chunk,budget", [
+    ("bf16", 128, 8, 2, 16, 90), ("bf16", 128, 2, 2, 0, 90), ("bf16", 64, 4, 2, 16, 90), ("f32", 64, 4, 2, 0, 90),
+    ("bf16", 128, 8, 1, 0, 900), ("bf16", 64, 16, 4, 0, 1500), ("bf16", 128, 32, 8, 0, 450), ("f32", 128, 4, 2, 0, 700)])
+def test_verify_with_in_cache_positions(gpu, dtype, d, hq, hkv, max_chunk, budget):
     import torch
 
-    budget, seen, T = 90, [0, 37, 90, 200], 21
+    seen, T = [0, 37, budget, 2 * budget + 20], 21
     lens = [21, 8, 21, 20]
     kv2, (K, V, S, P) = _filled(gpu, dtype, d, hq, hkv, budget, seen, max_chunk, seed=12)
     image, tokens = kv2.export_state()
