@@ -177,12 +177,12 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             ok = ok && mbar_wait(bar(FULL + ke.slot), ke.phase);
             unsigned char* tile = base_ptr + HALVES * q_rows * 128 + ke.slot * SLOT;
             if (t.draft && j == 0) {
-                encode_rows<D>(cv, tile, kKeys, VHALF, st_tid, 128, [&](int r) { return r < n ? st.L + draft_depth(draft_sees(dv, b, r, n)) : -1; });
+                encode_rows<D>(cv, tile, VHALF, st_tid, [&](int r) { return r < n ? st.L + draft_depth(draft_sees(dv, b, r, n)) : -1; });
             } else {
                 int row0, valid;
                 cached_tile<kKeys>(t, j, row0, valid);
                 const int slot0 = row0 < t.a ? row0 : row0 - t.i;
-                encode_rows<D>(cv, tile, kKeys, VHALF, st_tid, 128, [&](int r) { return r < valid ? slot0 + r : -1; });
+                encode_rows<D>(cv, tile, VHALF, st_tid, [&](int r) { return r < valid ? slot0 + r : -1; });
             }
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(KEYED + (j & 1)));
@@ -190,8 +190,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         };
         if (ROPE && NT > 0) {
             ok = ok && mbar_wait(bar(Q_FULL), 0);
-            encode_rows<D>(cv, base_ptr, rows, q_rows * 128, st_tid, 128,
-                           [&](int r) { return st.L + draft_depth(draft_sees(dv, b, (r0 + r) / G, n)); });
+            for (int x = 0; x < rows; x += 64)
+                encode_rows<D>(cv, base_ptr + x * 128, q_rows * 128, st_tid,
+                               [&](int r) { return x + r < rows ? st.L + draft_depth(draft_sees(dv, b, (r0 + x + r) / G, n)) : -1; });
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(KEYED + 2));
             for (int j = 0; j < 2 && j < NT; ++j) encode_keys(j);

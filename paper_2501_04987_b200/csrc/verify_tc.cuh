@@ -116,19 +116,31 @@ __device__ inline void stage_draft(const CacheView& cv, const DraftView& dv, int
     }
     fence_proxy_async_smem();
 }
-// In-cache positions: rows of a tile in shared memory (K, or the queries), encoded in place at slots slot(row) of the tables;
-// a negative slot leaves the row as it is.  Halves of 64 channels are `half` bytes apart.
+// In-cache positions: 64 rows of a tile in shared memory (K, or queries), encoded in place at slots slot(row) of the tables by
+// 128 threads t; a negative slot leaves the row as it is.  Halves of 64 channels are `half` bytes apart.  All of a thread's
+// table entries are on their way before the first is used.
 template <int D, typename Slot>
-__device__ inline void encode_rows(const CacheView& cv, unsigned char* tile, int rows, int half, int t, int nthr, Slot&& slot) {
-    constexpr int PAIRS = D / 16;  // 16-byte pieces c and c + PAIRS hold the partners
-    for (int e = t; e < rows * PAIRS; e += nthr) {
-        const int r = e / PAIRS, c = e % PAIRS, at = slot(r);
-        if (at < 0) continue;
-        auto piece = [&](int x) { return reinterpret_cast<uint4*>(tile + (x >> 3) * half + r * 128 + (((x & 7) ^ (r & 7)) << 4)); };
-        uint4 lo = *piece(c), hi = *piece(c + PAIRS);
-        rope_piece_pair(lo, hi, cv.rope_cos + (size_t)at * (D / 2) + c * 8, cv.rope_sin + (size_t)at * (D / 2) + c * 8);
-        *piece(c) = lo;
-        *piece(c + PAIRS) = hi;
+__device__ inline void encode_rows(const CacheView& cv, unsigned char* tile, int half, int t, Slot&& slot) {
+    constexpr int PAIRS = D / 16, N = 64 * PAIRS / 128;  // 16-byte pieces c and c + PAIRS hold the partners
+    auto piece = [&](int r, int x) { return reinterpret_cast<uint4*>(tile + (x >> 3) * half + r * 128 + (((x & 7) ^ (r & 7)) << 4)); };
+    RopeTab tab[N];
+    int at[N];
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int r = (t + 128 * u) / PAIRS, c = (t + 128 * u) % PAIRS;
+        at[u] = slot(r);
+        const size_t entry = (size_t)max(at[u], 0) * (D / 2) + c * 8;
+        tab[u] = rope_tab_load(cv.rope_cos + entry, cv.rope_sin + entry);
+    }
+#pragma unroll
+    for (int u = 0; u < N; ++u) {
+        const int r = (t + 128 * u) / PAIRS, c = (t + 128 * u) % PAIRS;
+        if (at[u] >= 0) {
+            uint4 lo = *piece(r, c), hi = *piece(r, c + PAIRS);
+            rope_piece_pair(lo, hi, tab[u]);
+            *piece(r, c) = lo;
+            *piece(r, c + PAIRS) = hi;
+        }
     }
     fence_proxy_async_smem();
 }
