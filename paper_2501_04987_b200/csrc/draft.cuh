@@ -7,6 +7,9 @@ namespace treekv {
 
 constexpr int kMaxDraft = 64;  // drafted tokens of a sequence: one 64-bit word of visibility per token
 
+// DevStats.error bit: a device-side index (a position, a node of a path) was out of range and was not followed
+constexpr unsigned int kErrBadIndex = 256u;
+
 // a draft's tensors as the caller passed them
 struct DraftView {
     const void* q;          // [B][stride][Hq][d]
@@ -62,5 +65,34 @@ cudaError_t launch_verify_tc(const CacheView& cv, const CUtensorMap& tmK, const 
 // the accepted path enters the cache: append, score update, evictions, token counters
 cudaError_t launch_accept(const CacheView& cv, treekv_dtype dt, const DraftView& dv, const float* lse, const int32_t* path,
                           int path_stride, const DraftLens& lens, int max_n, int sms, cudaStream_t stream);
+
+// split of a packed projection with the norms and the rotation of q and k (norm_rope.cu)
+struct NormRope {
+    const void* qkv;       // [tokens] rows of [Hq | Hkv | Hkv] heads, row_stride elements apart
+    long long row_stride;
+    const void *wq, *wk;   // [d]; nullptr: that tensor is not normalised
+    const float *cos, *sin;  // [slots][d/2]; nullptr: no rotation
+    const int32_t* pos;    // [tokens] table rows; negative: the token is padding and is skipped
+    void *q, *k, *v;       // v may be nullptr
+    float eps;
+    int slots, tokens, Hq, Hkv;
+};
+cudaError_t launch_norm_rope(const NormRope& a, treekv_dtype dt, int D, DevStats* stats, int sms, cudaStream_t stream);
+
+// Copies between the sequences of a batch (fork.cu): operations of each connected component of the copy graph in an
+// order in which no sequence is overwritten before all its copies have been taken.
+constexpr int kForkMaxOps = kMaxBatch + kMaxBatch / 2;  // every sequence once, and one kept value per ring
+constexpr uint16_t kForkKept = 0xffff;   // as a destination: keep the value; as a source: the kept value
+constexpr uint16_t kForkEmpty = 0xfffe;  // as a source: the destination is freed
+template <int MAXB>
+struct ForkPlan {
+    uint16_t src[MAXB], dst[MAXB], start[MAXB + 1];  // operations of component z: [start[z], start[z + 1])
+    int32_t seen[MAXB];                              // tokens seen by the sequence whose content moves (0: freed)
+};
+struct ForkPlanHost : ForkPlan<kForkMaxOps> {
+    int n_ops, n_comps;
+};
+void make_fork_plan(const int32_t* source, int B, const int64_t* seen, ForkPlanHost& plan);
+cudaError_t launch_fork(const CacheView& cv, treekv_dtype dt, const ForkPlanHost& plan, cudaStream_t stream);
 
 }  // namespace treekv

@@ -6,7 +6,7 @@
 // operations in the order the host put them in: a sequence is overwritten after everything that copies from it has read
 // it, and a ring of sequences is cut by one value kept in registers.  No thread reads what another writes: no staging
 // memory, no barrier, every source read once however many copies it has.  Bound by memory traffic.
-#include "common.cuh"
+#include "draft.cuh"
 
 namespace treekv {
 

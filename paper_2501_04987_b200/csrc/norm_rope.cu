@@ -8,7 +8,7 @@
 // Bound by memory traffic: every element is read once and written once.  A lane holds the same VEC channels of both
 // halves of a head, so a pair never leaves its lane, the norm is one butterfly over the D / (2 VEC) lanes of a head, and a
 // lane's cos, sin and weights serve all the heads its warp takes.
-#include "common.cuh"
+#include "draft.cuh"
 
 namespace treekv {
 
