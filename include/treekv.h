@@ -296,8 +296,9 @@ treekv_status treekv_norm_rope(treekv_ctx* ctx, const void* dev_qkv, int64_t row
  *                   the token sees, as treekv_accept_path takes it; may be NULL
  *   host_lens       [batch] int32 in 0..stride (0 = sequence not in this call); NULL = all `stride`.  Read before
  *                   returning.  stride: 1..64
+ * The outputs must not overlap the inputs.
  * A token that sees nothing (an empty cache and an empty word) gets an output of zeros and a log-sum-exp of minus
- * infinity.  Rows beyond a sequence's length are neither read as keys nor written.  With in-cache positions a drafted token
+ * infinity (accepted all the same, it adds to no score).  Rows beyond a sequence's length are neither read as keys nor written.  With in-cache positions a drafted token
  * is encoded behind the cache, at slot L + (number of drafted tokens it sees) - 1 - where it will sit if its path is
  * accepted - which needs tables of at least budget + stride slots (TREEKV_ERR_UNSUPPORTED otherwise).
  */

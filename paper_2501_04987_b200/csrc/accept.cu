@@ -54,6 +54,9 @@ __device__ inline size_t draft_row(const CacheView& cv, const DraftView& dv, con
     return (((size_t)p.b * dv.stride + p.node[j]) * cv.Hkv + p.kh) * D;
 }
 
+// exp2's reference of a row; one that saw nothing gives nothing: weight 0, not exp of infinity
+__device__ inline float row_reference(float lse) { return lse == -INFINITY ? INFINITY : lse * kLog2e; }
+
 // query row pitch in shared memory, bytes: rows g and g + 1 half the banks apart, so that eight lanes' 16-byte reads (two
 // rows, four pieces) meet no conflict
 template <int D> constexpr int q_pitch() { return D * 2 + 64; }
@@ -97,16 +100,13 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
     // ---- the path's queries (encoded at their slots with in-cache positions) and their log-sum-exps
     for (int e = tid; e < tiles_r * 8 * (D / 16); e += kThreads) {
         const int r = e / (D / 16), c = e % (D / 16);
-        uint4 lo = make_uint4(0, 0, 0, 0), hi = lo;
-        if (r < rows) {
-            const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
-            const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(dv.q) + at * D);
-            lo = src[c]; hi = src[c + D / 16];
-            if (ROPE) rope_piece_pair(lo, hi, cv.rope_cos + (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 8, cv.rope_sin + (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 8);
-            if (c == 0) s_lse[r] = lse[at] * kLog2e;
-        } else if (c == 0) {
-            s_lse[r] = INFINITY;  // weight 0
-        }
+        // rows that fill the last eight up repeat the last one, with weight 0: zeros would make NaN of a key that is not finite
+        const int x = min(r, rows - 1);
+        const size_t at = (((size_t)p.b * dv.stride + p.node[x >> lg]) * cv.Hq + p.kh * p.G + (x & (p.G - 1)));
+        const uint4* src = reinterpret_cast<const uint4*>(reinterpret_cast<const T*>(dv.q) + at * D);
+        uint4 lo = src[c], hi = src[c + D / 16];
+        if (ROPE) rope_piece_pair(lo, hi, cv.rope_cos + (size_t)(p.st.L + (x >> lg)) * (D / 2) + c * 8, cv.rope_sin + (size_t)(p.st.L + (x >> lg)) * (D / 2) + c * 8);
+        if (c == 0) s_lse[r] = row_reference(r < rows ? lse[at] : -INFINITY);
         *reinterpret_cast<uint4*>(sq + r * PITCH + c * 16) = lo;
         *reinterpret_cast<uint4*>(sq + r * PITCH + (c + D / 16) * 16) = hi;
     }
@@ -253,9 +253,7 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
                     const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 4;
                     rope_pairs(x, y, cv.rope_cos + tab, cv.rope_sin + tab);
                 }
-                if (c == 0) s_lse[r - c0] = lse[at] * kLog2e;
-            } else if (c == 0) {
-                s_lse[r - c0] = INFINITY;  // weight 0
+                if (c == 0) s_lse[r - c0] = row_reference(lse[at]);
             }
             float* dst = sq + (r - c0) * PITCH + c * 4;
             *reinterpret_cast<float4*>(dst) = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
@@ -291,7 +289,7 @@ __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, cons
                     const int j = k0 + l16 + 16 * k - p.st.L;  // a path token is seen from itself on
 #pragma unroll
                     for (int r = 0; r < 2; ++r)
-                        if (((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k].x + a[r][k].y - s_lse[r0 + r]);
+                        if (c0 + r0 + r < rows && ((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k].x + a[r][k].y - s_lse[r0 + r]);
                 }
             }
 #pragma unroll

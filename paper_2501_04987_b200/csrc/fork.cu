@@ -68,7 +68,7 @@ __global__ void __launch_bounds__(kForkThreads, RINGS ? 4 : 5) fork_kernel(Cache
         float s_kept = 0.f, sc[4];
         int p_kept = 0, w_kept = 0, ps[4], ws[4];
         bool lv[4];
-        auto fetch1 = [&](int o, float& sx, int& px, int& wx) { 
+        auto fetch1 = [&](int o, float& sx, int& px, int& wx) {
             const int src = plan.src[o];
             const UnitState st = unit_state(plan.seen[o], cv);
             const bool has = r < st.a || (r >= st.a + st.i && r < st.L + st.i);

@@ -1,5 +1,5 @@
-// Pieces shared by the two tensor-core kernels for drafted trees (verify_tc.cu: one tile of 128 query rows per block, two
-// blocks per SM; verify_tc2.cu: two tiles in one block).
+// Pieces of the tensor-core kernel for drafted trees (verify_tc.cu): tiles and ring, matrix descriptors, the drafted tokens'
+// tile, and what a row's result takes - its own block's, or the parts of a cluster joined.
 #pragma once
 
 #include "draft.cuh"

@@ -589,6 +589,31 @@ def test_accept_equals_a_chunk(gpu, dtype, d, hq, hkv):
     assert torch.equal(a, c)
 
 
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 4, 2), ("bf16", 64, 3, 3), ("f32", 64, 3, 3), ("f32", 128, 2, 1)])
+def test_accept_of_rows_and_keys_that_weigh_nothing(gpu, dtype, d, hq, hkv):
+    """A path token that saw nothing adds to no score, and a key whose logits are minus infinity gains exactly nothing, in
+    calls whose rows do not fill a tile."""
+    import torch
+
+    kv = gpu.TreeKV(40, hq, hkv, d, dtype, 2, 8)
+    q, k, v = _draft(kv, 3, 30)
+    blind = torch.tensor([[0, 2, 6], [1, 3, 7]], dtype=torch.int64, device="cuda")  # sequence 0: the first sees nothing
+    out, lse = kv.verify_tree(q, k, v, mask=blind)
+    assert bool((lse[0, 0] == -math.inf).all()) and bool((out[0, 0] == 0).all())
+    kv.accept_path(q, k, v, lse, torch.tensor([[0], [0]], dtype=torch.int32, device="cuda"))
+    S = kv.scores()
+    assert bool((S[0, :, 0] == 0).all()) and float((S[1, :, 0] - 1).abs().max()) <= (d + 16) * U32 * 60
+    q[..., 0] = q[..., 0].abs() + 0.5
+    k[:, 1, :, 0] = -math.inf                      # the path's second token: logits of minus infinity from every query
+    for _ in range(2):                             # as a token of the path, then as a cached one
+        out, lse = kv.verify_tree(q, k, v)
+        assert bool(torch.isfinite(lse[:, 0]).all()) and not bool(torch.isnan(out).any())
+        kv.accept_path(q, k, v, lse, torch.tensor([[0, 1, 2], [0, 1, 2]], dtype=torch.int32, device="cuda"))
+        S = kv.scores()
+        assert bool(torch.isfinite(S).all()) and bool((S[:, :, 2] == 0).all())
+    assert kv.stats()["device_error"] == 0
+
+
 @pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 64, 2, 2), ("f32", 64, 4, 1)])
 def test_a_draft_of_one_is_a_decode_step(gpu, dtype, d, hq, hkv):
     """One drafted token, accepted: the cache of a decode step, and its output."""
