@@ -394,7 +394,8 @@ class TreeKV:
         t, want, dt = self.torch, self._want, self.tdtype
         Hq, Hkv, d = self.n_heads, self.n_kv_heads, self.head_dim
         row = (Hq + 2 * Hkv) * d
-        if not (qkv.dim() == 2 and qkv.dtype is dt and qkv.device == self.device and qkv.shape[1] == row and qkv.stride(1) == 1):
+        steps = qkv.stride()
+        if not (len(steps) == 2 and steps[1] == 1 and qkv.shape[1] == row and qkv.dtype is dt and qkv.device == self.device):
             raise ValueError("expected a %s tensor [tokens, %d] with adjacent columns on %s, got %s %s on %s" %
                              (dt, row, self.device, qkv.dtype, tuple(qkv.shape), qkv.device))
         n = qkv.shape[0]
@@ -410,22 +411,22 @@ class TreeKV:
         if positions is not None:
             pp = want(positions, t.int32, (n,), "positions")
         if q is None:
-            q = qkv.new_empty((n, Hq, d))
+            q = qkv.new_empty(n, Hq, d)
             pq = q.data_ptr()
         else:
             pq = want(q, dt, (n, Hq, d), "q")
         if k is None:
-            k = qkv.new_empty((n, Hkv, d))
+            k = qkv.new_empty(n, Hkv, d)
             pk = k.data_ptr()
         else:
             pk = want(k, dt, (n, Hkv, d), "k")
         if v is None:
-            v = qkv.new_empty((n, Hkv, d))
+            v = qkv.new_empty(n, Hkv, d)
             pv = v.data_ptr()
         else:
             pv = want(v, dt, (n, Hkv, d), "v")
         # (torch reports any stride for the rows of a tensor of one row)
-        st = lib.treekv_norm_rope(self._h, qkv.data_ptr(), qkv.stride(0) if n > 1 else row, wq, wk, eps, pc, ps, slots, pp, pq, pk, pv,
+        st = lib.treekv_norm_rope(self._h, qkv.data_ptr(), steps[0] if n > 1 else row, wq, wk, eps, pc, ps, slots, pp, pq, pk, pv,
                                   n, self._stream())
         if st:
             _check(st, "treekv_norm_rope")
@@ -440,12 +441,12 @@ class TreeKV:
         pq, pk, pv = want(q, dt, (B, n, Hq, d), "q"), want(k, dt, (B, n, Hkv, d), "k"), want(v, dt, (B, n, Hkv, d), "v")
         pm = None if mask is None else want(mask, self.torch.int64, (B, n), "mask")
         if out is None:
-            out = q.new_empty((B, n, Hq, d))
+            out = q.new_empty(B, n, Hq, d)
             po = out.data_ptr()
         else:
             po = want(out, dt, (B, n, Hq, d), "out")
         if lse is None:
-            lse = q.new_empty((B, n, Hq), dtype=self.torch.float32)
+            lse = q.new_empty(B, n, Hq, dtype=self.torch.float32)
             pl = lse.data_ptr()
         else:
             pl = want(lse, self.torch.float32, (B, n, Hq), "lse")

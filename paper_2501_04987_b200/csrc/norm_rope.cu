@@ -8,6 +8,10 @@
 // Bound by memory traffic: every element is read once and written once.  A lane holds the same VEC channels of both
 // halves of a head, so a pair never leaves its lane, the norm is one butterfly over the D / (2 VEC) lanes of a head, and a
 // lane's cos, sin and weights serve all the heads its warp takes.
+//
+// Measured (B200, weights and tables given): 4096 tokens of 32 + 2 x 8 heads of 128 in bf16, 102.8 MB: 16.4 us = 6.27 TB/s,
+// 97 % of a copy's bandwidth.  1531 tokens of 12 heads of 64 in fp32: 3.2 us out of L2; 32 tokens of 48 heads in bf16: 2.0 us,
+// a launch and two trips to memory.
 #include "draft.cuh"
 
 namespace treekv {

@@ -20,6 +20,20 @@
 // In-cache positions (a variant of its own): the softmax warps encode each K tile in place at its cache slots, two tiles
 // ahead, and the queries and drafted keys at the slots where they will sit if accepted.
 //
+// Measured (B200, d = 128; drafted tokens x sequences x cached tokens x KV heads x query heads of each): 1 x 8 x 1024 x 32 x 1:
+// 26.8 us, 134 MB = 5.0 TB/s, 78 % of a copy's bandwidth.  16 x 32 x 2048 x 8 x 4 (ragged): 42.6 us, 220 MB = 5.2 TB/s, 80 %.
+// 64 x 32 x 2048 x 8 x 4: 94 us, 69.8 GFLOP = 743 TFLOP/s: two tiles of 128 rows per unit, so the keys are read twice (the
+// second time from L2), and a block's period of 1950 cycles per key tile is a chain - logits out of tensor memory, 64
+// exponentials per row, weights back, P V, each hand-over an mbarrier of 160 to 370 cycles - that the second block on the SM
+// hides in part.  24 x 1 x 4096 x 8 x 4: 18.4 us, an eighth of the machine's blocks at most 9 tiles long, then the join: some
+// 5 us of distributed shared memory at 10 bytes per clock and SM.  In-cache positions: 52.8, 95.4, 202 us for the first three.
+//
+// Not taken, with what the first three and the last took instead of 26.7 / 44.6 / 99.4 / 17.1 us at that time: key tiles of 128
+// with eight softmax warps and two ring slots (31.1 / 50.5 / 121.6 / 18.5); two groups of softmax warps on alternate tiles
+// (30.1 / 52.3 / 111 / 19.0); the rows repeated in idle lanes, each with a part of the exponentials (28.3 / 48.0 / 97.1 / 19.8);
+// S and P V issued by two warps (224 threads leave 128 registers: 28.4 / 48.7 / 124 / 21.2); first tiles asked into L2 ahead of
+// the stream-order wait (26.8 / 46.3 / 106 / 17.4).
+//
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
 #include <algorithm>
 
