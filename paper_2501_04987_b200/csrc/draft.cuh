@@ -49,6 +49,17 @@ __device__ inline float2 fma2(float2 a, float2 b, float2 c) {
     return d;
 }
 struct alignas(16) Float22 { float2 lo, hi; };  // four floats as the two pairs fma2() takes
+// reads of another block's shared memory, at an address of the cluster
+__device__ inline float4 ld_remote_v4(uint32_t caddr) {
+    float4 v;
+    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(caddr) : "memory");
+    return v;
+}
+__device__ inline float2 ld_remote_v2(uint32_t caddr) {
+    float2 v;
+    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(caddr) : "memory");
+    return v;
+}
 #endif
 
 // draft lengths of a verify call, accepted lengths of an accept call: 0..64

@@ -2,16 +2,23 @@
 //
 // Row r = token * G + head-in-group of one unit (sequence, KV head) attends to every cached row and to the drafted
 // tokens its mask names: out = softmax(q k / sqrt d) v in one pass over the keys with a running maximum and sum, all
-// fp32.  A block owns 8 RT rows and walks key tiles of 64 in shared memory.  A thread owns RT rows (with the fifteen others
-// of its half-warp) and takes four keys of each tile for the logits, D / 16 channels for the output: with four rows 64
-// multiply-adds for eight 16-byte reads of shared memory, most of them broadcasts, so the arithmetic is what bounds it once
-// there are enough rows.  RT follows the call's rows: every thread has some, and the keys are read by as few blocks as can
-// be.  A row's weights never leave its half-warp.  The next K tile is on its way while the weights meet V, the next V tile
-// while the logits are made.  With few units the keys of a unit are dealt to a cluster of blocks, which join their partial
-// results in shared memory.
+// fp32.  A block owns R rows; its four warps deal the key tiles of 16 among themselves and do all R rows of theirs, each
+// with a running maximum, a sum and an output of its own: no warp waits for another until the parts are joined.
 //
-// Measured (B200): 13 drafted tokens over 256 cached ones, 4 heads of 64: 7.9 us, the latency of two tiles and of the join.
-// Calls with enough rows for four per thread: 28 TFLOP/s.
+// What counts beside memory is registers filled from shared memory (128 bytes a clock, broadcasts too), so a lane takes 4 keys
+// x 8 rows at a time for the logits - 12 reads of 16 bytes for 64 packed multiply-adds - over an eighth of the channels, and
+// eight lanes add theirs up by halves, which leaves each with a row of its own; for the output it takes R rows x four (D = 64:
+// two) channels.  K of the next tile is on its way while the weights meet V, V of the next one during the logits.
+// With few units the keys of a unit are dealt to a cluster of blocks, which join their results in shared memory.
+//
+// Measured (B200, D = 128, 20 sequences x 1024 cached tokens x 3 KV heads of eight query heads): 1, 2, 8, 32, 64 drafted tokens
+// 29, 35, 96, 314, 622 us, the last at 27 TFLOP/s (packed multiply-adds take 2.7 to 3.5 cycles of a scheduler; as pairs of plain
+// ones 680 us).  6 x 494 x 16 x 8, one token: 18 us.  13 tokens over 256 cached ones, 4 heads of 64: 8.5 us, start and join.
+// The form that this one replaced - a thread one to eight rows against four keys, the block in step over tiles of 64 -
+// took 50, 47, 99, 312, 574 and 39 and 7.9 us: it read the keys four times as often for few rows, and its loads waited for a
+// block's barriers.
+#include <algorithm>
+
 #include "draft.cuh"
 #include "tma.cuh"
 
@@ -19,218 +26,285 @@ namespace treekv {
 
 namespace {
 
-constexpr int kThreads = 128;
-constexpr int kKeys = 64;
+constexpr int kThreads = 128, kWarps = kThreads / 32;
+constexpr int kKeys = 16;
 constexpr int kMaxSplit = 8;
 
-template <int D> constexpr int k_pitch() { return D + 4; }  // floats: sixteen keys' 16-byte reads meet no conflict
-template <int D, int RT> constexpr size_t smem_bytes() {
-    return sizeof(float) * ((size_t)(8 * RT + kKeys) * k_pitch<D>() + (size_t)kKeys * D + (size_t)8 * RT * (kKeys + 4));
-}
+constexpr int kPPitch = kKeys + 4;  // floats: eight rows' weights of four keys lie on different banks
+// floats of a warp: K, V, weights, factors of the rows
+template <int D, int R> constexpr int warp_floats() { return 2 * kKeys * D + R * kPPitch + R; }
+template <int D, int R> constexpr size_t smem_bytes() { return sizeof(float) * ((size_t)R * D + kWarps * (size_t)warp_floats<D, R>()); }
 
-__device__ inline void cp_async_16(float* dst, const void* src) {
-    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src) : "memory");
+// 16 bytes of global memory, or zeros
+__device__ inline void cp_async_16(float* dst, const float* src, bool real) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"((uint32_t)__cvta_generic_to_shared(dst)), "l"(src), "r"(real ? 16 : 0) : "memory");
 }
 __device__ inline void cp_async_commit() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 template <int N> __device__ inline void cp_async_wait() { asm volatile("cp.async.wait_group %0;" ::"n"(N) : "memory"); }
 
-template <int D, int RT>
-__global__ void __launch_bounds__(kThreads, 2)
+// A tile of up to 16 keys: cached rows below the split point of the slab, behind it, or drafted tokens.
+struct Tile {
+    const float *k, *v;  // first row
+    int step;            // floats between rows
+    int valid, slot, j;  // rows that exist; the first one's cache slot; its drafted token (-1: cached)
+};
+
+constexpr int blocks_per_sm(int R) { return R == 8 ? 3 : 2; }
+
+template <int D, int R>
+__global__ void __launch_bounds__(kThreads, blocks_per_sm(R))
 verify_f32_kernel(CacheView cv, DraftView dv, DraftLens lens, float* __restrict__ out, float* __restrict__ lse, int split) {
-    constexpr int kRows = 8 * RT;
-    constexpr int VEC = 4, HALF = D / 2 / VEC, KP = k_pitch<D>(), PP = kKeys + 4, NC = D / 64;  // NC: float4s of a thread's channels
+    constexpr int PP = kPPitch, RG = R / 8, CPL = D / 32;  // RG: groups of eight rows; CPL: a lane's channels of the output
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.z, b = unit / cv.Hkv, kh = unit % cv.Hkv, rank = blockIdx.x;
-    const int n = lens.n[b], G = cv.Hq / cv.Hkv, r0 = blockIdx.y * kRows, rows = min(kRows, n * G - r0);
+    const int n = lens.n[b], G = cv.Hq / cv.Hkv, r0 = blockIdx.y * R, rows = min(R, n * G - r0);
     if (rows <= 0) return;  // the whole cluster
     const UnitState st = unit_state(cv.n_seen[unit], cv);
-    const int total = st.L + n, per = ((total + split - 1) / split + kKeys - 1) / kKeys * kKeys;
-    const int lo = min(rank * per, total), hi = min(lo + per, total);  // this block's live indices
-    const float* Kc = reinterpret_cast<const float*>(cv.K) + (size_t)unit * cv.R * D;
-    const float* Vc = reinterpret_cast<const float*>(cv.V) + (size_t)unit * cv.R * D;
-    const float* kd = reinterpret_cast<const float*>(dv.k) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
-    const float* vd = reinterpret_cast<const float*>(dv.v) + ((size_t)b * dv.stride * cv.Hkv + kh) * D;
-    const size_t dstep = (size_t)cv.Hkv * D;
+    const int a = min(st.a, st.L), nA = (a + kKeys - 1) / kKeys, nC = nA + (st.L - a + kKeys - 1) / kKeys;  // tiles below the split point, cached ones
+    const int all = nC + (n + kKeys - 1) / kKeys, per = (all + split - 1) / split, t0 = min(rank * per, all), t1 = min(t0 + per, all);
+    const int dstep = cv.Hkv * D;
+    const size_t dfirst = ((size_t)b * dv.stride * cv.Hkv + kh) * D;
+    const float* vd = reinterpret_cast<const float*>(dv.v) + dfirst;
 
     extern __shared__ __align__(16) float smem[];
-    float* sq = smem;                    // [kRows][KP]
-    float* sk = sq + kRows * KP;         // [kKeys][KP]
-    float* sv = sk + kKeys * KP;         // [kKeys][D]
-    float* sp = sv + kKeys * D;          // [kRows][PP]
-    __shared__ uint64_t s_sees[kRows];
-    __shared__ unsigned int s_bad[2];    // drafted tokens of this block's keys with a value that is not finite
-    const int tid = threadIdx.x;
+    __shared__ uint64_t s_sees[R];
+    __shared__ __align__(8) uint32_t s_bad[2];  // drafted tokens of this block's keys with a value that is not finite
+    __shared__ __align__(8) float s_stat[R][2];
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = lane & 7, kg = lane >> 3;
+    float* sq = smem;                                                    // [R][D]
+    auto area = [&](int w) { return smem + R * D + w * warp_floats<D, R>(); };
+    float* sk = area(warp);                                              // [kKeys][D]
+    float* sv = sk + kKeys * D;                                          // [kKeys][D]
+    float* sp = sv + kKeys * D;                                          // [R][PP]
+    float* sf = sp + R * PP;                                             // [R]
     const bool rope = cv.rope_cos != nullptr;
     const float scale = kLog2e * rsqrtf((float)D);
 
-    if (tid < kRows) s_sees[tid] = tid < rows ? draft_sees(dv, b, (r0 + tid) / G, n) : 0ull;
-    if (tid < 2) s_bad[tid] = 0u;
-
-    auto row_of = [&](const float* cache, const float* draft, int lam) { return lam < st.L ? cache + (size_t)phys_row(lam, st) * D : draft + (size_t)(lam - st.L) * dstep; };
-    // K tile at k0: straight from memory, or through registers where the keys are encoded at their slots
-    auto load_k = [&](int k0) {
-        const int kn = min(kKeys, hi - k0);
-        if (!rope) {
-            for (int e = tid; e < kn * (D / 4); e += kThreads) {
-                const int r = e / (D / 4), c = e % (D / 4);
-                cp_async_16(sk + r * KP + c * 4, reinterpret_cast<const float*>(row_of(Kc, kd, k0 + r)) + c * 4);
-            }
+    auto tile_at = [&](int x) {
+        Tile t;
+        if (x < nC) {
+            const int lam = x < nA ? x * kKeys : a + (x - nA) * kKeys, end = x < nA ? a : st.L;
+            const size_t at = ((size_t)unit * cv.R + (x < nA ? lam : lam + st.i)) * D;
+            t.k = reinterpret_cast<const float*>(cv.K) + at; t.v = reinterpret_cast<const float*>(cv.V) + at;
+            t.step = D; t.valid = min(kKeys, end - lam); t.slot = lam; t.j = -1;
         } else {
-            for (int e = tid; e < kn * HALF; e += kThreads) {
-                const int r = e / HALF, c = e % HALF, lam = k0 + r;
-                const float* row = row_of(Kc, kd, lam);
-                float x[VEC], y[VEC];
-                Elem<float>::unpack(ld_plain(row + c * VEC), x);
-                Elem<float>::unpack(ld_plain(row + D / 2 + c * VEC), y);
-                const int slot = lam < st.L ? lam : st.L + draft_depth(draft_sees(dv, b, lam - st.L, n));
-                rope_pairs(x, y, cv.rope_cos + (size_t)slot * (D / 2) + c * VEC, cv.rope_sin + (size_t)slot * (D / 2) + c * VEC);
-                *reinterpret_cast<float4*>(sk + r * KP + c * VEC) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4*>(sk + r * KP + D / 2 + c * VEC) = make_float4(y[0], y[1], y[2], y[3]);
-            }
+            t.j = (x - nC) * kKeys; t.valid = min(kKeys, n - t.j); t.slot = 0; t.step = dstep;
+            t.k = reinterpret_cast<const float*>(dv.k) + dfirst + t.j * dstep; t.v = vd + t.j * dstep;
         }
-        cp_async_commit();
+        return t;
     };
-    // V tile; a drafted value that is not finite is left out here - a weight of zero would spread it - and added at the end
-    auto load_v = [&](int k0) {
-        const int kn = min(kKeys, hi - k0);
-        for (int e = tid; e < kKeys * (D / VEC); e += kThreads) {
-            const int r = e / (D / VEC), c = e % (D / VEC), lam = k0 + r;
-            float* dst = sv + r * D + c * VEC;
-            if (r < kn && lam < st.L) {
-                cp_async_16(dst, reinterpret_cast<const float*>(Vc) + (size_t)phys_row(lam, st) * D + c * VEC);
-                continue;
-            }
-            float x[VEC];
+    // the rows of a tile, 16 bytes a lane; rows that do not exist become zeros
+    auto load = [&](float* dst, const float* src, const Tile& t) {
+        constexpr int PIECES = D / 4, RPI = 32 / PIECES;  // rows per instruction
+        const int r_ = RPI == 1 ? 0 : lane / PIECES, c = lane % PIECES * 4;
 #pragma unroll
-            for (int u = 0; u < VEC; ++u) x[u] = 0.f;
-            if (r < kn) {  // a drafted one
-                Elem<float>::unpack(ld_plain(vd + (size_t)(lam - st.L) * dstep + c * VEC), x);
-#pragma unroll
-                for (int u = 0; u < VEC; ++u)
-                    if (!(fabsf(x[u]) < INFINITY)) { x[u] = 0.f; atomicOr(&s_bad[(lam - st.L) >> 5], 1u << ((lam - st.L) & 31)); }
-            }
-            *reinterpret_cast<float4*>(dst) = make_float4(x[0], x[1], x[2], x[3]);
+        for (int x = 0; x < kKeys / RPI; ++x) {
+            const int r = x * RPI + r_;
+            const bool real = r < t.valid;
+            cp_async_16(dst + r * D + c, src + (real ? r * t.step : 0) + c, real);
         }
-        cp_async_commit();
     };
 
+    int x = t0 + warp;
+    if (x < t1) {
+        const Tile t = tile_at(x);
+        load(sk, t.k, t); cp_async_commit();
+        load(sv, t.v, t); cp_async_commit();
+    }
+    if (tid < R) s_sees[tid] = tid < rows ? draft_sees(dv, b, (r0 + tid) / G, n) : 0ull;
+    if (tid < 2) s_bad[tid] = 0u;
     __syncthreads();
-    if (lo < hi) { load_k(lo); load_v(lo); }
-    for (int e = tid; e < kRows * HALF; e += kThreads) {   // queries: encoded at their slot, scaled
-        const int r = e / HALF, c = e % HALF;
-        float x[VEC], y[VEC];
-#pragma unroll
-        for (int u = 0; u < VEC; ++u) { x[u] = 0.f; y[u] = 0.f; }
+    for (int e = tid; e < R * (D / 8); e += kThreads) {   // queries: encoded at their slot, scaled
+        const int r = e / (D / 8), c = e % (D / 8);
+        float u[4] = {0.f, 0.f, 0.f, 0.f}, w[4] = {0.f, 0.f, 0.f, 0.f};
         if (r < rows) {
             const float* row = reinterpret_cast<const float*>(dv.q) + (((size_t)b * dv.stride + (r0 + r) / G) * cv.Hq + kh * G + (r0 + r) % G) * D;
-            Elem<float>::unpack(ld_plain(row + c * VEC), x);
-            Elem<float>::unpack(ld_plain(row + D / 2 + c * VEC), y);
+            Elem<float>::unpack(ld_plain(row + c * 4), u);
+            Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), w);
             if (rope) {
-                const size_t at = (size_t)(st.L + draft_depth(s_sees[r])) * (D / 2) + c * VEC;
-                rope_pairs(x, y, cv.rope_cos + at, cv.rope_sin + at);
+                const size_t at = (size_t)(st.L + draft_depth(s_sees[r])) * (D / 2) + c * 4;
+                rope_pairs(u, w, cv.rope_cos + at, cv.rope_sin + at);
             }
         }
-#pragma unroll
-        for (int u = 0; u < VEC; ++u) { sq[r * KP + c * VEC + u] = x[u] * scale; sq[r * KP + D / 2 + c * VEC + u] = y[u] * scale; }
+        *reinterpret_cast<float4*>(sq + r * D + c * 4) = make_float4(u[0] * scale, u[1] * scale, u[2] * scale, u[3] * scale);
+        *reinterpret_cast<float4*>(sq + r * D + D / 2 + c * 4) = make_float4(w[0] * scale, w[1] * scale, w[2] * scale, w[3] * scale);
     }
+    __syncthreads();
 
-    const int rg = tid / 16 * RT, l16 = tid % 16;  // this thread's rows; its keys l16 + 16 i, its channels 4 l16 + 64 i
-    const bool live = rg < rows;                   // of the half-warp
-    const uint32_t mine = 0xffffu << (threadIdx.x & 16);  // its lanes
-    float m[RT], l[RT];
-    Float22 o[RT][NC];
+    float m[RG], l[RG];  // of rows 8 g + part; l: of this lane's keys
+    float2 o[R][CPL / 2];
 #pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        m[r] = -INFINITY; l[r] = 0.f;
+    for (int g = 0; g < RG; ++g) { m[g] = -INFINITY; l[g] = 0.f; }
 #pragma unroll
-        for (int c = 0; c < NC; ++c) o[r][c].lo = o[r][c].hi = make_float2(0.f, 0.f);
-    }
-    for (int k0 = lo; k0 < hi; k0 += kKeys) {
+    for (int r = 0; r < R; ++r)
+#pragma unroll
+        for (int c = 0; c < CPL / 2; ++c) o[r][c] = make_float2(0.f, 0.f);
+    for (; x < t1; x += kWarps) {
+        const Tile t = tile_at(x);
+        const bool more = x + kWarps < t1;
+        const Tile next = more ? tile_at(x + kWarps) : t;
         cp_async_wait<1>();   // K has arrived (V may still be on its way)
-        __syncthreads();
-        if (live) {
-            float2 a2[RT][4];  // even and odd channels
-#pragma unroll
-            for (int r = 0; r < RT; ++r)
-#pragma unroll
-                for (int k = 0; k < 4; ++k) a2[r][k] = make_float2(0.f, 0.f);
-#pragma unroll 4
-            for (int c = 0; c < D; c += 4) {
-                Float22 q4[RT], k4[4];
-#pragma unroll
-                for (int r = 0; r < RT; ++r) q4[r] = *reinterpret_cast<const Float22*>(sq + (rg + r) * KP + c);
-#pragma unroll
-                for (int k = 0; k < 4; ++k) k4[k] = *reinterpret_cast<const Float22*>(sk + (l16 + 16 * k) * KP + c);
-#pragma unroll
-                for (int r = 0; r < RT; ++r)
-#pragma unroll
-                    for (int k = 0; k < 4; ++k) a2[r][k] = fma2(q4[r].hi, k4[k].hi, fma2(q4[r].lo, k4[k].lo, a2[r][k]));
+        __syncwarp();
+        if (rope) {           // keys encoded at their slots, in place
+            for (int e = lane; e < t.valid * (D / 8); e += 32) {
+                const int r = e / (D / 8), c = e % (D / 8) * 4;
+                const int slot = t.j < 0 ? t.slot + r : st.L + draft_depth(draft_sees(dv, b, t.j + r, n));
+                float4 &lo = *reinterpret_cast<float4*>(sk + r * D + c), &hi = *reinterpret_cast<float4*>(sk + r * D + D / 2 + c);
+                float u[4] = {lo.x, lo.y, lo.z, lo.w}, w[4] = {hi.x, hi.y, hi.z, hi.w};
+                rope_pairs(u, w, cv.rope_cos + (size_t)slot * (D / 2) + c, cv.rope_sin + (size_t)slot * (D / 2) + c);
+                lo = make_float4(u[0], u[1], u[2], u[3]); hi = make_float4(w[0], w[1], w[2], w[3]);
             }
-            float a[RT][4];
+            __syncwarp();
+        }
+        float s[RG][4];       // logits of row 8 g + part and keys kg + 4 i
 #pragma unroll
-            for (int r = 0; r < RT; ++r)
+        for (int g = 0; g < RG; ++g) {
+            float2 acc[8][4];  // rows x keys, over this lane's pieces: even and odd channels
 #pragma unroll
-                for (int k = 0; k < 4; ++k) a[r][k] = a2[r][k].x + a2[r][k].y;
-            const bool all_seen = k0 + kKeys <= min(hi, st.L);
+            for (int r = 0; r < 8; ++r)
 #pragma unroll
-            for (int r = 0; r < RT; ++r) {
-                if (!all_seen) {
+                for (int i = 0; i < 4; ++i) acc[r][i] = make_float2(0.f, 0.f);
+#pragma unroll 1
+            for (int c = 4 * part; c < D; c += 32) {
+                Float22 k4[4];
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const int lam = k0 + l16 + 16 * k, j = lam - st.L;
-                        if (lam >= hi || (j >= 0 && !(s_sees[rg + r] >> j & 1))) a[r][k] = -INFINITY;
-                    }
+                for (int i = 0; i < 4; ++i) k4[i] = *reinterpret_cast<const Float22*>(sk + (kg + 4 * i) * D + c);
+#pragma unroll
+                for (int r = 0; r < 8; ++r) {
+                    const Float22 q4 = *reinterpret_cast<const Float22*>(sq + (8 * g + r) * D + c);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[r][i] = fma2(q4.hi, k4[i].hi, fma2(q4.lo, k4[i].lo, acc[r][i]));
                 }
-                float mx = fmaxf(fmaxf(a[r][0], a[r][1]), fmaxf(a[r][2], a[r][3]));
+            }
+            // eight lanes hold parts of 32 sums: halved three times, lane `part` is left with row `part`
+            float x4[4][4], x2[2][4];
+            const bool h4 = part & 4, h2 = part & 2, h1 = part & 1;
 #pragma unroll
-                for (int off = 8; off > 0; off >>= 1) mx = fmaxf(mx, __shfl_xor_sync(mine, mx, off, 16));
-                const float now = fmaxf(m[r], mx), ref = now == -INFINITY ? 0.f : now, fix = exp2f(m[r] - ref);
-                m[r] = now;
-                float sum = 0.f;
+            for (int r = 0; r < 4; ++r)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const float p = exp2f(a[r][k] - ref);
-                    sp[(rg + r) * PP + l16 + 16 * k] = p;
-                    sum += p;
+                for (int i = 0; i < 4; ++i) {
+                    const float lo = acc[r][i].x + acc[r][i].y, hi = acc[r + 4][i].x + acc[r + 4][i].y;
+                    x4[r][i] = (h4 ? hi : lo) + __shfl_xor_sync(0xffffffffu, h4 ? lo : hi, 4);
                 }
-                l[r] = l[r] * fix + sum;  // this thread's keys only
 #pragma unroll
-                for (int c = 0; c < NC; ++c) { o[r][c].lo.x *= fix; o[r][c].lo.y *= fix; o[r][c].hi.x *= fix; o[r][c].hi.y *= fix; }
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) x2[r][i] = (h2 ? x4[r + 2][i] : x4[r][i]) + __shfl_xor_sync(0xffffffffu, h2 ? x4[r][i] : x4[r + 2][i], 2);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s[g][i] = (h1 ? x2[1][i] : x2[0][i]) + __shfl_xor_sync(0xffffffffu, h1 ? x2[0][i] : x2[1][i], 1);
+        }
+        __syncwarp();         // nobody reads this K tile any more
+        if (more) load(sk, next.k, next);
+        cp_async_commit();
+        if (t.j >= 0 || t.valid < kKeys) {
+#pragma unroll
+            for (int g = 0; g < RG; ++g)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) {
+                    const int key = kg + 4 * i;
+                    if (key >= t.valid || (t.j >= 0 && !(s_sees[8 * g + part] >> (t.j + key) & 1))) s[g][i] = -INFINITY;
+                }
+        }
+        float now[RG];
+        bool grew = false;
+#pragma unroll
+        for (int g = 0; g < RG; ++g) {
+            now[g] = fmaxf(fmaxf(s[g][0], s[g][1]), fmaxf(s[g][2], s[g][3]));
+            now[g] = fmaxf(now[g], __shfl_xor_sync(0xffffffffu, now[g], 8));
+            now[g] = fmaxf(m[g], fmaxf(now[g], __shfl_xor_sync(0xffffffffu, now[g], 16)));
+            grew = grew || now[g] > m[g];
+        }
+        if (__any_sync(0xffffffffu, grew)) {
+#pragma unroll
+            for (int g = 0; g < RG; ++g) {
+                const float fix = now[g] == -INFINITY ? 1.f : exp2f(m[g] - now[g]);
+                m[g] = now[g]; l[g] *= fix;
+                if (kg == 0) sf[8 * g + part] = fix;
+            }
+            __syncwarp();
+#pragma unroll
+            for (int r = 0; r < R; ++r) {
+                const float fix = sf[r];
+#pragma unroll
+                for (int c = 0; c < CPL / 2; ++c) { o[r][c].x *= fix; o[r][c].y *= fix; }
             }
         }
-        cp_async_wait<0>();   // V has arrived
-        __syncthreads();      // and nobody reads this K tile any more
-        if (k0 + kKeys < hi) load_k(k0 + kKeys);
-        if (live) {
-#pragma unroll 2
-            for (int k = 0; k < kKeys; k += 4) {
-                float4 p4[RT];
 #pragma unroll
-                for (int r = 0; r < RT; ++r) p4[r] = *reinterpret_cast<const float4*>(sp + (rg + r) * PP + k);
+        for (int g = 0; g < RG; ++g)
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
+            for (int i = 0; i < 4; ++i) {
+                const float p = exp2f(s[g][i] - (m[g] == -INFINITY ? 0.f : m[g]));
+                l[g] += p;
+                sp[(8 * g + part) * PP + kg + 4 * i] = p;
+            }
+        cp_async_wait<1>();   // V has arrived
+        __syncwarp();
+        if (t.j >= 0) {       // a drafted value that is not finite is left out - a weight of zero would spread it - and added at the end
+            for (int e = lane; e < t.valid * D; e += 32)
+                if (!(fabsf(sv[e]) < INFINITY)) { sv[e] = 0.f; atomicOr(&s_bad[(t.j + e / D) >> 5], 1u << ((t.j + e / D) & 31)); }
+            __syncwarp();
+        }
+#pragma unroll 1
+        for (int k = 0; k < kKeys; k += 4) {
+            float2 v[4][CPL / 2];
 #pragma unroll
-                    for (int c = 0; c < NC; ++c) {
-                        const Float22 v4 = *reinterpret_cast<const Float22*>(sv + (k + u) * D + 64 * c + 4 * l16);
+            for (int u = 0; u < 4; ++u) {
+                if constexpr (CPL == 4) {
+                    const Float22 y = *reinterpret_cast<const Float22*>(sv + (k + u) * D + 4 * lane);
+                    v[u][0] = y.lo; v[u][1] = y.hi;
+                } else {
+                    v[u][0] = *reinterpret_cast<const float2*>(sv + (k + u) * D + 2 * lane);
+                }
+            }
 #pragma unroll
-                        for (int r = 0; r < RT; ++r) {
-                            const float p = u == 0 ? p4[r].x : u == 1 ? p4[r].y : u == 2 ? p4[r].z : p4[r].w;
-                            const float2 pp = make_float2(p, p);
-                            o[r][c].lo = fma2(pp, v4.lo, o[r][c].lo);
-                            o[r][c].hi = fma2(pp, v4.hi, o[r][c].hi);
-                        }
-                    }
+            for (int r = 0; r < R; ++r) {
+                const float4 p4 = *reinterpret_cast<const float4*>(sp + r * PP + k);
+#pragma unroll
+                for (int c = 0; c < CPL / 2; ++c) {
+                    o[r][c] = fma2(make_float2(p4.x, p4.x), v[0][c], o[r][c]);
+                    o[r][c] = fma2(make_float2(p4.y, p4.y), v[1][c], o[r][c]);
+                    o[r][c] = fma2(make_float2(p4.z, p4.z), v[2][c], o[r][c]);
+                    o[r][c] = fma2(make_float2(p4.w, p4.w), v[3][c], o[r][c]);
                 }
             }
         }
-        __syncthreads();      // nobody reads this V tile any more
-        if (k0 + kKeys < hi) load_v(k0 + kKeys);
+        __syncwarp();         // nobody reads this V tile, or these weights, any more
+        if (more) load(sv, next.v, next);
+        cp_async_commit();
+    }
+    cp_async_wait<0>();
+    __syncwarp();
+    // ---- the warps' parts meet: [R][D] of a warp's area, maximum and sum behind them where the weights were
+    static_assert(R <= 2 * kKeys, "a part fits the tiles' place");
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        if constexpr (CPL == 4) *reinterpret_cast<float4*>(sk + r * D + 4 * lane) = make_float4(o[r][0].x, o[r][0].y, o[r][1].x, o[r][1].y);
+        else *reinterpret_cast<float2*>(sk + r * D + 2 * lane) = o[r][0];
     }
 #pragma unroll
-    for (int r = 0; r < RT; ++r)
+    for (int g = 0; g < RG; ++g) {
+        l[g] += __shfl_xor_sync(0xffffffffu, l[g], 8);
+        l[g] += __shfl_xor_sync(0xffffffffu, l[g], 16);
+        if (kg == 0) { sp[2 * (8 * g + part)] = m[g]; sp[2 * (8 * g + part) + 1] = l[g]; }
+    }
+    __syncthreads();
+    auto weight = [](float m, float M) { return m == -INFINITY ? 0.f : exp2f(m - M); };
+    auto join_warps = [&](int row, int c, float& M, float& L) {
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+        M = -INFINITY; L = 0.f;
 #pragma unroll
-        for (int off = 8; off > 0; off >>= 1) l[r] += __shfl_xor_sync(mine, l[r], off, 16);
+        for (int w = 0; w < kWarps; ++w) M = fmaxf(M, area(w)[2 * kKeys * D + 2 * row]);
+#pragma unroll
+        for (int w = 0; w < kWarps; ++w) {
+            const float* stat = area(w) + 2 * kKeys * D + 2 * row;
+            const float f = weight(stat[0], M);
+            const float4 y = *reinterpret_cast<const float4*>(area(w) + row * D + 4 * c);
+            L += stat[1] * f;
+            sum.x += y.x * f; sum.y += y.y * f; sum.z += y.z * f; sum.w += y.w * f;
+        }
+        return sum;
+    };
 
     uint64_t bad = (uint64_t)s_bad[0] | (uint64_t)s_bad[1] << 32;
     auto finish = [&](int row, int ch, float4 x, float M, float L) {  // four channels of one row, joined
@@ -248,69 +322,74 @@ verify_f32_kernel(CacheView cv, DraftView dv, DraftLens lens, float* __restrict_
         if (lse && ch == 0) lse[at] = L == 0.f ? -INFINITY : (M + log2f(L)) * (1.0f / kLog2e);
     };
     if (split == 1) {
-#pragma unroll
-        for (int r = 0; r < RT; ++r)
-#pragma unroll
-            for (int c = 0; c < NC; ++c)
-                if (rg + r < rows) finish(rg + r, 64 * c + 4 * l16, make_float4(o[r][c].lo.x, o[r][c].lo.y, o[r][c].hi.x, o[r][c].hi.y), m[r], l[r]);
+        for (int e = tid; e < rows * (D / 4); e += kThreads) {
+            float M, L;
+            const float4 sum = join_warps(e / (D / 4), e % (D / 4), M, L);
+            finish(e / (D / 4), 4 * (e % (D / 4)), sum, M, L);
+        }
         return;
     }
-    // ---- the cluster's parts meet: a block joins rpo rows, and gets m, l and O of those rows from every block
-    constexpr int PITCH = D + 4;
-    const int rpo = (rows + split - 1) / split;
-    __shared__ __align__(8) float s_bad_of[kMaxSplit][2];
-    const uint32_t sPart = smem_addr_u32(smem), sStat = sPart + split * rpo * PITCH * 4;
-    __syncwarp();
-    cluster_sync_all();   // every block is done with its tiles
-#pragma unroll
-    for (int r = 0; r < RT; ++r) {
-        const int row = rg + r;
-        if (row < rows) {
-            const int owner = row / rpo, at = rank * rpo + row % rpo;
-            const uint32_t dst = map_to_cta(sPart, owner) + at * PITCH * 4;
-#pragma unroll
-            for (int c = 0; c < NC; ++c) st_remote_v4(dst + (64 * c + 4 * l16) * 4, o[r][c].lo.x, o[r][c].lo.y, o[r][c].hi.x, o[r][c].hi.y);
-            if (l16 == 0) st_remote_v2(map_to_cta(sStat, owner) + at * 8, m[r], l[r]);
-        }
+    // ---- and the cluster's: joined over its warps (in the first one's place), every block joins its share of the rows
+    for (int e = tid; e < rows * (D / 4); e += kThreads) {
+        const int row = e / (D / 4), c = e % (D / 4);
+        float M, L;
+        const float4 sum = join_warps(row, c, M, L);
+        *reinterpret_cast<float4*>(area(0) + row * D + 4 * c) = sum;
+        if (c == 0) { s_stat[row][0] = M; s_stat[row][1] = L; }
     }
-    if (tid < split) st_remote_v2(map_to_cta(smem_addr_u32(&s_bad_of[rank][0]), tid), __uint_as_float(s_bad[0]), __uint_as_float(s_bad[1]));
     __syncwarp();
     cluster_sync_all();
     bad = 0ull;
-    for (int s = 0; s < split; ++s) bad |= (uint64_t)__float_as_uint(s_bad_of[s][0]) | (uint64_t)__float_as_uint(s_bad_of[s][1]) << 32;
-    const float* stat = smem + split * rpo * PITCH;
-    for (int e = tid; e < rpo * (D / 4); e += kThreads) {
-        const int rl = e / (D / 4), c = e % (D / 4);
-        if (rank * rpo + rl >= rows) continue;
-        float M = -INFINITY, L = 0.f;
-        for (int s = 0; s < split; ++s) M = fmaxf(M, stat[(s * rpo + rl) * 2]);
-        float4 x = make_float4(0.f, 0.f, 0.f, 0.f);
-        for (int s = 0; s < split; ++s) {
-            const float ms = stat[(s * rpo + rl) * 2], f = ms == -INFINITY ? 0.f : exp2f(ms - M);
-            L += stat[(s * rpo + rl) * 2 + 1] * f;
-            const float4 y = *reinterpret_cast<const float4*>(smem + (s * rpo + rl) * PITCH + 4 * c);
-            x.x += y.x * f; x.y += y.y * f; x.z += y.z * f; x.w += y.w * f;
-        }
-        finish(rank * rpo + rl, 4 * c, x, M, L);
+    for (int s = 0; s < split; ++s) {
+        const float2 y = ld_remote_v2(map_to_cta(smem_addr_u32(s_bad), s));
+        bad |= (uint64_t)__float_as_uint(y.x) | (uint64_t)__float_as_uint(y.y) << 32;
     }
+    const int rpo = (rows + split - 1) / split;
+    for (int e = tid; e < rpo * (D / 4); e += kThreads) {
+        const int row = rank * rpo + e / (D / 4), c = e % (D / 4);
+        if (row >= rows) continue;
+        float2 stat[kMaxSplit];
+        float4 y[kMaxSplit];
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s)
+            if (s < split) {
+                stat[s] = ld_remote_v2(map_to_cta(smem_addr_u32(&s_stat[row][0]), s));
+                y[s] = ld_remote_v4(map_to_cta(smem_addr_u32(area(0) + row * D + 4 * c), s));
+            }
+        float M = -INFINITY, L = 0.f;
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s)
+            if (s < split) M = fmaxf(M, stat[s].x);
+        float4 sum = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+        for (int s = 0; s < kMaxSplit; ++s)
+            if (s < split) {
+                const float f = weight(stat[s].x, M);
+                L += stat[s].y * f;
+                sum.x += y[s].x * f; sum.y += y[s].y * f; sum.z += y[s].z * f; sum.w += y[s].w * f;
+            }
+        finish(row, 4 * c, sum, M, L);
+    }
+    __syncwarp();
+    cluster_sync_all();  // nobody leaves while its part may be read
 }
 
-template <int D, int RT>
-cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int tiles_r, int split, void* out, float* lse, cudaStream_t s) {
-    auto kern = verify_f32_kernel<D, RT>;
+template <int D, int R>
+cudaError_t launch_r(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int tiles_r, int split, void* out, float* lse, cudaStream_t s) {
+    auto kern = verify_f32_kernel<D, R>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
     dev &= 63;
     if (!smem_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, RT>());
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem_bytes<D, R>());
         if (e != cudaSuccess) return e;
         smem_set[dev] = true;
     }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(split, tiles_r, cv.B * cv.Hkv);
     cfg.blockDim = dim3(kThreads);
-    cfg.dynamicSmemBytes = smem_bytes<D, RT>();
+    cfg.dynamicSmemBytes = smem_bytes<D, R>();
     cfg.stream = s;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
@@ -324,35 +403,31 @@ cudaError_t launch_rt(const CacheView& cv, const DraftView& dv, const DraftLens&
     return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<float*>(out), lse, split);
 }
 
-// Rows per thread and blocks per cluster, by the time they should take: waves of two blocks per SM, each as long as its key
-// tiles, a tile as long as a thread's rows and a part that does not grow with them - the rows count once where a block has
-// its SM to itself, twice where two share it.  Up to 48 rows a tile with D = 128, so that two blocks' shared memory still
-// fits an SM.
+// Rows per block and blocks per cluster, by the time they should take in cycles: a warp's way through a key tile alone, or what
+// the blocks that share an SM need for theirs together, whichever is more; and as many of those as a warp has tiles, with some
+// for start and join.
 template <int D>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
-    const int G = cv.Hq / cv.Hkv, keys = cv.c + max_n;
-    int rt = 1, split = 1;
+    const int G = cv.Hq / cv.Hkv, keys = (cv.c + max_n + kKeys - 1) / kKeys + 1;
+    int rows = 8, split = 1;
     long least = -1;
-    for (int r = 1; r <= (D == 128 ? 6 : 8); r += r == 6 ? 2 : 1) {
+    for (int r = 8; r <= 24; r += 8) {
         long tiles = 0;
-        for (int b = 0; b < cv.B; ++b) tiles += (lens.n[b] * G + 8 * r - 1) / (8 * r);
+        for (int b = 0; b < cv.B; ++b) tiles += (lens.n[b] * G + r - 1) / r;
+        const long alone = 3000 + 300 * r, shared = 450 + 150 * r;
+        auto step = [&](long blocks) { return std::max(alone, (blocks + sms - 1) / sms * shared); };
         for (int x = 1; x <= kMaxSplit; x *= 2) {
-            if (x > 1 && keys <= (x / 2) * kKeys) break;
-            const long blocks = tiles * cv.Hkv * x, steps = (keys + x * kKeys - 1) / (x * kKeys) + 1;
-            const long cost = blocks <= sms ? steps * (3 + r) : (blocks + 2L * sms - 1) / (2L * sms) * steps * (3 + 2 * r);
-            if (least < 0 || cost < least) { least = cost; rt = r; split = x; }
+            if (x > 1 && keys <= (x / 2) * kWarps) break;
+            const long blocks = tiles * cv.Hkv * x, wave = (long)blocks_per_sm(r) * sms, left = blocks % wave;
+            const long steps = 2 * ((keys + x * kWarps - 1) / (x * kWarps)) + (x > 1 ? 5 : 3);
+            const long cost = steps * (blocks / wave * step(wave) + (left ? step(left) : 0));
+            if (least < 0 || cost < least) { least = cost; rows = r; split = x; }
         }
     }
-    const int tiles = (max_n * G + 8 * rt - 1) / (8 * rt);
-    switch (rt) {
-        case 1: return launch_rt<D, 1>(cv, dv, lens, tiles, split, out, lse, s);
-        case 2: return launch_rt<D, 2>(cv, dv, lens, tiles, split, out, lse, s);
-        case 3: return launch_rt<D, 3>(cv, dv, lens, tiles, split, out, lse, s);
-        case 4: return launch_rt<D, 4>(cv, dv, lens, tiles, split, out, lse, s);
-        case 5: return launch_rt<D, 5>(cv, dv, lens, tiles, split, out, lse, s);
-        case 6: return launch_rt<D, 6>(cv, dv, lens, tiles, split, out, lse, s);
-        default: return launch_rt<D, D == 128 ? 6 : 8>(cv, dv, lens, tiles, split, out, lse, s);
-    }
+    const int tiles = (max_n * G + rows - 1) / rows;
+    if (rows == 8) return launch_r<D, 8>(cv, dv, lens, tiles, split, out, lse, s);
+    if (rows == 16) return launch_r<D, 16>(cv, dv, lens, tiles, split, out, lse, s);
+    return launch_r<D, 24>(cv, dv, lens, tiles, split, out, lse, s);
 }
 
 }  // namespace

@@ -197,16 +197,6 @@ __device__ inline void store_row(const CacheView& cv, const DraftView& dv, int b
 // ---- Keys of a unit dealt to a cluster: every block has m, l and O of all its rows (the first is r0 of the unit) at its own
 // reference, and leaves them in its shared memory: [128][D + 4] floats, then [128][2].  Block q joins rows [q rpo, (q + 1) rpo),
 // reading the others' parts there (stores into the owner's memory took twice as long: 96 rows of eight blocks 4300 cycles).
-__device__ inline float4 ld_remote_v4(uint32_t caddr) {
-    float4 v;
-    asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(caddr) : "memory");
-    return v;
-}
-__device__ inline float2 ld_remote_v2(uint32_t caddr) {
-    float2 v;
-    asm volatile("ld.shared::cluster.v2.f32 {%0, %1}, [%2];" : "=f"(v.x), "=f"(v.y) : "r"(caddr) : "memory");
-    return v;
-}
 constexpr int kPartRows = 128;
 template <int D>
 __device__ inline void keep_row(float* part, int row, bool real, bool any, uint32_t tm, float m, float l) {
