@@ -4,7 +4,7 @@
 // and to the drafted tokens its mask names, in one pass over key tiles of 64:
 //     S = Q K^T        both from TMA-fed, 128-byte-swizzled shared memory, S in tensor memory (lane = query row)
 //     p = exp2(S c - m)  one thread per row: the running maximum m never leaves the thread
-//     O += P V         P goes back to tensor memory over S, as the matrix operand; O accumulates there
+//     O += P V         P goes back to tensor memory, beside S, as the matrix operand; O accumulates there
 // The reference m is moved - and O rescaled - only when a row's maximum outgrows it by 2^8: the weights stay within fp32's
 // and bf16's range, their relative precision is the same, and after the first tiles rescaling is rare.
 //
@@ -21,18 +21,21 @@
 // ahead, and the queries and drafted keys at the slots where they will sit if accepted.
 //
 // Measured (B200, d = 128; drafted tokens x sequences x cached tokens x KV heads x query heads of each): 1 x 8 x 1024 x 32 x 1:
-// 26.8 us, 134 MB = 5.0 TB/s, 78 % of a copy's bandwidth.  16 x 32 x 2048 x 8 x 4 (ragged): 42.6 us, 220 MB = 5.2 TB/s, 80 %.
-// 64 x 32 x 2048 x 8 x 4: 94 us, 69.8 GFLOP = 743 TFLOP/s: two tiles of 128 rows per unit, so the keys are read twice (the
-// second time from L2), and a block's period of 1950 cycles per key tile is a chain - logits out of tensor memory, 64
-// exponentials per row, weights back, P V, each hand-over an mbarrier of 160 to 370 cycles - that the second block on the SM
-// hides in part.  24 x 1 x 4096 x 8 x 4: 18.4 us, an eighth of the machine's blocks at most 9 tiles long, then the join: some
-// 5 us of distributed shared memory at 10 bytes per clock and SM.  In-cache positions: 52.8, 95.4, 202 us for the first three.
+// 26.3 us, 134 MB = 5.1 TB/s, 79 % of a copy's bandwidth.  16 x 32 x 2048 x 8 x 4 (ragged): 42.1 us, 220 MB = 5.2 TB/s, 81 %.
+// 24 x 1 x 4096 x 8 x 4: 18.4 us, an eighth of the machine's blocks at most 9 tiles long, then the join: some 2.5 us of
+// distributed shared memory at 10 bytes per clock and SM.  64 x 32 x 2048 x 8 x 4: 96 us, 69.8 GFLOP = 730 TFLOP/s, 1950 cycles
+// of a block per key tile, two blocks side by side: two tiles of 128 rows per unit, so the keys are fetched twice (the second
+// time from L2).  What that leaves idle is little: the MMAs of a tile take 650 cycles of the tensor core, their operands and
+// the arriving tiles some 770 of shared memory's bandwidth (Q is read again for each tile), and that twice.  In-cache positions:
+// 52.5, 91.5, 196 us for 1, 16 and 64 drafted tokens.
 //
-// Not taken, with what the first three and the last took instead of 26.7 / 44.6 / 99.4 / 17.1 us at that time: key tiles of 128
-// with eight softmax warps and two ring slots (31.1 / 50.5 / 121.6 / 18.5); two groups of softmax warps on alternate tiles
-// (30.1 / 52.3 / 111 / 19.0); the rows repeated in idle lanes, each with a part of the exponentials (28.3 / 48.0 / 97.1 / 19.8);
-// S and P V issued by two warps (224 threads leave 128 registers: 28.4 / 48.7 / 124 / 21.2); first tiles asked into L2 ahead of
-// the stream-order wait (26.8 / 46.3 / 106 / 17.4).
+// Not taken, with what the first two, 64 tokens and the single sequence took instead of 26.7 / 44.6 / 99.4 / 17.1 us at that time:
+// key tiles of 128 with eight softmax warps and two ring slots (31.1 / 50.5 / 121.6 / 18.5); two groups of softmax warps on
+// alternate tiles (30.1 / 52.3 / 111 / 19.0); the rows repeated in idle lanes, each with a part of the exponentials (28.3 / 48.0 /
+// 97.1 / 19.8); first tiles asked into L2 ahead of the stream-order wait (26.8 / 46.3 / 106 / 17.4).  And instead of 26.3 / 42.1 /
+// 96 / 18.4: two buffers for S with P over S (26.5 / 42.6 / 96 / 18.4; with positions 52.8 / 95.4 / 202); named barriers between
+// softmax and issuing warp (26.2 / 44.7 / 101 / 18.7; with positions 48.9 / 82.8 / 186); S and P V issued by two warps and K and V
+// loaded by two, 72 registers for those and 184 for a softmax warp (27.5 / 48.3 / 102 / 18.8).
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
 #include <algorithm>
@@ -49,7 +52,7 @@ constexpr int kThreads = 192;
 constexpr int kKeys = 64;                  // keys of a tile
 constexpr int kMaxSplit = 8;
 constexpr int kMaxSlots = 8;
-constexpr uint32_t kTmemCols = 256;        // S 64, S 64, O 128: two blocks share an SM's 512 columns
+constexpr uint32_t kTmemCols = 256;        // S 64, P 32 + 32, O 128: two blocks share an SM's 512 columns
 constexpr size_t kSmemMin = 80 * 1024;     // never a third block on an SM: it would wait for tensor memory inside a cluster
 constexpr size_t kSmemMax = 112 * 1024;
 static_assert(kKeys == kMaxDraft, "the drafted tokens are one tile");
@@ -57,8 +60,9 @@ static_assert(kKeys == kMaxDraft, "the drafted tokens are one tile");
 // FULL: a slot's tile has arrived.  USED: the MMAs that read it are done - for a K tile that also says that its logits are
 // there, for a V tile that its share of O is in: one commit and one barrier for both (a commit holds the issuing thread
 // for some 80 cycles).
+// S_READ: a tile's logits are in the softmax warps' registers, the next tile's may take their place.
 // KEYED: (in-cache positions) the softmax warps have encoded the K tile of that parity, or - the last one - the queries.
-enum Bar { Q_FULL = 0, P_FULL = 1, KEYED = 3, FULL = 6, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
+enum Bar { Q_FULL = 0, P_FULL = 1, KEYED = 3, S_READ = 6, FULL = 7, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
 
 template <int D, bool ROPE>
 __global__ void __launch_bounds__(kThreads, 2)
@@ -84,6 +88,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 
     if (tid == 0) {
         mbar_init(bar(Q_FULL), 1);
+        mbar_init(bar(S_READ), 4);
         for (int s = 0; s < 2; ++s) mbar_init(bar(P_FULL + s), 4);
         for (int s = 0; s < 3; ++s) mbar_init(bar(KEYED + s), 4);
         for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(USED + s), 1); }
@@ -94,7 +99,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, tmO = tmem + 128;  // S / P of tile j at column 64 (j & 1)
+    const uint32_t tmem = tmem_slot, tmP = tmem + 64, tmO = tmem + 128;  // P of tile j at column 64 + 32 (j & 1)
     pdl_wait();
     const UnitState st = unit_state(cv.n_seen[unit], cv);
     const Tiles t = my_tiles<kKeys>(st, rank, split);
@@ -135,36 +140,34 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             Ring rk(0, slots), rv(1, slots);
             int js = 0;  // the next tile whose logits are issued
             auto keyed = [&]() { return !ROPE || mbar_wait(bar(KEYED + (js & 1)), (js >> 1) & 1); };
-            auto issue_s = [&](int buf) {  // the next tile's logits
+            auto issue_s = [&]() {  // the next tile's logits
                 ++js;
                 tc_fence_after();
                 const uint32_t lo = k_lo + rk.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < D / 16; ++kk)
-                    umma_bf16(tmem + 64 * buf, desc_of(q_lo + (kk >> 2) * q_half + (kk & 3) * 2),
+                    umma_bf16(tmem, desc_of(q_lo + (kk >> 2) * q_half + (kk & 3) * 2),
                               desc_of(lo + (kk >> 2) * (VHALF / 16) + (kk & 3) * 2), idesc_s, kk > 0);
                 umma_commit(bar(USED + rk.slot));
                 rk.next(); rk.next();
             };
             ok = mbar_wait2(bar(Q_FULL), 0, bar(FULL + rk.slot), rk.phase) && (!ROPE || mbar_wait(bar(KEYED + 2), 0)) && keyed();
-            if (ok) issue_s(0);
-            if (ok && NT > 1 && (ok = mbar_wait(bar(FULL + rk.slot), rk.phase) && keyed())) issue_s(1);
+            if (ok) issue_s();
             int last = 0, last_phase = 0;
             for (int j = 0; j < NT && ok; ++j) {
-                const int buf = j & 1;
-                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + buf), (j >> 1) & 1))) break;
+                if (j + 1 < NT) {  // the logits of tile j are in registers: those of tile j + 1 take their place
+                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_READ), j & 1) && keyed())) break;
+                    issue_s();
+                }
+                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + (j & 1)), (j >> 1) & 1))) break;
                 tc_fence_after();
                 const uint32_t lo = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < kKeys / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes, 8 columns of packed P
-                    umma_bf16_ta(tmO, tmem + 64 * buf + 8 * kk, desc_of(lo + kk * (2048 / 16)), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
+                    umma_bf16_ta(tmO, tmP + 32 * (j & 1) + 8 * kk, desc_of(lo + kk * (2048 / 16)), idesc_o, (j > 0 || kk > 0) ? 1u : 0u);
                 last = rv.slot; last_phase = rv.phase;
                 umma_commit(bar(USED + last));
                 rv.next(); rv.next();
-                if (j + 2 < NT) {  // the logits of tile j + 2 overwrite P_j
-                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(USED + last), last_phase) && keyed())) break;
-                    issue_s(buf);
-                }
             }
             // every MMA of this block has finished before its memory and tensor memory are given to anything else
             if (ok) ok = mbar_wait(bar(USED + last), last_phase);
@@ -214,7 +217,7 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         Ring rk(0, slots), rv(1, slots);  // this tile's K and V
         int done = 0, done_phase = 0;     // V of the tile before
         for (int j = 0; j < NT && ok; ++j) {
-            const uint32_t tmS = tmem + 64 * (j & 1) + lane_off;
+            const uint32_t tmS = tmem + lane_off;
             const bool draft = t.draft && j == 0;
             int row0 = 0, valid = kKeys;
             if (!draft) cached_tile<kKeys>(t, j, row0, valid);
@@ -226,6 +229,9 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 tmem_ld32(tmS + 32, s1);
                 tmem_ld_wait_for(s0);
                 tmem_ld_wait_for(s1);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(S_READ));
                 if (draft || valid < kKeys) {
                     const uint64_t see = draft ? sees : low_bits(valid);
                     const uint32_t see0 = (uint32_t)see, see1 = (uint32_t)(see >> 32);
@@ -268,8 +274,11 @@ verify_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     p[e] = rope_pack_bf16(a, c); p[16 + e] = rope_pack_bf16(g, h);
                 }
                 l_run += sum0 + sum1;
-                tmem_st32(tmS, p);
+                // (the P of two tiles ago has been multiplied: those MMAs were committed with this tile's logits)
+                tmem_st32(tmP + 32 * (j & 1) + lane_off, p);
                 tmem_st_wait();
+            } else if (lane == 0) {
+                mbar_arrive(bar(S_READ));
             }
             if (!draft && valid < kKeys) {
                 if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
