@@ -8,14 +8,15 @@
 // the path's queries, 8 at a time, as its columns.  The contraction runs over channels in any order, so a lane's fragments
 // are 16-byte pieces of the rows (channels 32u + 8t.. of keys g and g + 8, of query g): no transposition.  A warp has a
 // ring of its own in shared memory, filled by bulk copies - 16 keys are 4 KB in one piece, or two at the ends of the cached
-// segments - and no other warp to wait for.  fp32: tiles of 64 keys and 32 query rows in shared memory, a thread two rows
-// against four keys.
+// segments - and no other warp to wait for.  fp32: a warp's tile is 16 keys too, a lane takes four of them against eight
+// rows over an eighth of the channels, and eight lanes add up by halves, which leaves each with one row's logits.
 //
 // Measured (B200, bf16, d = 128): up to six tokens into 32 sequences of up to 2048 x 8 heads, four query heads each, 103 MB:
 // 32.4 us = 3.2 TB/s; four tokens into 8 x 1024 x 32 heads, 74 MB: 16.4 us = 4.5 TB/s.  Half to two thirds of a copy's
 // bandwidth: one round of blocks on the machine, each with a serial head (path, queries) and tail (evictions: two trips to
-// memory); in between the keys stream.  fp32: 38 sequences x 16 heads, 1472 tokens, d = 128: 234 us (tiles of 32 rows x 64 keys;
-// one row of a thread against one key took 437).
+// memory); in between the keys stream, and the SMs that were dealt two full units end last.  fp32: one token of 12 sequences of
+// up to 929 x 16 heads, eight query heads each: 34.5 us (50.5 when a block went through tiles of 64 keys in step, a thread two
+// rows against four keys); up to five of 17 x 3604 x 8 x 8, d = 64: 75 (92).
 #include <cooperative_groups.h>
 
 #include "draft.cuh"
@@ -28,7 +29,7 @@ namespace {
 
 constexpr int kThreads = 256, kWarps = kThreads / 32;
 constexpr int kMaxDepth = 3;  // tiles of 16 keys a warp has on their way
-constexpr int kRows32 = 32, kKeys32 = 64;  // fp32: query rows and keys in shared memory at a time
+constexpr int kRows32 = 88;  // fp32: query rows in shared memory at a time, so that two blocks share an SM
 
 __device__ inline float ex2(float x) {
     float y;
@@ -201,127 +202,115 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
     if (!ok && lane == 0) atomicOr(&cv.stats->error, 4u);
 }
 
-// fp32, shared memory: [kRows32][D + 4] queries, two tiles [kKeys32][D + 4] of keys, [16][kKeys32] partial sums, [kRows32]
-// log-sum-exps, [keys of the block] sums
-template <int D> constexpr size_t f32_smem_floats(int keys) {
-    return (size_t)(kRows32 + 2 * kKeys32) * (D + 4) + 16 * kKeys32 + kRows32 + keys;
+// fp32, shared memory: [rows] queries of D channels (kRows32 at a time), their log-sum-exps, a tile of 16 keys per warp
+template <int D> constexpr size_t f32_smem_bytes(int rows8) {
+    const int rows = rows8 < kRows32 ? rows8 : kRows32;
+    return sizeof(float) * ((size_t)rows * (D + 1) + (size_t)kWarps * 16 * D);
 }
 template <int D>
 __device__ inline void scores_f32(const CacheView& cv, const DraftView& dv, const Path& p, const float* __restrict__ lse, int rank, int nblocks,
-                                  unsigned char* smem) {
-    constexpr int PITCH = D + 4;
-    float* sq = reinterpret_cast<float*>(smem);
-    float* sk = sq + kRows32 * PITCH;                // [2][kKeys32][PITCH]
-    float* red = sk + 2 * kKeys32 * PITCH;           // [16][kKeys32]
-    float* s_lse = red + 16 * kKeys32;
-    float* sums = s_lse + kRows32;
-    const int rows = p.n * p.G, tid = threadIdx.x, lg = __ffs(p.G) - 1;
-    const int per = (p.total + nblocks - 1) / nblocks, lo = min(rank * per, p.total), hi = min(lo + per, p.total);
+                                  unsigned char* smem, int rows8) {
+    const int at_once = min(rows8, kRows32), rows = p.n * p.G, lg = __ffs(p.G) - 1;
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, part = lane & 7, kg = lane >> 3;
+    float* sq = reinterpret_cast<float*>(smem);      // [at_once][D]
+    float* sk = sq + (size_t)at_once * D + warp * 16 * D;
+    float* s_lse = sq + (size_t)at_once * D + kWarps * 16 * D;
     const float scale = kLog2e * rsqrtf((float)D);
-    const int r0 = tid / 16 * 2, l16 = tid % 16;     // this thread's two rows; its keys l16 + 16 i
-    auto load_k = [&](int k0, int buf) {
-        float* dst = sk + buf * kKeys32 * PITCH;
-        const int kn = min(kKeys32, hi - k0);
-        if (!cv.rope_cos) {
-            for (int e = tid; e < kn * (D / 4); e += kThreads) {
-                const int r = e / (D / 4), c = e % (D / 4);
-                asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_addr_u32(dst + r * PITCH + c * 4)),
-                             "l"(key_row<float, D>(cv, dv, p, k0 + r) + c * 4) : "memory");
-            }
-        } else {
-            for (int e = tid; e < kn * (D / 8); e += kThreads) {
-                const int r = e / (D / 8), c = e % (D / 8);
-                const float* row = key_row<float, D>(cv, dv, p, k0 + r);
-                float x[4], y[4];
-                Elem<float>::unpack(ld_plain(row + c * 4), x);
-                Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
-                const size_t at = (size_t)(k0 + r) * (D / 2) + c * 4;
-                rope_pairs(x, y, cv.rope_cos + at, cv.rope_sin + at);
-                *reinterpret_cast<float4*>(dst + r * PITCH + c * 4) = make_float4(x[0], x[1], x[2], x[3]);
-                *reinterpret_cast<float4*>(dst + r * PITCH + D / 2 + c * 4) = make_float4(y[0], y[1], y[2], y[3]);
-            }
+    const int ntiles = (p.total + 15) / 16, step = nblocks * kWarps, first = rank * kWarps + warp;
+    auto load = [&](int tile) {  // rows that do not exist become zeros
+        constexpr int PIECES = D / 4, RPI = 32 / PIECES;  // rows per instruction
+#pragma unroll
+        for (int x = 0; x < 16 / RPI; ++x) {
+            const int r = x * RPI + (RPI == 1 ? 0 : lane / PIECES), c = lane % PIECES * 4, lam = tile * 16 + r;
+            asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(smem_addr_u32(sk + r * D + c)),
+                         "l"(key_row<float, D>(cv, dv, p, min(lam, p.total - 1)) + c), "r"(lam < p.total ? 16 : 0) : "memory");
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
-    for (int e = tid; e < hi - lo; e += kThreads) sums[e] = 0.f;
-    for (int c0 = 0; c0 < rows; c0 += kRows32) {     // 32 rows at a time over this block's keys
-        __syncthreads();
-        if (lo < hi) load_k(lo, 0);
-        for (int e = tid; e < kRows32 * (D / 8); e += kThreads) {  // queries: encoded at their slots, scaled
-            const int r = c0 + e / (D / 8), c = e % (D / 8);
-            float x[4] = {0.f, 0.f, 0.f, 0.f}, y[4] = {0.f, 0.f, 0.f, 0.f};
-            if (r < rows) {
-                const size_t at = (((size_t)p.b * dv.stride + p.node[r >> lg]) * cv.Hq + p.kh * p.G + (r & (p.G - 1)));
-                const float* row = reinterpret_cast<const float*>(dv.q) + at * D;
-                Elem<float>::unpack(ld_plain(row + c * 4), x);
-                Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), y);
-                if (cv.rope_cos) {
-                    const size_t tab = (size_t)(p.st.L + (r >> lg)) * (D / 2) + c * 4;
-                    rope_pairs(x, y, cv.rope_cos + tab, cv.rope_sin + tab);
-                }
-                if (c == 0) s_lse[r - c0] = row_reference(lse[at]);
+    for (int c0 = 0; c0 < rows; c0 += kRows32) {
+        const int here = min(kRows32, rows - c0), groups = (here + 7) / 8;
+        if (first < ntiles) load(first);
+        if (c0 > 0) __syncthreads();                 // nobody reads the last rows any more
+        for (int e = tid; e < groups * 8 * (D / 8); e += kThreads) {  // queries: encoded at their slots, scaled
+            const int r = e / (D / 8), c = e % (D / 8), x = c0 + min(r, here - 1);  // (rows that fill the last eight up: as in bf16)
+            const size_t at = (((size_t)p.b * dv.stride + p.node[x >> lg]) * cv.Hq + p.kh * p.G + (x & (p.G - 1)));
+            const float* row = reinterpret_cast<const float*>(dv.q) + at * D;
+            float u[4], w[4];
+            Elem<float>::unpack(ld_plain(row + c * 4), u);
+            Elem<float>::unpack(ld_plain(row + D / 2 + c * 4), w);
+            if (cv.rope_cos) {
+                const size_t tab = (size_t)(p.st.L + (x >> lg)) * (D / 2) + c * 4;
+                rope_pairs(u, w, cv.rope_cos + tab, cv.rope_sin + tab);
             }
-            float* dst = sq + (r - c0) * PITCH + c * 4;
-            *reinterpret_cast<float4*>(dst) = make_float4(x[0] * scale, x[1] * scale, x[2] * scale, x[3] * scale);
-            *reinterpret_cast<float4*>(dst + D / 2) = make_float4(y[0] * scale, y[1] * scale, y[2] * scale, y[3] * scale);
+            if (c == 0) s_lse[r] = row_reference(r < here ? lse[at] : -INFINITY);
+            *reinterpret_cast<float4*>(sq + r * D + c * 4) = make_float4(u[0] * scale, u[1] * scale, u[2] * scale, u[3] * scale);
+            *reinterpret_cast<float4*>(sq + r * D + D / 2 + c * 4) = make_float4(w[0] * scale, w[1] * scale, w[2] * scale, w[3] * scale);
         }
-        const bool live = c0 + r0 < rows;
-        int buf = 0;
-        for (int k0 = lo; k0 < hi; k0 += kKeys32, buf ^= 1) {
-            if (k0 + kKeys32 < hi) {
-                load_k(k0 + kKeys32, buf ^ 1);
-                asm volatile("cp.async.wait_group 1;" ::: "memory");
-            } else {
-                asm volatile("cp.async.wait_group 0;" ::: "memory");
+        __syncthreads();
+        for (int tile = first; tile < ntiles; tile += step) {
+            const int lam0 = tile * 16, keys = min(16, p.total - lam0);
+            asm volatile("cp.async.wait_group 0;" ::: "memory");
+            __syncwarp();
+            if (c0 == 0 && lam0 + keys > p.st.L) {   // append, as they came
+                const int r0 = max(p.st.L - lam0, 0);
+                for (int e = lane; e < (keys - r0) * (D / 4); e += 32) {
+                    const int r = r0 + e / (D / 4), c = e % (D / 4) * 4, j = lam0 + r - p.st.L;
+                    const size_t row = ((size_t)p.unit * cv.R + lam0 + r + p.st.i) * D + c;
+                    *reinterpret_cast<uint4*>(reinterpret_cast<float*>(cv.K) + row) = *reinterpret_cast<const uint4*>(sk + r * D + c);
+                    *reinterpret_cast<uint4*>(reinterpret_cast<float*>(cv.V) + row) = ld_plain(reinterpret_cast<const float*>(dv.v) + draft_row<float, D>(cv, dv, p, j) + c);
+                }
+                __syncwarp();
             }
-            __syncthreads();
-            float part[4] = {0.f, 0.f, 0.f, 0.f};
-            if (live) {
-                const float* kt = sk + buf * kKeys32 * PITCH + l16 * PITCH;
-                const float* qt = sq + r0 * PITCH;
-                float2 a[2][4] = {};  // even and odd channels
-#pragma unroll 4
-                for (int c = 0; c < D; c += 4) {
-                    const Float22 q0 = *reinterpret_cast<const Float22*>(qt + c), q1 = *reinterpret_cast<const Float22*>(qt + PITCH + c);
+            if (cv.rope_cos) {                       // keys encoded at their slots, in place
+                for (int e = lane; e < keys * (D / 8); e += 32) {
+                    const int r = e / (D / 8), c = e % (D / 8) * 4;
+                    float4 &lo = *reinterpret_cast<float4*>(sk + r * D + c), &hi = *reinterpret_cast<float4*>(sk + r * D + D / 2 + c);
+                    float u[4] = {lo.x, lo.y, lo.z, lo.w}, w[4] = {hi.x, hi.y, hi.z, hi.w};
+                    rope_pairs(u, w, cv.rope_cos + (size_t)(lam0 + r) * (D / 2) + c, cv.rope_sin + (size_t)(lam0 + r) * (D / 2) + c);
+                    lo = make_float4(u[0], u[1], u[2], u[3]); hi = make_float4(w[0], w[1], w[2], w[3]);
+                }
+                __syncwarp();
+            }
+            float sum[4] = {0.f, 0.f, 0.f, 0.f};     // keys kg + 4 i, rows 8 g + part
+            for (int g = 0; g < groups; ++g) {
+                float2 acc[8][4];                    // rows x keys, over this lane's pieces: even and odd channels
 #pragma unroll
-                    for (int k = 0; k < 4; ++k) {
-                        const Float22 x = *reinterpret_cast<const Float22*>(kt + 16 * k * PITCH + c);
-                        a[0][k] = fma2(q0.hi, x.hi, fma2(q0.lo, x.lo, a[0][k]));
-                        a[1][k] = fma2(q1.hi, x.hi, fma2(q1.lo, x.lo, a[1][k]));
+                for (int r = 0; r < 8; ++r)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) acc[r][i] = make_float2(0.f, 0.f);
+#pragma unroll 1
+                for (int c = 4 * part; c < D; c += 32) {
+                    Float22 k4[4];
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) k4[i] = *reinterpret_cast<const Float22*>(sk + (kg + 4 * i) * D + c);
+#pragma unroll
+                    for (int r = 0; r < 8; ++r) {
+                        const Float22 q4 = *reinterpret_cast<const Float22*>(sq + (8 * g + r) * D + c);
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) acc[r][i] = fma2(q4.hi, k4[i].hi, fma2(q4.lo, k4[i].lo, acc[r][i]));
                     }
                 }
+                float s[4];
+                halve_sums(acc, part, s);
+                const float ls = s_lse[8 * g + part];
+                const int seen = ((c0 + 8 * g + part) >> lg) + p.st.L;  // a path token is seen from itself on
 #pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const int j = k0 + l16 + 16 * k - p.st.L;  // a path token is seen from itself on
-#pragma unroll
-                    for (int r = 0; r < 2; ++r)
-                        if (c0 + r0 + r < rows && ((c0 + r0 + r) >> lg) >= j) part[k] += exp2f(a[r][k].x + a[r][k].y - s_lse[r0 + r]);
-                }
+                for (int i = 0; i < 4; ++i)
+                    if (lam0 + kg + 4 * i <= seen) sum[i] += exp2f(s[i] - ls);
             }
 #pragma unroll
-            for (int k = 0; k < 4; ++k) red[(tid / 16) * kKeys32 + l16 + 16 * k] = part[k];
-            __syncthreads();  // the tile's shares are there, and nobody reads its keys any more
-            if (tid < kKeys32 && k0 + tid < hi) {
-                float x = 0.f;
+            for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int g = 0; g < 16; ++g) x += red[g * kKeys32 + tid];
-                sums[k0 - lo + tid] += x;
+                for (int off = 1; off < 8; off <<= 1) sum[i] += __shfl_xor_sync(0xffffffffu, sum[i], off);
+            __syncwarp();                            // nobody reads this tile any more
+            if (tile + step < ntiles) load(tile + step);
+            const int lam = lam0 + kg + 4 * part;
+            if (part < 4 && lam < p.total) {
+                const float gain = (part & 2 ? (part & 1 ? sum[3] : sum[2]) : (part & 1 ? sum[1] : sum[0])) * (1.0f / (float)p.G);
+                const size_t row = (size_t)p.unit * cv.R + (lam < p.st.L ? phys_row(lam, p.st) : lam + p.st.i);
+                cv.S[row] = (lam < p.st.L || c0 > 0 ? cv.S[row] : 0.f) + gain;
+                if (lam >= p.st.L) cv.pos[row] = p.N + lam - p.st.L;
             }
-        }
-    }
-    __syncthreads();
-    for (int e = tid; e < hi - lo; e += kThreads) {
-        const int lam = lo + e;
-        const size_t row = (size_t)p.unit * cv.R + (lam < p.st.L ? phys_row(lam, p.st) : lam + p.st.i);
-        cv.S[row] = (lam < p.st.L ? cv.S[row] : 0.f) + sums[e] * (1.0f / (float)p.G);
-        if (lam >= p.st.L) cv.pos[row] = p.N + lam - p.st.L;
-    }
-    for (int e = tid; e < p.n * (D / 4); e += kThreads) {  // append
-        const int j = e / (D / 4), c = e % (D / 4), lam = p.st.L + j;
-        if (lam >= lo && lam < hi) {
-            const size_t row = ((size_t)p.unit * cv.R + lam + p.st.i) * (D / 4) + c, src = draft_row<float, D>(cv, dv, p, j) / 4 + c;
-            reinterpret_cast<uint4*>(cv.K)[row] = reinterpret_cast<const uint4*>(dv.k)[src];
-            reinterpret_cast<uint4*>(cv.V)[row] = reinterpret_cast<const uint4*>(dv.v)[src];
         }
     }
 }
@@ -352,7 +341,7 @@ accept_kernel(CacheView cv, DraftView dv, const float* __restrict__ lse, const i
     }
     __syncthreads();
     if constexpr (sizeof(T) == 2) scores_bf16<D, ROPE>(cv, dv, p, lse, rank, CL, smem, rows8, depth, bars);
-    else scores_f32<D>(cv, dv, p, lse, rank, CL, smem);
+    else scores_f32<D>(cv, dv, p, lse, rank, CL, smem, rows8);
     auto unit_sync = [&]() { if (CL == 1) __syncthreads(); else cluster.sync(); };
     unit_sync();  // every score and every appended row of the unit is in place; every block has read n_seen
     if (rank == 0 && threadIdx.x == 0) cv.n_seen[p.unit] = p.N + p.n;
@@ -370,7 +359,7 @@ cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse,
     const size_t queries = (size_t)rows8 * (q_pitch<D>() + 4);
     const size_t room = (queries + 2 * kRing <= kHalfSm ? kHalfSm : kSm) - queries;
     const int depth = (int)(room / kRing < kMaxDepth ? room / kRing : kMaxDepth);
-    const size_t smem = sizeof(T) == 2 ? queries + depth * kRing : f32_smem_floats<D>((cv.c + max_n + CL - 1) / CL) * 4;
+    const size_t smem = sizeof(T) == 2 ? queries + depth * kRing : f32_smem_bytes<D>(rows8);
     if (smem > 48 * 1024) {
         static bool smem_set[64] = {};  // per device: the opt-in is needed once
         int dev = 0;
@@ -406,11 +395,9 @@ template <typename T, int D, bool ROPE>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const float* lse, const int32_t* path, int path_stride, const DraftLens& lens,
                      int max_n, int sms, cudaStream_t s) {
     const long units = (long)cv.B * cv.Hkv;
-    const int keys = sizeof(T) == 2 ? kWarps * 16 : 2 * kKeys32;
+    const int keys = kWarps * 16;
     int cl = 1;
     while (cl < 8 && units * cl < sms && cv.c / (2 * cl) >= keys) cl *= 2;
-    // (fp32: a block keeps its keys' sums in shared memory, and two blocks share an SM's)
-    while (sizeof(T) == 4 && cl < 8 && f32_smem_floats<D>((cv.c + max_n + cl - 1) / cl) * 4 > 112 * 1024) cl *= 2;
     switch (cl) {
         case 1: return launch_c<T, D, 1, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);
         case 2: return launch_c<T, D, 2, ROPE>(cv, dv, lse, path, path_stride, lens, max_n, s);

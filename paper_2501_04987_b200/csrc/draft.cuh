@@ -49,6 +49,24 @@ __device__ inline float2 fma2(float2 a, float2 b, float2 c) {
     return d;
 }
 struct alignas(16) Float22 { float2 lo, hi; };  // four floats as the two pairs fma2() takes
+// Eight lanes (part = lane & 7) hold parts of 8 x 4 sums, each as a pair: halved three times, lane `part` is left with row `part`.
+__device__ inline void halve_sums(const float2 (&acc)[8][4], int part, float (&s)[4]) {
+    float x4[4][4], x2[2][4];
+    const bool h4 = part & 4, h2 = part & 2, h1 = part & 1;
+#pragma unroll
+    for (int r = 0; r < 4; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const float lo = acc[r][i].x + acc[r][i].y, hi = acc[r + 4][i].x + acc[r + 4][i].y;
+            x4[r][i] = (h4 ? hi : lo) + __shfl_xor_sync(0xffffffffu, h4 ? lo : hi, 4);
+        }
+#pragma unroll
+    for (int r = 0; r < 2; ++r)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x2[r][i] = (h2 ? x4[r + 2][i] : x4[r][i]) + __shfl_xor_sync(0xffffffffu, h2 ? x4[r][i] : x4[r + 2][i], 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s[i] = (h1 ? x2[1][i] : x2[0][i]) + __shfl_xor_sync(0xffffffffu, h1 ? x2[0][i] : x2[1][i], 1);
+}
 // reads of another block's shared memory, at an address of the cluster
 __device__ inline float4 ld_remote_v4(uint32_t caddr) {
     float4 v;

@@ -177,22 +177,7 @@ verify_f32_kernel(CacheView cv, DraftView dv, DraftLens lens, float* __restrict_
                     for (int i = 0; i < 4; ++i) acc[r][i] = fma2(q4.hi, k4[i].hi, fma2(q4.lo, k4[i].lo, acc[r][i]));
                 }
             }
-            // eight lanes hold parts of 32 sums: halved three times, lane `part` is left with row `part`
-            float x4[4][4], x2[2][4];
-            const bool h4 = part & 4, h2 = part & 2, h1 = part & 1;
-#pragma unroll
-            for (int r = 0; r < 4; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float lo = acc[r][i].x + acc[r][i].y, hi = acc[r + 4][i].x + acc[r + 4][i].y;
-                    x4[r][i] = (h4 ? hi : lo) + __shfl_xor_sync(0xffffffffu, h4 ? lo : hi, 4);
-                }
-#pragma unroll
-            for (int r = 0; r < 2; ++r)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) x2[r][i] = (h2 ? x4[r + 2][i] : x4[r][i]) + __shfl_xor_sync(0xffffffffu, h2 ? x4[r][i] : x4[r + 2][i], 2);
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s[g][i] = (h1 ? x2[1][i] : x2[0][i]) + __shfl_xor_sync(0xffffffffu, h1 ? x2[0][i] : x2[1][i], 1);
+            halve_sums(acc, part, s[g]);
         }
         __syncwarp();         // nobody reads this K tile any more
         if (more) load(sk, next.k, next);
