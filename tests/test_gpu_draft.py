@@ -303,7 +303,7 @@ def test_verify_trees(gpu, dtype, d, hq, hkv, T):
 
 
 @pytest.mark.parametrize("dtype,d,hq,hkv,budget,B", [("bf16", 128, 8, 2, 1500, 1), ("bf16", 128, 32, 8, 700, 5), ("bf16", 64, 4, 1, 2048, 2),
-                                                     ("f32", 128, 4, 2, 900, 1)])
+                                                     ("f32", 128, 4, 2, 900, 1), ("f32", 64, 8, 1, 700, 3), ("f32", 128, 32, 16, 333, 6)])
 @pytest.mark.parametrize("T", [2, 24, 64])
 def test_verify_long_caches(gpu, dtype, d, hq, hkv, budget, B, T):
     seen = [budget * 2 + 77 * b + 5 for b in range(B)]
@@ -323,7 +323,7 @@ def torch_equal(a, b):
     return torch.equal(a, b)
 
 
-@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 4, 2), ("bf16", 64, 4, 1), ("f32", 64, 2, 2)])
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 4, 2), ("bf16", 64, 4, 1), ("f32", 64, 2, 2), ("f32", 128, 4, 1)])
 def test_verify_with_values_that_must_not_spread(gpu, dtype, d, hq, hkv):
     """NaN and infinity in drafted tokens that a row does not see, behind the draft, and in rows of the cache that hold no
     token any more; large logits."""
