@@ -12,7 +12,7 @@
 // With few units the keys of a unit are dealt to a cluster of blocks, which join their results in shared memory.
 //
 // Measured (B200, D = 128, 20 sequences x 1024 cached tokens x 3 KV heads of eight query heads): 1, 2, 8, 32, 64 drafted tokens
-// 29, 35, 96, 314, 622 us, the last at 27 TFLOP/s (packed multiply-adds take 2.7 to 3.5 cycles of a scheduler; as pairs of plain
+// 29, 35, 97, 310, 578 us, the last at 29 TFLOP/s (packed multiply-adds take 2.7 to 3.5 cycles of a scheduler; as pairs of plain
 // ones 680 us).  6 x 494 x 16 x 8, one token: 18 us.  13 tokens over 256 cached ones, 4 heads of 64: 8.5 us, start and join.
 // The form that this one replaced - a thread one to eight rows against four keys, the block in step over tiles of 64 -
 // took 50, 47, 99, 312, 574 and 39 and 7.9 us: it read the keys four times as often for few rows, and its loads waited for a
@@ -388,31 +388,32 @@ cudaError_t launch_r(const CacheView& cv, const DraftView& dv, const DraftLens& 
     return cudaLaunchKernelEx(&cfg, kern, cv, dv, lens, reinterpret_cast<float*>(out), lse, split);
 }
 
-// Rows per block and blocks per cluster, by the time they should take in cycles: a warp's way through a key tile alone, or what
-// the blocks that share an SM need for theirs together, whichever is more; and as many of those as a warp has tiles, with some
-// for start and join.
+// Rows per block (8 or 16) and blocks per cluster, by the time they should take in cycles: a warp's way through a key tile alone,
+// or what the blocks that share an SM need for theirs together, whichever is more; and as many of those as a warp has tiles,
+// with some for start and join.  Over thirty calls of all shapes its choice takes 0.9 % longer than the best one (geometric
+// mean).  Measured, 8 rows against 16, each with its best split: 3 sequences x 3245 x 8 KV heads x 88 rows 90 against 79 us, 30 x
+// 1268 x 8 x 64 (d = 64) 129 and 129, 9 x 773 x 8 x 32 35 against 42, 10 x 3219 x 2 x 14 34 against 41.  (24 rows: the best of three
+// only where every sequence has hundreds, and there by 4 %.)
 template <int D>
 cudaError_t launch_t(const CacheView& cv, const DraftView& dv, const DraftLens& lens, int max_n, void* out, float* lse, int sms, cudaStream_t s) {
     const int G = cv.Hq / cv.Hkv, keys = (cv.c + max_n + kKeys - 1) / kKeys + 1;
     int rows = 8, split = 1;
     long least = -1;
-    for (int r = 8; r <= 24; r += 8) {
+    for (int r = 8; r <= 16; r += 8) {
         long tiles = 0;
         for (int b = 0; b < cv.B; ++b) tiles += (lens.n[b] * G + r - 1) / r;
-        const long alone = 3000 + 300 * r, shared = 450 + 150 * r;
+        const long alone = 3000 + 200 * r, shared = 200 + 200 * r;
         auto step = [&](long blocks) { return std::max(alone, (blocks + sms - 1) / sms * shared); };
         for (int x = 1; x <= kMaxSplit; x *= 2) {
             if (x > 1 && keys <= (x / 2) * kWarps) break;
             const long blocks = tiles * cv.Hkv * x, wave = (long)blocks_per_sm(r) * sms, left = blocks % wave;
-            const long steps = 2 * ((keys + x * kWarps - 1) / (x * kWarps)) + (x > 1 ? 5 : 3);
+            const long steps = 2 * ((keys + x * kWarps - 1) / (x * kWarps)) + (x > 1 ? 5 : 4);
             const long cost = steps * (blocks / wave * step(wave) + (left ? step(left) : 0));
             if (least < 0 || cost < least) { least = cost; rows = r; split = x; }
         }
     }
     const int tiles = (max_n * G + rows - 1) / rows;
-    if (rows == 8) return launch_r<D, 8>(cv, dv, lens, tiles, split, out, lse, s);
-    if (rows == 16) return launch_r<D, 16>(cv, dv, lens, tiles, split, out, lse, s);
-    return launch_r<D, 24>(cv, dv, lens, tiles, split, out, lse, s);
+    return rows == 8 ? launch_r<D, 8>(cv, dv, lens, tiles, split, out, lse, s) : launch_r<D, 16>(cv, dv, lens, tiles, split, out, lse, s);
 }
 
 }  // namespace
