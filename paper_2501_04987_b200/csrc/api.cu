@@ -176,8 +176,8 @@ treekv_status treekv_create(treekv_ctx** out, int budget, int n_heads, int n_kv_
                        make_tensor_map_bf16(&ctx->tmKrot, ctx->k_rot, 2, dims, strides, box);
     }
     ctx->has_tmv = dtype == TREEKV_BF16 && make_verify_maps(ctx->cv, &ctx->tmKv, &ctx->tmVv);
-    // The workspace starts as zeros: the tensor-core prefill reads whole 128-row tiles, and rows that hold no token
-    // yet must be finite (they are multiplied by a probability of exactly zero).
+    // The workspace starts as zeros.  No result depends on rows that hold no token: the tensor-core kernels, which read
+    // whole tiles, mask their logits and take their values out of the tile.
     cudaError_t e = cudaMemsetAsync(dev_workspace, 0, L.total, static_cast<cudaStream_t>(stream));
     if (e == cudaSuccess) e = launch_init_state(ctx->cv, static_cast<cudaStream_t>(stream));
     if (e != cudaSuccess) { delete ctx; return TREEKV_ERR_CUDA; }

@@ -363,6 +363,11 @@ prefill_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant
                 asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
                 if (kvalid) part[lam] = colsum + xch[grp * 128 + row];
             }
+            if (valid < 128) {  // the V tile of this group's P^T, before the MMA warp is told that both are there
+                const int ld = NT + min(3, NT) + j + min(j, max(0, NT - 3)), slot = ld % kRing;
+                if (!mbar_wait(bar(RING_FULL + slot), (ld / kRing) & 1)) ok = false;
+                clear_value_rows(base_ptr + (1 + slot) * kSlot, valid, (sw & 7) * 32 + lane, 256);
+            }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(P_FULL + grp));

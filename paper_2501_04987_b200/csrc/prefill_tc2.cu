@@ -416,6 +416,11 @@ prefill_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constan
                 asm volatile("bar.sync %0, 64;" ::"r"(pair_bar) : "memory");
                 if (kvalid && sub_live) part[lam] = colsum + xrow[row];
             }
+            if (sub == 0 && valid < 128) {  // the V tile that both sub-tiles multiply, sub-tile 0 first: the MMA warp waits for this group
+                const int ld = nt + min(2 + 2 * j, 2 * nt - 1), slot = ld % kRing;
+                if (!mbar_wait(bar(RING_FULL + slot), (ld / kRing) & 1)) ok = false;
+                clear_value_rows(smem_raw + (2 + slot) * kSlot, valid, (sw & 7) * 32 + lane, 256);
+            }
             fence_proxy_async_smem();
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(P_FULL + sub));

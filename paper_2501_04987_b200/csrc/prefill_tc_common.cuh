@@ -80,6 +80,17 @@ __device__ inline void append_own_tokens(const CacheView& cv, const ChunkDirect&
     }
 }
 
+// Rows [valid, 128) of a V tile hold no token that these queries see, and may hold anything: what an evicted token or an earlier
+// request has left there, or the next unit's rows.  Their weight is zero, but zero times NaN or infinity is NaN, so they are
+// taken out of the tile.  `nthr` threads with index `t` take part; a fence_proxy_async_smem() has to follow.  (Partly filled
+// tiles only: at most one per segment.)
+__device__ inline void clear_value_rows(unsigned char* v_tile, int valid, int t, int nthr) {
+    for (int e = t; e < (128 - valid) * (kD / 8); e += nthr) {
+        const int r = valid + (e >> 4), c = e & 15;
+        *reinterpret_cast<uint4*>(v_tile + (c >> 3) * kHalf + r * 128 + ((c & 7) << 4)) = make_uint4(0, 0, 0, 0);
+    }
+}
+
 // 2^x on the special-function unit, one instruction (inputs here are <= ~0; results below 2^-126 flush to zero)
 __device__ inline float ex2(float x) {
     float y;
