@@ -327,8 +327,9 @@ treekv_status treekv_accept_path(treekv_ctx* ctx, const void* dev_q, const void*
  * replaced or emptied by the same call and may have any number of copies: beams take their parents' caches, one prompt
  * becomes several samples, a shrinking batch is packed.
  *   host_source  [batch] int32 in -1..batch-1.  Read before returning
- * treekv_stats.evictions stays (copies are no evictions).  Not while the stream is being captured (TREEKV_ERR_BAD_STATE);
- * the lengths that are copied are the host-side token counts, which replays of captured steps do not advance.
+ * treekv_stats.evictions stays (copies are no evictions).  Not while the stream is being captured (TREEKV_ERR_BAD_STATE).
+ * What is copied is what the caches hold when the stream gets there, also after replays of captured steps; the host-side
+ * counts (treekv_tokens_seen), which replays do not advance, are copied as they stand.
  */
 treekv_status treekv_fork_sequences(treekv_ctx* ctx, const int32_t* host_source, void* stream);
 

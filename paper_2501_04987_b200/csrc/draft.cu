@@ -150,7 +150,7 @@ treekv_status treekv_fork_sequences(treekv_ctx* ctx, const int32_t* host_source,
     cudaError_t e = join_eviction_stream(ctx, s);
     if (e == cudaSuccess) e = launch_fork(ctx->cv, ctx->dt, plan, s);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
-    ctx->launches += 1;
+    ctx->launches += 2;
     int64_t before[kMaxBatch];
     memcpy(before, ctx->n_seen, sizeof(before));
     for (int b = 0; b < B; ++b) ctx->n_seen[b] = host_source[b] < 0 ? 0 : before[host_source[b]];

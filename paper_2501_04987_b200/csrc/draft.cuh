@@ -116,9 +116,10 @@ constexpr uint16_t kForkEmpty = 0xfffe;  // as a source: the destination is free
 template <int MAXB>
 struct ForkPlan {
     uint16_t src[MAXB], dst[MAXB], start[MAXB + 1];  // operations of component z: [start[z], start[z + 1])
-    int32_t seen[MAXB];                              // tokens seen by the sequence whose content moves (0: freed)
 };
 struct ForkPlanHost : ForkPlan<kForkMaxOps> {
+    int32_t seen[kForkMaxOps];   // tokens seen by the sequence whose content moves (0: freed), by the host's record
+    int16_t source[kMaxBatch];   // [batch] whose content each sequence gets: itself, another, -1: none
     int n_ops, n_comps;
 };
 void make_fork_plan(const int32_t* source, int B, const int64_t* seen, ForkPlanHost& plan);

@@ -830,3 +830,48 @@ def test_a_drafted_step_from_projection_to_cache(gpu):
         kv.fork_sequences([b if (b + step) % 3 else (b + 1) % B for b in range(B)])
     st = kv.stats()
     assert st["device_error"] == 0
+
+
+# ---- copies after replays of captured steps --------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype,d,hkv,budget,B,steps", [("bf16", 128, 2, 40, 5, 31), ("bf16", 64, 1, 300, 3, 9), ("f32", 64, 2, 33, 70, 50),
+                                                        ("f32", 128, 1, 90, 2, 700)])
+def test_fork_after_replayed_steps(gpu, dtype, d, hkv, budget, B, steps):
+    """The copies follow the caches as they are, which replays of a captured step move without the host's counts: a twin takes
+    the same steps by calls."""
+    import torch
+
+    r = np.random.default_rng(steps)
+    seen = [int(x) for x in r.integers(0, 2 * budget, B)]
+    seen[0] = 0
+    kv, _ = _filled(gpu, dtype, d, 2 * hkv, hkv, budget, seen, 4, seed=80)
+    twin, _ = _filled(gpu, dtype, d, 2 * hkv, hkv, budget, seen, 4, seed=80)
+    g = torch.Generator(device="cuda").manual_seed(81)
+    tok = [torch.randn((B, h, d), generator=g, device="cuda").to(kv.tdtype) for h in (2 * hkv, hkv, hkv)]
+    out = torch.empty_like(tok[0])
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        kv.decode_step(*tok, out=out)
+    at = 0
+    for source in ([int(x) for x in r.permutation(B)], [int(x) for x in r.integers(-1, B, B)], [B - 1] * B, [(b + 1) % B for b in range(B)]):
+        for _ in range(steps):
+            for x in tok:
+                x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+            graph.replay()
+            want = twin.decode_step(*tok)
+            assert torch.equal(out, want), at
+            at += 1
+        for c in (kv, twin):
+            c.fork_sequences(source)
+        (a, _), (b, _) = kv.export_state(), twin.export_state()
+        assert torch.equal(a, b), source
+    assert kv.stats()["device_error"] == 0
+
+
+def test_fork_keeps_the_count_of_evictions(gpu):
+    kv, _ = _filled(gpu, "bf16", 64, 4, 2, 30, [100, 7, 0], 4, seed=82)
+    before = kv.stats()["evictions"]
+    assert before == 70
+    for source in ([1, 0, 2], [0, 0, 0], [-1, -1, 0], [2, 2, -1]):
+        kv.fork_sequences(source)
+        assert kv.stats()["evictions"] == before
