@@ -346,7 +346,8 @@ int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64
  * when a kernel's bounded wait gave up (bits: 4 TMA producer, 8 MMA issuer, 16 softmax / epilogue warps of the
  * tensor-core prefill kernels, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v), or
  * TREEKV_ERR_INVALID_ARG when its only bit is 256: an index in device memory was out of range and was not followed
- * (treekv_norm_rope, treekv_accept_path).  treekv_reset clears it. */
+ * (treekv_norm_rope, treekv_accept_path).  treekv_reset clears it; caches that a bad index of treekv_norm_rope has not
+ * touched survive that as an image (treekv_export_state before it, treekv_import_state after it). */
 treekv_status treekv_get_stats(treekv_ctx* ctx, treekv_stats* host_out, void* stream);
 
 /*

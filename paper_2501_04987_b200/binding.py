@@ -491,9 +491,10 @@ class TreeKV:
 
     def stats(self, check=True):
         """Counters as a dict.  With check=False what the device recorded - a give-up (TREEKV_ERR_TIMEOUT), an index out of
-        range (TREEKV_ERR_INVALID_ARG) - is reported through 'device_error' and 'status' instead of raising."""
+        range (TREEKV_ERR_INVALID_ARG) - is reported through 'device_error' and 'status' instead of raising; a call that could
+        not read it raises all the same."""
         st, s = treekv_get_stats(self._h, self._stream())
-        if check or st not in (TREEKV_OK, 1, 6):
+        if check or not s.device_error:
             _check(st, "treekv_get_stats")
         return {"status": st, "evictions": s.evictions, "near_ties": s.near_ties, "kernel_launches": s.kernel_launches,
                 "device_error": s.device_error, "last_cuda_error": s.last_cuda_error}

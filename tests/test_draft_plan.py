@@ -96,3 +96,14 @@ def test_null_context_is_an_error_not_a_crash(binding):
     assert binding.treekv_verify_tree(None, 16, 16, 16, 0, 16, 16, None, 1) == 1
     assert binding.treekv_accept_path(None, 16, 16, 16, 16, 1, 16, 1, None) == 1
     assert binding.treekv_fork_sequences(None, [0]) == 1
+
+
+def test_stats_that_could_not_be_read_raise(binding):
+    """check=False reports what the device recorded; a call on a closed context has nothing to report."""
+    import types
+
+    closed = types.SimpleNamespace(_h=None, _stream=lambda: 0)
+    for check in (True, False):
+        with pytest.raises(binding.TreeKVError) as e:
+            binding.TreeKV.stats(closed, check=check)
+        assert e.value.status == 1

@@ -875,3 +875,19 @@ def test_fork_keeps_the_count_of_evictions(gpu):
     for source in ([1, 0, 2], [0, 0, 0], [-1, -1, 0], [2, 2, -1]):
         kv.fork_sequences(source)
         assert kv.stats()["evictions"] == before
+
+
+def test_caches_survive_a_bad_position_as_an_image(gpu):
+    import torch
+
+    kv, _ = _filled(gpu, "bf16", 64, 4, 2, 30, [100, 7, 0], 4, seed=83)
+    cos, sin = _tables(8, 64)
+    kv.norm_rope(torch.zeros((1, 8 * 64), device="cuda", dtype=kv.tdtype), cos=cos, sin=sin,
+                 positions=torch.tensor([8], dtype=torch.int32, device="cuda"))
+    assert kv.stats(check=False)["device_error"] == BAD_INDEX
+    image, tokens = kv.export_state()
+    kv.reset()
+    kv.import_state(image, tokens)
+    assert kv.stats()["device_error"] == 0
+    again, tokens2 = kv.export_state()
+    assert tokens2 == tokens and torch.equal(again, image)
