@@ -125,7 +125,14 @@ __device__ inline void scores_bf16(const CacheView& cv, const DraftView& dv, con
         const int lam0 = tile * 16, mine = lam0 + g + 8 * (t & 1);  // the key whose score this lane (t < 2) writes
         const size_t mine_row = (size_t)p.unit * cv.R + (mine < p.st.L ? phys_row(mine, p.st) : mine + p.st.i);
         const float s_old = t < 2 && mine < p.st.L ? cv.S[mine_row] : 0.f;
-        ok = ok && mbar_wait(smem_addr_u32(&bars[warp][stage]), phase);
+        ok = __all_sync(0xffffffffu, mbar_wait(smem_addr_u32(&bars[warp][stage]), phase));
+        if (!ok) {  // gave up: no more loads, and none of the ones on their way may outlive the block
+            for (int x = tile, left = depth; left > 0 && x < ntiles; x += step, --left) {
+                mbar_wait(smem_addr_u32(&bars[warp][stage]), phase);
+                if (++stage == depth) { stage = 0; phase ^= 1; }
+            }
+            break;
+        }
         uint4 kf[2][NU];
 #pragma unroll
         for (int h = 0; h < 2; ++h) {  // rows two apart lie on the same banks: odd ones take their pieces in the other order
