@@ -64,7 +64,8 @@ def _with_positions(gpu, kv, chunk, tables, protect):
     return other
 
 
-@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 128, 2, 2), ("bf16", 64, 8, 1), ("f32", 128, 4, 2), ("f32", 64, 8, 1)])
+@pytest.mark.parametrize("dtype,d,hq,hkv", [("bf16", 128, 8, 2), ("bf16", 128, 2, 2), ("bf16", 128, 8, 1), ("bf16", 64, 8, 1), ("f32", 128, 4, 2),
+                                            ("f32", 128, 8, 1), ("f32", 64, 8, 1)])
 @pytest.mark.parametrize("budget", [300, 700, 1500])
 @pytest.mark.parametrize("rope,protect", [(False, None), (True, None), (True, (4, 40)), (False, (4, 40))])
 def test_accept_of_few_long_sequences(gpu, dtype, d, hq, hkv, budget, rope, protect):
