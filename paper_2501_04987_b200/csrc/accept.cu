@@ -360,8 +360,8 @@ cudaError_t launch_c(const CacheView& cv, const DraftView& dv, const float* lse,
                      int max_n, cudaStream_t s) {
     auto kern = accept_kernel<T, D, CL, ROPE>;
     const int rows8 = (max_n * (cv.Hq / cv.Hkv) + 7) / 8 * 8;
-    // Two blocks per SM while the queries leave room for it beside rings of two tiles per warp; the widest ones (512 rows)
-    // leave one tile per warp in the one block that then fits.
+    // Two blocks per SM while the queries leave room for it beside rings of two tiles per warp; the widest ones (512 rows of
+    // 128 channels) leave those two tiles in the one block that then fits.
     constexpr size_t kTile = 16 * D * 2, kRing = kWarps * kTile, kHalfSm = 112 * 1024, kSm = 226 * 1024;
     const size_t queries = (size_t)rows8 * (q_pitch<D>() + 4);
     const size_t room = (queries + 2 * kRing <= kHalfSm ? kHalfSm : kSm) - queries;

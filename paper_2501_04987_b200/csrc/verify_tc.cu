@@ -6,7 +6,14 @@
 //     p = exp2(S c - m)  one thread per row: the running maximum m never leaves the thread
 //     O += P V         P goes back to tensor memory, beside S, as the matrix operand; O accumulates there
 // The reference m is moved - and O rescaled - only when a row's maximum outgrows it by 2^8: the weights stay within fp32's
-// and bf16's range, their relative precision is the same, and after the first tiles rescaling is rare.
+// and bf16's range, their relative precision is the same, and after the first tiles rescaling is rare.  (A lazy form of the
+// softmax in one pass with running maximum and sum, Milakov and Gimelshein 2018.)
+//
+// Rounded to fewer bits than 32: the weights P as an operand of P V, to bf16, since both operands of an MMA have one type
+// and V's is bf16 - each by at most half a step, 2^-8 of itself; the sum that divides them is of the unrounded ones.  Against
+// 64 bits the outputs are off by 0.0022 to 0.0024 (root of the mean square, relative), where rounding the output alone makes
+// 0.0017.  Two bf16 parts of P would double the products P V; by estimate the tensor core's part of a key tile, two blocks side
+// by side, would then be longer than the tile is now.
 //
 // Memory bound up to about 128 rows per KV head, so what matters is bytes in flight: a block takes under half an SM's
 // shared memory and half its tensor memory, two run per SM, and each hides the other's exponentials, first loads and
@@ -23,11 +30,14 @@
 // Measured (B200, d = 128; drafted tokens x sequences x cached tokens x KV heads x query heads of each): 1 x 8 x 1024 x 32 x 1:
 // 26.3 us, 134 MB = 5.1 TB/s, 79 % of a copy's bandwidth.  16 x 32 x 2048 x 8 x 4 (ragged): 42.1 us, 220 MB = 5.2 TB/s, 81 %.
 // 24 x 1 x 4096 x 8 x 4: 18.4 us, an eighth of the machine's blocks at most 9 tiles long, then the join: some 2.5 us of
-// distributed shared memory at 10 bytes per clock and SM.  64 x 32 x 2048 x 8 x 4: 96 us, 69.8 GFLOP = 730 TFLOP/s, 1950 cycles
-// of a block per key tile, two blocks side by side: two tiles of 128 rows per unit, so the keys are fetched twice (the second
-// time from L2).  What that leaves idle is little: the MMAs of a tile take 650 cycles of the tensor core, their operands and
-// the arriving tiles some 770 of shared memory's bandwidth (Q is read again for each tile), and that twice.  In-cache positions:
-// 52.5, 91.5, 196 us for 1, 16 and 64 drafted tokens.
+// distributed shared memory at 10 bytes per clock and SM.  64 x 32 x 2048 x 8 x 4: 94 us at an SM clock of 1.79 GHz, 69.8 GFLOP =
+// 740 TFLOP/s.  Two tiles of 128 rows per unit (the keys are fetched twice, the second time from L2) make 512 blocks on 296
+// places: two rounds, the second 73 % full.  A block is 8.5 us on its way to its first logits (queries, drafted tile, first key
+// tile), 33.6 us in 34 key tiles of 1770 cycles, two blocks side by side, and 2.3 us in its end.  Within the tiles little is idle, by
+// estimate: the MMAs of one take 650 cycles of the tensor core, their operands and the arriving tiles some 770 of shared memory's
+// bandwidth (Q is read again for each tile), and that twice.  Over the launch the tensor pipe is active for 38 %.  A second of
+// such calls without a pause runs into the power limit: 1.5 GHz, 110 us.  In-cache positions: 52.5, 91.5, 196 us for 1, 16 and 64
+// drafted tokens.
 //
 // Not taken, with what the first two, 64 tokens and the single sequence took instead of 26.7 / 44.6 / 99.4 / 17.1 us at that time:
 // key tiles of 128 with eight softmax warps and two ring slots (31.1 / 50.5 / 121.6 / 18.5); two groups of softmax warps on
