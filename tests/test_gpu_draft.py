@@ -891,3 +891,31 @@ def test_caches_survive_a_bad_position_as_an_image(gpu):
     assert kv.stats()["device_error"] == 0
     again, tokens2 = kv.export_state()
     assert tokens2 == tokens and torch.equal(again, image)
+
+
+@pytest.mark.parametrize("dtype,d,hkv", [("bf16", 128, 2), ("bf16", 64, 1), ("f32", 128, 1)])
+def test_fork_of_caches_that_only_replays_have_filled(gpu, dtype, d, hkv):
+    """The host has counted one step, the caches hold hundreds of tokens: many more rows than the launch was sized for."""
+    import torch
+
+    B, budget = 4, 250
+    kv, twin = (gpu.TreeKV(budget, hkv, hkv, d, dtype, B, 0) for _ in range(2))
+    g = torch.Generator(device="cuda").manual_seed(84)
+    tok = [torch.randn((B, hkv, d), generator=g, device="cuda").to(kv.tdtype) for _ in range(3)]
+    out = torch.empty_like(tok[0])
+    stream, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=stream):
+        kv.decode_step(*tok, out=out)
+    for source in ([1, 2, 3, 0], [2, 2, 2, 2], [-1, 0, -1, 1], [1, 0, 3, 2]):
+        for _ in range(310):
+            for x in tok:
+                x.copy_(torch.randn(x.shape, generator=g, device="cuda"))
+            graph.replay()
+            twin.decode_step(*tok)
+        for c in (kv, twin):
+            c.fork_sequences(source)
+        (a, n), (b, _) = kv.export_state(), twin.export_state()
+        assert torch.equal(a, b), source
+        assert max(n) <= 1
+    assert kv.stats()["device_error"] == 0
