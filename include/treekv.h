@@ -341,12 +341,104 @@ treekv_status treekv_fork_sequences(treekv_ctx* ctx, const int32_t* host_source,
  */
 int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64_t* host_seen, int32_t* ops);
 
+/*
+ * ---- Prompts in pages ------------------------------------------------------------------------------------------------
+ * A prompt can be kept whole while it is read - chunk by chunk, of any length, its first pages shared with other sequences -
+ * and be evicted at once: treekv_paged_attend runs the prompt's chunks, treekv_paged_score adds up what chosen rows gave to
+ * every token, treekv_adopt_pages makes the heaviest tokens the context's cache, which decode steps, chunks and drafts then
+ * go on from.  (The paper keeps no prompt whole; keeping the tokens of the largest accumulated weight is the policy that
+ * Section 5 compares Algorithm 1 with.)
+ *
+ * Pages: dev_k_pages, dev_v_pages [n_pages][n_kv_heads][page_size][head_dim], the context's dtype, 16-byte aligned; page_size
+ * 16, 32, 64, 128 or 256 (TREEKV_ERR_UNSUPPORTED otherwise), n_pages * n_kv_heads * page_size < 2^31.  dev_table
+ * [batch][table_stride] int32: the page of the sequence's tokens [x page_size, (x + 1) page_size); entries behind its last
+ * token are not followed.  Keys carry their position encoding.  An entry outside 0..n_pages-1 is not followed: page 0 is
+ * read in its place, nothing is written, and device_error gets bit 256.
+ * dev_past [batch] int32, read on the device (a captured call can be replayed while the sequences grow): tokens in the
+ * pages before the call, 0..max_past with past + length <= table_stride * page_size; a sequence for which that does not hold
+ * sits the call out, and device_error gets bit 256.  max_past bounds what the call may meet and sizes its launch.
+ * Of the context treekv_paged_attend, treekv_paged_score and treekv_pick_path use the shape, the dtype and the error word;
+ * its cache takes no part.  All four calls need the context's device to be the current one (TREEKV_ERR_BAD_STATE).
+ */
+
+/*
+ * Attention of a chunk of new tokens over the pages, which they enter: token i of sequence b is written to position past + i
+ * and attends to positions 0..past + i.
+ *   dev_q, dev_out  [batch][stride][n_heads][head_dim]     dev_k, dev_v  [batch][stride][n_kv_heads][head_dim]
+ *   dev_lse         [batch][stride][n_heads] float: natural logarithm of the sum of exp(q k / sqrt(head_dim)); may be NULL
+ *   host_lens       [batch] int32 in 0..stride (0 = sequence not in this call); NULL = all `stride`.  Read before returning.
+ *                   stride: 1..32768
+ * Rows beyond a sequence's length are neither read nor written.  A page that receives tokens must belong to one sequence of
+ * the call; pages that are only read can be shared.  The outputs must not overlap the inputs.  A token's value never enters
+ * rows in front of it, also where it is not finite.
+ */
+treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,
+                                  void* dev_v_pages, int n_pages, int page_size, const int32_t* dev_table, int table_stride,
+                                  const int32_t* dev_past, int max_past, void* dev_out, float* dev_lse, const int32_t* host_lens,
+                                  int stride, void* stream);
+
+/*
+ * What rows of a chunk gave to the tokens of their sequence: scores[b][h][j] becomes (add = 0), or grows by (add != 0), the mean
+ * over the query heads of KV head h of sum over i with past + i >= j of exp(q_i k_j / sqrt(head_dim) - lse_i), for the
+ * positions j < past + length; Algorithm 1's sums S when all rows of a prompt are counted, those of an observation window when
+ * only its last rows are passed.
+ *   dev_q, dev_lse, host_lens, stride   as in the treekv_paged_attend call of these rows, or of the last of them, with past the
+ *                                       position of the first one passed.  A row whose log-sum-exp is infinite gives nothing
+ *   dev_scores      [batch][n_kv_heads][score_stride] float, score_stride >= max_past + the longest length
+ * Positions at and beyond past + length are not written.  Every sum has one order: results do not vary from run to run.
+ */
+treekv_status treekv_paged_score(treekv_ctx* ctx, const void* dev_q, const float* dev_lse, const void* dev_k_pages, int n_pages,
+                                 int page_size, const int32_t* dev_table, int table_stride, const int32_t* dev_past, int max_past,
+                                 float* dev_scores, int64_t score_stride, int add, const int32_t* host_lens, int stride, void* stream);
+
+/*
+ * Eviction by accumulated attention weight: the first host_lens[b] tokens of the pages become what sequence b of the context
+ * has seen.  Up to the budget all of them stay; beyond it, per KV head, the protected first and newest tokens
+ * (treekv_set_protection) and the heaviest of the others do, in their order: by S / C under TREEKV_RULE_SCORES (the quotient
+ * as a float), by S under TREEKV_RULE_ACCUMULATED; of equal ones the older stays, a NaN is below all numbers.  The other rules
+ * are TREEKV_ERR_UNSUPPORTED, and so is a context with in-cache positions.
+ *   dev_scores      [batch][n_kv_heads][score_stride] float: S, as treekv_paged_score leaves it
+ *   host_lens       [batch] int32: tokens of the prompt; 0 = the sequence stays as it is.  Any other sequence's cache is replaced
+ *   host_first      [batch] int32: first token whose row counted (C of token j = length - max(j, first)), 0..length-1; NULL = 0
+ * Both are read before returning.  The kept tokens' S and positions carry on; treekv_stats.evictions grows by what did not stay.
+ * Not while the stream is being captured (TREEKV_ERR_BAD_STATE): the host-side token counts are set.
+ */
+treekv_status treekv_adopt_pages(treekv_ctx* ctx, const void* dev_k_pages, const void* dev_v_pages, int n_pages, int page_size,
+                                 const int32_t* dev_table, int table_stride, const float* dev_scores, int64_t score_stride,
+                                 const int32_t* host_lens, const int32_t* host_first, void* stream);
+
+/*
+ * The accepted path of a drafted tree, between treekv_verify_tree (whose outputs give the logits) and treekv_accept_path (which
+ * takes the path).  Node 0 is the token that the draft hangs on, accepted from the start; a node's parent is the last other
+ * node its mask word names, which must come before it.  At node x, p = softmax(logits[x] / temperature); its children are tried
+ * in order with r = p, R = 1: a child with token t is accepted when uniform[child] * q(t) * R < r(t); turned down, it leaves
+ * r = max(r / R - q, 0), R = sum r, with q = draft[x].  Without draft probabilities q(t) = 1 and a child turned down leaves r
+ * without t.  When none is accepted the next token is the v of the largest r(v) / noise[v], of equal ones the first: with
+ * exponential noise the path and the next token are distributed as if the target had been sampled token by token.
+ * temperature = 0: a child is accepted when its token has the row's largest logit (of equal ones the first).
+ *   dev_logits      [batch][stride][vocab], logits_type fp32 or bf16     dev_draft  [batch][stride][vocab] float, row x: what
+ *                   the children of node x were drawn from; NULL = the drafter was certain of each
+ *   dev_tokens      [batch][stride] int32 drafted tokens.  One outside the vocabulary is never accepted; device_error gets bit 256
+ *   dev_mask        as in treekv_verify_tree; NULL = a chain
+ *   dev_uniform     [batch][stride] float in [0, 1)      dev_noise  [batch][vocab] float > 0, exponential; both may be NULL at
+ *                   temperature 0
+ *   dev_path        [batch][stride] int32: nodes of the path, -1 behind it     dev_count  [batch] int32: how many
+ *   dev_next        [batch] int32: the token after the path; -1 where the row it would come from has a NaN or an infinite
+ *                   logit above, or none above minus infinity
+ *   host_lens       [batch] int32 in 0..stride (0: count 0, next -1); NULL = all `stride`.  Read before returning.  stride: 1..64
+ * vocab: 1..2^24.  Tensors are 16-byte aligned; the rows of an odd vocabulary start anywhere.
+ */
+treekv_status treekv_pick_path(treekv_ctx* ctx, const void* dev_logits, treekv_dtype logits_type, int vocab, const int32_t* dev_tokens,
+                               const uint64_t* dev_mask, const float* dev_draft, float temperature, const float* dev_uniform,
+                               const float* dev_noise, int32_t* dev_path, int32_t* dev_count, int32_t* dev_next,
+                               const int32_t* host_lens, int stride, void* stream);
+
 /* Counters and error words.  Synchronises `stream` to read the device-side counters.  *host_out is filled
  * whenever the read itself succeeded; the return value is TREEKV_ERR_TIMEOUT when device_error is non-zero, i.e.
  * when a kernel's bounded wait gave up (bits: 4 TMA producer, 8 MMA issuer, 16 softmax / epilogue warps of the
  * tensor-core prefill kernels, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v), or
  * TREEKV_ERR_INVALID_ARG when its only bit is 256: an index in device memory was out of range and was not followed
- * (treekv_norm_rope, treekv_accept_path).  treekv_reset clears it; caches that a bad index of treekv_norm_rope has not
+ * (treekv_norm_rope, treekv_accept_path, the calls on pages, treekv_pick_path).  treekv_reset clears it; caches that a bad index of treekv_norm_rope has not
  * touched survive that as an image (treekv_export_state before it, treekv_import_state after it). */
 treekv_status treekv_get_stats(treekv_ctx* ctx, treekv_stats* host_out, void* stream);
 

@@ -29,6 +29,7 @@ EXPORTS = [
     "treekv_state_bytes", "treekv_export_state", "treekv_import_state", "treekv_selftest_wait_giveup",
     "treekv_set_protection", "treekv_prefill_oneshot", "treekv_set_positions",
     "treekv_norm_rope", "treekv_verify_tree", "treekv_accept_path", "treekv_fork_sequences", "treekv_selftest_fork_plan",
+    "treekv_paged_attend", "treekv_paged_score", "treekv_adopt_pages", "treekv_pick_path",
 ]
 
 
@@ -114,6 +115,14 @@ def _load():
     lib.treekv_fork_sequences.argtypes = [vp, vp, vp]
     lib.treekv_selftest_fork_plan.restype = i32
     lib.treekv_selftest_fork_plan.argtypes = [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
+    lib.treekv_paged_attend.restype = i32
+    lib.treekv_paged_attend.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp]
+    lib.treekv_paged_score.restype = i32
+    lib.treekv_paged_score.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, C.c_int64, i32, vp, i32, vp]
+    lib.treekv_adopt_pages.restype = i32
+    lib.treekv_adopt_pages.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp, C.c_int64, vp, vp, vp]
+    lib.treekv_pick_path.restype = i32
+    lib.treekv_pick_path.argtypes = [vp, vp, i32, i32, vp, vp, vp, C.c_float, vp, vp, vp, vp, vp, vp, i32, vp]
     return lib
 
 
@@ -247,6 +256,29 @@ def treekv_accept_path(ctx, q, k, v, lse, stride, path, path_stride, lens, strea
 
 def treekv_fork_sequences(ctx, source, stream=0) -> int:
     return lib.treekv_fork_sequences(ctx, _i32(source), stream)
+
+
+def treekv_paged_attend(ctx, q, k, v, k_pages, v_pages, n_pages, page_size, table, table_stride, past, max_past, out, lse, lens, stride,
+                        stream=0) -> int:
+    return lib.treekv_paged_attend(ctx, q, k, v, k_pages, v_pages, n_pages, page_size, table, table_stride, past, max_past, out, lse,
+                                   _i32(lens), stride, stream)
+
+
+def treekv_paged_score(ctx, q, lse, k_pages, n_pages, page_size, table, table_stride, past, max_past, scores, score_stride, add, lens,
+                       stride, stream=0) -> int:
+    return lib.treekv_paged_score(ctx, q, lse, k_pages, n_pages, page_size, table, table_stride, past, max_past, scores, score_stride, add,
+                                  _i32(lens), stride, stream)
+
+
+def treekv_adopt_pages(ctx, k_pages, v_pages, n_pages, page_size, table, table_stride, scores, score_stride, lens, first, stream=0) -> int:
+    return lib.treekv_adopt_pages(ctx, k_pages, v_pages, n_pages, page_size, table, table_stride, scores, score_stride, _i32(lens),
+                                  _i32(first), stream)
+
+
+def treekv_pick_path(ctx, logits, logits_type, vocab, tokens, mask, draft, temperature, uniform, noise, path, count, next_, lens, stride,
+                     stream=0) -> int:
+    return lib.treekv_pick_path(ctx, logits, logits_type, vocab, tokens, mask, draft, temperature, uniform, noise, path, count, next_,
+                                _i32(lens), stride, stream)
 
 
 def treekv_selftest_fork_plan(source, seen):
@@ -474,6 +506,97 @@ class TreeKV:
         st = lib.treekv_fork_sequences(self._h, p, self._stream())
         if st:
             _check(st, "treekv_fork_sequences")
+
+    # Prompts in pages: pools [n_pages, n_kv_heads, page_size, head_dim], table [batch, pages of a sequence] int32, past [batch]
+    # int32, all on the device.
+    def _pages(self, k_pages, v_pages, table):
+        """(k, v, number of pages, tokens of a page, table, entries of its rows) as the library takes them."""
+        want = self._want
+        n, page, width = k_pages.shape[0], k_pages.shape[2] if k_pages.dim() == 4 else 0, table.shape[1] if table.dim() == 2 else 0
+        shape = (n, self.n_kv_heads, page, self.head_dim)
+        return (want(k_pages, self.tdtype, shape, "k_pages"), None if v_pages is None else want(v_pages, self.tdtype, shape, "v_pages"), n, page,
+                want(table, self.torch.int32, (self.batch, width), "table"), width)
+
+    def paged_attend(self, q, k, v, k_pages, v_pages, table, past, lens=None, max_past=None, out=None, lse=None):
+        """(out, lse) of a chunk of new tokens [batch, stride, heads, head_dim] over the pages, which it enters behind the
+        past[b] tokens there are.  max_past: no past is larger (what the table holds otherwise; a closer bound gives a better
+        launch)."""
+        want, dt = self._want, self.tdtype
+        B, Hq, Hkv, d = self.batch, self.n_heads, self.n_kv_heads, self.head_dim
+        n = q.shape[1]
+        pq, pk, pv = want(q, dt, (B, n, Hq, d), "q"), want(k, dt, (B, n, Hkv, d), "k"), want(v, dt, (B, n, Hkv, d), "v")
+        kp, vp, pages, page, pt, width = self._pages(k_pages, v_pages, table)
+        pp = want(past, self.torch.int32, (B,), "past")
+        if out is None:
+            out = q.new_empty(B, n, Hq, d)
+            po = out.data_ptr()
+        else:
+            po = want(out, dt, (B, n, Hq, d), "out")
+        if lse is None:
+            lse = q.new_empty(B, n, Hq, dtype=self.torch.float32)
+            pl = lse.data_ptr()
+        else:
+            pl = want(lse, self.torch.float32, (B, n, Hq), "lse")
+        pn, kept = self._lens(lens, "chunk lengths")
+        st = lib.treekv_paged_attend(self._h, pq, pk, pv, kp, vp, pages, page, pt, width, pp, width * page if max_past is None else max_past,
+                                     po, pl, pn, n, self._stream())
+        if st:
+            _check(st, "treekv_paged_attend")
+        return out, lse
+
+    def paged_score(self, q, lse, k_pages, table, past, scores, lens=None, max_past=None, add=False):
+        """scores [batch, n_kv_heads, tokens] float32: written, or with add=True increased by, what the rows q gave to every token
+        of their sequence; past[b] is the position of the first of them."""
+        want, t = self._want, self.torch
+        B, Hq = self.batch, self.n_heads
+        n = q.shape[1]
+        pq, pl = want(q, self.tdtype, (B, n, Hq, self.head_dim), "q"), want(lse, t.float32, (B, n, Hq), "lse")
+        kp, _, pages, page, pt, width = self._pages(k_pages, None, table)
+        pp = want(past, t.int32, (B,), "past")
+        steps = scores.shape[-1]
+        ps = want(scores, t.float32, (B, self.n_kv_heads, steps), "scores")
+        pn, kept = self._lens(lens, "chunk lengths")
+        if max_past is None:
+            max_past = max(0, min(width * page, steps - n))
+        st = lib.treekv_paged_score(self._h, pq, pl, kp, pages, page, pt, width, pp, max_past, ps, steps, 1 if add else 0, pn, n, self._stream())
+        if st:
+            _check(st, "treekv_paged_score")
+        return scores
+
+    def adopt_pages(self, k_pages, v_pages, table, scores, lens, first=None):
+        """The lens[b] first tokens of the pages become what sequence b has seen; beyond the budget the heaviest stay.  first[b]: the
+        first token whose row is in the scores."""
+        kp, vp, pages, page, pt, width = self._pages(k_pages, v_pages, table)
+        steps = scores.shape[-1]
+        ps = self._want(scores, self.torch.float32, (self.batch, self.n_kv_heads, steps), "scores")
+        pn, kept = self._lens(lens, "prompt lengths")
+        if pn is None:
+            raise ValueError("adopt_pages takes the prompts' lengths")
+        pf, kept2 = self._lens(first, "first counted tokens")
+        st = lib.treekv_adopt_pages(self._h, kp, vp, pages, page, pt, width, ps, steps, pn, pf, self._stream())
+        if st:
+            _check(st, "treekv_adopt_pages")
+
+    def pick_path(self, logits, tokens, uniform=None, noise=None, mask=None, lens=None, draft=None, temperature=1.0):
+        """(path [batch, stride], count [batch], next token [batch]), int32, of drafted trees whose node 0 is given: logits [batch,
+        stride, vocab] (float32 or bfloat16), tokens int32 [batch, stride], uniform float32 [batch, stride], noise float32 [batch,
+        vocab] (exponential), draft float32 [batch, stride, vocab] (what each node's children were drawn from)."""
+        t, want = self.torch, self._want
+        B, n, V = self.batch, tokens.shape[1], logits.shape[-1]
+        if logits.dtype not in (t.float32, t.bfloat16):
+            raise ValueError("expected float32 or bfloat16 logits, got %s" % logits.dtype)
+        pl, pt = want(logits, logits.dtype, (B, n, V), "logits"), want(tokens, t.int32, (B, n), "tokens")
+        pu = None if uniform is None else want(uniform, t.float32, (B, n), "uniform")
+        pe = None if noise is None else want(noise, t.float32, (B, V), "noise")
+        pm = None if mask is None else want(mask, t.int64, (B, n), "mask")
+        pd = None if draft is None else want(draft, t.float32, (B, n, V), "draft")
+        path, count, after = tokens.new_empty(B, n), tokens.new_empty(B), tokens.new_empty(B)
+        pn, kept = self._lens(lens, "draft lengths")
+        st = lib.treekv_pick_path(self._h, pl, TREEKV_F32 if logits.dtype is t.float32 else TREEKV_BF16, V, pt, pm, pd, temperature, pu, pe,
+                                  path.data_ptr(), count.data_ptr(), after.data_ptr(), pn, n, self._stream())
+        if st:
+            _check(st, "treekv_pick_path")
+        return path, count, after
 
     def retained_positions(self):
         t = self.torch

@@ -1,0 +1,360 @@
+// What the rows of a chunk gave to every token of their paged sequence, on the 5th-generation tensor cores (bf16):
+//     S_j (+)= 1 / G  sum over the rows r that see j of exp(q_r k_j / sqrt d - lse_r)
+//
+// The logits are taken transposed, S^T = K Q^T with a tile of 128 keys as the matrix rows: a thread then holds one key and runs
+// along 128 query rows, whose log-sum-exps it reads from shared memory, so a key's sum never leaves its thread - no atomics,
+// one order of additions, one write.  Sums of a tile of rows are added up with a compensation (Kahan), whatever the chunk's
+// length.  Nothing is rounded to fewer than 32 bits.
+//
+// An item is one key tile of one unit (sequence, KV head).  Blocks take items in a row when one tile of queries is all there is
+// (an observation window: the queries stay in shared memory, the keys stream by), and every gridDim-th one otherwise, so that
+// long and short items mix.  With fewer items than the machine has SMs a cluster shares an item's query tiles.
+//
+// Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 and 6-9 are two groups that take alternate logit tiles.
+#include <algorithm>
+
+#include "paged.cuh"
+#include "verify_tc.cuh"
+
+namespace treekv {
+
+namespace {
+
+using namespace vtc;
+
+constexpr int kThreads = 320;
+constexpr int kTile = 128;                 // keys of an item, query rows of a step
+constexpr uint32_t kTmemCols = 512;        // four logit tiles
+constexpr size_t kSmemMin = 120 * 1024;    // one block on an SM: it holds all of the tensor memory
+constexpr int kMaxSplit = 8;
+
+enum Bar { K_FULL = 0, K_FREE = 2, Q_FULL = 4, Q_FREE = 6, S_FULL = 8, S_FREE = 12, JOIN = 16, N_BARS = 17 };
+
+// The items of a block in order, the same for every role.
+struct Walk {
+    const int* first;
+    int B, Hkv, G, item, step, end, split, rank;
+    const PagedView* pv;
+    const ChunkLens* lens;
+    int b, kh, k0, past, n, rows, nvis, qa, qb;  // of the item: sequence, head, first key, query tiles [qa, qb) that see the keys
+    __device__ bool get() {
+        if (item >= end) return false;
+        int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item and has any
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= item) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+        n = lens->m[b];
+        past = pv->past[b];
+        rows = n * G; nvis = past + n;
+        const int tiles = (nvis + kTile - 1) / kTile, at = item - first[b];
+        kh = at / tiles; k0 = (at - kh * tiles) * kTile;
+        qa = max(0, k0 - past) * G / kTile;
+        qb = (rows + kTile - 1) / kTile;
+        return true;
+    }
+    __device__ void next() { item += step; }
+};
+
+template <int D>
+__global__ void __launch_bounds__(kThreads, 1)
+score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PagedView pv, ChunkView ch, ChunkLens lens,
+                ScoreArgs sa, int B, int Hq, int Hkv, DevStats* stats, int q_bytes, int in_a_row, int split) {
+    constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128;
+    pdl_trigger();
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[N_BARS];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_first[kMaxBatch + 1];
+    __shared__ __align__(16) float s_lse[2][2][kTile];     // [group][parity of its steps] minus log-sum-exps in units of log 2
+    __shared__ float s_part[2][kTile];                      // the second group's sums
+    __shared__ __align__(8) float s_join[kMaxSplit][kTile]; // (block 0 of a cluster) the blocks' sums
+    const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
+    const uint32_t sK = base, sQ = base + 2 * SLOT;
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bar0 = smem_addr_u32(&bars[0]);
+    auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(K_FULL + s), 1); mbar_init(bar(K_FREE + s), 1); mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1); }
+        for (int s = 0; s < 4; ++s) { mbar_init(bar(S_FULL + s), 1); mbar_init(bar(S_FREE + s), 4); }
+        mbar_init(bar(JOIN), 4 * kMaxSplit);
+        mbar_fence_init();
+    }
+    if (warp == 1) { tmem_alloc(smem_addr_u32(&tmem_slot), kTmemCols); tmem_relinquish(); }
+    pdl_wait();
+    if (warp == 0) {  // items of each sequence, in order
+        int sum = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            const int b = b0 + lane, n = b < B ? lens.m[b] : 0;
+            int items = 0;
+            if (n > 0) {
+                const int past = paged_past(pv, b, n);
+                if (past < 0) { if (blockIdx.x == 0) atomicOr(&stats->error, kErrBadIndex); }
+                else items = (past + n + kTile - 1) / kTile * Hkv;
+            }
+            int inc = items;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
+            if (b < B) s_first[b] = sum + inc - items;
+            sum += __shfl_sync(0xffffffffu, inc, 31);
+        }
+        if (lane == 0) s_first[B] = sum;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot;
+    const int rank = split > 1 ? (int)cluster_cta_rank() : 0, blocks = gridDim.x / split, block = blockIdx.x / split, total = s_first[B];
+    Walk w;
+    w.first = s_first; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.pv = &pv; w.lens = &lens; w.split = split; w.rank = rank;
+    if (in_a_row) {
+        const int per = (total + blocks - 1) / blocks;
+        w.item = min(block * per, total); w.end = min(w.item + per, total); w.step = 1;
+    } else {
+        w.item = block; w.end = total; w.step = blocks;
+    }
+    if (split > 1) cluster_sync_all();  // the blocks of a cluster are running and their barriers are there
+
+    bool ok = true;
+    if (warp == 0) {
+        // ================= TMA producer
+        int kl = 0, ql = 0, last_unit = -1, last_q = -1;
+        fence_proxy_async_global();
+        for (; ok && w.get(); w.next()) {
+            if (w.qa + rank >= w.qb) continue;
+            // a key tile: boxes of its pages
+            const int box = min(pv.page, kTile), boxes = (min(kTile, w.nvis - w.k0) + box - 1) / box, p0 = w.k0 >> pv.plog;
+            int e = 0;
+            if (lane < boxes) e = checked_page(pv, __ldg(pv.table + (size_t)w.b * pv.width + p0 + lane), stats);
+            const int row = (e * Hkv + w.kh) * pv.page + (lane == 0 ? w.k0 & (pv.page - 1) : 0);
+            const int slot = kl & 1;
+            if (lane == 0) {
+                ok = mbar_wait(bar(K_FREE + slot), ((kl >> 1) & 1) ^ 1);
+                if (ok) mbar_arrive_expect_tx(bar(K_FULL + slot), boxes * box * D * 2);
+            }
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            if (!ok) break;
+            if (lane < boxes)
+#pragma unroll
+                for (int h = 0; h < HALVES; ++h) tma_load_2d(sK + slot * SLOT + h * HALF + lane * box * 128, &tmK, 64 * h, row, bar(K_FULL + slot));
+            ++kl;
+            __syncwarp();
+            if (lane == 0) {
+                const int unit = w.b * Hkv + w.kh;
+                for (int qt = w.qa + rank; qt < w.qb; qt += split) {
+                    if (unit == last_unit && qt == last_q) continue;
+                    const int qs = ql & 1;
+                    if (!mbar_wait(bar(Q_FREE + qs), ((ql >> 1) & 1) ^ 1)) { ok = false; break; }
+                    mbar_arrive_expect_tx(bar(Q_FULL + qs), q_bytes);
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h)
+                        tma_load_3d(sQ + qs * SLOT + h * HALF, &tmQ, 64 * h, w.kh * w.G, w.b * ch.stride + qt * (kTile / w.G), bar(Q_FULL + qs));
+                    ++ql;
+                    last_unit = unit; last_q = qt;
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+        }
+        // nothing may still be on its way into this block's memory when it ends, whatever gave up
+        if (lane == 0) {
+            for (int x = max(0, kl - 2); x < kl; ++x) ok = mbar_wait(bar(K_FULL + (x & 1)), (x >> 1) & 1) && ok;
+            for (int x = max(0, ql - 2); x < ql; ++x) ok = mbar_wait(bar(Q_FULL + (x & 1)), (x >> 1) & 1) && ok;
+            if (!ok) atomicOr(&stats->error, 4u);
+        }
+    } else if (warp == 1) {
+        // ================= MMA issuer
+        if (lane == 0) {
+            constexpr uint32_t idesc = umma_idesc_bf16(kTile, kTile, 0, 0);  // both operands K-major (rows x channels)
+            const uint32_t k_lo = desc_lo(sK, 16), q_lo = desc_lo(sQ, 16);
+            int kl = 0, ql = -1, st = 0, last_unit = -1, last_q = -1;
+            for (; ok && w.get(); w.next()) {
+                if (w.qa + rank >= w.qb) continue;
+                const int slot = kl & 1, unit = w.b * Hkv + w.kh;
+                if (!(ok = mbar_wait(bar(K_FULL + slot), (kl >> 1) & 1))) break;
+                for (int qt = w.qa + rank; qt < w.qb; qt += split) {
+                    if (!(unit == last_unit && qt == last_q)) {
+                        if (ql >= 0) umma_commit(bar(Q_FREE + (ql & 1)));  // the tile before is not needed any more
+                        ++ql;
+                        if (!(ok = mbar_wait(bar(Q_FULL + (ql & 1)), (ql >> 1) & 1))) break;
+                        last_unit = unit; last_q = qt;
+                    }
+                    const int buf = st & 3;
+                    if (!(ok = mbar_wait(bar(S_FREE + buf), ((st >> 2) & 1) ^ 1))) break;
+                    tc_fence_after();
+                    const uint32_t a = k_lo + slot * (SLOT / 16), q = q_lo + (ql & 1) * (SLOT / 16);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        umma_bf16(tmem + buf * kTile, desc_of(a + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), desc_of(q + (kk >> 2) * (HALF / 16) + (kk & 3) * 2),
+                                  idesc, kk > 0);
+                    umma_commit(bar(S_FULL + buf));
+                    ++st;
+                }
+                if (!ok) break;
+                umma_commit(bar(K_FREE + slot));
+                ++kl;
+            }
+            // every MMA has finished before its memory and tensor memory are given to anything else
+            for (int x = max(0, st - 4); x < st; ++x) ok = mbar_wait(bar(S_FULL + (x & 3)), (x >> 2) & 1) && ok;
+            if (ok && kl > 0) ok = mbar_wait(bar(K_FREE + ((kl - 1) & 1)), ((kl - 1) >> 1) & 1);
+            if (!ok) atomicOr(&stats->error, 8u);
+        }
+    } else {
+        // ================= the two groups
+        const int group = (warp - 2) >> 2, quarter = warp & 3, key = quarter * 32 + lane;
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+        const float sc2 = kLog2e * rsqrtf((float)D), over = 1.0f / (float)w.G;
+        int st = 0, mine = 0, shared = 0;  // steps of the block, of this group; items that both groups had steps of
+        for (; ok && w.get(); w.next()) {
+            float sum = 0.f, comp = 0.f;
+            const int kpos = w.k0 + key, r_min = max(0, kpos - w.past) * w.G;  // first row that sees this key
+            auto lse_of = [&](int qt) {  // of column `key` of a query tile
+                const int r = qt * kTile + key;
+                return qt < w.qb && r < w.rows ? sa.lse[((size_t)w.b * ch.stride + r / w.G) * Hq + w.kh * w.G + r % w.G] : INFINITY;
+            };
+            const int steps = w.qa + rank < w.qb ? (w.qb - w.qa - rank + split - 1) / split : 0;
+            const bool both = steps > 1;         // each group has steps of this item
+            int x = (st & 1) == group ? 0 : 1;   // this group's first step of the item
+            float l_next = x < steps ? lse_of(w.qa + rank + x * split) : 0.f;
+            for (; x < steps; x += 2) {
+                const int qt = w.qa + rank + x * split, s = st + x, buf = s & 3;
+                float* nl = s_lse[group][mine & 1];
+                nl[key] = l_next == -INFINITY ? -INFINITY : -l_next * kLog2e;  // (a row that saw nothing gives nothing; no row: minus infinity)
+                asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+                if (x + 2 < steps) l_next = lse_of(qt + 2 * split);
+                if (!mbar_wait(bar(S_FULL + buf), (s >> 2) & 1)) { ok = false; break; }
+                tc_fence_after();
+                const int cmin = r_min - qt * kTile, cmax = w.rows - qt * kTile;     // columns [cmin, cmax) are rows that see the key
+                const bool full = __all_sync(0xffffffffu, cmin <= 0) && cmax >= kTile;
+                float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+                uint32_t v[2][32];
+                tmem_ld32(tmem + buf * kTile + lane_off, v[0]);
+#pragma unroll
+                for (int cg = 0; cg < 4; ++cg) {
+                    tmem_ld_wait_for(v[cg & 1]);
+                    if (cg < 3) {
+                        tmem_ld32(tmem + buf * kTile + lane_off + (cg + 1) * 32, v[(cg + 1) & 1]);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 32; e += 4) {
+                        const float4 l4 = *reinterpret_cast<const float4*>(nl + cg * 32 + e);
+                        float p0 = ex2(fmaf(__uint_as_float(v[cg & 1][e]), sc2, l4.x)), p1 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 1]), sc2, l4.y));
+                        float p2 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 2]), sc2, l4.z)), p3 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 3]), sc2, l4.w));
+                        if (!full) {
+                            const int c = cg * 32 + e;
+                            p0 = c >= cmin && c < cmax ? p0 : 0.f; p1 = c + 1 >= cmin && c + 1 < cmax ? p1 : 0.f;
+                            p2 = c + 2 >= cmin && c + 2 < cmax ? p2 : 0.f; p3 = c + 3 >= cmin && c + 3 < cmax ? p3 : 0.f;
+                        }
+                        a0 += p0; a1 += p1; a2 += p2; a3 += p3;
+                    }
+                }
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(S_FREE + buf));
+                const float y = ((a0 + a1) + (a2 + a3)) - comp, t = sum + y;  // compensated
+                comp = (t - sum) - y;
+                sum = t;
+                ++mine;
+            }
+            if (!ok) break;
+            // the group that took the item's first step writes; the other one's sum comes through shared memory
+            const bool writer = (st & 1) == group;
+            st += steps;
+            if (both) {
+                if (!writer) {
+                    s_part[shared & 1][key] = sum;
+                    asm volatile("bar.sync 3, 256;" ::: "memory");
+                } else {
+                    asm volatile("bar.sync 3, 256;" ::: "memory");
+                    sum += s_part[shared & 1][key];
+                }
+                ++shared;
+            }
+            if (split > 1) {  // (one item per cluster) block 0 adds the blocks' sums in order
+                const bool sends = steps > 0 ? writer : group == 0;
+                if (sends) {
+                    const uint32_t to = map_to_cta(smem_addr_u32(&s_join[rank][key]), 0);
+                    asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(steps > 0 ? sum : 0.f) : "memory");
+                    fence_cluster();
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive_remote(map_to_cta(bar(JOIN), 0));
+                    if (rank == 0) {
+                        // (blocks beyond `split` do not exist: their arrivals are made here)
+                        if (lane == 0) for (int x2 = split; x2 < kMaxSplit; ++x2) mbar_arrive(bar(JOIN));
+                        if (!mbar_wait_cluster(bar(JOIN), 0)) { ok = false; break; }
+                        sum = 0.f;
+                        for (int r = 0; r < split; ++r) sum += s_join[r][key];
+                        if (kpos < w.nvis) {
+                            float* at = sa.scores + ((size_t)w.b * Hkv + w.kh) * sa.score_stride + kpos;
+                            *at = sa.add ? *at + sum * over : sum * over;
+                        }
+                    }
+                }
+            } else if (writer && kpos < w.nvis) {
+                float* at = sa.scores + ((size_t)w.b * Hkv + w.kh) * sa.score_stride + kpos;
+                *at = sa.add ? *at + sum * over : sum * over;
+            }
+        }
+        if (!ok && lane == 0) atomicOr(&stats->error, 16u);
+        tc_fence_before();
+    }
+    __syncwarp();
+    __syncthreads();
+    if (split > 1) cluster_sync_all();  // nobody leaves while its memory may be written or its barrier signalled
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
+}
+
+template <int D>
+cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const ScoreArgs& a, int sms,
+                     cudaStream_t stream) {
+    const int G = cv.Hq / cv.Hkv, box = std::min(kTile / G, ch.stride);
+    CUtensorMap tmQ, tmK;
+    const DraftView dv = {ch.q, nullptr, nullptr, nullptr, ch.stride};
+    if (!make_q_map(&tmQ, cv, dv, box)) return cudaErrorInvalidValue;
+    const uint64_t dims[2] = {(uint64_t)cv.d, (uint64_t)pv.n_pages * cv.Hkv * pv.page};
+    const uint64_t strides[1] = {(uint64_t)cv.d * 2};
+    const uint32_t kbox[2] = {64u, (uint32_t)std::min(pv.page, kTile)};
+    if (!make_tensor_map_bf16(&tmK, pv.kp, 2, dims, strides, kbox)) return cudaErrorInvalidValue;
+    auto kern = score_tc_kernel<D>;
+    const size_t smem = std::max(kSmemMin, (size_t)1024 + 4 * kTile * D * 2);
+    static bool smem_set[64] = {};  // per device: the opt-in is needed once
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    if (!smem_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        smem_set[dev] = true;
+    }
+    long items = 0;  // at most
+    int active = 0;
+    for (int b = 0; b < cv.B; ++b)
+        if (lens.m[b]) { items += (long)(pv.max_past + lens.m[b] + kTile - 1) / kTile * cv.Hkv; ++active; }
+    const int qtiles = (max_n * G + kTile - 1) / kTile;
+    int split = 1;
+    while (split < kMaxSplit && items * split * 2 <= sms && qtiles >= split * 4) split *= 2;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3((unsigned)(split > 1 ? items * split : std::min<long>(items, sms)));
+    cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = smem;
+    cfg.stream = stream;
+    cudaLaunchAttribute attr[2];
+    attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
+    attr[0].val.programmaticStreamSerializationAllowed = 1;
+    attr[1].id = cudaLaunchAttributeClusterDimension;
+    attr[1].val.clusterDim.x = split;
+    attr[1].val.clusterDim.y = 1;
+    attr[1].val.clusterDim.z = 1;
+    cfg.attrs = attr;
+    cfg.numAttrs = split > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, tmQ, tmK, pv, ch, lens, a, cv.B, cv.Hq, cv.Hkv, cv.stats, (D / 64) * box * G * 128, qtiles == 1 ? 1 : 0, split);
+}
+
+}  // namespace
+
+cudaError_t launch_score_tc(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const ScoreArgs& a,
+                            int sms, cudaStream_t stream) {
+    return cv.d == 64 ? launch_t<64>(cv, pv, ch, lens, max_n, a, sms, stream) : launch_t<128>(cv, pv, ch, lens, max_n, a, sms, stream);
+}
+
+}  // namespace treekv
