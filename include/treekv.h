@@ -426,7 +426,7 @@ treekv_status treekv_adopt_pages(treekv_ctx* ctx, const void* dev_k_pages, const
  *   dev_next        [batch] int32: the token after the path; -1 where the row it would come from has a NaN or an infinite
  *                   logit above, or none above minus infinity
  *   host_lens       [batch] int32 in 0..stride (0: count 0, next -1); NULL = all `stride`.  Read before returning.  stride: 1..64
- * vocab: 1..2^24.  Tensors are 16-byte aligned; the rows of an odd vocabulary start anywhere.
+ * vocab: 1..500000 (TREEKV_ERR_UNSUPPORTED above).  Tensors are 16-byte aligned; the rows of an odd vocabulary start anywhere.
  */
 treekv_status treekv_pick_path(treekv_ctx* ctx, const void* dev_logits, treekv_dtype logits_type, int vocab, const int32_t* dev_tokens,
                                const uint64_t* dev_mask, const float* dev_draft, float temperature, const float* dev_uniform,

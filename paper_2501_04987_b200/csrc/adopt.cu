@@ -3,9 +3,12 @@
 //
 // Two launches.  The first one finds, per unit (sequence, KV head), which tokens stay, by a radix selection on the weights
 // (as integers in the order of the numbers): three rounds of histograms - 11, 11 and 10 bits - narrow the last weight that
-// stays down to one value; of the tokens that have exactly that one the oldest stay.  A cluster of blocks shares a unit, its
-// histograms meet in shared memory.  A second walk writes the tokens' positions and sums to the rows where they will lie.  The
-// second launch moves the keys and values: it reads a row's position and fetches the token from its page.
+// stays down to one value; of the tokens that have exactly that one the oldest stay.  The weights are read once and held in
+// shared memory (a block's share of more than 48 K is read again from L2).  A cluster of blocks shares a long unit: each block adds
+// a slice of the histograms up over the cluster - all of them in every block would move eight times as much through distributed
+// shared memory - and what the slices hold tells where to look.  A last walk writes the tokens' positions and sums to the rows
+// where they will lie.  The second launch moves the keys and values: it reads a row's position and fetches the token from its
+// page.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -18,6 +21,7 @@ namespace {
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxSplit = 8;
 constexpr int kBins = 2048;
+constexpr int kHeld = 48 * 1024;  // weights in shared memory
 
 // Weights as integers in the order of the numbers; NaN below all of them, minus zero as zero.
 __device__ inline uint32_t order_key(float w) {
@@ -26,112 +30,142 @@ __device__ inline uint32_t order_key(float w) {
     return u & 0x80000000u ? ~u : u | 0x80000000u;
 }
 
-struct Select {
-    const float* scores;
-    long long stride;
-    int first;   // of this sequence
-    int n, lo, hi;  // tokens [lo, hi) can be evicted
-    bool average;
-    __device__ uint32_t key(const float* row, int t) const {
-        const float s = __ldg(row + t);
-        return order_key(average ? __fdiv_rn(s, (float)score_count(n, t, first)) : s);
-    }
-};
+// inclusive sums over the block's threads; s_warp: kWarps words that nobody else uses before the next block barrier but one
+__device__ inline uint32_t block_scan(uint32_t x, uint32_t* s_warp, uint32_t& total) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+#pragma unroll
+    for (int o = 1; o < 32; o *= 2) { const uint32_t y = __shfl_up_sync(0xffffffffu, x, o); if (lane >= o) x += y; }
+    if (lane == 31) s_warp[warp] = x;
+    __syncthreads();
+    uint32_t w = lane < kWarps ? s_warp[lane] : 0u;
+#pragma unroll
+    for (int o = 1; o < kWarps; o *= 2) { const uint32_t y = __shfl_up_sync(0xffffffffu, w, o); if (lane >= o) w += y; }
+    total = __shfl_sync(0xffffffffu, w, kWarps - 1);
+    return x + (warp ? __shfl_sync(0xffffffffu, w, (warp + 31) & 31) : 0u);
+}
 
-__global__ void __launch_bounds__(kThreads) adopt_select_kernel(CacheView cv, const float* __restrict__ scores, long long stride, AdoptLens lens, int split) {
+template <int SPLIT>
+__global__ void __launch_bounds__(kThreads) adopt_select_kernel(CacheView cv, const float* __restrict__ scores, long long stride, AdoptLens lens, int held) {
+    constexpr int SLICE = kBins / SPLIT, PER = (SLICE + kThreads - 1) / kThreads;
     pdl_trigger();
     pdl_wait();
     const int unit = blockIdx.y, b = unit / cv.Hkv, rank = blockIdx.x, n = lens.n[b];
     if (n == 0) return;  // the whole cluster
-    __shared__ uint32_t s_hist[kBins];
-    __shared__ uint32_t s_scan[kWarps];
-    __shared__ uint32_t s_pick[2];             // the bin, tokens above it
-    __shared__ uint32_t s_count[2][kWarps];    // tokens of each warp above the last weight, at it
-    __shared__ __align__(8) uint32_t s_total[2];  // of this block
-    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
-    Select sel;
-    sel.n = n; sel.first = lens.first[b]; sel.average = cv.rule != TREEKV_RULE_ACCUMULATED;
+    extern __shared__ __align__(16) uint32_t s_key[];   // [held]
+    __shared__ __align__(16) uint32_t s_hist[kBins];    // from the largest weights down
+    __shared__ __align__(16) uint32_t s_sum[2][SLICE];  // this block's slice over the cluster
+    __shared__ uint32_t s_tot[2][SPLIT];                // the slices' sums
+    __shared__ uint32_t s_warp[4][kWarps];
+    __shared__ uint32_t s_pick[2];                      // the bin, tokens above it
+    __shared__ uint32_t s_count[2][kWarps];             // tokens of each warp above the last weight, at it
+    __shared__ __align__(8) uint32_t s_block[SPLIT][2]; // of each block
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31, first = lens.first[b];
+    const bool average = cv.rule != TREEKV_RULE_ACCUMULATED;
     const float* row = scores + (size_t)unit * stride;
     const UnitState st = unit_state(n, cv);
     const bool all = n <= cv.c;
-    sel.lo = all ? n : cv.ns; sel.hi = all ? n : n - cv.nr;
-    const int free = sel.hi - sel.lo;                                    // tokens to choose from, cm of them stay
+    const int lo = all ? n : cv.ns, hi = all ? n : n - cv.nr;            // tokens to choose from, cm of them stay
     // this warp's tokens: a stretch of its own, whole groups of 32
-    const int groups = (free + 31) / 32, per = (groups + split * kWarps - 1) / (split * kWarps) * 32;
-    const int w0 = min(sel.lo + (rank * kWarps + warp) * per, sel.hi), w1 = min(w0 + per, sel.hi);
+    const int groups = (hi - lo + 31) / 32, per = (groups + SPLIT * kWarps - 1) / (SPLIT * kWarps) * 32;
+    const int b0 = min(lo + rank * kWarps * per, hi), w0 = min(b0 + warp * per, hi), w1 = min(w0 + per, hi);
+    const bool keep = kWarps * per <= held;
+    auto key_of = [&](int t) {
+        const float s = __ldg(row + t);
+        return order_key(average ? __fdiv_rn(s, (float)score_count(n, t, first)) : s);
+    };
+    auto key = [&](int t) { return keep ? s_key[t - b0] : key_of(t); };
     uint32_t prefix = 0, need = (uint32_t)cv.cm;                          // bits of the last weight so far; tokens still to find
     if (!all) {
-        const int shifts[3] = {21, 10, 0}, bits[3] = {11, 11, 10};
 #pragma unroll 1
         for (int round = 0; round < 3; ++round) {
-            const int shift = shifts[round], nbins = 1 << bits[round];
+            const int shift = round == 0 ? 21 : round == 1 ? 10 : 0, bins = round == 2 ? 1024 : 2048, par = round & 1;
             for (int i = tid; i < kBins; i += kThreads) s_hist[i] = 0u;
             __syncthreads();
-            const uint32_t above = round == 0 ? 0u : ~0u << (shift + bits[round]);
-            for (int t = w0 + lane; t < w1; t += 32) {
-                const uint32_t k = sel.key(row, t);
-                if ((k & above) == prefix) atomicAdd(&s_hist[k >> shift & (nbins - 1)], 1u);
+            if (round == 0) {
+#pragma unroll 8
+                for (int t = w0 + lane; t < w1; t += 32) {
+                    const uint32_t k = key_of(t);
+                    if (keep) s_key[t - b0] = k;
+                    atomicAdd(&s_hist[2047u - (k >> 21)], 1u);
+                }
+            } else {
+                const uint32_t above = ~0u << (shift + (round == 2 ? 10 : 11));
+#pragma unroll 4
+                for (int t = w0 + lane; t < w1; t += 32) {
+                    const uint32_t k = key(t);
+                    if ((k & above) == prefix) atomicAdd(&s_hist[bins - 1 - (k >> shift & (bins - 1))], 1u);
+                }
             }
             __syncthreads();
-            // the cluster's histograms: a thread adds four bins up, from the largest weights down
-            if (split > 1) cluster_sync_all();
-            constexpr int PER = kBins / kThreads;
-            uint32_t h[PER], mine = 0;
+            uint32_t before = 0, h[PER], mine = 0, total;
+            int owner = 0;
+            if constexpr (SPLIT > 1) {
+                cluster_sync_all();                                        // the histograms are complete
+#pragma unroll
+                for (int x = 0; x < PER; ++x) {
+                    const int j = tid * PER + x;
+                    uint32_t sum = 0;
+                    if (j < SLICE) {
+                        uint32_t y[SPLIT];
+#pragma unroll
+                        for (int s = 0; s < SPLIT; ++s)
+                            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y[s]) : "r"(map_to_cta(smem_addr_u32(&s_hist[rank * SLICE + j]), s)) : "memory");
+#pragma unroll
+                        for (int s = 0; s < SPLIT; ++s) sum += y[s];
+                        s_sum[par][j] = sum;
+                    }
+                    mine += sum;
+                }
+                block_scan(mine, s_warp[2 * par], total);
+                if (tid < SPLIT) asm volatile("st.shared::cluster.u32 [%0], %1;" ::"r"(map_to_cta(smem_addr_u32(&s_tot[par][rank]), tid)), "r"(total) : "memory");
+                __syncwarp();
+                cluster_sync_all();                                        // the slices are
+                while (owner < SPLIT - 1 && before + s_tot[par][owner] < need) before += s_tot[par][owner++];
+                mine = 0;
+            }
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
-                const int bin = kBins - 1 - (tid * PER + x);
-                h[x] = s_hist[bin];
-                if (split > 1) {
-                    for (int s = 0; s < split; ++s)
-                        if (s != rank) {
-                            uint32_t y;
-                            asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(y) : "r"(map_to_cta(smem_addr_u32(&s_hist[bin]), s)) : "memory");
-                            h[x] += y;
-                        }
+                const int j = tid * PER + x;
+                h[x] = 0;
+                if (j < SLICE) {
+                    if constexpr (SPLIT > 1)
+                        asm volatile("ld.shared::cluster.u32 %0, [%1];" : "=r"(h[x]) : "r"(map_to_cta(smem_addr_u32(&s_sum[par][j]), owner)) : "memory");
+                    else
+                        h[x] = s_hist[j];
                 }
                 mine += h[x];
             }
-            uint32_t inc = mine;
-#pragma unroll
-            for (int o = 1; o < 32; o *= 2) { const uint32_t y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
-            if (lane == 31) s_scan[warp] = inc;
-            __syncthreads();
-            uint32_t before = inc - mine;
-            for (int w = 0; w < warp; ++w) before += s_scan[w];
+            before += block_scan(mine, s_warp[2 * par + 1], total) - mine;
 #pragma unroll
             for (int x = 0; x < PER; ++x) {
-                if (before < need && before + h[x] >= need) { s_pick[0] = kBins - 1 - (tid * PER + x); s_pick[1] = before; }
+                if (before < need && before + h[x] >= need) { s_pick[0] = bins - 1 - (owner * SLICE + tid * PER + x); s_pick[1] = before; }
                 before += h[x];
             }
             __syncthreads();
             prefix |= s_pick[0] << shift;
             need -= s_pick[1];
-            if (split > 1) cluster_sync_all();  // nobody clears a histogram that is read
-            else __syncthreads();
         }
     }
     // prefix: the last weight that stays; `need` of the tokens that have it stay
     uint32_t more = 0, same = 0;
     if (!all)
         for (int t = w0 + lane; t - lane < w1; t += 32) {
-            const uint32_t k = t < w1 ? sel.key(row, t) : 0u;
+            const uint32_t k = t < w1 ? key(t) : 0u;
             more += __popc(__ballot_sync(0xffffffffu, t < w1 && k > prefix));
             same += __popc(__ballot_sync(0xffffffffu, t < w1 && k == prefix));
         }
     if (lane == 0) { s_count[0][warp] = more; s_count[1][warp] = same; }
     __syncthreads();
-    if (tid == 0) {
-        uint32_t x = 0, y = 0;
-        for (int w = 0; w < kWarps; ++w) { x += s_count[0][w]; y += s_count[1][w]; }
-        s_total[0] = x; s_total[1] = y;
-    }
-    __syncthreads();
-    if (split > 1) cluster_sync_all();
     uint32_t n_more = 0, n_same = 0;  // before this warp's tokens
-    for (int s = 0; s < rank; ++s) {
-        uint32_t x, y;
-        asm volatile("ld.shared::cluster.v2.u32 {%0, %1}, [%2];" : "=r"(x), "=r"(y) : "r"(map_to_cta(smem_addr_u32(s_total), s)) : "memory");
-        n_more += x; n_same += y;
+    if constexpr (SPLIT > 1) {
+        if (tid < SPLIT) {
+            uint32_t x = 0, y = 0;
+            for (int w = 0; w < kWarps; ++w) { x += s_count[0][w]; y += s_count[1][w]; }
+            asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(s_block[rank]), tid)), "r"(x), "r"(y) : "memory");
+        }
+        __syncwarp();
+        cluster_sync_all();           // the last word from any other block
+        for (int s = 0; s < rank; ++s) { n_more += s_block[s][0]; n_same += s_block[s][1]; }
     }
     for (int w = 0; w < warp; ++w) { n_more += s_count[0][w]; n_same += s_count[1][w]; }
     int32_t* pos = cv.pos + (size_t)unit * cv.R;
@@ -139,7 +173,7 @@ __global__ void __launch_bounds__(kThreads) adopt_select_kernel(CacheView cv, co
     auto put = [&](int lam, int t) { const int r = phys_row(lam, st); pos[r] = t; sum[r] = __ldg(row + t); };
     if (!all) {
         for (int t = w0 + lane; t - lane < w1; t += 32) {
-            const uint32_t k = t < w1 ? sel.key(row, t) : 0u, below = (1u << lane) - 1u;
+            const uint32_t k = t < w1 ? key(t) : 0u, below = (1u << lane) - 1u;
             const uint32_t m = __ballot_sync(0xffffffffu, t < w1 && k > prefix), e = __ballot_sync(0xffffffffu, t < w1 && k == prefix);
             const uint32_t at_m = n_more + __popc(m & below), at_e = n_same + __popc(e & below);
             if ((m >> lane & 1u) || ((e >> lane & 1u) && at_e < need)) put(cv.ns + (int)(at_m + min(at_e, need)), t);
@@ -147,11 +181,10 @@ __global__ void __launch_bounds__(kThreads) adopt_select_kernel(CacheView cv, co
         }
     }
     // the protected ones, or all there are
-    const int lead = all ? n : cv.ns, tail = all ? 0 : cv.nr, step = split * kThreads;
+    const int lead = all ? n : cv.ns, tail = all ? 0 : cv.nr, step = SPLIT * kThreads;
     for (int t = rank * kThreads + tid; t < lead; t += step) put(t, t);
     for (int t = rank * kThreads + tid; t < tail; t += step) put(cv.c - cv.nr + t, n - cv.nr + t);
-    if (rank == 0 && tid == 0) { cv.n_seen[unit] = n; cv.w0[unit] = sel.first; }
-    if (split > 1) cluster_sync_all();  // nobody leaves while its counts may be read
+    if (rank == 0 && tid == 0) { cv.n_seen[unit] = n; cv.w0[unit] = first; }
 }
 
 // Keys and values of the tokens that stay: LPR lanes a row, a warp has four of its turns under way.
@@ -194,25 +227,49 @@ __global__ void __launch_bounds__(256) adopt_move_kernel(CacheView cv, PagedView
 
 }  // namespace
 
-cudaError_t launch_adopt(const CacheView& cv, treekv_dtype dt, const PagedView& pv, const float* scores, long long score_stride,
-                         const AdoptLens& lens, int max_n, int sms, cudaStream_t stream) {
-    const int units = cv.B * cv.Hkv;
-    int split = 1;
-    while (split < kMaxSplit && units * split * 2 <= 2 * sms && max_n / (split * 2) >= 2048) split *= 2;
+namespace {
+
+template <int SPLIT>
+cudaError_t launch_select(const CacheView& cv, const float* scores, long long stride, const AdoptLens& lens, int max_n, cudaStream_t stream) {
+    auto kern = adopt_select_kernel<SPLIT>;
+    static bool smem_set[64] = {};  // per device: the opt-in is needed once
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    if (!smem_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
+        if (e != cudaSuccess) return e;
+        smem_set[dev] = true;
+    }
+    const int share = ((max_n + 31) / 32 + SPLIT * kWarps - 1) / (SPLIT * kWarps) * 32 * kWarps, held = std::min(share, kHeld);
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(split, units);
+    cfg.gridDim = dim3(SPLIT, cv.B * cv.Hkv);
     cfg.blockDim = dim3(kThreads);
+    cfg.dynamicSmemBytes = (size_t)held * 4;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
     attr[0].id = cudaLaunchAttributeProgrammaticStreamSerialization;  // the kernel orders itself with griddepcontrol.wait
     attr[0].val.programmaticStreamSerializationAllowed = 1;
     attr[1].id = cudaLaunchAttributeClusterDimension;
-    attr[1].val.clusterDim.x = split;
+    attr[1].val.clusterDim.x = SPLIT;
     attr[1].val.clusterDim.y = 1;
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
-    cfg.numAttrs = split > 1 ? 2 : 1;
-    const cudaError_t e = cudaLaunchKernelEx(&cfg, adopt_select_kernel, cv, scores, score_stride, lens, split);
+    cfg.numAttrs = SPLIT > 1 ? 2 : 1;
+    return cudaLaunchKernelEx(&cfg, kern, cv, scores, stride, lens, held);
+}
+
+}  // namespace
+
+cudaError_t launch_adopt(const CacheView& cv, treekv_dtype dt, const PagedView& pv, const float* scores, long long score_stride,
+                         const AdoptLens& lens, int max_n, int sms, cudaStream_t stream) {
+    const int units = cv.B * cv.Hkv;
+    int split = 1;
+    while (split < kMaxSplit && units * split * 2 <= sms && max_n / split > 4096) split *= 2;
+    const cudaError_t e = split == 8   ? launch_select<8>(cv, scores, score_stride, lens, max_n, stream)
+                          : split == 4 ? launch_select<4>(cv, scores, score_stride, lens, max_n, stream)
+                          : split == 2 ? launch_select<2>(cv, scores, score_stride, lens, max_n, stream)
+                                       : launch_select<1>(cv, scores, score_stride, lens, max_n, stream);
     if (e != cudaSuccess) return e;
     const int bytes = cv.d * (dt == TREEKV_F32 ? 4 : 2), rows = 8 * 4 * (32 / (bytes / 16)), most = std::min(max_n, cv.c);
     const dim3 grid((most + rows - 1) / rows, units);

@@ -187,7 +187,8 @@ treekv_status treekv_pick_path(treekv_ctx* ctx, const void* dev_logits, treekv_d
         !aligned(dev_noise, 16) || !aligned(dev_path, 4) || !aligned(dev_count, 4) || !aligned(dev_next, 4))
         return TREEKV_ERR_INVALID_ARG;
     if (!(logits_type == TREEKV_F32 || logits_type == TREEKV_BF16)) return TREEKV_ERR_UNSUPPORTED;
-    if (stride < 1 || stride > kMaxDraft || vocab < 1 || vocab > (1 << 24)) return TREEKV_ERR_INVALID_ARG;
+    if (stride < 1 || stride > kMaxDraft || vocab < 1) return TREEKV_ERR_INVALID_ARG;
+    if (vocab > kMaxVocab) return TREEKV_ERR_UNSUPPORTED;
     if (!(temperature >= 0.f && temperature < 1e30f)) return TREEKV_ERR_INVALID_ARG;
     if (temperature > 0.f && (!dev_uniform || !dev_noise)) return TREEKV_ERR_INVALID_ARG;
     DraftLens lens;

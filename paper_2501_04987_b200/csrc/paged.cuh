@@ -77,6 +77,7 @@ cudaError_t launch_adopt(const CacheView& cv, treekv_dtype dt, const PagedView& 
                          const AdoptLens& lens, int max_n, int sms, cudaStream_t stream);
 
 // the accepted path of a draft (pick.cu)
+constexpr int kMaxVocab = 500000;  // (a cluster's registers hold a row)
 struct PickArgs {
     const void* logits;     // [B][stride][vocab]
     const int32_t* tokens;  // [B][stride]

@@ -8,10 +8,12 @@
 // argmax r / e: with e exponential that draws from r / R (the race of exponential clocks; Leviathan et al. 2023 and Miao et al.
 // 2023 for the acceptance).  T = 0: the children are compared with the largest logit.
 //
-// One row of logits is read per node of the path, no other one, and one row of e: memory, or for few sequences the latency of
-// one row after the other.  A cluster of blocks takes a sequence, every thread the same 16-byte pieces of a row in each of the
-// passes, so the second reading comes from the cache of its SM.  Sums and maxima are joined in shared memory, in one order.
-// All arithmetic is fp32.
+// One row of logits is read per node of the path, no other one, and one row of e, so little memory is moved: what counts is
+// the way from one row to the next.  A cluster of blocks takes a sequence; a thread loads its E numbers of a row at once and
+// keeps what is left of their probabilities in registers, so a row is read once and its exponentials are taken once, whatever
+// happens at its node.  The row of the first child is asked into L2 while its parent's is worked on, the children's own logits are
+// fetched beside the row.  Sums and maxima are joined by pushing a block's pair into every block of the cluster: one barrier, then
+// each warp joins the pairs it finds at home, in one order.  All arithmetic is fp32.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -22,7 +24,13 @@ namespace treekv {
 namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxSplit = 8;
+constexpr int kMaxSplit = 16;
+
+__device__ inline float ex2(float x) {
+    float y;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+    return y;
+}
 
 // A row's 16-byte pieces; rows start anywhere.  Piece x holds the elements [x VEC - off, ...) that exist.
 template <typename T>
@@ -35,15 +43,18 @@ struct Row {
         pieces = (n + off + VEC - 1) / VEC;
     }
     __device__ int first(int x) const { return x * VEC - off; }
-    // elements of piece x, `none` where there are none
-    __device__ void get(int x, float (&f)[VEC], float none) const {
+    // elements of piece x, minus infinity where there are none
+    __device__ void get(int x, float* f) const {
         const int at = first(x);
+        float y[VEC];
         if (at >= 0 && at + VEC <= n) {
-            Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(p + at)), f);
+            Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(p + at)), y);
         } else {
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) f[e] = at + e >= 0 && at + e < n ? Elem<T>::to_float(p[at + e]) : none;
+            for (int e = 0; e < VEC; ++e) y[e] = at + e >= 0 && at + e < n ? Elem<T>::to_float(p[at + e]) : -INFINITY;
         }
+#pragma unroll
+        for (int e = 0; e < VEC; ++e) f[e] = y[e];
     }
 };
 // N floats from element `at` of a row of n, as far as they exist
@@ -60,63 +71,73 @@ __device__ inline void get_floats(const float* row, int at, int n, float (&f)[N]
         for (int e = 0; e < N; ++e) f[e] = at + e >= 0 && at + e < n ? __ldg(row + at + e) : 0.f;
     }
 }
+__device__ inline void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
 
 struct Pair {
     float a, b;
 };
-
-// Joins one pair per thread over the cluster: `op` on warps by shuffles, on the warps' and the blocks' pairs in order.
-// Every thread gets the result.  `slot` alternates from call to call.
-template <typename Op>
-__device__ inline Pair join(Pair x, Pair (*s_warp)[kWarps], Pair* s_block, int& slot, int rank, int split, Op&& op) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+template <int LANES, typename Op>
+__device__ inline Pair join_lanes(Pair x, Op&& op) {
+    const int lane = threadIdx.x & 31;
 #pragma unroll
-    for (int o = 16; o > 0; o /= 2) {
+    for (int o = LANES / 2; o > 0; o /= 2) {
         Pair y;
         y.a = __shfl_xor_sync(0xffffffffu, x.a, o); y.b = __shfl_xor_sync(0xffffffffu, x.b, o);
-        x = lane & o ? op(y, x) : op(x, y);
+        x = lane & o ? op(y, x) : op(x, y);   // (every lane joins in the same order)
     }
-    if (lane == 0) s_warp[slot][warp] = x;
+    return x;
+}
+struct JoinSpace {
+    Pair warp[2][kWarps];
+    Pair block[2][kMaxSplit];
+};
+// Joins one pair per thread over the cluster; every thread gets the result.  `none` is what changes nothing.  `slot` alternates
+// from call to call: a slot is written again two calls on, which the barrier of the call between comes before.
+template <typename Op>
+__device__ inline Pair join(Pair x, Pair none, JoinSpace& js, int& slot, int rank, int split, Op&& op) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    x = join_lanes<32>(x, op);
+    if (lane == 0) js.warp[slot][warp] = x;
     __syncthreads();
-    x = s_warp[slot][0];
-    for (int w = 1; w < kWarps; ++w) x = op(x, s_warp[slot][w]);
-    if (split > 1) {
-        if (threadIdx.x == 0) s_block[slot] = x;
+    if (split == 1) {
+        x = join_lanes<kWarps>(js.warp[slot][lane & (kWarps - 1)], op);
+    } else {
+        if (warp == 0) {
+            x = join_lanes<kWarps>(js.warp[slot][lane & (kWarps - 1)], op);
+            if (lane < split)
+                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(&js.block[slot][rank]), lane)), "f"(x.a), "f"(x.b) : "memory");
+        }
         __syncwarp();
         cluster_sync_all();
-        Pair all;
-        for (int s = 0; s < split; ++s) {
-            const float2 y = ld_remote_v2(map_to_cta(smem_addr_u32(&s_block[slot]), s));
-            Pair p; p.a = y.x; p.b = y.y;
-            all = s == 0 ? p : op(all, p);
-        }
-        x = all;
-        // (the slot is written again two calls on, which this thread's next cluster barrier comes before)
+        x = join_lanes<kMaxSplit>((lane & (kMaxSplit - 1)) < split ? js.block[slot][lane & (kMaxSplit - 1)] : none, op);
     }
     slot ^= 1;
     return x;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(kThreads) pick_kernel(PickArgs a, DraftLens lens, DevStats* stats, int split) {
-    constexpr int VEC = Elem<T>::kVec;
+// E: numbers of a row that a thread holds
+template <typename T, int E>
+__global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArgs a, DraftLens lens, DevStats* stats, int split) {
+    constexpr int VEC = Elem<T>::kVec, U = E / VEC;
     pdl_trigger();
     pdl_wait();
     const int b = blockIdx.y, rank = blockIdx.x, n = lens.n[b], tid = threadIdx.x, lane = tid & 31;
-    const bool speaks = rank == 0 && tid == 0;
     __shared__ int s_parent[kMaxDraft];
     __shared__ int s_token[kMaxDraft];
     __shared__ float s_uniform[kMaxDraft];
-    __shared__ float s_inv[kMaxDraft];       // 1 / R before each rejection at this node
-    __shared__ int s_out[kMaxDraft];         // rejected tokens of this node (without draft probabilities)
-    __shared__ Pair s_warp[2][kWarps];
-    __shared__ __align__(8) Pair s_block[2];
+    __shared__ float s_logit[2][kMaxDraft], s_draft[2][kMaxDraft];  // of the children of a node (the parity of its depth)
+    __shared__ float s_over[kWarps][kMaxDraft];                     // 1 / R before each rejection at a node, each warp's own
+    __shared__ __align__(8) JoinSpace s_join;
     int32_t* path = a.path + (size_t)b * a.stride;
     if (n == 0) {  // the whole cluster
         if (rank == 0 && tid < a.stride) path[tid] = -1;
-        if (speaks) { a.count[b] = 0; a.next[b] = -1; }
+        if (rank == 0 && tid == 0) { a.count[b] = 0; a.next[b] = -1; }
         return;
     }
+    const bool greedy = a.temperature == 0.f;
+    const T* logits = reinterpret_cast<const T*>(a.logits) + (size_t)b * a.stride * a.vocab;
+    const float* noise = a.noise + (size_t)b * a.vocab;
+    const int first = rank * kThreads + tid, step = split * kThreads;
     if (tid < n) {
         const uint64_t below = (a.mask ? a.mask[(size_t)b * a.stride + tid] : low_bits(tid)) & low_bits(tid);
         s_parent[tid] = below ? 63 - __clzll((long long)below) : -1;
@@ -125,34 +146,56 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(PickArgs a, DraftLens le
         s_token[tid] = t;
         s_uniform[tid] = a.uniform ? a.uniform[(size_t)b * a.stride + tid] : 0.f;
     }
+    if (!greedy) // the one row of random numbers that is needed, a line of 128 bytes at a time
+        for (int x = first * 32; x < a.vocab; x += step * 32) ask_l2(noise + x);
     __syncthreads();
-    const bool greedy = a.temperature == 0.f;
+    if (split > 1) cluster_sync_all();  // every block is running before pairs are pushed to it
     const float sc = greedy ? 1.f : kLog2e / a.temperature;
-    const int first = rank * kThreads + tid, step = split * kThreads;
     int at = 0, depth = 0, slot = 0, next = -1;
     for (;;) {
         if (rank == 0 && tid == 0) path[depth] = at;
-        ++depth;
-        const Row<T> row(reinterpret_cast<const T*>(a.logits) + ((size_t)b * a.stride + at) * a.vocab, a.vocab);
+        const Row<T> row(logits + (size_t)at * a.vocab, a.vocab);
         const float* q = a.draft && !greedy ? a.draft + ((size_t)b * a.stride + at) * a.vocab : nullptr;
+        float r[E];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (first + u * step < row.pieces) row.get(first + u * step, r + u * VEC);
+            else
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) r[u * VEC + e] = -INFINITY;
+        }
         uint64_t kids = __ballot_sync(0xffffffffu, lane > at && lane < n && s_parent[lane] == at);
         kids |= (uint64_t)__ballot_sync(0xffffffffu, lane + 32 > at && lane + 32 < n && s_parent[min(lane + 32, kMaxDraft - 1)] == at) << 32;
+        // what the children need beside the row, and the first one's row on its way
+        if (!greedy && tid < n && (kids >> tid & 1) && s_token[tid] >= 0) {
+            s_logit[depth & 1][tid] = Elem<T>::to_float(row.p[s_token[tid]]);
+            s_draft[depth & 1][tid] = q ? __ldg(q + s_token[tid]) : 1.f;
+        }
+        if (kids) {
+            const Row<T> ahead(logits + (size_t)(__ffsll((long long)kids) - 1) * a.vocab, a.vocab);
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int x = first + u * step;
+                if (x < ahead.pieces && (lane & 7) == 0) ask_l2(ahead.p + max(0, ahead.first(x)));
+            }
+        }
+        ++depth;
         int child = -1;
+        auto larger = [](Pair x, Pair y) { return y.a > x.a || (y.a == x.a && __float_as_int(y.b) < __float_as_int(x.b)) ? y : x; };
+        const Pair nobody = {-INFINITY, __int_as_float(0x7fffffff)};
         if (greedy) {
-            Pair best; best.a = -INFINITY; best.b = __int_as_float(0x7fffffff);
+            Pair best = nobody;
             bool wrong = false;
-            for (int x = first; x < row.pieces; x += step) {
-                float f[VEC];
-                row.get(x, f, -INFINITY);
+#pragma unroll
+            for (int u = 0; u < U; ++u)
 #pragma unroll
                 for (int e = 0; e < VEC; ++e) {
-                    wrong |= f[e] != f[e];
-                    if (f[e] > best.a) { best.a = f[e]; best.b = __int_as_float(row.first(x) + e); }
+                    const float f = r[u * VEC + e];
+                    wrong |= f != f;
+                    if (f > best.a) { best.a = f; best.b = __int_as_float(row.first(first + u * step) + e); }
                 }
-            }
-            if (wrong) best.a = INFINITY, best.b = __int_as_float(-1);   // a row with a NaN picks nothing
-            best = join(best, s_warp, s_block, slot, rank, split, [](Pair x, Pair y) {
-                return y.a > x.a || (y.a == x.a && __float_as_int(y.b) < __float_as_int(x.b)) ? y : x; });
+            if (wrong) { best.a = INFINITY; best.b = __int_as_float(-1); }   // a row with a NaN picks nothing
+            best = join(best, nobody, s_join, slot, rank, split, larger);
             int token = __float_as_int(best.b);
             if (token == 0x7fffffff) token = -1;
             for (uint64_t left = kids; left; left &= left - 1) {
@@ -163,104 +206,129 @@ __global__ void __launch_bounds__(kThreads) pick_kernel(PickArgs a, DraftLens le
             at = child;
             continue;
         }
-        // ---- largest logit and sum of the row
-        Pair ms; ms.a = -INFINITY; ms.b = 0.f;
-        for (int x = first; x < row.pieces; x += step) {
-            float f[VEC];
-            row.get(x, f, -INFINITY);
-            float mx = f[0], sum = 0.f;
+        // ---- largest logit and sum of the row; r becomes the exponentials at the thread's own reference
+        Pair ms = {r[0], 0.f};
 #pragma unroll
-            for (int e = 1; e < VEC; ++e) mx = fmaxf(mx, f[e]);
-            if (mx > ms.a) { ms.b *= exp2f((ms.a - mx) * sc); ms.a = mx; }
-            const float ref = ms.a == -INFINITY ? 0.f : ms.a;
+        for (int e = 1; e < E; ++e) ms.a = fmaxf(ms.a, r[e]);
+        const float mine = ms.a == -INFINITY ? 0.f : ms.a;
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) sum += exp2f((f[e] - ref) * sc);
-            ms.b += sum;
+        for (int e = 0; e < E; ++e) {
+            r[e] = ex2((r[e] - mine) * sc);
+            ms.b += r[e];
         }
-        ms = join(ms, s_warp, s_block, slot, rank, split, [sc](Pair x, Pair y) {
+        const Pair nothing = {-INFINITY, 0.f};
+        ms = join(ms, nothing, s_join, slot, rank, split, [sc](Pair x, Pair y) {
             Pair z;
             z.a = fmaxf(x.a, y.a);
-            z.b = (x.a == -INFINITY ? x.b : x.b * exp2f((x.a - z.a) * sc)) + (y.a == -INFINITY ? y.b : y.b * exp2f((y.a - z.a) * sc));
+            const float ref = z.a == -INFINITY ? 0.f : z.a;
+            z.b = x.b * ex2((x.a - ref) * sc) + y.b * ex2((y.a - ref) * sc);
             return z; });
-        if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;   // NaN, an infinite logit, or nothing above minus infinity
-        const float top = ms.a, inv = 1.0f / ms.b;
-        auto prob = [&](float x) { return exp2f((x - top) * sc) * inv; };
-        // what is left of element v's probability after `times` rejections
-        auto left_of = [&](float r, float qv, int times) {
-            for (int k = 0; k < times; ++k) r = fmaxf(fmaf(r, s_inv[k], -qv), 0.f);
-            return r;
-        };
+        // NaN, an infinite logit, or nothing above minus infinity
+        if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;
+        const float top = ms.a, inv = 1.0f / ms.b, own = ex2((mine - top) * sc) * inv;
+#pragma unroll
+        for (int e = 0; e < E; ++e) r[e] = r[e] == 0.f ? 0.f : r[e] * own;  // (a thread without numbers has any reference)
         float R = 1.f;
         int rejected = 0;
+        bool lost = false;
         for (uint64_t left = kids; left; left &= left - 1) {
             const int c = __ffsll((long long)left) - 1, t = s_token[c];
-            if (t < 0) continue;             // (a token that cannot be is no child)
-            float r = prob(Elem<T>::to_float(row.p[t])), qt = 1.f;
-            if (q) { qt = __ldg(q + t); r = left_of(r, qt, rejected); }
-            else for (int k = 0; k < rejected; ++k) if (s_out[k] == t) r = 0.f;
-            if (s_uniform[c] * qt * R < r) { child = c; break; }
-            __syncthreads();                 // the lists are not read any more
-            if (tid == 0) { s_inv[rejected] = 1.0f / R; s_out[rejected] = t; }
-            __syncthreads();
-            ++rejected;
+            if (t < 0) continue;                 // (a token that cannot be is no child)
+            // what is left of the child's own probability: the thread that holds it would have to tell all others, so everyone
+            // goes through the rejections again
+            float rt = ex2((s_logit[(depth - 1) & 1][c] - top) * sc) * inv;
+            const float qt = s_draft[(depth - 1) & 1][c];
+            if (q) {
+                for (int k = 0; k < rejected; ++k) rt = fmaxf(fmaf(rt, s_over[tid >> 5][k], -qt), 0.f);
+            } else {
+                for (uint64_t seen = kids; seen != left; seen &= seen - 1)
+                    if (s_token[__ffsll((long long)seen) - 1] == t) rt = 0.f;
+            }
+            if (s_uniform[c] * qt * R < rt) { child = c; break; }
             if (!q) {
-                R = fmaxf(R - r, 0.f);
-            } else if (left & (left - 1)) {  // another child: how much is left
-                Pair sum; sum.a = 0.f; sum.b = 0.f;
-                for (int x = first; x < row.pieces; x += step) {
-                    float f[VEC], qv[VEC];
-                    row.get(x, f, -INFINITY);
-                    get_floats<VEC>(q, row.first(x), a.vocab, qv);
+                R = fmaxf(R - rt, 0.f);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e) sum.a += left_of(prob(f[e]), qv[e], rejected);
+                for (int u = 0; u < U; ++u) {
+                    const int v0 = row.first(first + u * step);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (v0 + e == t) r[u * VEC + e] = 0.f;
                 }
-                sum = join(sum, s_warp, s_block, slot, rank, split, [](Pair x, Pair y) { Pair z; z.a = x.a + y.a; z.b = 0.f; return z; });
-                R = sum.a;
-                if (!(R > 0.f)) break;       // nothing is left
+                ++rejected;
+            } else {
+                const float over = 1.0f / R;
+                Pair sum = {0.f, 0.f};
+#pragma unroll
+                for (int u = 0; u < U; ++u) {
+                    const int x = first + u * step;
+                    if (x < row.pieces) {
+                        float qv[VEC];
+                        get_floats<VEC>(q, row.first(x), a.vocab, qv);
+#pragma unroll
+                        for (int e = 0; e < VEC; ++e) {
+                            r[u * VEC + e] = fmaxf(fmaf(r[u * VEC + e], over, -qv[e]), 0.f);
+                            sum.a += r[u * VEC + e];
+                        }
+                    }
+                }
+                if (lane == 0) s_over[tid >> 5][rejected] = over;
+                __syncwarp();
+                ++rejected;
+                if (left & (left - 1)) {         // another child: how much is left
+                    const Pair zero = {0.f, 0.f};
+                    sum = join(sum, zero, s_join, slot, rank, split, [](Pair x, Pair y) { Pair z = {x.a + y.a, 0.f}; return z; });
+                    R = sum.a;
+                    if (!(R > 0.f)) { lost = true; break; }  // nothing is left
+                }
             }
         }
-        if (child >= 0) { at = child; __syncthreads(); continue; }
+        if (child >= 0) { at = child; continue; }
         // ---- the next token: the largest r / e
-        const float* noise = a.noise + (size_t)b * a.vocab;
-        auto race = [&](int times) {
-            Pair best; best.a = 0.f; best.b = __int_as_float(0x7fffffff);
-            for (int x = first; x < row.pieces; x += step) {
-                float f[VEC], qv[VEC], e4[VEC];
-                row.get(x, f, -INFINITY);
-                const int v0 = row.first(x);
-                get_floats<VEC>(noise, v0, a.vocab, e4);
-                if (q && times) get_floats<VEC>(q, v0, a.vocab, qv);
+        auto race = [&]() {
+            Pair best = {0.f, __int_as_float(0x7fffffff)};
+            const Pair none = best;
 #pragma unroll
-                for (int e = 0; e < VEC; ++e) {
-                    float r = prob(f[e]);
-                    if (times) {
-                        if (q) r = left_of(r, qv[e], times);
-                        else for (int k = 0; k < times; ++k) if (s_out[k] == v0 + e) r = 0.f;
-                    }
-                    if (r > 0.f) {
-                        const float z = __fdiv_rn(r, e4[e]);
-                        if (z > best.a) { best.a = z; best.b = __int_as_float(v0 + e); }
-                    }
+            for (int u = 0; u < U; ++u) {
+                const int x = first + u * step;
+                if (x < row.pieces) {
+                    float e4[VEC];
+                    const int v0 = row.first(x);
+                    get_floats<VEC>(noise, v0, a.vocab, e4);
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e)
+                        if (r[u * VEC + e] > 0.f) {
+                            const float z = __fdiv_rn(r[u * VEC + e], e4[e]);
+                            if (z > best.a) { best.a = z; best.b = __int_as_float(v0 + e); }
+                        }
                 }
             }
-            best = join(best, s_warp, s_block, slot, rank, split, [](Pair x, Pair y) {
-                return y.a > x.a || (y.a == x.a && __float_as_int(y.b) < __float_as_int(x.b)) ? y : x; });
-            return __float_as_int(best.b);
+            return __float_as_int(join(best, none, s_join, slot, rank, split, larger).b);
         };
-        next = race(rejected);
-        if (next == 0x7fffffff && rejected) next = race(0);   // rounding has left nothing: the target's own probabilities
+        next = lost ? 0x7fffffff : race();
+        if (next == 0x7fffffff && rejected) {    // rounding has left nothing: the target's own probabilities
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (first + u * step < row.pieces) row.get(first + u * step, r + u * VEC);
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) r[u * VEC + e] = first + u * step < row.pieces ? ex2((r[u * VEC + e] - top) * sc) * inv : 0.f;
+            }
+            next = race();
+        }
         if (next == 0x7fffffff) next = -1;
         break;
     }
     if (rank == 0 && tid >= depth && tid < a.stride) path[tid] = -1;
-    if (speaks) { a.count[b] = depth; a.next[b] = next; }
-    if (split > 1) { __syncwarp(); cluster_sync_all(); }  // nobody leaves while its pairs may be read
+    if (rank == 0 && tid == 0) { a.count[b] = depth; a.next[b] = next; }
+    if (split > 1) { __syncwarp(); cluster_sync_all(); }  // nobody leaves while pairs may be pushed to it
 }
 
-template <typename T>
-cudaError_t launch_t(const PickArgs& a, const DraftLens& lens, int B, DevStats* stats, int sms, cudaStream_t stream) {
-    int split = 1;
-    while (split < kMaxSplit && B * split * 2 <= 2 * sms && a.vocab / (split * 2) >= kThreads * Elem<T>::kVec) split *= 2;
+template <typename T, int E>
+cudaError_t launch_e(const PickArgs& a, const DraftLens& lens, int B, DevStats* stats, int split, cudaStream_t stream) {
+    auto kern = pick_kernel<T, E>;
+    if (split > 8) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+        if (e != cudaSuccess) return e;
+    }
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3(split, B);
     cfg.blockDim = dim3(kThreads);
@@ -274,7 +342,20 @@ cudaError_t launch_t(const PickArgs& a, const DraftLens& lens, int B, DevStats* 
     attr[1].val.clusterDim.z = 1;
     cfg.attrs = attr;
     cfg.numAttrs = split > 1 ? 2 : 1;
-    return cudaLaunchKernelEx(&cfg, pick_kernel<T>, a, lens, stats, split);
+    return cudaLaunchKernelEx(&cfg, kern, a, lens, stats, split);
+}
+
+// Blocks per sequence: as many as find a place at once, and no more than have 16 numbers a thread; at least what holds a row at 64.
+template <typename T>
+cudaError_t launch_t(const PickArgs& a, const DraftLens& lens, int B, DevStats* stats, int sms, cudaStream_t stream) {
+    const int need = a.vocab + Elem<T>::kVec - 1;  // (a row that starts inside a piece)
+    auto holds = [&](int split, int e) { return split * kThreads * e >= need; };
+    int split = 1;
+    while (split < 8 && B * split * 2 <= sms && !holds(split, 16)) split *= 2;
+    while (split < kMaxSplit && !holds(split, 64)) split *= 2;
+    if (holds(split, 16)) return launch_e<T, 16>(a, lens, B, stats, split, stream);
+    if (holds(split, 32)) return launch_e<T, 32>(a, lens, B, stats, split, stream);
+    return launch_e<T, 64>(a, lens, B, stats, split, stream);
 }
 
 }  // namespace

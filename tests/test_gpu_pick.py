@@ -90,7 +90,7 @@ def _masks(parents, T):
     return rows
 
 
-@pytest.mark.parametrize("B,T,V", [(1, 1, 1), (1, 8, 2), (5, 3, 50), (7, 64, 333), (3, 16, 4099), (40, 7, 1000), (2, 5, 40001), (1, 33, 128000), (300, 4, 70)])
+@pytest.mark.parametrize("B,T,V", [(1, 1, 1), (1, 8, 2), (5, 3, 50), (7, 64, 333), (3, 16, 4099), (40, 7, 1000), (2, 5, 40001), (1, 33, 128000), (300, 4, 70), (2, 3, 300001), (150, 2, 20001)])
 @pytest.mark.parametrize("kind", ["chain", "tree", "star"])
 @pytest.mark.parametrize("dtype", ["f32", "bf16"])
 @pytest.mark.parametrize("given,temperature", [(False, 1.0), (True, 1.0), (False, 0.6), (True, 1.7), (False, 0.0)])
