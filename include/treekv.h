@@ -371,11 +371,14 @@ int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64
  * Rows beyond a sequence's length are neither read nor written.  A page that receives tokens must belong to one sequence of
  * the call; pages that are only read can be shared.  The outputs must not overlap the inputs.  A token's value never enters
  * rows in front of it, also where it is not finite.
+ *   dev_scratch     treekv_paged_scratch_bytes(ctx, stride) bytes, 256-byte aligned, used until the call's work is done: calls that
+ *                   may overlap need one each (TREEKV_ERR_WORKSPACE; 0 bytes and NULL for fp32)
  */
+size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride);
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,
                                   void* dev_v_pages, int n_pages, int page_size, const int32_t* dev_table, int table_stride,
                                   const int32_t* dev_past, int max_past, void* dev_out, float* dev_lse, const int32_t* host_lens,
-                                  int stride, void* stream);
+                                  int stride, void* dev_scratch, size_t scratch_bytes, void* stream);
 
 /*
  * What rows of a chunk gave to the tokens of their sequence: scores[b][h][j] becomes (add = 0), or grows by (add != 0), the mean

@@ -29,7 +29,7 @@ EXPORTS = [
     "treekv_state_bytes", "treekv_export_state", "treekv_import_state", "treekv_selftest_wait_giveup",
     "treekv_set_protection", "treekv_prefill_oneshot", "treekv_set_positions",
     "treekv_norm_rope", "treekv_verify_tree", "treekv_accept_path", "treekv_fork_sequences", "treekv_selftest_fork_plan",
-    "treekv_paged_attend", "treekv_paged_score", "treekv_adopt_pages", "treekv_pick_path",
+    "treekv_paged_scratch_bytes", "treekv_paged_attend", "treekv_paged_score", "treekv_adopt_pages", "treekv_pick_path",
 ]
 
 
@@ -116,7 +116,9 @@ def _load():
     lib.treekv_selftest_fork_plan.restype = i32
     lib.treekv_selftest_fork_plan.argtypes = [C.POINTER(C.c_int32), i32, C.POINTER(C.c_int64), C.POINTER(C.c_int32)]
     lib.treekv_paged_attend.restype = i32
-    lib.treekv_paged_attend.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp]
+    lib.treekv_paged_attend.argtypes = [vp, vp, vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, i32, vp, C.c_size_t, vp]
+    lib.treekv_paged_scratch_bytes.restype = C.c_size_t
+    lib.treekv_paged_scratch_bytes.argtypes = [vp, i32]
     lib.treekv_paged_score.restype = i32
     lib.treekv_paged_score.argtypes = [vp, vp, vp, vp, i32, i32, vp, i32, vp, i32, vp, C.c_int64, i32, vp, i32, vp]
     lib.treekv_adopt_pages.restype = i32
@@ -258,10 +260,14 @@ def treekv_fork_sequences(ctx, source, stream=0) -> int:
     return lib.treekv_fork_sequences(ctx, _i32(source), stream)
 
 
+def treekv_paged_scratch_bytes(ctx, stride) -> int:
+    return lib.treekv_paged_scratch_bytes(ctx, stride)
+
+
 def treekv_paged_attend(ctx, q, k, v, k_pages, v_pages, n_pages, page_size, table, table_stride, past, max_past, out, lse, lens, stride,
-                        stream=0) -> int:
+                        scratch, scratch_bytes, stream=0) -> int:
     return lib.treekv_paged_attend(ctx, q, k, v, k_pages, v_pages, n_pages, page_size, table, table_stride, past, max_past, out, lse,
-                                   _i32(lens), stride, stream)
+                                   _i32(lens), stride, scratch, scratch_bytes, stream)
 
 
 def treekv_paged_score(ctx, q, lse, k_pages, n_pages, page_size, table, table_stride, past, max_past, scores, score_stride, add, lens,
@@ -538,8 +544,10 @@ class TreeKV:
         else:
             pl = want(lse, self.torch.float32, (B, n, Hq), "lse")
         pn, kept = self._lens(lens, "chunk lengths")
+        nbytes = lib.treekv_paged_scratch_bytes(self._h, n)
+        scratch = q.new_empty(nbytes, dtype=self.torch.uint8) if nbytes else None   # (torch keeps it for this stream's later work)
         st = lib.treekv_paged_attend(self._h, pq, pk, pv, kp, vp, pages, page, pt, width, pp, width * page if max_past is None else max_past,
-                                     po, pl, pn, n, self._stream())
+                                     po, pl, pn, n, None if scratch is None else scratch.data_ptr(), nbytes, self._stream())
         if st:
             _check(st, "treekv_paged_attend")
         return out, lse

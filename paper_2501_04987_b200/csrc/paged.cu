@@ -83,10 +83,16 @@ treekv_status chunk_lens(const treekv_ctx* ctx, const int32_t* host_lens, int st
 
 extern "C" {
 
+size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride) {
+    if (!ctx || stride < 1 || stride > kMaxChunkRows || ctx->dt != TREEKV_BF16) return 0;
+    const int rows = stride * ctx->G;  // (a call of a longer chunk may still have few tokens in every sequence)
+    return paged_few_scratch(paged_few_takes(rows) ? rows : 64, ctx->cv.d, ctx->sm_count);
+}
+
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,
                                   void* dev_v_pages, int n_pages, int page_size, const int32_t* dev_table, int table_stride,
                                   const int32_t* dev_past, int max_past, void* dev_out, float* dev_lse, const int32_t* host_lens,
-                                  int stride, void* stream) {
+                                  int stride, void* dev_scratch, size_t scratch_bytes, void* stream) {
     if (!ctx || !dev_q || !dev_k || !dev_v || !dev_past || !dev_out) return TREEKV_ERR_INVALID_ARG;
     if (!aligned(dev_q, 16) || !aligned(dev_k, 16) || !aligned(dev_v, 16) || !aligned(dev_out, 16) || !aligned(dev_lse, 4) || !aligned(dev_past, 4))
         return TREEKV_ERR_INVALID_ARG;
@@ -98,17 +104,26 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
     ChunkLens lens;
     int max_n;
     st = chunk_lens(ctx, host_lens, stride, &lens, &max_n);
-    if (st != TREEKV_OK || max_n == 0) return st;
+    if (st != TREEKV_OK) return st;
+    if (scratch_bytes < treekv_paged_scratch_bytes(ctx, stride) || (ctx->dt == TREEKV_BF16 && (!dev_scratch || !aligned(dev_scratch, 256))))
+        return TREEKV_ERR_WORKSPACE;
+    if (max_n == 0) return TREEKV_OK;
     if (!on_own_device(ctx)) return TREEKV_ERR_BAD_STATE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);
     const ChunkView ch = {dev_q, dev_k, dev_v, stride};
     const PagedOut o = {dev_out, dev_lse};
-    cudaError_t e = launch_paged_append(ctx->cv, ctx->dt, pv, ch, lens, max_n, s);
-    if (e == cudaSuccess)
-        e = ctx->dt == TREEKV_BF16 ? launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s)
-                                   : launch_paged_f32(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s);
+    cudaError_t e;
+    int launches = 2;
+    if (ctx->dt == TREEKV_BF16 && paged_few_takes(max_n * ctx->G)) {
+        e = launch_paged_few(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
+    } else {
+        e = launch_paged_append(ctx->cv, ctx->dt, pv, ch, lens, max_n, s);
+        if (e == cudaSuccess)
+            e = ctx->dt == TREEKV_BF16 ? launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s)
+                                       : launch_paged_f32(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s);
+    }
     if (e != cudaSuccess) return cuda_fail(ctx, e);
-    ctx->launches += 2;
+    ctx->launches += launches;
     return TREEKV_OK;
 }
 

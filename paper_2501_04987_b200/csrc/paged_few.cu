@@ -1,0 +1,600 @@
+// Attention of few new tokens over a paged cache on the 5th-generation tensor cores (bf16): up to 64 query rows a KV head, a decode
+// step or a short draft of every sequence.
+//
+// Such a call is bound by the pages it reads, so it is built around a ring of key and value tiles that never runs dry: one
+// block per SM, 160 KB of tiles in flight, and the tiles of all units (sequence, KV head) in a row, of which every block takes the
+// same number, wherever the units end.  A block that has a unit to itself writes its rows; otherwise it leaves its part - maximum,
+// sum, unnormalised output - in the caller's scratch, and a second small launch joins the parts in order.
+//
+// With few rows the logits are taken transposed, so that the tensor core's 128 matrix rows are 128 keys:
+//     S^T = K Q^T   thread = key;  p = exp2(S^T c - m_row), the reference m_row common to the block
+//     O^T += V^T P^T   thread = channel
+// m_row moves - and O is rescaled - only when a logit outgrows it by 2^8: one vote of the 128 threads per tile.  A row's sum is
+// kept per key thread and added up at the end.
+//
+// Rounded to fewer bits than 32: the weights P as an operand, to bf16, since both operands of an MMA have one type and V's is
+// bf16 - each by at most half a step, 2^-8 of itself; the sum that divides them is of the unrounded ones.
+//
+// The new tokens' keys and values enter their pages here too: by the block that will read the tile they lie in, before its TMA
+// load is issued.
+//
+// Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
+#include <algorithm>
+
+#include "paged.cuh"
+#include "verify_tc.cuh"
+
+namespace treekv {
+
+namespace {
+
+using namespace vtc;
+
+constexpr int kThreads = 192;
+constexpr int kTile = 128;                 // keys of a tile
+constexpr int kRows = 64;                  // query rows as the tensor core sees them
+constexpr int kMaxSlots = 8;
+constexpr uint32_t kTmemCols = 256;        // S^T 64 + 64, O^T 64
+constexpr size_t kSmemMax = 224 * 1024;
+constexpr int kPBytes = kTile * 128;       // P^T: a key's 64 rows
+
+enum Bar { Q_FULL = 0, Q_FREE = 2, S_FULL = 4, S_FREE = 6, P_FULL = 8, O_FULL = 10, O_FREE = 11, APPENDED = 12, FULL = 13, USED = FULL + kMaxSlots,
+           N_BARS = USED + kMaxSlots };
+
+__device__ inline void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0,%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15}, [%16];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]),
+          "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+        : "r"(taddr) : "memory");
+}
+__device__ inline void tmem_ld16_wait(uint32_t (&r)[16]) {
+    asm volatile("tcgen05.wait::ld.sync.aligned;"
+                 : "+r"(r[0]), "+r"(r[1]), "+r"(r[2]), "+r"(r[3]), "+r"(r[4]), "+r"(r[5]), "+r"(r[6]), "+r"(r[7]),
+                   "+r"(r[8]), "+r"(r[9]), "+r"(r[10]), "+r"(r[11]), "+r"(r[12]), "+r"(r[13]), "+r"(r[14]), "+r"(r[15]) :: "memory");
+}
+__device__ inline void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+    asm volatile(
+        "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], {%1,%2,%3,%4,%5,%6,%7,%8,%9,%10,%11,%12,%13,%14,%15,%16};"
+        ::"r"(taddr), "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+          "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]) : "memory");
+}
+
+// What blocks leave for the second launch: parts in slots 2 x block (the part continues a unit) and 2 x block + 1 (it starts one).
+struct Parts {
+    int* plan;        // [kMaxBatch + 1] first tile of each sequence, then the tiles of a block
+    uint32_t* bad;    // [slots][2] new tokens with a value that is not finite
+    float2* stat;     // [slots][rows] reference, sum
+    float* o;         // [slots][rows][D]
+};
+constexpr size_t kPlanBytes = (kMaxBatch + 2) * 4 + 248;  // (a multiple of 256)
+static_assert(kPlanBytes % 256 == 0, "parts start aligned");
+inline size_t part_bytes(int rows, int D) { return 16 + (size_t)rows * 8 + (size_t)rows * D * 4; }
+
+// The pieces of units that a block works on, in order, the same for every role.
+struct Walk {
+    const int* first;   // [B + 1] first item of each sequence: a tile, or with `whole` a unit
+    const int* pasts;   // [B]
+    const ChunkLens* lens;
+    int B, Hkv, G, item, end;
+    bool whole;
+    int b, kh, past, n, rows, nvis, tiles, t0, t1;  // of the piece: tiles [t0, t1) of the unit's
+    __device__ bool get() {
+        if (item >= end) return false;
+        int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item
+        while (lo < hi) {
+            const int mid = (lo + hi + 1) >> 1;
+            if (first[mid] <= item) lo = mid; else hi = mid - 1;
+        }
+        b = lo;
+        n = lens->m[b]; past = pasts[b];
+        rows = n * G; nvis = past + n;
+        tiles = (nvis + kTile - 1) / kTile;
+        const int at = item - first[b];
+        if (whole) { kh = at; t0 = 0; t1 = tiles; }
+        else { kh = at / tiles; t0 = at - kh * tiles; t1 = min(tiles, t0 + end - item); }
+        return true;
+    }
+    __device__ void next() { item += whole ? 1 : t1 - t0; }
+};
+
+// Values that are not finite, of new tokens that not all rows see, were taken out of the tiles: those that a row sees (its
+// token and those in front of it) go into its sum.
+__device__ inline float bad_values(const __nv_bfloat16* v, uint32_t bad0, uint32_t bad1, int token, int vstep) {
+    float sum = 0.f;
+    for (uint64_t left = ((uint64_t)bad1 << 32 | bad0) & (2ull << token) - 1ull; left; left &= left - 1) {
+        const float y = __bfloat162float(v[(size_t)(__ffsll((long long)left) - 1) * vstep]);
+        if (!(fabsf(y) < INFINITY)) sum += y;
+    }
+    return sum;
+}
+
+// NG: groups of 16 query rows that can hold a row
+template <int D, int NG>
+__global__ void __launch_bounds__(kThreads, 1)
+paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
+                 PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int B, int Hq, int Hkv, DevStats* stats, int q_bytes,
+                 int slots, int whole) {
+    constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128, R = 16 * NG, QB = R * D * 2;
+    pdl_trigger();
+    extern __shared__ unsigned char smem_raw[];
+    __shared__ __align__(8) uint64_t bars[N_BARS];
+    __shared__ uint32_t tmem_slot;
+    __shared__ int s_first[kMaxBatch + 1];
+    __shared__ int s_past[kMaxBatch];
+    __shared__ __align__(16) float s_ref[R], s_fix[R], s_max[4][R];
+    __shared__ uint32_t s_bad[2];
+    const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
+    unsigned char* base_ptr = smem_raw + (base - smem_addr_u32(smem_raw));
+    const uint32_t sQ = base, sP = base + 2 * QB, sRing = sP + 2 * kPBytes;   // two of each
+    const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+    const uint32_t bar0 = smem_addr_u32(&bars[0]);
+    auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
+    if (tid == 0) {
+        for (int s = 0; s < 2; ++s) {
+            mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1);
+            mbar_init(bar(S_FULL + s), 1); mbar_init(bar(S_FREE + s), 4); mbar_init(bar(P_FULL + s), 4);
+        }
+        mbar_init(bar(O_FULL), 1); mbar_init(bar(O_FREE), 4); mbar_init(bar(APPENDED), 4);
+        for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(USED + s), 1); }
+        mbar_fence_init();
+        s_bad[0] = s_bad[1] = 0u;
+    }
+    if (warp == 1) { tmem_alloc(smem_addr_u32(&tmem_slot), kTmemCols); tmem_relinquish(); }
+    pdl_wait();
+    if (warp == 0) {   // items of each sequence, in order
+        int sum = 0;
+        for (int b0 = 0; b0 < B; b0 += 32) {
+            const int b = b0 + lane, n = b < B ? lens.m[b] : 0;
+            int items = 0, past = -1;
+            if (n > 0) {
+                past = paged_past(pv, b, n);
+                if (past < 0) { if (blockIdx.x == 0) atomicOr(&stats->error, kErrBadIndex); }
+                else items = whole ? Hkv : (past + n + kTile - 1) / kTile * Hkv;
+            }
+            int inc = items;
+#pragma unroll
+            for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
+            if (b < B) { s_first[b] = sum + inc - items; s_past[b] = past; }
+            sum += __shfl_sync(0xffffffffu, inc, 31);
+        }
+        if (lane == 0) s_first[B] = sum;
+    }
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = tmem_slot, tmO = tmem + 2 * kRows;
+    const int total = s_first[B], per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
+    Walk w;
+    w.first = s_first; w.pasts = s_past; w.lens = &lens; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.whole = whole;
+    w.item = min((int)blockIdx.x * per, total); w.end = min(w.item + per, total);
+    if (!whole && blockIdx.x == 0) {
+        for (int b = tid; b <= B; b += kThreads) parts.plan[b] = s_first[b];
+        if (tid == 0) parts.plan[kMaxBatch + 1] = per;
+    }
+
+    bool ok = true;
+    if (warp == 0) {
+        // ================= TMA producer: K and V of a tile in turn
+        const int box = min(pv.page, kTile);
+        int issued = 0, piece = 0;
+        bool appended = false;
+        Ring r(0, slots);
+        for (; ok && w.get(); w.next(), ++piece) {
+            const int qs = piece & 1;
+            if (lane == 0) {
+                ok = mbar_wait(bar(Q_FREE + qs), ((piece >> 1) & 1) ^ 1);
+                if (ok) {
+                    mbar_arrive_expect_tx(bar(Q_FULL + qs), q_bytes);
+#pragma unroll
+                    for (int h = 0; h < HALVES; ++h) tma_load_3d(sQ + qs * QB + h * R * 128, &tmQ, 64 * h, w.kh * w.G, w.b * ch.stride, bar(Q_FULL + qs));
+                }
+            }
+            ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+            if (!ok) break;
+            // a lane's box of a tile: its page, asked for a tile ahead
+            auto entry_of = [&](int t) {
+                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) / box;
+                return lane < boxes ? __ldg(pv.table + (size_t)w.b * pv.width + (k0 >> pv.plog) + lane) : 0;
+            };
+            int e = entry_of(w.t0);
+            for (int t = w.t0; t < w.t1 && ok; ++t) {
+                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) / box;
+                const int row = (checked_page(pv, e, stats) * Hkv + w.kh) * pv.page + (lane == 0 ? k0 & (pv.page - 1) : 0);
+                if (t + 1 < w.t1) e = entry_of(t + 1);
+                if (!appended && k0 + kTile > w.past) {  // new tokens in it
+                    if (lane == 0) ok = mbar_wait(bar(APPENDED), 0);
+                    appended = true;
+                }
+#pragma unroll
+                for (int kv = 0; kv < 2; ++kv) {
+                    if (lane == 0 && ok) {
+                        ok = mbar_wait(bar(USED + r.slot), r.phase ^ 1);
+                        if (ok) mbar_arrive_expect_tx(bar(FULL + r.slot), boxes * box * D * 2);
+                    }
+                    ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
+                    if (!ok) break;
+                    if (lane < boxes)
+#pragma unroll
+                        for (int h = 0; h < HALVES; ++h)
+                            tma_load_2d(sRing + r.slot * SLOT + h * HALF + lane * box * 128, kv ? &tmV : &tmK, 64 * h, row, bar(FULL + r.slot));
+                    __syncwarp();
+                    r.next();
+                    ++issued;
+                }
+            }
+        }
+        // nothing may still be on its way into this block's memory when it ends, whatever gave up
+        if (lane == 0) {
+            for (int x = max(0, issued - slots); x < issued; ++x) ok = mbar_wait(bar(FULL + x % slots), (x / slots) & 1) && ok;
+            for (int x = max(0, piece - 2); x < piece; ++x) ok = mbar_wait(bar(Q_FULL + (x & 1)), (x >> 1) & 1) && ok;
+            if (!ok) atomicOr(&stats->error, 4u);
+        }
+    } else if (warp == 1) {
+        // ================= MMA issuer: S^T of a tile, then O^T of the one before
+        if (lane == 0) {
+            constexpr uint32_t idesc_s = umma_idesc_bf16(128, R, 0, 0);      // both operands K-major (rows x channels)
+            constexpr uint32_t idesc_o = umma_idesc_bf16(128, kRows, 1, 1);  // V^T and P^T: MN-major.  (Columns beyond R are
+                                                                              // whatever lies there, and make columns that nobody reads)
+            // (D = 64: the matrix rows 64 to 127 are what lies behind the tile, and make lanes that nobody reads)
+            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, HALF), p_lo = desc_lo(sP, kPBytes);
+            Ring rk(0, slots), rv(1, slots);
+            int g = 0, piece = 0;         // tiles of the block so far
+            bool behind = false, behind_first = false, behind_last = false;   // a tile whose O^T is to be issued: first, last of its piece
+            int behind_piece = 0, last_slot = 0, last_phase = 0;
+            auto issue_o = [&]() {
+                const int j = g - 1;      // (g: tiles whose S^T is issued)
+                if (behind_first && !(ok = mbar_wait(bar(O_FREE), (behind_piece & 1) ^ 1))) return;
+                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + (j & 1)), (j >> 1) & 1))) return;
+                tc_fence_after();
+                const uint32_t v = v_lo + rv.slot * (SLOT / 16), p = p_lo + (j & 1) * (kPBytes / 16);
+#pragma unroll
+                for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes
+                    umma_bf16(tmO, desc_of(v + kk * (2048 / 16)), desc_of(p + kk * (2048 / 16)), idesc_o, (!behind_first || kk > 0) ? 1u : 0u);
+                umma_commit(bar(USED + rv.slot));
+                if (behind_last) umma_commit(bar(O_FULL));
+                last_slot = rv.slot; last_phase = rv.phase;
+                rv.next(); rv.next();
+            };
+            for (; ok && w.get(); w.next(), ++piece) {
+                const int qs = piece & 1;
+                if (!(ok = mbar_wait(bar(Q_FULL + qs), (piece >> 1) & 1))) break;
+                for (int t = w.t0; t < w.t1; ++t) {
+                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_FREE + (g & 1)), ((g >> 1) & 1) ^ 1))) break;
+                    tc_fence_after();
+                    const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (QB / 16);
+#pragma unroll
+                    for (int kk = 0; kk < D / 16; ++kk)
+                        umma_bf16(tmem + (g & 1) * kRows, desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2),
+                                  desc_of(q + (kk >> 2) * (R * 128 / 16) + (kk & 3) * 2), idesc_s, kk > 0);
+                    umma_commit(bar(S_FULL + (g & 1)));
+                    umma_commit(bar(USED + rk.slot));
+                    if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
+                    rk.next(); rk.next();
+                    if (behind) { issue_o(); if (!ok) break; }
+                    behind = true; behind_first = t == w.t0; behind_last = t + 1 == w.t1; behind_piece = piece;
+                    ++g;
+                }
+            }
+            if (ok && behind) issue_o();
+            // every MMA has finished before its memory and tensor memory are given to anything else
+            if (ok && behind) ok = mbar_wait(bar(USED + last_slot), last_phase);
+            if (ok && behind) ok = mbar_wait(bar(O_FULL), (piece - 1) & 1);
+            if (!ok) atomicOr(&stats->error, 8u);
+        }
+    } else {
+        // ================= softmax warps
+        const int quarter = warp & 3, key = quarter * 32 + lane, st_tid = tid - 64, hk = st_tid;
+        const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
+        const float sc2 = kLog2e * rsqrtf((float)D);
+        {   // new tokens into their pages, before the tiles that hold them are asked for
+            Walk a = w;
+            for (; a.get(); a.next()) {
+                const int lo = max(0, a.t0 * kTile - a.past), hi = min(a.n, a.t1 * kTile - a.past);
+                for (int e = st_tid; e < (hi - lo) * (D / 8); e += 128) {
+                    const int tok = lo + e / (D / 8), c = e % (D / 8), at = a.past + tok;
+                    const int page = __ldg(pv.table + (size_t)a.b * pv.width + (at >> pv.plog));
+                    if ((unsigned)page >= (unsigned)pv.n_pages) { atomicOr(&stats->error, kErrBadIndex); continue; }  // nothing is written
+                    const size_t src = (((size_t)a.b * ch.stride + tok) * Hkv + a.kh) * (D / 8) + c;
+                    const size_t dst = (((size_t)page * Hkv + a.kh) * pv.page + (at & (pv.page - 1))) * (D / 8) + c;
+                    reinterpret_cast<uint4*>(pv.kp)[dst] = reinterpret_cast<const uint4*>(ch.k)[src];
+                    reinterpret_cast<uint4*>(pv.vp)[dst] = reinterpret_cast<const uint4*>(ch.v)[src];
+                }
+            }
+            __threadfence();
+            fence_proxy_async_global();
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(APPENDED));
+        }
+        Ring rv(1, slots);
+        int g = 0, piece = 0, done = 0, done_phase = 0;   // done: V of the tile before
+        for (; ok && w.get(); w.next(), ++piece) {
+            float l[R];
+#pragma unroll
+            for (int x = 0; x < R; ++x) l[x] = 0.f;
+            if (hk < R) s_ref[hk] = -INFINITY;
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            const bool edges = w.rows < R;
+            for (int t = w.t0; t < w.t1; ++t, ++g) {
+                const int k0 = t * kTile, kpos = k0 + key;
+                const bool partly = k0 + kTile > w.past + 1;   // some row does not see some key of this tile
+                if (!mbar_wait(bar(S_FULL + (g & 1)), (g >> 1) & 1)) { ok = false; break; }
+                tc_fence_after();
+                uint32_t s[NG][16];
+#pragma unroll
+                for (int x = 0; x < NG; ++x) tmem_ld16(tmem + (g & 1) * kRows + x * 16 + lane_off, s[x]);
+#pragma unroll
+                for (int x = 0; x < NG; ++x) tmem_ld16_wait(s[x]);
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(S_FREE + (g & 1)));
+                if (partly || edges) {   // rows [rmin, rows) see this key
+                    const int rmin = max(0, kpos - w.past) * w.G;
+                    const uint64_t see = rmin >= 64 ? 0ull : low_bits(w.rows) & ~low_bits(rmin);
+#pragma unroll
+                    for (int x = 0; x < R; ++x)
+                        if (!(see >> x & 1ull)) s[x / 16][x % 16] = 0xff800000u;
+                }
+                bool grow = false;
+#pragma unroll
+                for (int x = 0; x < R; x += 4) {
+                    const float4 m4 = *reinterpret_cast<const float4*>(s_ref + x);
+                    const uint32_t* v = &s[x / 16][x % 16];
+                    grow |= __uint_as_float(v[0]) * sc2 > m4.x + kSlack; grow |= __uint_as_float(v[1]) * sc2 > m4.y + kSlack;
+                    grow |= __uint_as_float(v[2]) * sc2 > m4.z + kSlack; grow |= __uint_as_float(v[3]) * sc2 > m4.w + kSlack;
+                }
+                uint32_t vote;
+                asm volatile("{\n\t.reg .pred p, q;\n\tsetp.ne.u32 p, %1, 0;\n\tbar.red.or.pred q, 2, 128, p;\n\tselp.u32 %0, 1, 0, q;\n\t}"
+                             : "=r"(vote) : "r"((uint32_t)grow) : "memory");
+                if (vote) {
+#pragma unroll
+                    for (int x = 0; x < R; ++x) {
+                        const uint32_t u = s[x / 16][x % 16];
+                        const uint32_t mx = __reduce_max_sync(0xffffffffu, u & 0x80000000u ? ~u : u | 0x80000000u);
+                        if (lane == 0) s_max[quarter][x] = __uint_as_float(mx & 0x80000000u ? mx & 0x7fffffffu : ~mx);
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+                    if (hk < R) {
+                        const float mx = fmaxf(fmaxf(s_max[0][hk], s_max[1][hk]), fmaxf(s_max[2][hk], s_max[3][hk])) * sc2, ref = s_ref[hk];
+                        const bool up = mx > ref + kSlack;
+                        s_fix[hk] = up ? ex2(ref - mx) : 1.f;
+                        if (up) s_ref[hk] = mx;
+                    }
+                    asm volatile("bar.sync 1, 128;" ::: "memory");
+#pragma unroll
+                    for (int x = 0; x < R; ++x) l[x] *= s_fix[x];
+                    if (t > w.t0) {
+                        if (!mbar_wait(bar(USED + done), done_phase)) { ok = false; break; }
+                        tc_fence_after();
+#pragma unroll
+                        for (int x = 0; x < NG; ++x) {
+                            uint32_t o[16];
+                            tmem_ld16(tmO + x * 16 + lane_off, o);
+                            tmem_ld16_wait(o);
+#pragma unroll
+                            for (int e = 0; e < 16; ++e) o[e] = __float_as_uint(__uint_as_float(o[e]) * s_fix[x * 16 + e]);
+                            tmem_st16(tmO + x * 16 + lane_off, o);
+                        }
+                        tmem_st_wait();
+                    }
+                }
+                unsigned char* prow = base_ptr + 2 * QB + (g & 1) * kPBytes + key * 128;
+                // (the P^T of two tiles ago has been multiplied: those MMAs were committed with this tile's logits)
+#pragma unroll
+                for (int x = 0; x < R; x += 8) {
+                    float p[8];
+#pragma unroll
+                    for (int e = 0; e < 8; e += 4) {
+                        const float4 m4 = *reinterpret_cast<const float4*>(s_ref + x + e);
+                        const float mr[4] = {m4.x, m4.y, m4.z, m4.w};
+#pragma unroll
+                        for (int u = 0; u < 4; ++u)
+                            p[e + u] = ex2(fmaf(__uint_as_float(s[(x + e + u) / 16][(x + e + u) % 16]), sc2, mr[u] == -INFINITY ? 0.f : -mr[u]));
+                    }
+#pragma unroll
+                    for (int e = 0; e < 8; ++e) l[x + e] += p[e];
+                    *reinterpret_cast<uint4*>(prow + (((x >> 3) ^ (key & 7)) << 4)) =
+                        make_uint4(rope_pack_bf16(p[0], p[1]), rope_pack_bf16(p[2], p[3]), rope_pack_bf16(p[4], p[5]), rope_pack_bf16(p[6], p[7]));
+                }
+                if (partly) {
+                    // Tokens that not all rows see: a value that is not finite is taken out of the tile and its token noted.  Rows behind the
+                    // last token hold none and become zeros.
+                    if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
+                    unsigned char* tile = base_ptr + 2 * QB + 2 * kPBytes + rv.slot * SLOT;
+                    const int valid = min(kTile, w.nvis - k0);
+                    for (int e = st_tid + max(0, w.past + 1 - k0) * (D / 8); e < kTile * (D / 8); e += 128) {
+                        const int rr = e / (D / 8), c = e % (D / 8);
+                        uint4* at = reinterpret_cast<uint4*>(tile + (c >> 3) * HALF + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
+                        uint4 y = make_uint4(0, 0, 0, 0);
+                        bool changed = rr >= valid;
+                        if (rr < valid) {
+                            y = *at;
+                            uint32_t* v = &y.x;
+#pragma unroll
+                            for (int u = 0; u < 4; ++u) {
+                                const uint32_t lo = (v[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (v[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
+                                if (lo | hi) { v[u] &= ~(lo | hi); changed = true; }
+                            }
+                            if (changed) atomicOr(&s_bad[(k0 + rr - w.past) >> 5], 1u << ((k0 + rr - w.past) & 31));
+                        }
+                        if (changed) *at = y;
+                    }
+                }
+                fence_proxy_async_smem();
+                tc_fence_before();
+                __syncwarp();
+                if (lane == 0) mbar_arrive(bar(P_FULL + (g & 1)));
+                done = rv.slot; done_phase = rv.phase;
+                rv.next(); rv.next();
+            }
+            if (!ok) break;
+            // ---- the piece's rows: sums over the keys, O^T from tensor memory (thread = channel)
+#pragma unroll
+            for (int x = 0; x < R; ++x) {
+#pragma unroll
+                for (int o = 16; o > 0; o /= 2) l[x] += __shfl_xor_sync(0xffffffffu, l[x], o);
+                if (lane == 0) s_max[quarter][x] = l[x];
+            }
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (hk < R) s_fix[hk] = (s_max[0][hk] + s_max[1][hk]) + (s_max[2][hk] + s_max[3][hk]);
+            asm volatile("bar.sync 1, 128;" ::: "memory");
+            if (!mbar_wait(bar(O_FULL), piece & 1)) { ok = false; break; }
+            tc_fence_after();
+            const bool direct = w.t0 == 0 && w.t1 == w.tiles;
+            const uint32_t bad0 = s_bad[0], bad1 = s_bad[1];
+            const int slot = 2 * blockIdx.x + (w.t0 == 0 ? 1 : 0);
+            const size_t out0 = (size_t)w.b * ch.stride * Hq + w.kh * w.G;
+#pragma unroll
+            for (int x = 0; x < NG; ++x) {
+                if (x * 16 >= w.rows) break;
+                uint32_t o[16];
+                tmem_ld16(tmO + x * 16 + lane_off, o);
+                tmem_ld16_wait(o);
+                if (key < D)
+#pragma unroll
+                    for (int e = 0; e < 16; ++e) {
+                        const int r = x * 16 + e;
+                        if (r < w.rows) {
+                            if (direct) {
+                                float y = __uint_as_float(o[e]) * (1.0f / s_fix[r]);
+                                if (bad0 | bad1)
+                                    y += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)w.b * ch.stride * Hkv + w.kh) * D + key, bad0, bad1,
+                                                    r / w.G, Hkv * D);
+                                reinterpret_cast<__nv_bfloat16*>(po.out)[(out0 + (size_t)(r / w.G) * Hq + r % w.G) * D + key] = __float2bfloat16_rn(y);
+                            } else {
+                                parts.o[((size_t)slot * R + r) * D + key] = __uint_as_float(o[e]);
+                            }
+                        }
+                    }
+            }
+            tc_fence_before();
+            if (hk < w.rows) {
+                if (!direct) parts.stat[(size_t)slot * R + hk] = make_float2(s_ref[hk], s_fix[hk]);
+                else if (po.lse) po.lse[out0 + (size_t)(hk / w.G) * Hq + hk % w.G] = (s_ref[hk] + log2f(s_fix[hk])) * (1.0f / kLog2e);
+            }
+            if (!direct && hk < 2) parts.bad[2 * slot + hk] = s_bad[hk];
+            asm volatile("bar.sync 1, 128;" ::: "memory");   // everybody is through with the statistics
+            if (hk < 2) s_bad[hk] = 0u;
+            __syncwarp();
+            if (lane == 0) mbar_arrive(bar(O_FREE));
+        }
+        if (!ok && lane == 0) atomicOr(&stats->error, 16u);
+        tc_fence_before();
+    }
+    __syncwarp();
+    __syncthreads();
+    if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
+}
+
+// Joins the parts of the units that several blocks shared: D / 4 threads a row.
+template <int D>
+__global__ void __launch_bounds__(128)
+paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv, int R) {
+    constexpr int LPR = D / 4;
+    pdl_trigger();
+    pdl_wait();
+    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv;
+    const int row = blockIdx.y * (128 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;
+    if (row >= n * G) return;
+    const int past = paged_past(pv, b, n);
+    if (past < 0) return;
+    const int tiles = (past + n + kTile - 1) / kTile, per = parts.plan[kMaxBatch + 1], f = parts.plan[b] + kh * tiles;
+    const int c0 = f / per, c1 = (f + tiles - 1) / per;
+    if (c0 == c1) return;   // one block had it all
+    auto slot_of = [&](int x) { return 2 * x + (x == c0 ? 1 : 0); };
+    float M = -INFINITY;
+    for (int x = c0; x <= c1; ++x) M = fmaxf(M, parts.stat[(size_t)slot_of(x) * R + row].x);
+    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t bad0 = 0, bad1 = 0;
+#pragma unroll 8
+    for (int x = c0; x <= c1; ++x) {
+        const size_t at = (size_t)slot_of(x) * R + row;
+        const float2 st = parts.stat[at];
+        const float4 y = *reinterpret_cast<const float4*>(parts.o + at * D + 4 * c);
+        const float wgt = st.x == -INFINITY ? 0.f : ex2(st.x - M);
+        l += st.y * wgt;
+        o[0] += y.x * wgt; o[1] += y.y * wgt; o[2] += y.z * wgt; o[3] += y.w * wgt;
+        bad0 |= parts.bad[2 * slot_of(x)]; bad1 |= parts.bad[2 * slot_of(x) + 1];
+    }
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+        o[u] *= inv;
+        if (bad0 | bad1)
+            o[u] += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + 4 * c + u, bad0, bad1, row / G, Hkv * D);
+    }
+    const size_t at = ((size_t)b * ch.stride + row / G) * Hq + kh * G + row % G;
+    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(po.out) + at * D + 4 * c) = make_uint2(rope_pack_bf16(o[0], o[1]), rope_pack_bf16(o[2], o[3]));
+    if (po.lse && c == 0) po.lse[at] = (M + log2f(l)) * (1.0f / kLog2e);
+}
+
+template <int D, int NG>
+cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o, void* scratch,
+                     int sms, cudaStream_t stream, int* launches) {
+    const int G = cv.Hq / cv.Hkv, box = std::min(16 * NG / G, ch.stride);
+    CUtensorMap tmQ, tmK, tmV;
+    const DraftView dv = {ch.q, ch.k, ch.v, nullptr, ch.stride};
+    if (!make_q_map(&tmQ, cv, dv, box)) return cudaErrorInvalidValue;
+    const uint64_t dims[2] = {(uint64_t)cv.d, (uint64_t)pv.n_pages * cv.Hkv * pv.page};
+    const uint64_t strides[1] = {(uint64_t)cv.d * 2};
+    const uint32_t kbox[2] = {64u, (uint32_t)std::min(pv.page, kTile)};
+    if (!make_tensor_map_bf16(&tmK, pv.kp, 2, dims, strides, kbox) || !make_tensor_map_bf16(&tmV, pv.vp, 2, dims, strides, kbox)) return cudaErrorInvalidValue;
+    auto kern = paged_few_kernel<D, NG>;
+    static bool smem_set[64] = {};  // per device: the opt-in is needed once
+    int dev = 0;
+    cudaGetDevice(&dev);
+    dev &= 63;
+    const size_t fixed = 1024 + 2 * (size_t)(16 * NG) * D * 2 + 2 * kPBytes + (D == 64 ? kTile * 128 : 0), slot = (size_t)kTile * D * 2;
+    const int slots = (int)std::min<size_t>(kMaxSlots, (kSmemMax - 14 * 1024 - fixed) / slot);   // (14 KB: the tables of sequences)
+    const size_t smem = fixed + slots * slot;
+    if (!smem_set[dev]) {
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        if (e != cudaSuccess) return e;
+        smem_set[dev] = true;
+    }
+    long units = 0, tiles = 0;
+    for (int b = 0; b < cv.B; ++b)
+        if (lens.m[b]) { units += cv.Hkv; tiles += (long)((pv.max_past + lens.m[b] + kTile - 1) / kTile) * cv.Hkv; }
+    // Units are shared by blocks only where that saves more than the second launch costs, about two tiles' time.
+    const int per_unit = (pv.max_past + max_n + kTile - 1) / kTile;
+    const long alone = (units + sms - 1) / sms * per_unit, shared = (tiles + sms - 1) / sms + 4;
+    const bool whole = alone <= shared;
+    Parts parts;
+    char* at = static_cast<char*>(scratch);
+    const size_t n_slots = 2 * (size_t)sms;
+    parts.plan = reinterpret_cast<int*>(at); at += kPlanBytes;
+    parts.bad = reinterpret_cast<uint32_t*>(at); at += n_slots * 16;
+    parts.stat = reinterpret_cast<float2*>(at); at += n_slots * 16 * NG * 8;
+    parts.o = reinterpret_cast<float*>(at);
+    const cudaError_t e = launch_pdl(kern, dim3((unsigned)std::min<long>(whole ? units : tiles, sms)), dim3(kThreads), smem, stream, tmQ, tmK, tmV, pv, ch,
+                                     lens, o, parts, cv.B, cv.Hq, cv.Hkv, cv.stats, (D / 64) * box * G * 128, slots, whole ? 1 : 0);
+    *launches = whole ? 1 : 2;
+    if (e != cudaSuccess || whole) return e;
+    return launch_pdl(paged_join_kernel<D>, dim3(cv.B * cv.Hkv, (max_n * G + 128 / (D / 4) - 1) / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o,
+                      parts, cv.Hq, cv.Hkv, 16 * NG);
+}
+
+template <int D>
+cudaError_t launch_d(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o, void* scratch,
+                     int sms, cudaStream_t stream, int* launches) {
+    const int rows = max_n * (cv.Hq / cv.Hkv);
+    return rows <= 16   ? launch_t<D, 1>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
+           : rows <= 32 ? launch_t<D, 2>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
+                        : launch_t<D, 4>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches);
+}
+
+}  // namespace
+
+size_t paged_few_scratch(int rows, int D, int sms) {
+    const int R = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
+    return kPlanBytes + 2 * (size_t)sms * part_bytes(R, D);
+}
+bool paged_few_takes(int rows) { return rows <= kRows; }
+
+cudaError_t launch_paged_few(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
+                             void* scratch, int sms, cudaStream_t stream, int* launches) {
+    return cv.d == 64 ? launch_d<64>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
+                      : launch_d<128>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches);
+}
+
+}  // namespace treekv

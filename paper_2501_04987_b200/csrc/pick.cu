@@ -43,32 +43,48 @@ struct Row {
         pieces = (n + off + VEC - 1) / VEC;
     }
     __device__ int first(int x) const { return x * VEC - off; }
-    // elements of piece x, minus infinity where there are none
-    __device__ void get(int x, float* f) const {
-        const int at = first(x);
-        float y[VEC];
-        if (at >= 0 && at + VEC <= n) {
-            Elem<T>::unpack(__ldg(reinterpret_cast<const uint4*>(p + at)), y);
-        } else {
+    // Pieces first, first + step, ... into U VEC numbers, minus infinity where there are none.  All 16-byte loads go out before the first
+    // one is looked at; pieces that hang over an end of the row are filled in behind them.
+    template <int U>
+    __device__ void get(int x0, int step, float (&f)[U * VEC]) const {
+        uint4 raw[U];
 #pragma unroll
-            for (int e = 0; e < VEC; ++e) y[e] = at + e >= 0 && at + e < n ? Elem<T>::to_float(p[at + e]) : -INFINITY;
+        for (int u = 0; u < U; ++u) {
+            const int at = first(x0 + u * step);
+            raw[u] = make_uint4(0, 0, 0, 0);
+            if (at >= 0 && at + VEC <= n) raw[u] = __ldg(reinterpret_cast<const uint4*>(p + at));
         }
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) f[e] = y[e];
+        for (int u = 0; u < U; ++u) {
+            const int at = first(x0 + u * step);
+            float y[VEC];
+            Elem<T>::unpack(raw[u], y);
+            if (at < 0 || at + VEC > n) {
+#pragma unroll
+                for (int e = 0; e < VEC; ++e) y[e] = at + e >= 0 && at + e < n ? Elem<T>::to_float(p[at + e]) : -INFINITY;
+            }
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[u * VEC + e] = y[e];
+        }
     }
 };
-// N floats from element `at` of a row of n, as far as they exist
-template <int N>
-__device__ inline void get_floats(const float* row, int at, int n, float (&f)[N]) {
-    if (at >= 0 && at + N <= n && !(reinterpret_cast<uintptr_t>(row + at) & 15u)) {
+// Floats of another row beside the pieces first + u step (u < W) of a row of logits; `none` where there are none.  `whole`: its
+// pieces are 16-byte aligned too.
+template <int W, int VEC>
+__device__ inline void get_beside(const float* p, bool whole, int n, int at0, int stride, float none, float (&f)[W * VEC]) {
 #pragma unroll
-        for (int e = 0; e < N; e += 4) {
-            const float4 y = __ldg(reinterpret_cast<const float4*>(row + at + e));
-            f[e] = y.x; f[e + 1] = y.y; f[e + 2] = y.z; f[e + 3] = y.w;
+    for (int u = 0; u < W; ++u) {
+        const int at = at0 + u * stride;
+        if (whole && at >= 0 && at + VEC <= n) {
+#pragma unroll
+            for (int e = 0; e < VEC; e += 4) {
+                const float4 y = __ldg(reinterpret_cast<const float4*>(p + at + e));
+                f[u * VEC + e] = y.x; f[u * VEC + e + 1] = y.y; f[u * VEC + e + 2] = y.z; f[u * VEC + e + 3] = y.w;
+            }
+        } else {
+#pragma unroll
+            for (int e = 0; e < VEC; ++e) f[u * VEC + e] = at + e >= 0 && at + e < n ? __ldg(p + at + e) : none;
         }
-    } else {
-#pragma unroll
-        for (int e = 0; e < N; ++e) f[e] = at + e >= 0 && at + e < n ? __ldg(row + at + e) : 0.f;
     }
 }
 __device__ inline void ask_l2(const void* p) { asm volatile("prefetch.global.L2 [%0];" ::"l"(p)); }
@@ -76,40 +92,66 @@ __device__ inline void ask_l2(const void* p) { asm volatile("prefetch.global.L2 
 struct Pair {
     float a, b;
 };
-template <int LANES, typename Op>
-__device__ inline Pair join_lanes(Pair x, Op&& op) {
-    const int lane = threadIdx.x & 31;
+// Floats as integers in the order of the numbers, and back: the largest of a warp's lanes is one instruction.
+__device__ inline uint32_t ordered(float x) {
+    const uint32_t u = __float_as_uint(x);
+    return u & 0x80000000u ? ~u : u | 0x80000000u;
+}
+__device__ inline float unordered(uint32_t u) { return __uint_as_float(u & 0x80000000u ? u & 0x7fffffffu : ~u); }
+__device__ inline float warp_max(float x) { return unordered(__reduce_max_sync(0xffffffffu, ordered(x))); }
+__device__ inline float warp_sum(float x) {  // (additions of two: every lane has the same result)
 #pragma unroll
-    for (int o = LANES / 2; o > 0; o /= 2) {
-        Pair y;
-        y.a = __shfl_xor_sync(0xffffffffu, x.a, o); y.b = __shfl_xor_sync(0xffffffffu, x.b, o);
-        x = lane & o ? op(y, x) : op(x, y);   // (every lane joins in the same order)
-    }
+    for (int o = 16; o > 0; o /= 2) x += __shfl_xor_sync(0xffffffffu, x, o);
     return x;
 }
+// What a warp's lanes join to, the same in every lane.  SumOp: (reference, sum at it); LargestOp: (value, index), the first of
+// equals; AddOp: two sums.
+struct SumOp {
+    float sc;
+    __device__ Pair none() const { return {-INFINITY, 0.f}; }
+    __device__ Pair operator()(Pair x) const {
+        Pair z;
+        z.a = warp_max(x.a);
+        z.b = warp_sum(x.b * (x.a == -INFINITY ? 0.f : ex2((x.a - z.a) * sc)));
+        return z;
+    }
+};
+struct LargestOp {
+    __device__ Pair none() const { return {-INFINITY, __int_as_float(0x7fffffff)}; }
+    __device__ Pair operator()(Pair x) const {
+        Pair z;
+        z.a = warp_max(x.a);
+        z.b = __int_as_float(__reduce_min_sync(0xffffffffu, x.a == z.a ? __float_as_int(x.b) : 0x7fffffff));
+        return z;
+    }
+};
+struct AddOp {
+    __device__ Pair none() const { return {0.f, 0.f}; }
+    __device__ Pair operator()(Pair x) const { return {warp_sum(x.a), 0.f}; }
+};
 struct JoinSpace {
     Pair warp[2][kWarps];
     Pair block[2][kMaxSplit];
 };
-// Joins one pair per thread over the cluster; every thread gets the result.  `none` is what changes nothing.  `slot` alternates
-// from call to call: a slot is written again two calls on, which the barrier of the call between comes before.
+// Joins one pair per thread over the cluster; every thread gets the result.  `slot` alternates from call to call: a slot is
+// written again two calls on, which the barrier of the call between comes before.
 template <typename Op>
-__device__ inline Pair join(Pair x, Pair none, JoinSpace& js, int& slot, int rank, int split, Op&& op) {
+__device__ inline Pair join(Pair x, JoinSpace& js, int& slot, int rank, int split, Op op) {
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-    x = join_lanes<32>(x, op);
+    x = op(x);
     if (lane == 0) js.warp[slot][warp] = x;
     __syncthreads();
     if (split == 1) {
-        x = join_lanes<kWarps>(js.warp[slot][lane & (kWarps - 1)], op);
+        x = op(lane < kWarps ? js.warp[slot][lane] : op.none());
     } else {
         if (warp == 0) {
-            x = join_lanes<kWarps>(js.warp[slot][lane & (kWarps - 1)], op);
+            x = op(lane < kWarps ? js.warp[slot][lane] : op.none());
             if (lane < split)
                 asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(&js.block[slot][rank]), lane)), "f"(x.a), "f"(x.b) : "memory");
         }
         __syncwarp();
         cluster_sync_all();
-        x = join_lanes<kMaxSplit>((lane & (kMaxSplit - 1)) < split ? js.block[slot][lane & (kMaxSplit - 1)] : none, op);
+        x = op(lane < split ? js.block[slot][lane] : op.none());
     }
     slot ^= 1;
     return x;
@@ -118,13 +160,14 @@ __device__ inline Pair join(Pair x, Pair none, JoinSpace& js, int& slot, int ran
 // E: numbers of a row that a thread holds
 template <typename T, int E>
 __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArgs a, DraftLens lens, DevStats* stats, int split) {
-    constexpr int VEC = Elem<T>::kVec, U = E / VEC;
+    constexpr int VEC = Elem<T>::kVec, U = E / VEC, W = (E < 32 ? E : 32) / VEC;  // W: pieces of a second row on their way at a time
     pdl_trigger();
     pdl_wait();
     const int b = blockIdx.y, rank = blockIdx.x, n = lens.n[b], tid = threadIdx.x, lane = tid & 31;
     __shared__ int s_parent[kMaxDraft];
     __shared__ int s_token[kMaxDraft];
     __shared__ float s_uniform[kMaxDraft];
+    __shared__ int s_path[kMaxDraft];
     __shared__ float s_logit[2][kMaxDraft], s_draft[2][kMaxDraft];  // of the children of a node (the parity of its depth)
     __shared__ float s_over[kWarps][kMaxDraft];                     // 1 / R before each rejection at a node, each warp's own
     __shared__ __align__(8) JoinSpace s_join;
@@ -153,17 +196,11 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
     const float sc = greedy ? 1.f : kLog2e / a.temperature;
     int at = 0, depth = 0, slot = 0, next = -1;
     for (;;) {
-        if (rank == 0 && tid == 0) path[depth] = at;
+        if (tid == 0) s_path[depth] = at;       // (in memory at the end: a store under way would hold up the cluster's barriers)
         const Row<T> row(logits + (size_t)at * a.vocab, a.vocab);
         const float* q = a.draft && !greedy ? a.draft + ((size_t)b * a.stride + at) * a.vocab : nullptr;
         float r[E];
-#pragma unroll
-        for (int u = 0; u < U; ++u) {
-            if (first + u * step < row.pieces) row.get(first + u * step, r + u * VEC);
-            else
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) r[u * VEC + e] = -INFINITY;
-        }
+        row.template get<U>(first, step, r);
         uint64_t kids = __ballot_sync(0xffffffffu, lane > at && lane < n && s_parent[lane] == at);
         kids |= (uint64_t)__ballot_sync(0xffffffffu, lane + 32 > at && lane + 32 < n && s_parent[min(lane + 32, kMaxDraft - 1)] == at) << 32;
         // what the children need beside the row, and the first one's row on its way
@@ -181,10 +218,8 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
         }
         ++depth;
         int child = -1;
-        auto larger = [](Pair x, Pair y) { return y.a > x.a || (y.a == x.a && __float_as_int(y.b) < __float_as_int(x.b)) ? y : x; };
-        const Pair nobody = {-INFINITY, __int_as_float(0x7fffffff)};
         if (greedy) {
-            Pair best = nobody;
+            Pair best = LargestOp().none();
             bool wrong = false;
 #pragma unroll
             for (int u = 0; u < U; ++u)
@@ -195,7 +230,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                     if (f > best.a) { best.a = f; best.b = __int_as_float(row.first(first + u * step) + e); }
                 }
             if (wrong) { best.a = INFINITY; best.b = __int_as_float(-1); }   // a row with a NaN picks nothing
-            best = join(best, nobody, s_join, slot, rank, split, larger);
+            best = join(best, s_join, slot, rank, split, LargestOp());
             int token = __float_as_int(best.b);
             if (token == 0x7fffffff) token = -1;
             for (uint64_t left = kids; left; left &= left - 1) {
@@ -206,28 +241,23 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
             at = child;
             continue;
         }
-        // ---- largest logit and sum of the row; r becomes the exponentials at the thread's own reference
+        // ---- largest logit and sum of the row; r becomes the exponentials at the warp's own reference
         Pair ms = {r[0], 0.f};
 #pragma unroll
         for (int e = 1; e < E; ++e) ms.a = fmaxf(ms.a, r[e]);
+        ms.a = warp_max(ms.a);
         const float mine = ms.a == -INFINITY ? 0.f : ms.a;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             r[e] = ex2((r[e] - mine) * sc);
             ms.b += r[e];
         }
-        const Pair nothing = {-INFINITY, 0.f};
-        ms = join(ms, nothing, s_join, slot, rank, split, [sc](Pair x, Pair y) {
-            Pair z;
-            z.a = fmaxf(x.a, y.a);
-            const float ref = z.a == -INFINITY ? 0.f : z.a;
-            z.b = x.b * ex2((x.a - ref) * sc) + y.b * ex2((y.a - ref) * sc);
-            return z; });
+        ms = join(ms, s_join, slot, rank, split, SumOp{sc});
         // NaN, an infinite logit, or nothing above minus infinity
         if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;
         const float top = ms.a, inv = 1.0f / ms.b, own = ex2((mine - top) * sc) * inv;
 #pragma unroll
-        for (int e = 0; e < E; ++e) r[e] = r[e] == 0.f ? 0.f : r[e] * own;  // (a thread without numbers has any reference)
+        for (int e = 0; e < E; ++e) r[e] = r[e] == 0.f ? 0.f : r[e] * own;  // (a warp without numbers has any reference)
         float R = 1.f;
         int rejected = 0;
         bool lost = false;
@@ -258,25 +288,22 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
             } else {
                 const float over = 1.0f / R;
                 Pair sum = {0.f, 0.f};
+                const bool whole = !((reinterpret_cast<uintptr_t>(q) - row.off * 4) & 15u);
 #pragma unroll
-                for (int u = 0; u < U; ++u) {
-                    const int x = first + u * step;
-                    if (x < row.pieces) {
-                        float qv[VEC];
-                        get_floats<VEC>(q, row.first(x), a.vocab, qv);
+                for (int u0 = 0; u0 < U; u0 += W) {
+                    float qv[W * VEC];
+                    get_beside<W, VEC>(q, whole, a.vocab, row.first(first + u0 * step), step * VEC, 0.f, qv);
 #pragma unroll
-                        for (int e = 0; e < VEC; ++e) {
-                            r[u * VEC + e] = fmaxf(fmaf(r[u * VEC + e], over, -qv[e]), 0.f);
-                            sum.a += r[u * VEC + e];
-                        }
+                    for (int e = 0; e < W * VEC; ++e) {
+                        r[u0 * VEC + e] = fmaxf(fmaf(r[u0 * VEC + e], over, -qv[e]), 0.f);
+                        sum.a += r[u0 * VEC + e];
                     }
                 }
                 if (lane == 0) s_over[tid >> 5][rejected] = over;
                 __syncwarp();
                 ++rejected;
                 if (left & (left - 1)) {         // another child: how much is left
-                    const Pair zero = {0.f, 0.f};
-                    sum = join(sum, zero, s_join, slot, rank, split, [](Pair x, Pair y) { Pair z = {x.a + y.a, 0.f}; return z; });
+                    sum = join(sum, s_join, slot, rank, split, AddOp());
                     R = sum.a;
                     if (!(R > 0.f)) { lost = true; break; }  // nothing is left
                 }
@@ -286,38 +313,33 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
         // ---- the next token: the largest r / e
         auto race = [&]() {
             Pair best = {0.f, __int_as_float(0x7fffffff)};
-            const Pair none = best;
+            const bool whole = !((reinterpret_cast<uintptr_t>(noise) - row.off * 4) & 15u);   // pieces of 16 bytes here too
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const int x = first + u * step;
-                if (x < row.pieces) {
-                    float e4[VEC];
-                    const int v0 = row.first(x);
-                    get_floats<VEC>(noise, v0, a.vocab, e4);
+            for (int u0 = 0; u0 < U; u0 += W) {
+                float e4[W * VEC];
+                get_beside<W, VEC>(noise, whole, a.vocab, row.first(first + u0 * step), step * VEC, 1.f, e4);
 #pragma unroll
-                    for (int e = 0; e < VEC; ++e)
-                        if (r[u * VEC + e] > 0.f) {
-                            const float z = __fdiv_rn(r[u * VEC + e], e4[e]);
-                            if (z > best.a) { best.a = z; best.b = __int_as_float(v0 + e); }
-                        }
-                }
+                for (int u = 0; u < W; ++u)
+#pragma unroll
+                    for (int e = 0; e < VEC; ++e) {
+                        const float z = __fdividef(r[(u0 + u) * VEC + e], e4[u * VEC + e]);   // (2 ulp: two that are closer count as equal)
+                        if (z > best.a) { best.a = z; best.b = __int_as_float(row.first(first + (u0 + u) * step) + e); }
+                    }
             }
-            return __float_as_int(join(best, none, s_join, slot, rank, split, larger).b);
+            return __float_as_int(join(best, s_join, slot, rank, split, LargestOp()).b);
         };
         next = lost ? 0x7fffffff : race();
         if (next == 0x7fffffff && rejected) {    // rounding has left nothing: the target's own probabilities
+            row.template get<U>(first, step, r);
 #pragma unroll
-            for (int u = 0; u < U; ++u) {
-                if (first + u * step < row.pieces) row.get(first + u * step, r + u * VEC);
-#pragma unroll
-                for (int e = 0; e < VEC; ++e) r[u * VEC + e] = first + u * step < row.pieces ? ex2((r[u * VEC + e] - top) * sc) * inv : 0.f;
-            }
+            for (int e = 0; e < E; ++e) r[e] = ex2((r[e] - top) * sc) * inv;
             next = race();
         }
         if (next == 0x7fffffff) next = -1;
         break;
     }
-    if (rank == 0 && tid >= depth && tid < a.stride) path[tid] = -1;
+    __syncthreads();
+    if (rank == 0 && tid < a.stride) path[tid] = tid < depth ? s_path[tid] : -1;
     if (rank == 0 && tid == 0) { a.count[b] = depth; a.next[b] = next; }
     if (split > 1) { __syncwarp(); cluster_sync_all(); }  // nobody leaves while pairs may be pushed to it
 }
