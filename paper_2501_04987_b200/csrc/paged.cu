@@ -85,8 +85,7 @@ extern "C" {
 
 size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride) {
     if (!ctx || stride < 1 || stride > kMaxChunkRows || ctx->dt != TREEKV_BF16) return 0;
-    const int rows = stride * ctx->G;  // (a call of a longer chunk may still have few tokens in every sequence)
-    return paged_few_scratch(paged_few_takes(rows) ? rows : 64, ctx->cv.d, ctx->sm_count);
+    return paged_few_scratch(ctx->cv.d, ctx->sm_count);  // (a call of a longer chunk may still have few tokens in every sequence)
 }
 
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,

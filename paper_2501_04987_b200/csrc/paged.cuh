@@ -50,9 +50,9 @@ __device__ inline int checked_page(const PagedView& pv, int e, DevStats* stats) 
 // new tokens into their pages
 cudaError_t launch_paged_append(const CacheView& cv, treekv_dtype dt, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n,
                                 cudaStream_t stream);
-// attention of few new tokens - up to 64 query rows a KV head - which enter their pages with it (bf16); `launches`: kernels launched
+// attention of few new tokens - up to 16 query rows a KV head - which enter their pages with it (bf16); `launches`: kernels launched
 bool paged_few_takes(int rows);
-size_t paged_few_scratch(int rows, int D, int sms);
+size_t paged_few_scratch(int D, int sms);
 cudaError_t launch_paged_few(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches);
 // attention of the new tokens, which are in their pages

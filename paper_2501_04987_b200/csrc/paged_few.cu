@@ -1,9 +1,8 @@
-// Attention of few new tokens over a paged cache on the 5th-generation tensor cores (bf16): up to 64 query rows a KV head, a decode
+// Attention of few new tokens over a paged cache on the 5th-generation tensor cores (bf16): up to 16 query rows a KV head, a decode
 // step or a short draft of every sequence.
 //
-// Such a call is bound by the pages it reads, so it is built around a ring of key and value tiles that never runs dry: one
-// block per SM, 160 KB of tiles in flight, and the tiles of all units (sequence, KV head) in a row, of which every block takes the
-// same number, wherever the units end.  A block that has a unit to itself writes its rows; otherwise it leaves its part - maximum,
+// Such a call is bound by the pages it reads: two blocks per SM, each with tiles in flight while the other works on its own, and
+// the tiles of all units (sequence, KV head) in a row, of which every block takes the same number, wherever the units end.  A block that has a unit to itself writes its rows; otherwise it leaves its part - maximum,
 // sum, unnormalised output - in the caller's scratch, and a second small launch joins the parts in order.
 //
 // With few rows the logits are taken transposed, so that the tensor core's 128 matrix rows are 128 keys:
@@ -32,14 +31,18 @@ using namespace vtc;
 
 constexpr int kThreads = 192;
 constexpr int kTile = 128;                 // keys of a tile
-constexpr int kRows = 64;                  // query rows as the tensor core sees them
+constexpr int kRows = 16;                  // query rows, at most
 constexpr int kMaxSlots = 8;
-constexpr uint32_t kTmemCols = 256;        // S^T 64 + 64, O^T 64
-constexpr size_t kSmemMax = 224 * 1024;
-constexpr int kPBytes = kTile * 128;       // P^T: a key's 64 rows
+constexpr uint32_t kTmemCols = 32;         // S^T 16, O^T 16
+constexpr size_t kSmemMax = 113 * 1024;    // two blocks on an SM
+constexpr int kPHalf = kRows * 128, kPBytes = 2 * kPHalf;  // P: [64 keys, 64 keys][rows][128 bytes]
+constexpr int kStart = 2;                  // what a unit costs beside its tiles, in tiles
 
-enum Bar { Q_FULL = 0, Q_FREE = 2, S_FULL = 4, S_FREE = 6, P_FULL = 8, O_FULL = 10, O_FREE = 11, APPENDED = 12, FULL = 13, USED = FULL + kMaxSlots,
-           N_BARS = USED + kMaxSlots };
+// FULL: a slot's tile has arrived.  USED: the MMAs that read it are done - for a K tile that also says that its logits are there.
+// O_DONE: a tile's share of O is in, P may be written again.  (With three slots the K tile after next takes the V tile's place, and
+// its logits may be there before a softmax warp has asked for that V tile's barrier: two phases on, it would wait for ever.  So
+// the softmax warps wait for O_DONE, which cannot move on without them.)  S_READ: a tile's logits are in registers.
+enum Bar { Q_FULL = 0, Q_FREE = 2, S_READ = 4, P_FULL = 5, O_FREE = 6, APPENDED = 7, O_DONE = 8, FULL = 9, USED = FULL + kMaxSlots, N_BARS = USED + kMaxSlots };
 
 __device__ inline void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
     asm volatile(
@@ -80,22 +83,26 @@ struct Walk {
     bool whole;
     int b, kh, past, n, rows, nvis, tiles, t0, t1;  // of the piece: tiles [t0, t1) of the unit's
     __device__ bool get() {
-        if (item >= end) return false;
-        int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (first[mid] <= item) lo = mid; else hi = mid - 1;
+        while (item < end) {
+            int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= item) lo = mid; else hi = mid - 1;
+            }
+            b = lo;
+            n = lens->m[b]; past = pasts[b];
+            rows = n * G; nvis = past + n;
+            tiles = (nvis + kTile - 1) / kTile;
+            int at = item - first[b];
+            if (whole) { kh = at; t0 = 0; t1 = tiles; ++item; return true; }
+            kh = at / (tiles + kStart);
+            at -= kh * (tiles + kStart) + kStart;
+            t0 = max(0, at); t1 = min(tiles, at + end - item);
+            item += tiles - at;
+            if (t0 < t1) return true;    // (else the block's share ends in the unit's start)
         }
-        b = lo;
-        n = lens->m[b]; past = pasts[b];
-        rows = n * G; nvis = past + n;
-        tiles = (nvis + kTile - 1) / kTile;
-        const int at = item - first[b];
-        if (whole) { kh = at; t0 = 0; t1 = tiles; }
-        else { kh = at / tiles; t0 = at - kh * tiles; t1 = min(tiles, t0 + end - item); }
-        return true;
+        return false;
     }
-    __device__ void next() { item += whole ? 1 : t1 - t0; }
 };
 
 // Values that are not finite, of new tokens that not all rows see, were taken out of the tiles: those that a row sees (its
@@ -109,33 +116,29 @@ __device__ inline float bad_values(const __nv_bfloat16* v, uint32_t bad0, uint32
     return sum;
 }
 
-// NG: groups of 16 query rows that can hold a row
-template <int D, int NG>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int D>
+__global__ void __launch_bounds__(kThreads, 2)
 paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int B, int Hq, int Hkv, DevStats* stats, int q_bytes,
                  int slots, int whole) {
-    constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128, R = 16 * NG, QB = R * D * 2;
+    constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128, R = kRows, NG = 1, QB = R * D * 2;
     pdl_trigger();
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     __shared__ uint32_t tmem_slot;
-    __shared__ int s_first[kMaxBatch + 1];
-    __shared__ int s_past[kMaxBatch];
     __shared__ __align__(16) float s_ref[R], s_fix[R], s_max[4][R];
     __shared__ uint32_t s_bad[2];
     const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
     unsigned char* base_ptr = smem_raw + (base - smem_addr_u32(smem_raw));
-    const uint32_t sQ = base, sP = base + 2 * QB, sRing = sP + 2 * kPBytes;   // two of each
+    const uint32_t sQ = base, sP = base + 2 * QB, sRing = sP + kPBytes;   // (two Q tiles)
+    int* s_first = reinterpret_cast<int*>(base_ptr + 2 * QB + kPBytes + slots * SLOT + (D == 64 ? HALF : 0));   // [B + 1]
+    int* s_past = s_first + B + 1;                                                                                // [B]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bar0 = smem_addr_u32(&bars[0]);
     auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) {
-            mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1);
-            mbar_init(bar(S_FULL + s), 1); mbar_init(bar(S_FREE + s), 4); mbar_init(bar(P_FULL + s), 4);
-        }
-        mbar_init(bar(O_FULL), 1); mbar_init(bar(O_FREE), 4); mbar_init(bar(APPENDED), 4);
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1); }
+        mbar_init(bar(S_READ), 4); mbar_init(bar(P_FULL), 4); mbar_init(bar(O_FREE), 4); mbar_init(bar(APPENDED), 4); mbar_init(bar(O_DONE), 1);
         for (int s = 0; s < kMaxSlots; ++s) { mbar_init(bar(FULL + s), 1); mbar_init(bar(USED + s), 1); }
         mbar_fence_init();
         s_bad[0] = s_bad[1] = 0u;
@@ -150,7 +153,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             if (n > 0) {
                 past = paged_past(pv, b, n);
                 if (past < 0) { if (blockIdx.x == 0) atomicOr(&stats->error, kErrBadIndex); }
-                else items = whole ? Hkv : (past + n + kTile - 1) / kTile * Hkv;
+                else items = whole ? Hkv : ((past + n + kTile - 1) / kTile + kStart) * Hkv;
             }
             int inc = items;
 #pragma unroll
@@ -163,7 +166,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     tc_fence_before();
     __syncthreads();
     tc_fence_after();
-    const uint32_t tmem = tmem_slot, tmO = tmem + 2 * kRows;
+    const uint32_t tmem = tmem_slot, tmO = tmem + 16;
     const int total = s_first[B], per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
     Walk w;
     w.first = s_first; w.pasts = s_past; w.lens = &lens; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.whole = whole;
@@ -180,7 +183,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         int issued = 0, piece = 0;
         bool appended = false;
         Ring r(0, slots);
-        for (; ok && w.get(); w.next(), ++piece) {
+        for (; ok && w.get(); ++piece) {
             const int qs = piece & 1;
             if (lane == 0) {
                 ok = mbar_wait(bar(Q_FREE + qs), ((piece >> 1) & 1) ^ 1);
@@ -234,52 +237,46 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         // ================= MMA issuer: S^T of a tile, then O^T of the one before
         if (lane == 0) {
             constexpr uint32_t idesc_s = umma_idesc_bf16(128, R, 0, 0);      // both operands K-major (rows x channels)
-            constexpr uint32_t idesc_o = umma_idesc_bf16(128, kRows, 1, 1);  // V^T and P^T: MN-major.  (Columns beyond R are
-                                                                              // whatever lies there, and make columns that nobody reads)
+            constexpr uint32_t idesc_o = umma_idesc_bf16(128, R, 1, 0);      // V^T: MN-major; P: rows x keys
             // (D = 64: the matrix rows 64 to 127 are what lies behind the tile, and make lanes that nobody reads)
-            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, HALF), p_lo = desc_lo(sP, kPBytes);
+            const uint32_t q_lo = desc_lo(sQ, 16), k_lo = desc_lo(sRing, 16), v_lo = desc_lo(sRing, HALF), p_lo = desc_lo(sP, 16);
             Ring rk(0, slots), rv(1, slots);
-            int g = 0, piece = 0;         // tiles of the block so far
-            bool behind = false, behind_first = false, behind_last = false;   // a tile whose O^T is to be issued: first, last of its piece
-            int behind_piece = 0, last_slot = 0, last_phase = 0;
-            auto issue_o = [&]() {
-                const int j = g - 1;      // (g: tiles whose S^T is issued)
-                if (behind_first && !(ok = mbar_wait(bar(O_FREE), (behind_piece & 1) ^ 1))) return;
-                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + (j & 1)), (j >> 1) & 1))) return;
+            int g = 0, piece = 0;         // tiles whose S^T is issued
+            bool starts = false;                                   // the tile whose O^T comes next is the first of its piece
+            auto issue_o = [&](int of_piece) {
+                if (starts && !(ok = mbar_wait(bar(O_FREE), (of_piece & 1) ^ 1))) return;
+                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL), (g - 1) & 1))) return;
                 tc_fence_after();
-                const uint32_t v = v_lo + rv.slot * (SLOT / 16), p = p_lo + (j & 1) * (kPBytes / 16);
+                const uint32_t v = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes
-                    umma_bf16(tmO, desc_of(v + kk * (2048 / 16)), desc_of(p + kk * (2048 / 16)), idesc_o, (!behind_first || kk > 0) ? 1u : 0u);
+                    umma_bf16(tmO, desc_of(v + kk * (2048 / 16)), desc_of(p_lo + (kk >> 2) * (kPHalf / 16) + (kk & 3) * 2), idesc_o, (!starts || kk > 0) ? 1u : 0u);
                 umma_commit(bar(USED + rv.slot));
-                if (behind_last) umma_commit(bar(O_FULL));
-                last_slot = rv.slot; last_phase = rv.phase;
+                umma_commit(bar(O_DONE));
                 rv.next(); rv.next();
             };
-            for (; ok && w.get(); w.next(), ++piece) {
+            for (; ok && w.get(); ++piece) {
                 const int qs = piece & 1;
                 if (!(ok = mbar_wait(bar(Q_FULL + qs), (piece >> 1) & 1))) break;
                 for (int t = w.t0; t < w.t1; ++t) {
-                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_FREE + (g & 1)), ((g >> 1) & 1) ^ 1))) break;
+                    // the logits of the tile before are in registers: this one's take their place
+                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_READ), (g & 1) ^ 1))) break;
                     tc_fence_after();
                     const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (QB / 16);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tmem + (g & 1) * kRows, desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2),
-                                  desc_of(q + (kk >> 2) * (R * 128 / 16) + (kk & 3) * 2), idesc_s, kk > 0);
-                    umma_commit(bar(S_FULL + (g & 1)));
+                        umma_bf16(tmem, desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), desc_of(q + (kk >> 2) * (R * 128 / 16) + (kk & 3) * 2), idesc_s, kk > 0);
                     umma_commit(bar(USED + rk.slot));
                     if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
                     rk.next(); rk.next();
-                    if (behind) { issue_o(); if (!ok) break; }
-                    behind = true; behind_first = t == w.t0; behind_last = t + 1 == w.t1; behind_piece = piece;
+                    if (g > 0) { issue_o(t == w.t0 ? piece - 1 : piece); if (!ok) break; }
+                    starts = t == w.t0;
                     ++g;
                 }
             }
-            if (ok && behind) issue_o();
+            if (ok && g > 0) issue_o(piece - 1);
             // every MMA has finished before its memory and tensor memory are given to anything else
-            if (ok && behind) ok = mbar_wait(bar(USED + last_slot), last_phase);
-            if (ok && behind) ok = mbar_wait(bar(O_FULL), (piece - 1) & 1);
+            if (ok && g > 0) ok = mbar_wait(bar(O_DONE), (g - 1) & 1);
             if (!ok) atomicOr(&stats->error, 8u);
         }
     } else {
@@ -289,7 +286,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         const float sc2 = kLog2e * rsqrtf((float)D);
         {   // new tokens into their pages, before the tiles that hold them are asked for
             Walk a = w;
-            for (; a.get(); a.next()) {
+            while (a.get()) {
                 const int lo = max(0, a.t0 * kTile - a.past), hi = min(a.n, a.t1 * kTile - a.past);
                 for (int e = st_tid; e < (hi - lo) * (D / 8); e += 128) {
                     const int tok = lo + e / (D / 8), c = e % (D / 8), at = a.past + tok;
@@ -306,9 +303,9 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             __syncwarp();
             if (lane == 0) mbar_arrive(bar(APPENDED));
         }
-        Ring rv(1, slots);
-        int g = 0, piece = 0, done = 0, done_phase = 0;   // done: V of the tile before
-        for (; ok && w.get(); w.next(), ++piece) {
+        Ring rk(0, slots), rv(1, slots);
+        int g = 0;   // tiles of the block so far
+        while (ok && w.get()) {
             float l[R];
 #pragma unroll
             for (int x = 0; x < R; ++x) l[x] = 0.f;
@@ -318,16 +315,16 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             for (int t = w.t0; t < w.t1; ++t, ++g) {
                 const int k0 = t * kTile, kpos = k0 + key;
                 const bool partly = k0 + kTile > w.past + 1;   // some row does not see some key of this tile
-                if (!mbar_wait(bar(S_FULL + (g & 1)), (g >> 1) & 1)) { ok = false; break; }
+                if (!mbar_wait(bar(USED + rk.slot), rk.phase)) { ok = false; break; }
                 tc_fence_after();
                 uint32_t s[NG][16];
 #pragma unroll
-                for (int x = 0; x < NG; ++x) tmem_ld16(tmem + (g & 1) * kRows + x * 16 + lane_off, s[x]);
+                for (int x = 0; x < NG; ++x) tmem_ld16(tmem + x * 16 + lane_off, s[x]);
 #pragma unroll
                 for (int x = 0; x < NG; ++x) tmem_ld16_wait(s[x]);
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(S_FREE + (g & 1)));
+                if (lane == 0) mbar_arrive(bar(S_READ));
                 if (partly || edges) {   // rows [rmin, rows) see this key
                     const int rmin = max(0, kpos - w.past) * w.G;
                     const uint64_t see = rmin >= 64 ? 0ull : low_bits(w.rows) & ~low_bits(rmin);
@@ -364,7 +361,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 #pragma unroll
                     for (int x = 0; x < R; ++x) l[x] *= s_fix[x];
                     if (t > w.t0) {
-                        if (!mbar_wait(bar(USED + done), done_phase)) { ok = false; break; }
+                        if (!mbar_wait(bar(O_DONE), (g - 1) & 1)) { ok = false; break; }
                         tc_fence_after();
 #pragma unroll
                         for (int x = 0; x < NG; ++x) {
@@ -378,29 +375,28 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                         tmem_st_wait();
                     }
                 }
-                unsigned char* prow = base_ptr + 2 * QB + (g & 1) * kPBytes + key * 128;
-                // (the P^T of two tiles ago has been multiplied: those MMAs were committed with this tile's logits)
+                float p[R];
 #pragma unroll
-                for (int x = 0; x < R; x += 8) {
-                    float p[8];
+                for (int x = 0; x < R; x += 4) {
+                    const float4 m4 = *reinterpret_cast<const float4*>(s_ref + x);
+                    const float mr[4] = {m4.x, m4.y, m4.z, m4.w};
 #pragma unroll
-                    for (int e = 0; e < 8; e += 4) {
-                        const float4 m4 = *reinterpret_cast<const float4*>(s_ref + x + e);
-                        const float mr[4] = {m4.x, m4.y, m4.z, m4.w};
-#pragma unroll
-                        for (int u = 0; u < 4; ++u)
-                            p[e + u] = ex2(fmaf(__uint_as_float(s[(x + e + u) / 16][(x + e + u) % 16]), sc2, mr[u] == -INFINITY ? 0.f : -mr[u]));
+                    for (int u = 0; u < 4; ++u) {
+                        p[x + u] = ex2(fmaf(__uint_as_float(s[0][x + u]), sc2, mr[u] == -INFINITY ? 0.f : -mr[u]));
+                        l[x + u] += p[x + u];
                     }
-#pragma unroll
-                    for (int e = 0; e < 8; ++e) l[x + e] += p[e];
-                    *reinterpret_cast<uint4*>(prow + (((x >> 3) ^ (key & 7)) << 4)) =
-                        make_uint4(rope_pack_bf16(p[0], p[1]), rope_pack_bf16(p[2], p[3]), rope_pack_bf16(p[4], p[5]), rope_pack_bf16(p[6], p[7]));
                 }
+                // P of the tile before has been multiplied
+                if (g > 0 && !mbar_wait(bar(O_DONE), (g - 1) & 1)) { ok = false; break; }
+                unsigned char* pk = base_ptr + 2 * QB + (key >> 6) * kPHalf + (key & 7) * 2;
+#pragma unroll
+                for (int x = 0; x < R; ++x)
+                    *reinterpret_cast<__nv_bfloat16*>(pk + x * 128 + ((((key & 63) >> 3) ^ (x & 7)) << 4)) = __float2bfloat16_rn(p[x]);
                 if (partly) {
                     // Tokens that not all rows see: a value that is not finite is taken out of the tile and its token noted.  Rows behind the
                     // last token hold none and become zeros.
                     if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
-                    unsigned char* tile = base_ptr + 2 * QB + 2 * kPBytes + rv.slot * SLOT;
+                    unsigned char* tile = base_ptr + 2 * QB + kPBytes + rv.slot * SLOT;
                     const int valid = min(kTile, w.nvis - k0);
                     for (int e = st_tid + max(0, w.past + 1 - k0) * (D / 8); e < kTile * (D / 8); e += 128) {
                         const int rr = e / (D / 8), c = e % (D / 8);
@@ -423,9 +419,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 fence_proxy_async_smem();
                 tc_fence_before();
                 __syncwarp();
-                if (lane == 0) mbar_arrive(bar(P_FULL + (g & 1)));
-                done = rv.slot; done_phase = rv.phase;
-                rv.next(); rv.next();
+                if (lane == 0) mbar_arrive(bar(P_FULL));
+                rk.next(); rk.next(); rv.next(); rv.next();
             }
             if (!ok) break;
             // ---- the piece's rows: sums over the keys, O^T from tensor memory (thread = channel)
@@ -438,7 +433,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (hk < R) s_fix[hk] = (s_max[0][hk] + s_max[1][hk]) + (s_max[2][hk] + s_max[3][hk]);
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (!mbar_wait(bar(O_FULL), piece & 1)) { ok = false; break; }
+            if (!mbar_wait(bar(O_DONE), (g - 1) & 1)) { ok = false; break; }
             tc_fence_after();
             const bool direct = w.t0 == 0 && w.t1 == w.tiles;
             const uint32_t bad0 = s_bad[0], bad1 = s_bad[1];
@@ -486,52 +481,91 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
 }
 
-// Joins the parts of the units that several blocks shared: D / 4 threads a row.
+// Joins the parts of the units that several blocks shared.  A block has a row: its warps deal the parts, each with four
+// of them on their way, and meet in shared memory, in order.
 template <int D>
-__global__ void __launch_bounds__(128)
-paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv, int R) {
-    constexpr int LPR = D / 4;
+__global__ void __launch_bounds__(256)
+paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv) {
+    constexpr int R = kRows, CPL = D / 32, W = 8;   // a lane's channels; warps
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv;
-    const int row = blockIdx.y * (128 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;
+    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv, row = blockIdx.y;
     if (row >= n * G) return;
     const int past = paged_past(pv, b, n);
     if (past < 0) return;
-    const int tiles = (past + n + kTile - 1) / kTile, per = parts.plan[kMaxBatch + 1], f = parts.plan[b] + kh * tiles;
+    const int tiles = (past + n + kTile - 1) / kTile, per = parts.plan[kMaxBatch + 1], f = parts.plan[b] + kh * (tiles + kStart) + kStart;
     const int c0 = f / per, c1 = (f + tiles - 1) / per;
     if (c0 == c1) return;   // one block had it all
-    auto slot_of = [&](int x) { return 2 * x + (x == c0 ? 1 : 0); };
-    float M = -INFINITY;
-    for (int x = c0; x <= c1; ++x) M = fmaxf(M, parts.stat[(size_t)slot_of(x) * R + row].x);
-    float l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
-    uint32_t bad0 = 0, bad1 = 0;
-#pragma unroll 8
-    for (int x = c0; x <= c1; ++x) {
-        const size_t at = (size_t)slot_of(x) * R + row;
-        const float2 st = parts.stat[at];
-        const float4 y = *reinterpret_cast<const float4*>(parts.o + at * D + 4 * c);
-        const float wgt = st.x == -INFINITY ? 0.f : ex2(st.x - M);
-        l += st.y * wgt;
-        o[0] += y.x * wgt; o[1] += y.y * wgt; o[2] += y.z * wgt; o[3] += y.w * wgt;
-        bad0 |= parts.bad[2 * slot_of(x)]; bad1 |= parts.bad[2 * slot_of(x) + 1];
-    }
-    const float inv = 1.0f / l;
+    __shared__ float s_o[W][D], s_stat[W][2];
+    __shared__ uint32_t s_bad[2];
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
+    __syncthreads();
+    float M = -INFINITY, l = 0.f, o[CPL];
 #pragma unroll
-    for (int u = 0; u < 4; ++u) {
-        o[u] *= inv;
-        if (bad0 | bad1)
-            o[u] += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + 4 * c + u, bad0, bad1, row / G, Hkv * D);
+    for (int e = 0; e < CPL; ++e) o[e] = 0.f;
+    for (int x0 = c0 + warp; x0 <= c1; x0 += 4 * W) {
+        float2 st[4];
+        float y[4][CPL];
+        uint32_t bad0 = 0, bad1 = 0;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            const int x = x0 + u * W, slot = 2 * x + (x == c0 ? 1 : 0);
+            st[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) y[u][e] = 0.f;
+            if (x <= c1) {
+                st[u] = parts.stat[(size_t)slot * R + row];
+                const float* src = parts.o + ((size_t)slot * R + row) * D + CPL * lane;
+                if constexpr (CPL == 4) { const float4 z = *reinterpret_cast<const float4*>(src); y[u][0] = z.x; y[u][1] = z.y; y[u][2] = z.z; y[u][3] = z.w; }
+                else { const float2 z = *reinterpret_cast<const float2*>(src); y[u][0] = z.x; y[u][1] = z.y; }
+                if (lane == 0) { bad0 |= parts.bad[2 * slot]; bad1 |= parts.bad[2 * slot + 1]; }
+            }
+        }
+        if (bad0) atomicOr(&s_bad[0], bad0);
+        if (bad1) atomicOr(&s_bad[1], bad1);
+        const float top = fmaxf(fmaxf(fmaxf(M, st[0].x), fmaxf(st[1].x, st[2].x)), st[3].x);
+        if (top > -INFINITY) {
+            const float fix = ex2(M - top);
+            M = top; l *= fix;
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) o[e] *= fix;
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const float wgt = ex2(st[u].x - M);
+                l += st[u].y * wgt;
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
+            }
+        }
     }
+#pragma unroll
+    for (int e = 0; e < CPL; ++e) s_o[warp][CPL * lane + e] = o[e];
+    if (lane == 0) { s_stat[warp][0] = M; s_stat[warp][1] = l; }
+    __syncthreads();
+    const int c = threadIdx.x;
+    if (c >= D) return;
+    M = s_stat[0][0];
+    for (int x = 1; x < W; ++x) M = fmaxf(M, s_stat[x][0]);
+    float sum = 0.f;
+    l = 0.f;
+    for (int x = 0; x < W; ++x) {
+        const float wgt = s_stat[x][0] == -INFINITY ? 0.f : ex2(s_stat[x][0] - M);
+        l += s_stat[x][1] * wgt;
+        sum += s_o[x][c] * wgt;
+    }
+    sum *= 1.0f / l;
+    if (s_bad[0] | s_bad[1])
+        sum += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + c, s_bad[0], s_bad[1], row / G, Hkv * D);
     const size_t at = ((size_t)b * ch.stride + row / G) * Hq + kh * G + row % G;
-    *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(po.out) + at * D + 4 * c) = make_uint2(rope_pack_bf16(o[0], o[1]), rope_pack_bf16(o[2], o[3]));
+    reinterpret_cast<__nv_bfloat16*>(po.out)[at * D + c] = __float2bfloat16_rn(sum);
     if (po.lse && c == 0) po.lse[at] = (M + log2f(l)) * (1.0f / kLog2e);
 }
 
-template <int D, int NG>
+template <int D>
 cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o, void* scratch,
                      int sms, cudaStream_t stream, int* launches) {
-    const int G = cv.Hq / cv.Hkv, box = std::min(16 * NG / G, ch.stride);
+    const int G = cv.Hq / cv.Hkv, box = std::min(kRows / G, ch.stride);
     CUtensorMap tmQ, tmK, tmV;
     const DraftView dv = {ch.q, ch.k, ch.v, nullptr, ch.stride};
     if (!make_q_map(&tmQ, cv, dv, box)) return cudaErrorInvalidValue;
@@ -539,16 +573,17 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     const uint64_t strides[1] = {(uint64_t)cv.d * 2};
     const uint32_t kbox[2] = {64u, (uint32_t)std::min(pv.page, kTile)};
     if (!make_tensor_map_bf16(&tmK, pv.kp, 2, dims, strides, kbox) || !make_tensor_map_bf16(&tmV, pv.vp, 2, dims, strides, kbox)) return cudaErrorInvalidValue;
-    auto kern = paged_few_kernel<D, NG>;
+    auto kern = paged_few_kernel<D>;
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
     dev &= 63;
-    const size_t fixed = 1024 + 2 * (size_t)(16 * NG) * D * 2 + 2 * kPBytes + (D == 64 ? kTile * 128 : 0), slot = (size_t)kTile * D * 2;
-    const int slots = (int)std::min<size_t>(kMaxSlots, (kSmemMax - 14 * 1024 - fixed) / slot);   // (14 KB: the tables of sequences)
-    const size_t smem = fixed + slots * slot;
+    const size_t tables = 4 * (2 * (size_t)cv.B + 1), fixed = 1024 + 2 * (size_t)kRows * D * 2 + kPBytes + (D == 64 ? kTile * 128 : 0);
+    const size_t slot = (size_t)kTile * D * 2;
+    const int slots = (int)std::min<size_t>(kMaxSlots, (kSmemMax - 2048 - fixed - tables) / slot);
+    const size_t smem = fixed + slots * slot + tables;
     if (!smem_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kSmemMax);
         if (e != cudaSuccess) return e;
         smem_set[dev] = true;
     }
@@ -557,44 +592,31 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
         if (lens.m[b]) { units += cv.Hkv; tiles += (long)((pv.max_past + lens.m[b] + kTile - 1) / kTile) * cv.Hkv; }
     // Units are shared by blocks only where that saves more than the second launch costs, about two tiles' time.
     const int per_unit = (pv.max_past + max_n + kTile - 1) / kTile;
-    const long alone = (units + sms - 1) / sms * per_unit, shared = (tiles + sms - 1) / sms + 4;
+    const long places = 2L * sms, alone = (units + places - 1) / places * (per_unit + kStart), shared = (tiles + kStart * units + places - 1) / places + 4;
     const bool whole = alone <= shared;
     Parts parts;
     char* at = static_cast<char*>(scratch);
-    const size_t n_slots = 2 * (size_t)sms;
+    const size_t n_slots = 4 * (size_t)sms;
     parts.plan = reinterpret_cast<int*>(at); at += kPlanBytes;
     parts.bad = reinterpret_cast<uint32_t*>(at); at += n_slots * 16;
-    parts.stat = reinterpret_cast<float2*>(at); at += n_slots * 16 * NG * 8;
+    parts.stat = reinterpret_cast<float2*>(at); at += n_slots * kRows * 8;
     parts.o = reinterpret_cast<float*>(at);
-    const cudaError_t e = launch_pdl(kern, dim3((unsigned)std::min<long>(whole ? units : tiles, sms)), dim3(kThreads), smem, stream, tmQ, tmK, tmV, pv, ch,
+    const cudaError_t e = launch_pdl(kern, dim3((unsigned)std::min<long>(whole ? units : tiles, places)), dim3(kThreads), smem, stream, tmQ, tmK, tmV, pv, ch,
                                      lens, o, parts, cv.B, cv.Hq, cv.Hkv, cv.stats, (D / 64) * box * G * 128, slots, whole ? 1 : 0);
     *launches = whole ? 1 : 2;
     if (e != cudaSuccess || whole) return e;
-    return launch_pdl(paged_join_kernel<D>, dim3(cv.B * cv.Hkv, (max_n * G + 128 / (D / 4) - 1) / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o,
-                      parts, cv.Hq, cv.Hkv, 16 * NG);
-}
-
-template <int D>
-cudaError_t launch_d(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o, void* scratch,
-                     int sms, cudaStream_t stream, int* launches) {
-    const int rows = max_n * (cv.Hq / cv.Hkv);
-    return rows <= 16   ? launch_t<D, 1>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
-           : rows <= 32 ? launch_t<D, 2>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
-                        : launch_t<D, 4>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches);
+    return launch_pdl(paged_join_kernel<D>, dim3(cv.B * cv.Hkv, max_n * G), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
 }
 
 }  // namespace
 
-size_t paged_few_scratch(int rows, int D, int sms) {
-    const int R = rows <= 16 ? 16 : rows <= 32 ? 32 : 64;
-    return kPlanBytes + 2 * (size_t)sms * part_bytes(R, D);
-}
+size_t paged_few_scratch(int D, int sms) { return kPlanBytes + 4 * (size_t)sms * part_bytes(kRows, D); }
 bool paged_few_takes(int rows) { return rows <= kRows; }
 
 cudaError_t launch_paged_few(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches) {
-    return cv.d == 64 ? launch_d<64>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
-                      : launch_d<128>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches);
+    return cv.d == 64 ? launch_t<64>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches)
+                      : launch_t<128>(cv, pv, ch, lens, max_n, o, scratch, sms, stream, launches);
 }
 
 }  // namespace treekv

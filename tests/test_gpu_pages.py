@@ -170,6 +170,22 @@ def test_attend_long(gpu, dtype, d, hq, hkv, past, new, page):
     _check_pages(P)
 
 
+@pytest.mark.parametrize("d,hq,hkv,page", [(128, 16, 16, 16), (64, 32, 8, 64), (128, 32, 4, 128)])
+@pytest.mark.parametrize("longest,count", [(3000, 48), (700, 48), (130, 100), (9000, 5)])
+def test_attend_steps_of_ragged_batches(gpu, d, hq, hkv, page, longest, count):
+    """Blocks take many short units, parts of long ones, and both."""
+    past = [(7919 * i * i + 131 * i) % (longest + 1) for i in range(count)]
+    past[0] = longest
+    new = [1 if i % 5 else 2 for i in range(count)]
+    new[count // 2] = 0
+    P = Prompts(gpu, "bf16", d, hq, hkv, page, past, new, 2, seed=longest)
+    for bound in (longest, None):
+        out, lse = P.attend(max_past=bound)
+        _check_attend(P, out, lse)
+    _check_pages(P)
+    assert P.kv.stats()["device_error"] == 0
+
+
 @pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 128, 32)])
 @pytest.mark.parametrize("past,n", [(0, 200), (70, 7), (300, 150), (64, 64)])
 def test_values_that_are_not_finite(gpu, dtype, d, page, past, n):
