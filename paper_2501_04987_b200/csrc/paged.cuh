@@ -39,6 +39,12 @@ __device__ inline int paged_past(const PagedView& pv, int b, int n) {
 }
 // orders what earlier kernels stored to global memory (the new tokens' rows) before this thread's TMA loads of it
 __device__ inline void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
+// true in one lane of a converged warp
+__device__ inline bool elect_one() {
+    uint32_t p;
+    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
+    return p != 0;
+}
 // a page that cannot be is not followed: page 0 stands in
 __device__ inline int checked_page(const PagedView& pv, int e, DevStats* stats) {
     if ((unsigned)e < (unsigned)pv.n_pages) return e;

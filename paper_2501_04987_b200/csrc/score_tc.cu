@@ -6,9 +6,10 @@
 // one order of additions, one write.  Sums of a tile of rows are added up with a compensation (Kahan), whatever the chunk's
 // length.  Nothing is rounded to fewer than 32 bits.
 //
-// An item is one key tile of one unit (sequence, KV head).  Blocks take items in a row when one tile of queries is all there is
-// (an observation window: the queries stay in shared memory, the keys stream by), and every gridDim-th one otherwise, so that
-// long and short items mix.  With fewer items than the machine has SMs a cluster shares an item's query tiles.
+// An item is one key tile of one unit (sequence, KV head).  Blocks take items in a row when one tile of queries is all there is (an
+// observation window: the queries stay in shared memory, the keys stream by), and every gridDim-th one otherwise, the key tiles that
+// all rows see in front of those that fewer and fewer do: so the blocks end together.  With fewer items than the machine has SMs a
+// cluster shares an item's query tiles.
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 and 6-9 are two groups that take alternate logit tiles.
 #include <algorithm>
@@ -28,34 +29,87 @@ constexpr uint32_t kTmemCols = 512;        // four logit tiles
 constexpr size_t kSmemMin = 120 * 1024;    // one block on an SM: it holds all of the tensor memory
 constexpr int kMaxSplit = 8;
 
-enum Bar { K_FULL = 0, K_FREE = 2, Q_FULL = 4, Q_FREE = 6, S_FULL = 8, S_FREE = 12, JOIN = 16, N_BARS = 17 };
+// Tiles in shared memory: four of keys and two of queries where one query tile is all there is, two and four otherwise.
+constexpr int kTiles = 6, kMost = 4;
 
-// The items of a block in order, the same for every role.
+enum Bar { K_FULL = 0, K_FREE = K_FULL + kMost, Q_FULL = K_FREE + kMost, Q_FREE = Q_FULL + kMost, S_FULL = Q_FREE + kMost, S_FREE = S_FULL + 4,
+           JOIN = S_FREE + 4, N_BARS = JOIN + 1 };
+
+// The items of a block in order, the same for every role: in a row (step 1; a sequence's key tiles head by head, where a division
+// per item would cost as much as its arithmetic), or every step-th (all heads of a key tile, then the next).
 struct Walk {
-    const int* first;
-    int B, Hkv, G, item, step, end, split, rank;
-    const PagedView* pv;
+    const int* first;   // [B + 1] first item of each sequence
+    const int* pasts;   // [B]
     const ChunkLens* lens;
-    int b, kh, k0, past, n, rows, nvis, qa, qb;  // of the item: sequence, head, first key, query tiles [qa, qb) that see the keys
+    int B, Hkv, G, item, step, end;
+    int b, kh, kt, tiles, k0, past, n, rows, nvis, qa, qb;  // of the item: sequence, head, key tile, first key, query tiles [qa, qb) that see the keys
     __device__ bool get() {
         if (item >= end) return false;
-        int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item and has any
-        while (lo < hi) {
-            const int mid = (lo + hi + 1) >> 1;
-            if (first[mid] <= item) lo = mid; else hi = mid - 1;
+        if (b >= 0 && item < first[b + 1]) {
+            if (step == 1) {
+                if (++kt == tiles) { kt = 0; ++kh; }
+            } else {
+                const int at = item - first[b];
+                kt = at / Hkv; kh = at - kt * Hkv;
+            }
+        } else {
+            int lo = max(b, 0), hi = B - 1;   // the last sequence that starts at or before the item
+            while (lo < hi) {
+                const int mid = (lo + hi + 1) >> 1;
+                if (first[mid] <= item) lo = mid; else hi = mid - 1;
+            }
+            b = lo;
+            n = lens->m[b]; past = pasts[b];
+            rows = n * G; nvis = past + n;
+            tiles = (nvis + kTile - 1) / kTile;
+            qb = (rows + kTile - 1) / kTile;
+            const int at = item - first[b];
+            if (step == 1) { kh = at / tiles; kt = at - kh * tiles; }
+            else { kt = at / Hkv; kh = at - kt * Hkv; }
         }
-        b = lo;
-        n = lens->m[b];
-        past = pv->past[b];
-        rows = n * G; nvis = past + n;
-        const int tiles = (nvis + kTile - 1) / kTile, at = item - first[b];
-        kh = at / tiles; k0 = (at - kh * tiles) * kTile;
+        k0 = kt * kTile;
         qa = max(0, k0 - past) * G / kTile;
-        qb = (rows + kTile - 1) / kTile;
         return true;
     }
     __device__ void next() { item += step; }
 };
+
+// 2^x of a pair on the multiply-add units, for the share of the exponentials that the special-function unit would keep waiting:
+// x = n + f with n the nearest integer (Cody and Waite's reduction, here without error) and 2^f by the polynomial of degree 5 with
+// value 1 at 0 and the least largest relative error on [-1/2, 1/2] (found by Lawson's iteration; 1.7e-07 with its roundings, as much
+// as the unit's own).  n is added to the exponent; from 2^-127 down the result is 0.
+__device__ inline float2 ex2_fma(float2 x) {
+    const float big = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, which stands in the low bits
+    x.x = fmaxf(x.x, -127.f); x.y = fmaxf(x.y, -127.f);
+    const float2 one = make_float2(1.f, 1.f);
+    const float2 t = fma2(x, one, make_float2(big, big)), n = fma2(t, one, make_float2(-big, -big)), f = fma2(n, make_float2(-1.f, -1.f), x);
+    float2 p = make_float2(0x1.5bba14p-10f, 0x1.5bba14p-10f);
+    p = fma2(p, f, make_float2(0x1.3cea88p-7f, 0x1.3cea88p-7f));
+    p = fma2(p, f, make_float2(0x1.c6b752p-5f, 0x1.c6b752p-5f));
+    p = fma2(p, f, make_float2(0x1.ebf9bcp-3f, 0x1.ebf9bcp-3f));
+    p = fma2(p, f, make_float2(0x1.62e42ap-1f, 0x1.62e42ap-1f));
+    p = fma2(p, f, make_float2(1.f, 1.f));
+    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
+}
+
+// Sum of exp2(v sc2 + nl) of 32 columns; of those with `masked` only the ones in [lo, hi).  One pair in four goes to the multiply-add
+// units: of none 248 us, of half 262, of one in four 238 (4 x 1024 rows over 5120 keys, 8 KV heads).
+template <bool MASKED>
+__device__ inline void add_columns(const uint32_t (&v)[32], const float* nl, float sc2, int lo, int hi, float2& a, float2& b) {
+    const float2 sc = make_float2(sc2, sc2), one = make_float2(1.f, 1.f);
+#pragma unroll
+    for (int e = 0; e < 32; e += 4) {
+        const Float22 l4 = *reinterpret_cast<const Float22*>(nl + e);
+        const float2 x = fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), sc, l4.lo);
+        const float2 y = fma2(make_float2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), sc, l4.hi);
+        float2 p = make_float2(ex2(x.x), ex2(x.y)), q = (e & 4) == 0 ? ex2_fma(y) : make_float2(ex2(y.x), ex2(y.y));
+        if (MASKED) {
+            p.x = e >= lo && e < hi ? p.x : 0.f; p.y = e + 1 >= lo && e + 1 < hi ? p.y : 0.f;
+            q.x = e + 2 >= lo && e + 2 < hi ? q.x : 0.f; q.y = e + 3 >= lo && e + 3 < hi ? q.y : 0.f;
+        }
+        a = fma2(p, one, a); b = fma2(q, one, b);
+    }
+}
 
 template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
@@ -66,17 +120,19 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     __shared__ uint32_t tmem_slot;
-    __shared__ int s_first[kMaxBatch + 1];
     __shared__ __align__(16) float s_lse[2][2][kTile];     // [group][parity of its steps] minus log-sum-exps in units of log 2
     __shared__ float s_part[2][kTile];                      // the second group's sums
     __shared__ __align__(8) float s_join[kMaxSplit][kTile]; // (block 0 of a cluster) the blocks' sums
     const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
-    const uint32_t sK = base, sQ = base + 2 * SLOT;
+    const int k_log = in_a_row ? 2 : 1, k_slots = 1 << k_log, q_log = 3 - k_log, q_slots = 1 << q_log;
+    const uint32_t sK = base, sQ = base + k_slots * SLOT;
+    int* s_first = reinterpret_cast<int*>(smem_raw + (base - smem_addr_u32(smem_raw)) + kTiles * SLOT);   // [B + 1]
+    int* s_past = s_first + B + 1;                                                                        // [B]
     const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
     const uint32_t bar0 = smem_addr_u32(&bars[0]);
     auto bar = [&](int idx) { return bar0 + 8u * (uint32_t)idx; };
     if (tid == 0) {
-        for (int s = 0; s < 2; ++s) { mbar_init(bar(K_FULL + s), 1); mbar_init(bar(K_FREE + s), 1); mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1); }
+        for (int s = 0; s < kMost; ++s) { mbar_init(bar(K_FULL + s), 1); mbar_init(bar(K_FREE + s), 1); mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1); }
         for (int s = 0; s < 4; ++s) { mbar_init(bar(S_FULL + s), 1); mbar_init(bar(S_FREE + s), 4); }
         mbar_init(bar(JOIN), 4 * kMaxSplit);
         mbar_fence_init();
@@ -87,16 +143,16 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         int sum = 0;
         for (int b0 = 0; b0 < B; b0 += 32) {
             const int b = b0 + lane, n = b < B ? lens.m[b] : 0;
-            int items = 0;
+            int items = 0, past = -1;
             if (n > 0) {
-                const int past = paged_past(pv, b, n);
+                past = paged_past(pv, b, n);
                 if (past < 0) { if (blockIdx.x == 0) atomicOr(&stats->error, kErrBadIndex); }
                 else items = (past + n + kTile - 1) / kTile * Hkv;
             }
             int inc = items;
 #pragma unroll
             for (int o = 1; o < 32; o *= 2) { const int y = __shfl_up_sync(0xffffffffu, inc, o); if (lane >= o) inc += y; }
-            if (b < B) s_first[b] = sum + inc - items;
+            if (b < B) { s_first[b] = sum + inc - items; s_past[b] = past; }
             sum += __shfl_sync(0xffffffffu, inc, 31);
         }
         if (lane == 0) s_first[B] = sum;
@@ -107,7 +163,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     const uint32_t tmem = tmem_slot;
     const int rank = split > 1 ? (int)cluster_cta_rank() : 0, blocks = gridDim.x / split, block = blockIdx.x / split, total = s_first[B];
     Walk w;
-    w.first = s_first; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.pv = &pv; w.lens = &lens; w.split = split; w.rank = rank;
+    w.first = s_first; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.pasts = s_past; w.lens = &lens; w.b = -1;
     if (in_a_row) {
         const int per = (total + blocks - 1) / blocks;
         w.item = min(block * per, total); w.end = min(w.item + per, total); w.step = 1;
@@ -121,16 +177,26 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         // ================= TMA producer
         int kl = 0, ql = 0, last_unit = -1, last_q = -1;
         fence_proxy_async_global();
-        for (; ok && w.get(); w.next()) {
+        const int box = min(pv.page, kTile);
+        // a lane's box of an item's key tile: its page, asked for an item ahead
+        auto entry_of = [&](const Walk& x) {
+            return lane * box < min(kTile, x.nvis - x.k0) ? __ldg(pv.table + (size_t)x.b * pv.width + (x.k0 >> pv.plog) + lane) : 0;
+        };
+        Walk ahead = w;
+        bool more = ahead.get();
+        int e_next = more ? entry_of(ahead) : 0;
+        while (ok && more) {
+            w = ahead;
+            const int e = e_next;
+            ahead.next();
+            more = ahead.get();
+            if (more) e_next = entry_of(ahead);
             if (w.qa + rank >= w.qb) continue;
-            // a key tile: boxes of its pages
-            const int box = min(pv.page, kTile), boxes = (min(kTile, w.nvis - w.k0) + box - 1) / box, p0 = w.k0 >> pv.plog;
-            int e = 0;
-            if (lane < boxes) e = checked_page(pv, __ldg(pv.table + (size_t)w.b * pv.width + p0 + lane), stats);
-            const int row = (e * Hkv + w.kh) * pv.page + (lane == 0 ? w.k0 & (pv.page - 1) : 0);
-            const int slot = kl & 1;
+            const int boxes = (min(kTile, w.nvis - w.k0) + box - 1) / box;
+            const int row = (checked_page(pv, e, stats) * Hkv + w.kh) * pv.page + (lane == 0 ? w.k0 & (pv.page - 1) : 0);
+            const int slot = kl & (k_slots - 1);
             if (lane == 0) {
-                ok = mbar_wait(bar(K_FREE + slot), ((kl >> 1) & 1) ^ 1);
+                ok = mbar_wait(bar(K_FREE + slot), ((kl >> k_log) & 1) ^ 1);
                 if (ok) mbar_arrive_expect_tx(bar(K_FULL + slot), boxes * box * D * 2);
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
@@ -144,8 +210,8 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 const int unit = w.b * Hkv + w.kh;
                 for (int qt = w.qa + rank; qt < w.qb; qt += split) {
                     if (unit == last_unit && qt == last_q) continue;
-                    const int qs = ql & 1;
-                    if (!mbar_wait(bar(Q_FREE + qs), ((ql >> 1) & 1) ^ 1)) { ok = false; break; }
+                    const int qs = ql & (q_slots - 1);
+                    if (!mbar_wait(bar(Q_FREE + qs), ((ql >> q_log) & 1) ^ 1)) { ok = false; break; }
                     mbar_arrive_expect_tx(bar(Q_FULL + qs), q_bytes);
 #pragma unroll
                     for (int h = 0; h < HALVES; ++h)
@@ -158,8 +224,8 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         }
         // nothing may still be on its way into this block's memory when it ends, whatever gave up
         if (lane == 0) {
-            for (int x = max(0, kl - 2); x < kl; ++x) ok = mbar_wait(bar(K_FULL + (x & 1)), (x >> 1) & 1) && ok;
-            for (int x = max(0, ql - 2); x < ql; ++x) ok = mbar_wait(bar(Q_FULL + (x & 1)), (x >> 1) & 1) && ok;
+            for (int x = max(0, kl - k_slots); x < kl; ++x) ok = mbar_wait(bar(K_FULL + (x & (k_slots - 1))), (x >> k_log) & 1) && ok;
+            for (int x = max(0, ql - q_slots); x < ql; ++x) ok = mbar_wait(bar(Q_FULL + (x & (q_slots - 1))), (x >> q_log) & 1) && ok;
             if (!ok) atomicOr(&stats->error, 4u);
         }
     } else if (warp == 1) {
@@ -170,19 +236,21 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             int kl = 0, ql = -1, st = 0, last_unit = -1, last_q = -1;
             for (; ok && w.get(); w.next()) {
                 if (w.qa + rank >= w.qb) continue;
-                const int slot = kl & 1, unit = w.b * Hkv + w.kh;
-                if (!(ok = mbar_wait(bar(K_FULL + slot), (kl >> 1) & 1))) break;
+                const int slot = kl & (k_slots - 1), unit = w.b * Hkv + w.kh;
+                if (!(ok = mbar_wait(bar(K_FULL + slot), (kl >> k_log) & 1))) break;
                 for (int qt = w.qa + rank; qt < w.qb; qt += split) {
-                    if (!(unit == last_unit && qt == last_q)) {
-                        if (ql >= 0) umma_commit(bar(Q_FREE + (ql & 1)));  // the tile before is not needed any more
-                        ++ql;
-                        if (!(ok = mbar_wait(bar(Q_FULL + (ql & 1)), (ql >> 1) & 1))) break;
-                        last_unit = unit; last_q = qt;
-                    }
                     const int buf = st & 3;
-                    if (!(ok = mbar_wait(bar(S_FREE + buf), ((st >> 2) & 1) ^ 1))) break;
+                    if (!(unit == last_unit && qt == last_q)) {
+                        if (ql >= 0) umma_commit(bar(Q_FREE + (ql & (q_slots - 1))));  // the tile before is not needed any more
+                        ++ql;
+                        ok = mbar_wait2(bar(Q_FULL + (ql & (q_slots - 1))), (ql >> q_log) & 1, bar(S_FREE + buf), ((st >> 2) & 1) ^ 1);
+                        last_unit = unit; last_q = qt;
+                    } else {
+                        ok = mbar_wait(bar(S_FREE + buf), ((st >> 2) & 1) ^ 1);
+                    }
+                    if (!ok) break;
                     tc_fence_after();
-                    const uint32_t a = k_lo + slot * (SLOT / 16), q = q_lo + (ql & 1) * (SLOT / 16);
+                    const uint32_t a = k_lo + slot * (SLOT / 16), q = q_lo + (ql & (q_slots - 1)) * (SLOT / 16);
 #pragma unroll
                     for (int kk = 0; kk < D / 16; ++kk)
                         umma_bf16(tmem + buf * kTile, desc_of(a + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), desc_of(q + (kk >> 2) * (HALF / 16) + (kk & 3) * 2),
@@ -196,7 +264,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             }
             // every MMA has finished before its memory and tensor memory are given to anything else
             for (int x = max(0, st - 4); x < st; ++x) ok = mbar_wait(bar(S_FULL + (x & 3)), (x >> 2) & 1) && ok;
-            if (ok && kl > 0) ok = mbar_wait(bar(K_FREE + ((kl - 1) & 1)), ((kl - 1) >> 1) & 1);
+            if (ok && kl > 0) ok = mbar_wait(bar(K_FREE + ((kl - 1) & (k_slots - 1))), ((kl - 1) >> k_log) & 1);
             if (!ok) atomicOr(&stats->error, 8u);
         }
     } else {
@@ -204,7 +272,8 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const int group = (warp - 2) >> 2, quarter = warp & 3, key = quarter * 32 + lane;
         const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
         const float sc2 = kLog2e * rsqrtf((float)D), over = 1.0f / (float)w.G;
-        int st = 0, mine = 0, shared = 0;  // steps of the block, of this group; items that both groups had steps of
+        int st = 0, mine = 0, shared = 0;  // steps of the block; of this group, those with log-sum-exps of their own; items that both groups had steps of
+        int held_unit = -1, held_q = -1;   // whose log-sum-exps this group has in shared memory
         for (; ok && w.get(); w.next()) {
             float sum = 0.f, comp = 0.f;
             const int kpos = w.k0 + key, r_min = max(0, kpos - w.past) * w.G;  // first row that sees this key
@@ -212,21 +281,27 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 const int r = qt * kTile + key;
                 return qt < w.qb && r < w.rows ? sa.lse[((size_t)w.b * ch.stride + r / w.G) * Hq + w.kh * w.G + r % w.G] : INFINITY;
             };
-            const int steps = w.qa + rank < w.qb ? (w.qb - w.qa - rank + split - 1) / split : 0;
+            const int steps = w.qa + rank < w.qb ? split == 1 ? w.qb - w.qa : (w.qb - w.qa - rank + split - 1) / split : 0;
             const bool both = steps > 1;         // each group has steps of this item
             int x = (st & 1) == group ? 0 : 1;   // this group's first step of the item
-            float l_next = x < steps ? lse_of(w.qa + rank + x * split) : 0.f;
+            const int unit = w.b * Hkv + w.kh, q_first = w.qa + rank + x * split;
+            const bool held = steps == 1 && unit == held_unit && q_first == held_q;   // the log-sum-exps of the step before
+            float l_next = x < steps && !held ? lse_of(q_first) : 0.f;
+            if (x < steps) { held_unit = unit; held_q = w.qa + rank + (x + (steps - 1 - x) / 2 * 2) * split; }
             for (; x < steps; x += 2) {
                 const int qt = w.qa + rank + x * split, s = st + x, buf = s & 3;
-                float* nl = s_lse[group][mine & 1];
-                nl[key] = l_next == -INFINITY ? -INFINITY : -l_next * kLog2e;  // (a row that saw nothing gives nothing; no row: minus infinity)
-                asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+                if (!held) {
+                    ++mine;
+                    s_lse[group][mine & 1][key] = l_next == -INFINITY ? -INFINITY : -l_next * kLog2e;  // (a row that saw nothing gives nothing; no row: minus infinity)
+                    asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
+                }
+                const float* nl = s_lse[group][mine & 1];
                 if (x + 2 < steps) l_next = lse_of(qt + 2 * split);
                 if (!mbar_wait(bar(S_FULL + buf), (s >> 2) & 1)) { ok = false; break; }
                 tc_fence_after();
                 const int cmin = r_min - qt * kTile, cmax = w.rows - qt * kTile;     // columns [cmin, cmax) are rows that see the key
-                const bool full = __all_sync(0xffffffffu, cmin <= 0) && cmax >= kTile;
-                float a0 = 0.f, a1 = 0.f, a2 = 0.f, a3 = 0.f;
+                const int from = __reduce_max_sync(0xffffffffu, cmin), lead = __reduce_min_sync(0xffffffffu, cmin);
+                float2 a0 = make_float2(0.f, 0.f), a1 = a0;
                 uint32_t v[2][32];
                 tmem_ld32(tmem + buf * kTile + lane_off, v[0]);
 #pragma unroll
@@ -234,27 +309,18 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                     tmem_ld_wait_for(v[cg & 1]);
                     if (cg < 3) {
                         tmem_ld32(tmem + buf * kTile + lane_off + (cg + 1) * 32, v[(cg + 1) & 1]);
+                    } else {   // all logits are in registers
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) mbar_arrive(bar(S_FREE + buf));
                     }
-#pragma unroll
-                    for (int e = 0; e < 32; e += 4) {
-                        const float4 l4 = *reinterpret_cast<const float4*>(nl + cg * 32 + e);
-                        float p0 = ex2(fmaf(__uint_as_float(v[cg & 1][e]), sc2, l4.x)), p1 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 1]), sc2, l4.y));
-                        float p2 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 2]), sc2, l4.z)), p3 = ex2(fmaf(__uint_as_float(v[cg & 1][e + 3]), sc2, l4.w));
-                        if (!full) {
-                            const int c = cg * 32 + e;
-                            p0 = c >= cmin && c < cmax ? p0 : 0.f; p1 = c + 1 >= cmin && c + 1 < cmax ? p1 : 0.f;
-                            p2 = c + 2 >= cmin && c + 2 < cmax ? p2 : 0.f; p3 = c + 3 >= cmin && c + 3 < cmax ? p3 : 0.f;
-                        }
-                        a0 += p0; a1 += p1; a2 += p2; a3 += p3;
-                    }
+                    // (the warp agrees: all columns of all its keys, none, or some)
+                    if (from <= cg * 32 && cmax >= cg * 32 + 32) add_columns<false>(v[cg & 1], nl + cg * 32, sc2, 0, 32, a0, a1);
+                    else if (lead < cg * 32 + 32 && cmax > cg * 32) add_columns<true>(v[cg & 1], nl + cg * 32, sc2, cmin - cg * 32, cmax - cg * 32, a0, a1);
                 }
-                tc_fence_before();
-                __syncwarp();
-                if (lane == 0) mbar_arrive(bar(S_FREE + buf));
-                const float y = ((a0 + a1) + (a2 + a3)) - comp, t = sum + y;  // compensated
+                const float y = ((a0.x + a0.y) + (a1.x + a1.y)) - comp, t = sum + y;  // compensated
                 comp = (t - sum) - y;
                 sum = t;
-                ++mine;
             }
             if (!ok) break;
             // the group that took the item's first step writes; the other one's sum comes through shared memory
@@ -316,13 +382,13 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     const uint32_t kbox[2] = {64u, (uint32_t)std::min(pv.page, kTile)};
     if (!make_tensor_map_bf16(&tmK, pv.kp, 2, dims, strides, kbox)) return cudaErrorInvalidValue;
     auto kern = score_tc_kernel<D>;
-    const size_t smem = std::max(kSmemMin, (size_t)1024 + 4 * kTile * D * 2);
+    const size_t smem = std::max(kSmemMin, (size_t)1024 + kTiles * kTile * D * 2 + 4 * (2 * (size_t)cv.B + 1));
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
     cudaGetDevice(&dev);
     dev &= 63;
     if (!smem_set[dev]) {
-        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)smem);
+        const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 1024 + kTiles * kTile * 128 * 2 + 4 * (2 * kMaxBatch + 1));
         if (e != cudaSuccess) return e;
         smem_set[dev] = true;
     }
