@@ -42,6 +42,7 @@ cudaError_t launch_paged_append(const CacheView& cv, treekv_dtype dt, const Page
 namespace {
 
 constexpr int kMaxChunkRows = 32768;
+constexpr int kLongRows = 256;  // query rows a KV head beyond which a block takes 256 of them
 
 inline bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 
@@ -85,7 +86,9 @@ extern "C" {
 
 size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride) {
     if (!ctx || stride < 1 || stride > kMaxChunkRows || ctx->dt != TREEKV_BF16) return 0;
-    return paged_few_scratch(ctx->cv.d, ctx->sm_count);  // (a call of a longer chunk may still have few tokens in every sequence)
+    // (a call of a longer chunk may still have few tokens in every sequence)
+    const size_t few = paged_few_scratch(ctx->cv.d, ctx->sm_count), many = paged_tc2_scratch(ctx->cv.d, ctx->sm_count);
+    return stride * ctx->G > kLongRows && many > few ? many : few;
 }
 
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,
@@ -113,7 +116,9 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
     const PagedOut o = {dev_out, dev_lse};
     cudaError_t e;
     int launches = 2;
-    if (ctx->dt == TREEKV_BF16 && paged_few_takes(max_n * ctx->G)) {
+    if (ctx->dt == TREEKV_BF16 && max_n * ctx->G > kLongRows) {
+        e = launch_paged_tc2(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
+    } else if (ctx->dt == TREEKV_BF16 && paged_few_takes(max_n * ctx->G)) {
         e = launch_paged_few(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
     } else {
         e = launch_paged_append(ctx->cv, ctx->dt, pv, ch, lens, max_n, s);

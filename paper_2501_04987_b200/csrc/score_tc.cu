@@ -14,6 +14,7 @@
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 and 6-9 are two groups that take alternate logit tiles.
 #include <algorithm>
 
+#include "exp2_fma.cuh"
 #include "paged.cuh"
 #include "verify_tc.cuh"
 
@@ -74,24 +75,6 @@ struct Walk {
     __device__ void next() { item += step; }
 };
 
-// 2^x of a pair on the multiply-add units, for the share of the exponentials that the special-function unit would keep waiting:
-// x = n + f with n the nearest integer (Cody and Waite's reduction, here without error) and 2^f by the polynomial of degree 5 with
-// value 1 at 0 and the least largest relative error on [-1/2, 1/2] (found by Lawson's iteration; 1.7e-07 with its roundings, as much
-// as the unit's own).  n is added to the exponent; from 2^-127 down the result is 0.
-__device__ inline float2 ex2_fma(float2 x) {
-    const float big = 12582912.f;  // 1.5 * 2^23: adding it rounds to an integer, which stands in the low bits
-    x.x = fmaxf(x.x, -127.f); x.y = fmaxf(x.y, -127.f);
-    const float2 one = make_float2(1.f, 1.f);
-    const float2 t = fma2(x, one, make_float2(big, big)), n = fma2(t, one, make_float2(-big, -big)), f = fma2(n, make_float2(-1.f, -1.f), x);
-    float2 p = make_float2(0x1.5bba14p-10f, 0x1.5bba14p-10f);
-    p = fma2(p, f, make_float2(0x1.3cea88p-7f, 0x1.3cea88p-7f));
-    p = fma2(p, f, make_float2(0x1.c6b752p-5f, 0x1.c6b752p-5f));
-    p = fma2(p, f, make_float2(0x1.ebf9bcp-3f, 0x1.ebf9bcp-3f));
-    p = fma2(p, f, make_float2(0x1.62e42ap-1f, 0x1.62e42ap-1f));
-    p = fma2(p, f, make_float2(1.f, 1.f));
-    return make_float2(__int_as_float(__float_as_int(p.x) + (__float_as_int(t.x) << 23)), __int_as_float(__float_as_int(p.y) + (__float_as_int(t.y) << 23)));
-}
-
 // Sum of exp2(v sc2 + nl) of 32 columns; of those with `masked` only the ones in [lo, hi).  One pair in four goes to the multiply-add
 // units: of none 248 us, of half 262, of one in four 238 (4 x 1024 rows over 5120 keys, 8 KV heads).
 template <bool MASKED>
@@ -102,7 +85,7 @@ __device__ inline void add_columns(const uint32_t (&v)[32], const float* nl, flo
         const Float22 l4 = *reinterpret_cast<const Float22*>(nl + e);
         const float2 x = fma2(make_float2(__uint_as_float(v[e]), __uint_as_float(v[e + 1])), sc, l4.lo);
         const float2 y = fma2(make_float2(__uint_as_float(v[e + 2]), __uint_as_float(v[e + 3])), sc, l4.hi);
-        float2 p = make_float2(ex2(x.x), ex2(x.y)), q = (e & 4) == 0 ? ex2_fma(y) : make_float2(ex2(y.x), ex2(y.y));
+        float2 p = make_float2(ex2(x.x), ex2(x.y)), q = (e & 4) == 0 ? exp2_fma(y) : make_float2(ex2(y.x), ex2(y.y));
         if (MASKED) {
             p.x = e >= lo && e < hi ? p.x : 0.f; p.y = e + 1 >= lo && e + 1 < hi ? p.y : 0.f;
             q.x = e + 2 >= lo && e + 2 < hi ? q.x : 0.f; q.y = e + 3 >= lo && e + 3 < hi ? q.y : 0.f;

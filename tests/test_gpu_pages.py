@@ -236,6 +236,23 @@ def test_infinite_keys_behind_a_row(gpu):
         assert bool(s.isfinite().all()) and bool((s[0, 0, 70:] == 0).all())
 
 
+@pytest.mark.parametrize("dtype,n", [("bf16", 3), ("bf16", 40), ("bf16", 300), ("f32", 40)])
+def test_keys_that_are_nan_or_infinite_reach_every_row_that_sees_them(gpu, dtype, n):
+    """Wherever in a tile the key stands."""
+    import torch
+
+    for at in (0, 2, 5, 6, 7, 31, 63, 64, 70, 127, 133):
+        P = Prompts(gpu, dtype, 64, 2, 1, 16, [134], [n], n, seed=at)
+        P.kp[P.table[0, at // 16], 0, at % 16, 3] = math.nan
+        out, lse = P.attend()
+        assert bool(out.isnan().all()) and bool(lse.isnan().all())
+        s = torch.zeros((1, 1, 134 + n), device="cuda")
+        P.kv.paged_score(P.q, torch.full_like(lse, 3.0), P.kp, P.table, P.past_dev, s)
+        want = torch.zeros(134 + n, dtype=torch.bool, device="cuda")
+        want[at] = True
+        assert torch.equal(s[0, 0].isnan(), want)
+
+
 def test_shared_pages_and_an_identical_table(gpu):
     """Sequences that share the pages of a prefix, and the first page used twice by one."""
     import torch
