@@ -342,24 +342,32 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                         if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
                         unsigned char* tile = base_ptr + 2 * SLOT + rv.slot * SLOT;
                         const int valid = own ? min(kTile, it.t_end - i0) : it.past - jj * kTile, first = own ? max(0, it.tok0 + 1 - i0) : valid;
-                        for (int e = gt + first * (D / 8); e < kTile * (D / 8); e += 128) {
-                            const int rr = e / (D / 8), c = e % (D / 8);
-                            uint4* at = reinterpret_cast<uint4*>(tile + (c >> 3) * HALF + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
-                            uint4 y = make_uint4(0, 0, 0, 0);
-                            bool changed = rr >= valid;
-                            if (rr < valid) {
-                                y = *at;
-                                uint32_t* q = &y.x;
+                        // piece c of rows rr0, rr0 + RPI, ...: looked at first, and touched only where there is something to do
+                        constexpr int RPI = 128 / (D / 8), N = kTile / RPI;
+                        const int c = gt % (D / 8), rr0 = gt / (D / 8);
+                        auto piece = [&](int u) { const int rr = rr0 + RPI * u; return reinterpret_cast<uint4*>(tile + (c >> 3) * HALF + rr * 128 + (((c & 7) ^ (rr & 7)) << 4)); };
+                        auto odd = [](uint32_t w) { return (w & 0x7f80u) == 0x7f80u || (w & 0x7f800000u) == 0x7f800000u; };
+                        uint32_t some = 0;   // pieces with a value that is not finite
 #pragma unroll
-                                for (int u = 0; u < 4; ++u) {
-                                    const uint32_t lo = (q[u] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u, hi = (q[u] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u;
-                                    if (lo | hi) { q[u] &= ~(lo | hi); changed = true; }
-                                }
-                                const int bit = i0 + rr - it.tok0;
-                                if (changed) atomicOr(&s_bad[bit >> 5], 1u << (bit & 31));
-                            }
-                            if (changed) *at = y;
+                        for (int u = 0; u < N; ++u) {
+                            const uint4 y = *piece(u);
+                            if (odd(y.x) || odd(y.y) || odd(y.z) || odd(y.w)) some |= 1u << u;
                         }
+#pragma unroll 1
+                        for (; some; some &= some - 1) {
+                            const int u = __ffs((int)some) - 1, rr = rr0 + RPI * u;
+                            if (rr < first || rr >= valid) continue;
+                            uint4 y = *piece(u);
+                            uint32_t* q = &y.x;
+#pragma unroll
+                            for (int k = 0; k < 4; ++k)
+                                q[k] &= ~(((q[k] & 0x7f80u) == 0x7f80u ? 0xffffu : 0u) | ((q[k] & 0x7f800000u) == 0x7f800000u ? 0xffff0000u : 0u));
+                            *piece(u) = y;
+                            const int bit = i0 + rr - it.tok0;
+                            atomicOr(&s_bad[bit >> 5], 1u << (bit & 31));
+                        }
+#pragma unroll 1
+                        for (int u = (max(0, valid - rr0) + RPI - 1) / RPI; u < N; ++u) *piece(u) = make_uint4(0, 0, 0, 0);
                         fence_proxy_async_smem();
                     }
                     const float mr = ref == -INFINITY ? 0.f : -ref;
