@@ -50,12 +50,17 @@ struct Parts2 {
 };
 inline size_t part_bytes(int D) { return 32 + kRows * 8 + (size_t)kRows * D * 4; }
 
-// Item x of the call: units in a row, of each the rows at the end - the longest - first.
+// The order of a call's items: as many units at a time as make about one wave (their keys stay in L2), of all of them the rows at the
+// end - which see the most - first, so that blocks end together.
+struct Order {
+    int units, group, per_unit;  // units at a time; items of a unit, at most
+};
 struct Item {
     int b, kh, n, past, r0, rows, tok0, t_end, cached, tiles;  // tokens [tok0, t_end); key tiles over the pages, all
     // false: nothing to do
-    __device__ bool get(const PagedView& pv, const ChunkLens& lens, int x, int per_unit, int G, int Hkv) {
-        const int unit = x / per_unit, at = x - unit * per_unit;
+    __device__ bool get(const PagedView& pv, const ChunkLens& lens, int x, const Order& od, int G, int Hkv) {
+        const int wave = x / (od.group * od.per_unit), first = wave * od.group, here = min(od.group, od.units - first);
+        const int y = x - first * od.per_unit, at = y / here, unit = first + y - at * here;
         b = unit / Hkv; kh = unit - b * Hkv;
         n = lens.m[b];
         const int mine = (n * G + kRows - 1) / kRows;
@@ -107,7 +112,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, PagedView pv, ChunkView ch, ChunkLens lens,
-                 PagedOut po, Parts2 parts, int Hq, int Hkv, DevStats* stats, int per_unit, int n_whole, int q_bytes, int slots) {
+                 PagedOut po, Parts2 parts, int Hq, int Hkv, DevStats* stats, Order od, int n_whole, int q_bytes, int slots) {
     constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128;
     const int G = Hq / Hkv;
     pdl_trigger();
@@ -138,7 +143,7 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const bool whole = (int)blockIdx.x < n_whole;
     const int part = (int)blockIdx.x - n_whole, x = whole ? (int)blockIdx.x : n_whole + (part >> 1);
     Item it;
-    const bool some = it.get(pv, lens, x, per_unit, G, Hkv);
+    const bool some = it.get(pv, lens, x, od, G, Hkv);
     if (some && it.past < 0 && tid == 0) atomicOr(&stats->error, kErrBadIndex);
     // key tiles [j0, j0 + NT)
     const int j0 = some && !whole && (part & 1) ? (it.tiles + 1) / 2 : 0;
@@ -468,13 +473,13 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
 // Joins the two parts of the items that were cut: D / 4 threads a row.
 template <int D>
 __global__ void __launch_bounds__(128)
-paged_join2_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts2 parts, int Hq, int Hkv, int per_unit, int n_whole) {
+paged_join2_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts2 parts, int Hq, int Hkv, Order od, int n_whole) {
     constexpr int LPR = D / 4;
     pdl_trigger();
     pdl_wait();
     const int G = Hq / Hkv, row = blockIdx.y * (128 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;
     Item it;
-    if (!it.get(pv, lens, n_whole + blockIdx.x, per_unit, G, Hkv) || it.past < 0 || row >= it.rows) return;
+    if (!it.get(pv, lens, n_whole + blockIdx.x, od, G, Hkv) || it.past < 0 || row >= it.rows) return;
     const size_t p0 = 2 * (size_t)blockIdx.x, p1 = p0 + 1;
     const float2 s0 = parts.stat[p0 * kRows + row], s1 = parts.stat[p1 * kRows + row];
     const float4 x = *reinterpret_cast<const float4*>(parts.o + (p0 * kRows + row) * D + 4 * c), y = *reinterpret_cast<const float4*>(parts.o + (p1 * kRows + row) * D + 4 * c);
@@ -528,16 +533,17 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     // A last wave that is at most half full: its items are cut in two, where there are enough keys for two.
     const bool cut = left > 0 && 2 * left <= sms && (pv.max_past + max_n) >= 8 * kTile;
     const int n_whole = cut ? items - left : items;
+    const Order od = {cv.B * cv.Hkv, std::max(1, sms / per_unit), per_unit};
     Parts2 parts;
     char* at = static_cast<char*>(scratch);
     parts.bad = reinterpret_cast<uint32_t*>(at); at += (size_t)sms * 32;
     parts.stat = reinterpret_cast<float2*>(at); at += (size_t)sms * kRows * 8;
     parts.o = reinterpret_cast<float*>(at);
     cudaError_t e = launch_pdl(kern, dim3((unsigned)(n_whole + 2 * (items - n_whole))), dim3(kThreads), smem, stream, tmQ, tmK, tmV, tmKn, tmVn, pv, ch, lens, o,
-                               parts, cv.Hq, cv.Hkv, cv.stats, per_unit, n_whole, (D / 64) * 128 * box * G, slots);
+                               parts, cv.Hq, cv.Hkv, cv.stats, od, n_whole, (D / 64) * 128 * box * G, slots);
     *launches = cut ? 2 : 1;
     if (e != cudaSuccess || !cut) return e;
-    return launch_pdl(paged_join2_kernel<D>, dim3(items - n_whole, kRows / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, per_unit, n_whole);
+    return launch_pdl(paged_join2_kernel<D>, dim3(items - n_whole, kRows / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, od, n_whole);
 }
 
 }  // namespace
