@@ -372,7 +372,7 @@ int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64
  * the call; pages that are only read can be shared.  The outputs must not overlap the inputs.  A token's value never enters
  * rows in front of it, also where it is not finite.
  *   dev_scratch     treekv_paged_scratch_bytes(ctx, stride) bytes, 256-byte aligned, used until the call's work is done: calls that
- *                   may overlap need one each (TREEKV_ERR_WORKSPACE; 0 bytes and NULL for fp32)
+ *                   may overlap need one each (TREEKV_ERR_WORKSPACE when missing, misaligned or too small)
  */
 size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride);
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,

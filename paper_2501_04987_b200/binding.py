@@ -545,9 +545,9 @@ class TreeKV:
             pl = want(lse, self.torch.float32, (B, n, Hq), "lse")
         pn, kept = self._lens(lens, "chunk lengths")
         nbytes = lib.treekv_paged_scratch_bytes(self._h, n)
-        scratch = q.new_empty(nbytes, dtype=self.torch.uint8) if nbytes else None   # (torch keeps it for this stream's later work)
+        scratch = q.new_empty(nbytes, dtype=self.torch.uint8)   # (torch keeps it for this stream's later work)
         st = lib.treekv_paged_attend(self._h, pq, pk, pv, kp, vp, pages, page, pt, width, pp, width * page if max_past is None else max_past,
-                                     po, pl, pn, n, None if scratch is None else scratch.data_ptr(), nbytes, self._stream())
+                                     po, pl, pn, n, scratch.data_ptr(), nbytes, self._stream())
         if st:
             _check(st, "treekv_paged_attend")
         return out, lse

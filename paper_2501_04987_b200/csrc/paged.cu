@@ -85,7 +85,8 @@ treekv_status chunk_lens(const treekv_ctx* ctx, const int32_t* host_lens, int st
 extern "C" {
 
 size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride) {
-    if (!ctx || stride < 1 || stride > kMaxChunkRows || ctx->dt != TREEKV_BF16) return 0;
+    if (!ctx || stride < 1 || stride > kMaxChunkRows) return 0;
+    if (ctx->dt == TREEKV_F32) return paged_f32_scratch(ctx->cv.d);
     // (a call of a longer chunk may still have few tokens in every sequence)
     const size_t few = paged_few_scratch(ctx->cv.d, ctx->sm_count), many = paged_tc2_scratch(ctx->cv.d, ctx->sm_count);
     return stride * ctx->G > kLongRows && many > few ? many : few;
@@ -107,7 +108,7 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
     int max_n;
     st = chunk_lens(ctx, host_lens, stride, &lens, &max_n);
     if (st != TREEKV_OK) return st;
-    if (scratch_bytes < treekv_paged_scratch_bytes(ctx, stride) || (ctx->dt == TREEKV_BF16 && (!dev_scratch || !aligned(dev_scratch, 256))))
+    if (!dev_scratch || !aligned(dev_scratch, 256) || scratch_bytes < treekv_paged_scratch_bytes(ctx, stride))
         return TREEKV_ERR_WORKSPACE;
     if (max_n == 0) return TREEKV_OK;
     if (!on_own_device(ctx)) return TREEKV_ERR_BAD_STATE;
@@ -120,11 +121,11 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
         e = launch_paged_tc2(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
     } else if (ctx->dt == TREEKV_BF16 && paged_few_takes(max_n * ctx->G)) {
         e = launch_paged_few(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
-    } else {
+    } else if (ctx->dt == TREEKV_BF16) {
         e = launch_paged_append(ctx->cv, ctx->dt, pv, ch, lens, max_n, s);
-        if (e == cudaSuccess)
-            e = ctx->dt == TREEKV_BF16 ? launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s)
-                                       : launch_paged_f32(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s);
+        if (e == cudaSuccess) e = launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s);
+    } else {
+        e = launch_paged_f32(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
     }
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     ctx->launches += launches;

@@ -61,15 +61,17 @@ bool paged_few_takes(int rows);
 size_t paged_few_scratch(int D, int sms);
 cudaError_t launch_paged_few(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches);
-// the same of long chunks: 256 rows a block (bf16)
+// of long chunks: 256 rows a block; the new tokens enter their pages with it (bf16)
 size_t paged_tc2_scratch(int D, int sms);
 cudaError_t launch_paged_tc2(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches);
-// attention of the new tokens, which are in their pages
+// and between the two, of tokens that are in their pages already (bf16)
 cudaError_t launch_paged_tc(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                             int sms, cudaStream_t stream);
+// fp32; the new tokens enter their pages with it
+size_t paged_f32_scratch(int D);
 cudaError_t launch_paged_f32(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
-                             int sms, cudaStream_t stream);
+                             void* scratch, int sms, cudaStream_t stream, int* launches);
 
 // what rows of a chunk gave to the tokens of their sequence
 struct ScoreArgs {

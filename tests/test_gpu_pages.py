@@ -161,7 +161,7 @@ def test_attend(gpu, dtype, d, hq, hkv, page, past, new):
 
 @pytest.mark.parametrize("dtype,d,hq,hkv,past,new,page", [
     ("bf16", 128, 8, 2, [9000], [1], 16), ("bf16", 128, 32, 8, [2500, 40, 3100], [300, 700, 1], 64), ("bf16", 128, 8, 8, [0], [2049], 128),
-    ("bf16", 64, 8, 1, [5001], [600], 32), ("f32", 128, 8, 2, [4100, 1], [2, 70], 16), ("f32", 64, 2, 2, [70], [900], 64),
+    ("bf16", 64, 8, 1, [5001], [600], 32), ("f32", 128, 8, 2, [4100, 1], [2, 70], 16), ("f32", 64, 8, 1, [20000], [2], 64), ("f32", 128, 2, 1, [9000, 17, 0], [9, 0, 30], 16), ("f32", 64, 2, 2, [70], [900], 64),
     ("bf16", 128, 8, 8, [130, 7] * 20, [200, 260] * 20, 64)])
 def test_attend_long(gpu, dtype, d, hq, hkv, past, new, page):
     P = Prompts(gpu, dtype, d, hq, hkv, page, past, new, max(new), seed=7, scale=1.5)
@@ -187,7 +187,7 @@ def test_attend_steps_of_ragged_batches(gpu, d, hq, hkv, page, longest, count):
 
 
 @pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 128, 32)])
-@pytest.mark.parametrize("past,n", [(0, 200), (70, 7), (300, 150), (64, 64)])
+@pytest.mark.parametrize("past,n", [(0, 200), (70, 7), (300, 150), (64, 64), (9000, 6)])
 def test_values_that_are_not_finite(gpu, dtype, d, page, past, n):
     """A value of infinity or NaN reaches the rows that see its token and no other."""
     import torch
