@@ -9,6 +9,11 @@
 // shared memory - and what the slices hold tells where to look.  A last walk writes the tokens' positions and sums to the rows
 // where they will lie.  The second launch moves the keys and values: it reads a row's position and fetches the token from its
 // page.
+//
+// The bytes are few - the weights once, the kept rows in and out - so the second launch runs at memory's rate (64 units of 1024 rows,
+// 67 MB: 12 us) and the first one at the latency of its chain: weights from L2, shared-memory counters where most weights share a
+// few exponents, three walks over the counters.  64 units of up to 8192 tokens: 21 us for both, of which 10 are the bytes'; 8 units
+// of 100000 with averages: 27 us.  With blocks of 512 threads it was 31 and 37.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -18,9 +23,11 @@ namespace treekv {
 
 namespace {
 
-constexpr int kThreads = 512, kWarps = kThreads / 32;
-constexpr int kMaxSplit = 8;
+constexpr int kThreads = 1024, kWarps = kThreads / 32;
+constexpr int kMaxSplit = 16;
 constexpr int kBins = 2048;
+constexpr int kAlone = 12288;    // tokens that one block takes alone
+constexpr int kShare = 4096;     // of one that shares a unit
 constexpr int kHeld = 48 * 1024;  // weights in shared memory
 
 // Weights as integers in the order of the numbers; NaN below all of them, minus zero as zero.
@@ -148,36 +155,53 @@ __global__ void __launch_bounds__(kThreads) adopt_select_kernel(CacheView cv, co
     }
     // prefix: the last weight that stays; `need` of the tokens that have it stay
     uint32_t more = 0, same = 0;
-    if (!all)
-        for (int t = w0 + lane; t - lane < w1; t += 32) {
-            const uint32_t k = t < w1 ? key(t) : 0u;
-            more += __popc(__ballot_sync(0xffffffffu, t < w1 && k > prefix));
-            same += __popc(__ballot_sync(0xffffffffu, t < w1 && k == prefix));
+    if (!all) {
+#pragma unroll 4
+        for (int t = w0 + lane; t < w1; t += 32) {
+            const uint32_t k = key(t);
+            more += k > prefix;
+            same += k == prefix;
         }
+        more = __reduce_add_sync(0xffffffffu, more);
+        same = __reduce_add_sync(0xffffffffu, same);
+    }
     if (lane == 0) { s_count[0][warp] = more; s_count[1][warp] = same; }
     __syncthreads();
     uint32_t n_more = 0, n_same = 0;  // before this warp's tokens
     if constexpr (SPLIT > 1) {
-        if (tid < SPLIT) {
-            uint32_t x = 0, y = 0;
-            for (int w = 0; w < kWarps; ++w) { x += s_count[0][w]; y += s_count[1][w]; }
-            asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(s_block[rank]), tid)), "r"(x), "r"(y) : "memory");
+        if (warp == 0) {
+            const uint32_t x = __reduce_add_sync(0xffffffffu, s_count[0][lane]), y = __reduce_add_sync(0xffffffffu, s_count[1][lane]);
+            if (lane < SPLIT)
+                asm volatile("st.shared::cluster.v2.u32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(s_block[rank]), lane)), "r"(x), "r"(y) : "memory");
         }
         __syncwarp();
         cluster_sync_all();           // the last word from any other block
         for (int s = 0; s < rank; ++s) { n_more += s_block[s][0]; n_same += s_block[s][1]; }
     }
-    for (int w = 0; w < warp; ++w) { n_more += s_count[0][w]; n_same += s_count[1][w]; }
+    n_more += __reduce_add_sync(0xffffffffu, lane < warp ? s_count[0][lane] : 0u);
+    n_same += __reduce_add_sync(0xffffffffu, lane < warp ? s_count[1][lane] : 0u);
     int32_t* pos = cv.pos + (size_t)unit * cv.R;
     float* sum = cv.S + (size_t)unit * cv.R;
     auto put = [&](int lam, int t) { const int r = phys_row(lam, st); pos[r] = t; sum[r] = __ldg(row + t); };
     if (!all) {
-        for (int t = w0 + lane; t - lane < w1; t += 32) {
-            const uint32_t k = t < w1 ? key(t) : 0u, below = (1u << lane) - 1u;
-            const uint32_t m = __ballot_sync(0xffffffffu, t < w1 && k > prefix), e = __ballot_sync(0xffffffffu, t < w1 && k == prefix);
-            const uint32_t at_m = n_more + __popc(m & below), at_e = n_same + __popc(e & below);
-            if ((m >> lane & 1u) || ((e >> lane & 1u) && at_e < need)) put(cv.ns + (int)(at_m + min(at_e, need)), t);
-            n_more += __popc(m); n_same += __popc(e);
+        constexpr int U = 4;   // groups of 32 at a time, so that their sums are on the way together
+        const uint32_t below = (1u << lane) - 1u;
+        for (int t0 = w0 + lane; t0 - lane < w1; t0 += 32 * U) {
+            int lam[U];
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int t = t0 + 32 * u;
+                const uint32_t k = t < w1 ? key(t) : 0u;
+                const uint32_t m = __ballot_sync(0xffffffffu, t < w1 && k > prefix), e = __ballot_sync(0xffffffffu, t < w1 && k == prefix);
+                const uint32_t at_m = n_more + __popc(m & below), at_e = n_same + __popc(e & below);
+                lam[u] = (m >> lane & 1u) || ((e >> lane & 1u) && at_e < need) ? cv.ns + (int)(at_m + min(at_e, need)) : -1;
+                if (lam[u] >= 0) x[u] = __ldg(row + t);
+                n_more += __popc(m); n_same += __popc(e);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (lam[u] >= 0) { const int r = phys_row(lam[u], st); pos[r] = t0 + 32 * u; sum[r] = x[u]; }
         }
     }
     // the protected ones, or all there are
@@ -239,6 +263,10 @@ cudaError_t launch_select(const CacheView& cv, const float* scores, long long st
     if (!smem_set[dev]) {
         const cudaError_t e = cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, kHeld * 4);
         if (e != cudaSuccess) return e;
+        if (SPLIT > 8) {
+            const cudaError_t x = cudaFuncSetAttribute(kern, cudaFuncAttributeNonPortableClusterSizeAllowed, 1);
+            if (x != cudaSuccess) return x;
+        }
         smem_set[dev] = true;
     }
     const int share = ((max_n + 31) / 32 + SPLIT * kWarps - 1) / (SPLIT * kWarps) * 32 * kWarps, held = std::min(share, kHeld);
@@ -265,8 +293,14 @@ cudaError_t launch_adopt(const CacheView& cv, treekv_dtype dt, const PagedView& 
                          const AdoptLens& lens, int max_n, int sms, cudaStream_t stream) {
     const int units = cv.B * cv.Hkv;
     int split = 1;
-    while (split < kMaxSplit && units * split * 2 <= sms && max_n / split > 4096) split *= 2;
-    const cudaError_t e = split == 8   ? launch_select<8>(cv, scores, score_stride, lens, max_n, stream)
+    // One block up to 12288 tokens: a cluster's barriers and remote reads cost 3000 cycles a round (8 units of 8192: 15.0 us, 17.4 as
+    // two blocks each; of 16384: 20.0 us, 17.9 as four).  Of clusters of eight and more not all 148 SMs' worth are resident at once
+    // (16 units of 65536 as eight blocks each: 36 us, as four: 27).  Sixteen serve few units (4 of 100000: 21.5 us, 24.6 as eight).
+    auto fits = [&](int x) { return units * x <= (x < 8 ? sms : sms * 3 / 4); };
+    if (max_n > kAlone)
+        while (split < kMaxSplit && fits(2 * split) && max_n > split * kShare) split *= 2;
+    const cudaError_t e = split == 16  ? launch_select<16>(cv, scores, score_stride, lens, max_n, stream)
+                          : split == 8   ? launch_select<8>(cv, scores, score_stride, lens, max_n, stream)
                           : split == 4 ? launch_select<4>(cv, scores, score_stride, lens, max_n, stream)
                           : split == 2 ? launch_select<2>(cv, scores, score_stride, lens, max_n, stream)
                                        : launch_select<1>(cv, scores, score_stride, lens, max_n, stream);
