@@ -79,7 +79,7 @@ struct Walk {
     const int* first;   // [B + 1] first item of each sequence: a tile, or with `whole` a unit
     const int* pasts;   // [B]
     const ChunkLens* lens;
-    int B, Hkv, G, item, end;
+    int B, Hkv, G, glog, item, end;   // G = 2^glog
     bool whole;
     int b, kh, past, n, rows, nvis, tiles, t0, t1;  // of the piece: tiles [t0, t1) of the unit's
     __device__ bool get() {
@@ -91,12 +91,14 @@ struct Walk {
             }
             b = lo;
             n = lens->m[b]; past = pasts[b];
-            rows = n * G; nvis = past + n;
+            rows = n << glog; nvis = past + n;
             tiles = (nvis + kTile - 1) / kTile;
             int at = item - first[b];
             if (whole) { kh = at; t0 = 0; t1 = tiles; ++item; return true; }
-            kh = at / (tiles + kStart);
-            at -= kh * (tiles + kStart) + kStart;
+            const int each = tiles + kStart;
+            kh = (int)__fdividef((float)at, (float)each);   // (off by one at most)
+            kh += (at >= (kh + 1) * each) - (at < kh * each);
+            at -= kh * each + kStart;
             t0 = max(0, at); t1 = min(tiles, at + end - item);
             item += tiles - at;
             if (t0 < t1) return true;    // (else the block's share ends in the unit's start)
@@ -120,7 +122,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 2)
 paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int B, int Hq, int Hkv, DevStats* stats, int q_bytes,
-                 int slots, int whole) {
+                 int slots, int whole, int glog) {
     constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128, R = kRows, NG = 1, QB = R * D * 2;
     pdl_trigger();
     extern __shared__ unsigned char smem_raw[];
@@ -144,11 +146,12 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
         s_bad[0] = s_bad[1] = 0u;
     }
     if (warp == 1) { tmem_alloc(smem_addr_u32(&tmem_slot), kTmemCols); tmem_relinquish(); }
+    const int n_ahead = warp == 0 && lane < B ? lens.m[lane] : 0;
     pdl_wait();
     if (warp == 0) {   // items of each sequence, in order
         int sum = 0;
         for (int b0 = 0; b0 < B; b0 += 32) {
-            const int b = b0 + lane, n = b < B ? lens.m[b] : 0;
+            const int b = b0 + lane, n = b0 == 0 ? n_ahead : b < B ? lens.m[b] : 0;
             int items = 0, past = -1;
             if (n > 0) {
                 past = paged_past(pv, b, n);
@@ -169,7 +172,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t tmem = tmem_slot, tmO = tmem + 16;
     const int total = s_first[B], per = (total + (int)gridDim.x - 1) / (int)gridDim.x;
     Walk w;
-    w.first = s_first; w.pasts = s_past; w.lens = &lens; w.B = B; w.Hkv = Hkv; w.G = Hq / Hkv; w.whole = whole;
+    w.first = s_first; w.pasts = s_past; w.lens = &lens; w.B = B; w.Hkv = Hkv; w.G = 1 << glog; w.glog = glog; w.whole = whole;
     w.item = min((int)blockIdx.x * per, total); w.end = min(w.item + per, total);
     if (!whole && blockIdx.x == 0) {
         for (int b = tid; b <= B; b += kThreads) parts.plan[b] = s_first[b];
@@ -179,12 +182,18 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     bool ok = true;
     if (warp == 0) {
         // ================= TMA producer: K and V of a tile in turn
-        const int box = min(pv.page, kTile);
+        const int blog = min(pv.plog, 7), box = 1 << blog;
         int issued = 0, piece = 0;
         bool appended = false;
         Ring r(0, slots);
         for (; ok && w.get(); ++piece) {
             const int qs = piece & 1;
+            // a lane's box of a tile: its page, asked for a tile ahead
+            auto entry_of = [&](int t) {
+                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) >> blog;
+                return lane < boxes ? __ldg(pv.table + (size_t)w.b * pv.width + (k0 >> pv.plog) + lane) : 0;
+            };
+            int e = entry_of(w.t0);
             if (lane == 0) {
                 ok = mbar_wait(bar(Q_FREE + qs), ((piece >> 1) & 1) ^ 1);
                 if (ok) {
@@ -195,14 +204,8 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             }
             ok = __shfl_sync(0xffffffffu, (int)ok, 0) != 0;
             if (!ok) break;
-            // a lane's box of a tile: its page, asked for a tile ahead
-            auto entry_of = [&](int t) {
-                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) / box;
-                return lane < boxes ? __ldg(pv.table + (size_t)w.b * pv.width + (k0 >> pv.plog) + lane) : 0;
-            };
-            int e = entry_of(w.t0);
             for (int t = w.t0; t < w.t1 && ok; ++t) {
-                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) / box;
+                const int k0 = t * kTile, boxes = (min(kTile, w.nvis - k0) + box - 1) >> blog;
                 const int row = (checked_page(pv, e, stats) * Hkv + w.kh) * pv.page + (lane == 0 ? k0 & (pv.page - 1) : 0);
                 if (t + 1 < w.t1) e = entry_of(t + 1);
                 if (!appended && k0 + kTile > w.past) {  // new tokens in it
@@ -243,6 +246,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             Ring rk(0, slots), rv(1, slots);
             int g = 0, piece = 0;         // tiles whose S^T is issued
             bool starts = false;                                   // the tile whose O^T comes next is the first of its piece
+            int steps = 0;                                         // and its groups of 16 keys
             auto issue_o = [&](int of_piece) {
                 if (starts && !(ok = mbar_wait(bar(O_FREE), (of_piece & 1) ^ 1))) return;
                 if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL), (g - 1) & 1))) return;
@@ -250,7 +254,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 const uint32_t v = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
                 for (int kk = 0; kk < kTile / 16; ++kk)  // 16 keys per step: 16 rows of 128 bytes
-                    umma_bf16(tmO, desc_of(v + kk * (2048 / 16)), desc_of(p_lo + (kk >> 2) * (kPHalf / 16) + (kk & 3) * 2), idesc_o, (!starts || kk > 0) ? 1u : 0u);
+                    if (kk < steps) umma_bf16(tmO, desc_of(v + kk * (2048 / 16)), desc_of(p_lo + (kk >> 2) * (kPHalf / 16) + (kk & 3) * 2), idesc_o, (!starts || kk > 0) ? 1u : 0u);
                 umma_commit(bar(USED + rv.slot));
                 umma_commit(bar(O_DONE));
                 rv.next(); rv.next();
@@ -271,6 +275,7 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     rk.next(); rk.next();
                     if (g > 0) { issue_o(t == w.t0 ? piece - 1 : piece); if (!ok) break; }
                     starts = t == w.t0;
+                    steps = min(kTile / 16, (w.nvis - t * kTile + 15) / 16);
                     ++g;
                 }
             }
@@ -394,11 +399,11 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                     *reinterpret_cast<__nv_bfloat16*>(pk + x * 128 + ((((key & 63) >> 3) ^ (x & 7)) << 4)) = __float2bfloat16_rn(p[x]);
                 if (partly) {
                     // Tokens that not all rows see: a value that is not finite is taken out of the tile and its token noted.  Rows behind the
-                    // last token hold none and become zeros.
+                    // last token hold none and become zeros, as far as they are multiplied.
                     if (!mbar_wait(bar(FULL + rv.slot), rv.phase)) { ok = false; break; }
                     unsigned char* tile = base_ptr + 2 * QB + kPBytes + rv.slot * SLOT;
-                    const int valid = min(kTile, w.nvis - k0);
-                    for (int e = st_tid + max(0, w.past + 1 - k0) * (D / 8); e < kTile * (D / 8); e += 128) {
+                    const int valid = min(kTile, w.nvis - k0), end = (valid + 15) & ~15;
+                    for (int e = st_tid + max(0, w.past + 1 - k0) * (D / 8); e < end * (D / 8); e += 128) {
                         const int rr = e / (D / 8), c = e % (D / 8);
                         uint4* at = reinterpret_cast<uint4*>(tile + (c >> 3) * HALF + rr * 128 + (((c & 7) ^ (rr & 7)) << 4));
                         uint4 y = make_uint4(0, 0, 0, 0);
@@ -423,15 +428,19 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 rk.next(); rk.next(); rv.next(); rv.next();
             }
             if (!ok) break;
-            // ---- the piece's rows: sums over the keys, O^T from tensor memory (thread = channel)
+            // ---- the piece's rows.  Sums over the keys: halves of the rows change places with the lane 16 further, quarters 8 further, ...,
+            // so that a pair of lanes has a row at the end
 #pragma unroll
-            for (int x = 0; x < R; ++x) {
+            for (int h = R / 2; h >= 1; h /= 2) {
+                const bool up = lane & 2 * h;
 #pragma unroll
-                for (int o = 16; o > 0; o /= 2) l[x] += __shfl_xor_sync(0xffffffffu, l[x], o);
-                if (lane == 0) s_max[quarter][x] = l[x];
+                for (int x = 0; x < h; ++x) l[x] = (up ? l[x + h] : l[x]) + __shfl_xor_sync(0xffffffffu, up ? l[x] : l[x + h], 2 * h);
             }
+            l[0] += __shfl_xor_sync(0xffffffffu, l[0], 1);
+            if (!(lane & 1)) s_max[quarter][lane >> 1] = l[0];
             asm volatile("bar.sync 1, 128;" ::: "memory");
-            if (hk < R) s_fix[hk] = (s_max[0][hk] + s_max[1][hk]) + (s_max[2][hk] + s_max[3][hk]);
+            float sum = 1.f;
+            if (hk < R) { sum = (s_max[0][hk] + s_max[1][hk]) + (s_max[2][hk] + s_max[3][hk]); s_fix[hk] = 1.0f / sum; }
             asm volatile("bar.sync 1, 128;" ::: "memory");
             if (!mbar_wait(bar(O_DONE), (g - 1) & 1)) { ok = false; break; }
             tc_fence_after();
@@ -439,33 +448,34 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             const uint32_t bad0 = s_bad[0], bad1 = s_bad[1];
             const int slot = 2 * blockIdx.x + (w.t0 == 0 ? 1 : 0);
             const size_t out0 = (size_t)w.b * ch.stride * Hq + w.kh * w.G;
-#pragma unroll
-            for (int x = 0; x < NG; ++x) {
-                if (x * 16 >= w.rows) break;
+            if (quarter * 32 < D) {          // O^T from tensor memory (thread = channel)
                 uint32_t o[16];
-                tmem_ld16(tmO + x * 16 + lane_off, o);
+                tmem_ld16(tmO + lane_off, o);
                 tmem_ld16_wait(o);
-                if (key < D)
+                if (direct) {
+                    __nv_bfloat16* dst = reinterpret_cast<__nv_bfloat16*>(po.out) + out0 * D + key;
 #pragma unroll
-                    for (int e = 0; e < 16; ++e) {
-                        const int r = x * 16 + e;
-                        if (r < w.rows) {
-                            if (direct) {
-                                float y = __uint_as_float(o[e]) * (1.0f / s_fix[r]);
-                                if (bad0 | bad1)
-                                    y += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)w.b * ch.stride * Hkv + w.kh) * D + key, bad0, bad1,
-                                                    r / w.G, Hkv * D);
-                                reinterpret_cast<__nv_bfloat16*>(po.out)[(out0 + (size_t)(r / w.G) * Hq + r % w.G) * D + key] = __float2bfloat16_rn(y);
-                            } else {
-                                parts.o[((size_t)slot * R + r) * D + key] = __uint_as_float(o[e]);
-                            }
-                        }
+                    for (int r = 0; r < R; ++r) {
+                        if (r >= w.rows) break;
+                        const int tok = r >> w.glog;
+                        float y = __uint_as_float(o[r]) * s_fix[r];
+                        if (bad0 | bad1)
+                            y += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)w.b * ch.stride * Hkv + w.kh) * D + key, bad0, bad1, tok, Hkv * D);
+                        dst[((size_t)tok * Hq + (r & (w.G - 1))) * D] = __float2bfloat16_rn(y);
                     }
+                } else {
+                    float* dst = parts.o + (size_t)slot * R * D + key;
+#pragma unroll
+                    for (int r = 0; r < R; ++r) {
+                        if (r >= w.rows) break;
+                        dst[r * D] = __uint_as_float(o[r]);
+                    }
+                }
             }
             tc_fence_before();
             if (hk < w.rows) {
-                if (!direct) parts.stat[(size_t)slot * R + hk] = make_float2(s_ref[hk], s_fix[hk]);
-                else if (po.lse) po.lse[out0 + (size_t)(hk / w.G) * Hq + hk % w.G] = (s_ref[hk] + log2f(s_fix[hk])) * (1.0f / kLog2e);
+                if (!direct) parts.stat[(size_t)slot * R + hk] = make_float2(s_ref[hk], sum);
+                else if (po.lse) po.lse[out0 + (size_t)(hk >> w.glog) * Hq + (hk & (w.G - 1))] = (s_ref[hk] + log2f(sum)) * (1.0f / kLog2e);
             }
             if (!direct && hk < 2) parts.bad[2 * slot + hk] = s_bad[hk];
             asm volatile("bar.sync 1, 128;" ::: "memory");   // everybody is through with the statistics
@@ -481,24 +491,24 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
 }
 
-// Joins the parts of the units that several blocks shared.  A block has a row: its warps deal the parts, each with four
-// of them on their way, and meet in shared memory, in order.
-template <int D>
+// Joins the parts of the units that several blocks shared.  W warps have a row: they deal the parts, each with four of them on their
+// way, and meet in shared memory, in order.
+template <int D, int W>
 __global__ void __launch_bounds__(256)
 paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv) {
-    constexpr int R = kRows, CPL = D / 32, W = 8;   // a lane's channels; warps
+    constexpr int R = kRows, CPL = D / 32, RPB = 8 / W;   // a lane's channels; rows of the block
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv, row = blockIdx.y;
-    if (row >= n * G) return;
+    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv, row0 = blockIdx.y * RPB;
+    if (row0 >= n * G) return;
     const int past = paged_past(pv, b, n);
     if (past < 0) return;
     const int tiles = (past + n + kTile - 1) / kTile, per = parts.plan[kMaxBatch + 1], f = parts.plan[b] + kh * (tiles + kStart) + kStart;
     const int c0 = f / per, c1 = (f + tiles - 1) / per;
     if (c0 == c1) return;   // one block had it all
-    __shared__ float s_o[W][D], s_stat[W][2];
+    __shared__ float s_o[8][D], s_stat[8][2];
     __shared__ uint32_t s_bad[2];
-    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const int all = threadIdx.x >> 5, warp = all % W, lane = threadIdx.x & 31, row = row0 + all / W;   // (rows behind the last one: of the padding)
     if (threadIdx.x < 2) s_bad[threadIdx.x] = 0u;
     __syncthreads();
     float M = -INFINITY, l = 0.f, o[CPL];
@@ -540,32 +550,36 @@ paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts
         }
     }
 #pragma unroll
-    for (int e = 0; e < CPL; ++e) s_o[warp][CPL * lane + e] = o[e];
-    if (lane == 0) { s_stat[warp][0] = M; s_stat[warp][1] = l; }
+    for (int e = 0; e < CPL; ++e) s_o[all][CPL * lane + e] = o[e];
+    if (lane == 0) { s_stat[all][0] = M; s_stat[all][1] = l; }
     __syncthreads();
-    const int c = threadIdx.x;
-    if (c >= D) return;
-    M = s_stat[0][0];
-    for (int x = 1; x < W; ++x) M = fmaxf(M, s_stat[x][0]);
-    float sum = 0.f;
-    l = 0.f;
-    for (int x = 0; x < W; ++x) {
-        const float wgt = s_stat[x][0] == -INFINITY ? 0.f : ex2(s_stat[x][0] - M);
-        l += s_stat[x][1] * wgt;
-        sum += s_o[x][c] * wgt;
+    // the row's threads that write: a channel each, or several
+    constexpr int T = 32 * W;
+    const int first = all / W * W;
+    if (row >= n * G) return;
+    for (int c = threadIdx.x % T; c < D; c += T) {
+        M = s_stat[first][0];
+        for (int x = 1; x < W; ++x) M = fmaxf(M, s_stat[first + x][0]);
+        float sum = 0.f;
+        l = 0.f;
+        for (int x = 0; x < W; ++x) {
+            const float wgt = s_stat[first + x][0] == -INFINITY ? 0.f : ex2(s_stat[first + x][0] - M);
+            l += s_stat[first + x][1] * wgt;
+            sum += s_o[first + x][c] * wgt;
+        }
+        sum *= 1.0f / l;
+        if (s_bad[0] | s_bad[1])
+            sum += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + c, s_bad[0], s_bad[1], row / G, Hkv * D);
+        const size_t at = ((size_t)b * ch.stride + row / G) * Hq + kh * G + row % G;
+        reinterpret_cast<__nv_bfloat16*>(po.out)[at * D + c] = __float2bfloat16_rn(sum);
+        if (po.lse && c == 0) po.lse[at] = (M + log2f(l)) * (1.0f / kLog2e);
     }
-    sum *= 1.0f / l;
-    if (s_bad[0] | s_bad[1])
-        sum += bad_values(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + c, s_bad[0], s_bad[1], row / G, Hkv * D);
-    const size_t at = ((size_t)b * ch.stride + row / G) * Hq + kh * G + row % G;
-    reinterpret_cast<__nv_bfloat16*>(po.out)[at * D + c] = __float2bfloat16_rn(sum);
-    if (po.lse && c == 0) po.lse[at] = (M + log2f(l)) * (1.0f / kLog2e);
 }
 
 template <int D>
 cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o, void* scratch,
                      int sms, cudaStream_t stream, int* launches) {
-    const int G = cv.Hq / cv.Hkv, box = std::min(kRows / G, ch.stride);
+    const int G = cv.Hq / cv.Hkv, box = std::min(kRows / G, ch.stride), glog = G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3;
     CUtensorMap tmQ, tmK, tmV;
     const DraftView dv = {ch.q, ch.k, ch.v, nullptr, ch.stride};
     if (!make_q_map(&tmQ, cv, dv, box)) return cudaErrorInvalidValue;
@@ -602,10 +616,13 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     parts.stat = reinterpret_cast<float2*>(at); at += n_slots * kRows * 8;
     parts.o = reinterpret_cast<float*>(at);
     const cudaError_t e = launch_pdl(kern, dim3((unsigned)std::min<long>(whole ? units : tiles, places)), dim3(kThreads), smem, stream, tmQ, tmK, tmV, pv, ch,
-                                     lens, o, parts, cv.B, cv.Hq, cv.Hkv, cv.stats, (D / 64) * box * G * 128, slots, whole ? 1 : 0);
+                                     lens, o, parts, cv.B, cv.Hq, cv.Hkv, cv.stats, (D / 64) * box * G * 128, slots, whole ? 1 : 0, glog);
     *launches = whole ? 1 : 2;
     if (e != cudaSuccess || whole) return e;
-    return launch_pdl(paged_join_kernel<D>, dim3(cv.B * cv.Hkv, max_n * G), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
+    const int rows = max_n * G;
+    if (places > 4 * units)   // (a unit has up to about places / units + 1 parts)
+        return launch_pdl(paged_join_kernel<D, 8>, dim3(cv.B * cv.Hkv, rows), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
+    return launch_pdl(paged_join_kernel<D, 2>, dim3(cv.B * cv.Hkv, (rows + 3) / 4), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
 }
 
 }  // namespace
