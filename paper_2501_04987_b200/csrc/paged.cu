@@ -42,7 +42,7 @@ cudaError_t launch_paged_append(const CacheView& cv, treekv_dtype dt, const Page
 namespace {
 
 constexpr int kMaxChunkRows = 32768;
-constexpr int kLongRows = 256;  // query rows a KV head beyond which a block takes 256 of them
+constexpr int kLongRows = 128;  // query rows a KV head beyond which a block takes 256 of them
 
 inline bool aligned(const void* p, unsigned to) { return (reinterpret_cast<uintptr_t>(p) & (to - 1)) == 0; }
 

@@ -14,8 +14,8 @@
 // Rounded to fewer bits than 32: the weights P as an operand of P V, to bf16, since both operands of an MMA have one type and V's is
 // bf16 - each by at most half a step, 2^-8 of itself; the sum that divides them is of the unrounded ones.
 //
-// Items (256 rows of a unit) that would start a last wave of at most half the machine are cut in two along their keys; such parts
-// - maximum, sum, unnormalised output - go to the caller's scratch, and a second small launch joins them.
+// The items (256 rows of a unit) of a last wave that would leave SMs idle are cut along their keys; such parts - maximum, sum,
+// unnormalised output - go to the caller's scratch, and a second small launch joins them.
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 4-7 and 8-11 are the groups of the two row tiles, which take over
 // registers that the first four do not need.
@@ -35,6 +35,8 @@ constexpr int kRegsFew = 88, kRegsMany = 208;  // 4 x 88 + 8 x 208 registers a l
 constexpr int kTile = 128;                 // keys of a tile, rows of a row tile
 constexpr int kRows = 256;
 constexpr int kMaxSlots = 8;
+constexpr int kMaxShares = 64;             // of an item's keys
+constexpr int kMaxParts = 2;               // of a call, for each SM
 constexpr uint32_t kTmemCols = 512;        // S / P 128 + 128, O 128 + 128
 constexpr size_t kSmemMax = 225 * 1024;
 constexpr size_t kSmemMin = 120 * 1024;    // one block on an SM: it holds all of the tensor memory
@@ -112,7 +114,7 @@ template <int D>
 __global__ void __launch_bounds__(kThreads, 1)
 paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, const __grid_constant__ CUtensorMap tmV,
                  const __grid_constant__ CUtensorMap tmKn, const __grid_constant__ CUtensorMap tmVn, PagedView pv, ChunkView ch, ChunkLens lens,
-                 PagedOut po, Parts2 parts, int Hq, int Hkv, DevStats* stats, Order od, int n_whole, int q_bytes, int slots) {
+                 PagedOut po, Parts2 parts, int Hq, int Hkv, DevStats* stats, Order od, int n_whole, int shares, int q_bytes, int slots) {
     constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128;
     const int G = Hq / Hkv;
     pdl_trigger();
@@ -141,13 +143,13 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     const uint32_t tmem = tmem_slot;
     pdl_wait();
     const bool whole = (int)blockIdx.x < n_whole;
-    const int part = (int)blockIdx.x - n_whole, x = whole ? (int)blockIdx.x : n_whole + (part >> 1);
+    const int part = (int)blockIdx.x - n_whole, item = part / shares, share = part - item * shares, x = whole ? (int)blockIdx.x : n_whole + item;
     Item it;
     const bool some = it.get(pv, lens, x, od, G, Hkv);
     if (some && it.past < 0 && tid == 0) atomicOr(&stats->error, kErrBadIndex);
     // key tiles [j0, j0 + NT)
-    const int j0 = some && !whole && (part & 1) ? (it.tiles + 1) / 2 : 0;
-    const int NT = !some ? 0 : whole ? it.tiles : (part & 1) ? it.tiles - j0 : (it.tiles + 1) / 2;
+    const int each = (it.tiles + shares - 1) / shares, j0 = some && !whole ? min(it.tiles, share * each) : 0;
+    const int NT = !some ? 0 : whole ? it.tiles : min(each, it.tiles - j0);
     const bool two = some && it.rows > kTile;
     bool ok = true;
     const bool works = some && it.past >= 0;
@@ -264,7 +266,7 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                 if (ok) { umma_commit(bar(O_DONE)); ok = mbar_wait(bar(O_DONE), 0); }
                 if (!ok) atomicOr(&stats->error, 8u);
             }
-        } else if (works && warp >= 2 && (whole || !(part & 1))) {
+        } else if (works && warp >= 2 && (whole || share == 0)) {
             // ================= the tokens of this item's rows into their pages, beside everything else: four pieces of 16 bytes of the
             // keys and the values on their way
             constexpr int U = 4;
@@ -470,25 +472,51 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
 }
 
-// Joins the two parts of the items that were cut: D / 4 threads a row.
+// Joins the parts of the items that were cut, in order: D / 4 threads a row, four parts on their way at a time.
 template <int D>
 __global__ void __launch_bounds__(128)
-paged_join2_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts2 parts, int Hq, int Hkv, Order od, int n_whole) {
+paged_join2_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts2 parts, int Hq, int Hkv, Order od, int n_whole, int shares) {
     constexpr int LPR = D / 4;
     pdl_trigger();
     pdl_wait();
     const int G = Hq / Hkv, row = blockIdx.y * (128 / LPR) + threadIdx.x / LPR, c = threadIdx.x % LPR;
     Item it;
     if (!it.get(pv, lens, n_whole + blockIdx.x, od, G, Hkv) || it.past < 0 || row >= it.rows) return;
-    const size_t p0 = 2 * (size_t)blockIdx.x, p1 = p0 + 1;
-    const float2 s0 = parts.stat[p0 * kRows + row], s1 = parts.stat[p1 * kRows + row];
-    const float4 x = *reinterpret_cast<const float4*>(parts.o + (p0 * kRows + row) * D + 4 * c), y = *reinterpret_cast<const float4*>(parts.o + (p1 * kRows + row) * D + 4 * c);
-    const float M = fmaxf(s0.x, s1.x), f0 = s0.x == -INFINITY ? 0.f : ex2(s0.x - M), f1 = s1.x == -INFINITY ? 0.f : ex2(s1.x - M);
-    const float l = s0.y * f0 + s1.y * f1, inv = 1.0f / l;
-    float o[4] = {(x.x * f0 + y.x * f1) * inv, (x.y * f0 + y.y * f1) * inv, (x.z * f0 + y.z * f1) * inv, (x.w * f0 + y.w * f1) * inv};
-    uint32_t bad[8], any = 0;
+    const size_t p0 = (size_t)blockIdx.x * shares;
+    float M = -INFINITY, l = 0.f, o[4] = {0.f, 0.f, 0.f, 0.f};
+    uint32_t bad[8] = {}, any = 0;
+    for (int s0 = 0; s0 < shares; s0 += 4) {
+        float2 st[4];
+        float4 y[4];
+        float top = M;
 #pragma unroll
-    for (int w = 0; w < 8; ++w) { bad[w] = parts.bad[p0 * 8 + w] | parts.bad[p1 * 8 + w]; any |= bad[w]; }
+        for (int u = 0; u < 4; ++u) {
+            const size_t p = p0 + min(s0 + u, shares - 1);
+            st[u] = parts.stat[p * kRows + row];
+            y[u] = *reinterpret_cast<const float4*>(parts.o + (p * kRows + row) * D + 4 * c);
+            if (s0 + u >= shares) st[u].x = -INFINITY;
+            top = fmaxf(top, st[u].x);
+#pragma unroll
+            for (int w = 0; w < 8; ++w) bad[w] |= parts.bad[p * 8 + w];
+        }
+        if (top == -INFINITY) continue;
+        const float fix = ex2(M - top);
+        M = top; l *= fix;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) o[e] *= fix;
+#pragma unroll
+        for (int u = 0; u < 4; ++u) {
+            if (st[u].x == -INFINITY) continue;   // (no key of the part is seen, or there is none)
+            const float f = ex2(st[u].x - M);
+            l += st[u].y * f;
+            o[0] += y[u].x * f; o[1] += y[u].y * f; o[2] += y[u].z * f; o[3] += y[u].w * f;
+        }
+    }
+    const float inv = 1.0f / l;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) o[e] *= inv;
+#pragma unroll
+    for (int w = 0; w < 8; ++w) any |= bad[w];
     const int r = it.r0 + row;
     const size_t tok_at = (size_t)it.b * ch.stride;
     if (any)
@@ -530,25 +558,32 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
         smem_set[dev] = true;
     }
     const int per_unit = (max_n * G + kRows - 1) / kRows, items = cv.B * cv.Hkv * per_unit, left = items % sms;
-    // A last wave that is at most half full: its items are cut in two, where there are enough keys for two.
-    const bool cut = left > 0 && 2 * left <= sms && (pv.max_past + max_n) >= 8 * kTile;
+    // The last wave's items are cut along their keys where that ends it earlier: in tiles, a block costs about two beside its own, the
+    // second launch four.
+    const int tiles = (pv.max_past + max_n + kTile - 1) / kTile;
+    int shares = 1, least = 0;
+    for (int x = 1; left > 0 && x <= kMaxShares && left * x <= kMaxParts * sms && (x == 1 || tiles >= 2 * x); ++x) {
+        const int cost = (left * x + sms - 1) / sms * ((tiles + x - 1) / x + 2) + (x > 1 ? 4 : 0);
+        if (x == 1 || cost < least) { least = cost; shares = x; }
+    }
+    const bool cut = shares > 1;
     const int n_whole = cut ? items - left : items;
     const Order od = {cv.B * cv.Hkv, std::max(1, sms / per_unit), per_unit};
     Parts2 parts;
     char* at = static_cast<char*>(scratch);
-    parts.bad = reinterpret_cast<uint32_t*>(at); at += (size_t)sms * 32;
-    parts.stat = reinterpret_cast<float2*>(at); at += (size_t)sms * kRows * 8;
+    parts.bad = reinterpret_cast<uint32_t*>(at); at += (size_t)sms * kMaxParts * 32;
+    parts.stat = reinterpret_cast<float2*>(at); at += (size_t)sms * kMaxParts * kRows * 8;
     parts.o = reinterpret_cast<float*>(at);
-    cudaError_t e = launch_pdl(kern, dim3((unsigned)(n_whole + 2 * (items - n_whole))), dim3(kThreads), smem, stream, tmQ, tmK, tmV, tmKn, tmVn, pv, ch, lens, o,
-                               parts, cv.Hq, cv.Hkv, cv.stats, od, n_whole, (D / 64) * 128 * box * G, slots);
+    cudaError_t e = launch_pdl(kern, dim3((unsigned)(n_whole + shares * (items - n_whole))), dim3(kThreads), smem, stream, tmQ, tmK, tmV, tmKn, tmVn, pv, ch, lens, o,
+                               parts, cv.Hq, cv.Hkv, cv.stats, od, n_whole, shares, (D / 64) * 128 * box * G, slots);
     *launches = cut ? 2 : 1;
     if (e != cudaSuccess || !cut) return e;
-    return launch_pdl(paged_join2_kernel<D>, dim3(items - n_whole, kRows / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, od, n_whole);
+    return launch_pdl(paged_join2_kernel<D>, dim3(items - n_whole, kRows / (128 / (D / 4))), dim3(128), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, od, n_whole, shares);
 }
 
 }  // namespace
 
-size_t paged_tc2_scratch(int D, int sms) { return (size_t)sms * part_bytes(D); }
+size_t paged_tc2_scratch(int D, int sms) { return (size_t)sms * kMaxParts * part_bytes(D); }
 
 cudaError_t launch_paged_tc2(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches) {
