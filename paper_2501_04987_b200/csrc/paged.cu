@@ -1,43 +1,13 @@
-// C ABI of paged prompts and of the path of a draft: checks and launches; the kernels are in paged_tc.cu, paged_f32.cu,
-// score_*.cu, adopt.cu and pick.cu.  Here too: the kernel that puts new tokens into their pages.
+// C ABI of paged prompts and of the path of a draft: checks and launches; the kernels are in paged_*.cu,
+// score_*.cu, adopt.cu and pick.cu.
 #include <string.h>
+
+#include <algorithm>
 
 #include "ctx.cuh"
 #include "paged.cuh"
 
 using namespace treekv;
-
-namespace treekv {
-
-namespace {
-
-// One thread per 16 bytes of a new token's key and value.  Memory bound; 256 threads take whole rows, so what they read and
-// write is contiguous per head.
-__global__ void __launch_bounds__(256) paged_append_kernel(PagedView pv, ChunkView ch, ChunkLens lens, int Hkv, int pieces, DevStats* stats) {
-    pdl_trigger();
-    pdl_wait();
-    const int b = blockIdx.y, n = lens.m[b], e = blockIdx.x * 256 + threadIdx.x, row = e / pieces, c = e % pieces, tok = row / Hkv, kh = row % Hkv;
-    if (tok >= n) return;
-    const int past = paged_past(pv, b, n);
-    if (past < 0) return;   // (the attention kernel reports it)
-    const int at = past + tok, page = pv.table[(size_t)b * pv.width + (at >> pv.plog)];
-    if ((unsigned)page >= (unsigned)pv.n_pages) { atomicOr(&stats->error, kErrBadIndex); return; }  // nothing is written
-    const size_t src = ((size_t)b * ch.stride * Hkv + row) * pieces + c;
-    const size_t dst = (((size_t)page * Hkv + kh) * pv.page + (at & (pv.page - 1))) * pieces + c;
-    reinterpret_cast<uint4*>(pv.kp)[dst] = reinterpret_cast<const uint4*>(ch.k)[src];
-    reinterpret_cast<uint4*>(pv.vp)[dst] = reinterpret_cast<const uint4*>(ch.v)[src];
-}
-
-}  // namespace
-
-cudaError_t launch_paged_append(const CacheView& cv, treekv_dtype dt, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n,
-                                cudaStream_t stream) {
-    const int pieces = cv.d * (dt == TREEKV_F32 ? 4 : 2) / 16;
-    const long total = (long)max_n * cv.Hkv * pieces;
-    return launch_pdl(paged_append_kernel, dim3((unsigned)((total + 255) / 256), cv.B), dim3(256), 0, stream, pv, ch, lens, cv.Hkv, pieces, cv.stats);
-}
-
-}  // namespace treekv
 
 namespace {
 
@@ -88,8 +58,10 @@ size_t treekv_paged_scratch_bytes(const treekv_ctx* ctx, int stride) {
     if (!ctx || stride < 1 || stride > kMaxChunkRows) return 0;
     if (ctx->dt == TREEKV_F32) return paged_f32_scratch(ctx->cv.d);
     // (a call of a longer chunk may still have few tokens in every sequence)
-    const size_t few = paged_few_scratch(ctx->cv.d, ctx->sm_count), many = paged_tc2_scratch(ctx->cv.d, ctx->sm_count);
-    return stride * ctx->G > kLongRows && many > few ? many : few;
+    size_t most = paged_few_scratch(ctx->cv.d, ctx->sm_count);
+    if (!paged_few_takes(stride * ctx->G)) most = std::max(most, paged_tc_scratch(ctx->cv.d, ctx->sm_count));
+    if (stride * ctx->G > kLongRows) most = std::max(most, paged_tc2_scratch(ctx->cv.d, ctx->sm_count));
+    return most;
 }
 
 treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void* dev_k, const void* dev_v, void* dev_k_pages,
@@ -116,17 +88,15 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
     const ChunkView ch = {dev_q, dev_k, dev_v, stride};
     const PagedOut o = {dev_out, dev_lse};
     cudaError_t e;
-    int launches = 2;
-    if (ctx->dt == TREEKV_BF16 && max_n * ctx->G > kLongRows) {
-        e = launch_paged_tc2(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
-    } else if (ctx->dt == TREEKV_BF16 && paged_few_takes(max_n * ctx->G)) {
-        e = launch_paged_few(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
-    } else if (ctx->dt == TREEKV_BF16) {
-        e = launch_paged_append(ctx->cv, ctx->dt, pv, ch, lens, max_n, s);
-        if (e == cudaSuccess) e = launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, ctx->sm_count, s);
-    } else {
+    int launches = 0;
+    if (ctx->dt == TREEKV_F32)
         e = launch_paged_f32(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
-    }
+    else if (max_n * ctx->G > kLongRows)
+        e = launch_paged_tc2(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
+    else if (paged_few_takes(max_n * ctx->G))
+        e = launch_paged_few(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
+    else
+        e = launch_paged_tc(ctx->cv, pv, ch, lens, max_n, o, dev_scratch, ctx->sm_count, s, &launches);
     if (e != cudaSuccess) return cuda_fail(ctx, e);
     ctx->launches += launches;
     return TREEKV_OK;

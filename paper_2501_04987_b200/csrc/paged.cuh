@@ -39,11 +39,15 @@ __device__ inline int paged_past(const PagedView& pv, int b, int n) {
 }
 // orders what earlier kernels stored to global memory (the new tokens' rows) before this thread's TMA loads of it
 __device__ inline void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }
-// true in one lane of a converged warp
-__device__ inline bool elect_one() {
-    uint32_t p;
-    asm volatile("{\n\t.reg .pred p;\n\telect.sync _|p, 0xffffffff;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(p));
-    return p != 0;
+// values that are not finite of new tokens up to `token`, of those that were noted
+__device__ inline float bad_sum(const __nv_bfloat16* v, const uint32_t* bad, int token, size_t vstep) {
+    float sum = 0.f;
+    for (int w = 0; w <= token >> 5; ++w)
+        for (uint32_t left = w < token >> 5 ? bad[w] : bad[w] & (2u << (token & 31)) - 1u; left; left &= left - 1) {
+            const float y = __bfloat162float(v[(size_t)(32 * w + __ffs((int)left) - 1) * vstep]);
+            if (!(fabsf(y) < INFINITY)) sum += y;
+        }
+    return sum;
 }
 // a page that cannot be is not followed: page 0 stands in
 __device__ inline int checked_page(const PagedView& pv, int e, DevStats* stats) {
@@ -53,9 +57,6 @@ __device__ inline int checked_page(const PagedView& pv, int e, DevStats* stats) 
 }
 #endif
 
-// new tokens into their pages
-cudaError_t launch_paged_append(const CacheView& cv, treekv_dtype dt, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n,
-                                cudaStream_t stream);
 // attention of few new tokens - up to 16 query rows a KV head - which enter their pages with it (bf16); `launches`: kernels launched
 bool paged_few_takes(int rows);
 size_t paged_few_scratch(int D, int sms);
@@ -65,9 +66,10 @@ cudaError_t launch_paged_few(const CacheView& cv, const PagedView& pv, const Chu
 size_t paged_tc2_scratch(int D, int sms);
 cudaError_t launch_paged_tc2(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
                              void* scratch, int sms, cudaStream_t stream, int* launches);
-// and between the two, of tokens that are in their pages already (bf16)
+// and between the two, up to 128 rows a KV head; the new tokens enter their pages with it (bf16)
+size_t paged_tc_scratch(int D, int sms);
 cudaError_t launch_paged_tc(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
-                            int sms, cudaStream_t stream);
+                            void* scratch, int sms, cudaStream_t stream, int* launches);
 // fp32; the new tokens enter their pages with it
 size_t paged_f32_scratch(int D);
 cudaError_t launch_paged_f32(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,

@@ -76,17 +76,6 @@ struct Item {
     }
 };
 
-// values that are not finite of new tokens up to `token`, of those that were noted
-__device__ inline float bad_sum(const __nv_bfloat16* v, const uint32_t* bad, int token, size_t vstep) {
-    float sum = 0.f;
-    for (int w = 0; w <= token >> 5; ++w)
-        for (uint32_t left = w < token >> 5 ? bad[w] : bad[w] & (2u << (token & 31)) - 1u; left; left &= left - 1) {
-            const float y = __bfloat162float(v[(size_t)(32 * w + __ffs((int)left) - 1) * vstep]);
-            if (!(fabsf(y) < INFINITY)) sum += y;
-        }
-    return sum;
-}
-
 // O of some rows of the warp is multiplied by f, the reference's step (1 for the other rows).
 template <int D>
 __device__ __forceinline__ void rescale(uint32_t tmO, float f) {
