@@ -404,7 +404,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
                                      cv.stats, (D / 64) * box * G * 128, slots, d.whole ? 1 : 0, glog);
     *launches = d.whole ? 1 : 2;
     if (e != cudaSuccess || d.whole) return e;
-    return launch_join<D, kTile, kRows>(cv, pv, ch, lens, max_n, o, parts, d, stream);
+    return launch_join<D, kTile, kRows>(cv, pv, ch, lens, max_n, o, parts, d, sms, stream);
 }
 
 }  // namespace

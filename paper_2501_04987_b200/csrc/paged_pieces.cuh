@@ -178,93 +178,114 @@ __device__ inline void clean_values(unsigned char* tile, int first, int valid, i
     }
 }
 
+inline int group_log(int G) { return G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3; }
+
 // Joins the parts of the units that several blocks shared.  W warps have a row: they deal the parts, each with four of them on their
-// way, and meet in shared memory, in order.  R: rows of a part.
+// way, and meet in shared memory, in order.  A block takes every gridDim.y-th group of 8 / W rows.  R: rows of a part.
 template <int D, int TILE, int R, int W>
 __global__ void __launch_bounds__(256)
-paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv) {
-    constexpr int CPL = D / 32, RPB = 8 / W;   // a lane's channels; rows of the block
+paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts parts, int Hq, int Hkv, int glog) {
+    constexpr int CPL = D / 32, RPB = 8 / W;   // a lane's channels; rows at a time
     pdl_trigger();
+    const int unit = blockIdx.x, b = unit / Hkv, kh = unit - b * Hkv, n = lens.m[b], rows = n << glog;
+    if ((int)blockIdx.y * RPB >= rows) return;
     pdl_wait();
-    const int unit = blockIdx.x, b = unit / Hkv, kh = unit % Hkv, n = lens.m[b], G = Hq / Hkv, row0 = blockIdx.y * RPB;
-    if (row0 >= n * G) return;
-    const int past = paged_past(pv, b, n);
+    const int past = paged_past(pv, b, n), per = parts.plan[kMaxBatch + 1], at0 = parts.plan[b];
     if (past < 0) return;
-    const int tiles = (past + n + TILE - 1) / TILE, per = parts.plan[kMaxBatch + 1], f = parts.plan[b] + kh * (tiles + kStart<TILE>) + kStart<TILE>;
+    const int tiles = (past + n + TILE - 1) / TILE, f = at0 + kh * (tiles + kStart<TILE>) + kStart<TILE>;
     const int c0 = f / per, c1 = (f + tiles - 1) / per;
     if (c0 == c1) return;   // one block had it all
-    __shared__ float s_o[8][D], s_stat[8][2];
+    __shared__ float s_o[W > 1 ? 8 : 1][D], s_stat[8][2];
     __shared__ uint32_t s_bad[4];
-    const int all = threadIdx.x >> 5, warp = all % W, lane = threadIdx.x & 31, row = min(row0 + all / W, n * G - 1);
+    const int all = threadIdx.x >> 5, warp = all % W, lane = threadIdx.x & 31;
     if (threadIdx.x < 4) s_bad[threadIdx.x] = 0u;
     __syncthreads();
-    float M = -INFINITY, l = 0.f, o[CPL];
-#pragma unroll
-    for (int e = 0; e < CPL; ++e) o[e] = 0.f;
-    for (int x0 = c0 + warp; x0 <= c1; x0 += 4 * W) {
-        float2 st[4];
-        float y[4][CPL];
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-            const int x = x0 + u * W, slot = 2 * x + (x == c0 ? 1 : 0);
-            st[u] = make_float2(-INFINITY, 0.f);
-#pragma unroll
-            for (int e = 0; e < CPL; ++e) y[u][e] = 0.f;
-            if (x <= c1) {
-                st[u] = parts.stat[(size_t)slot * R + row];
-                const float* src = parts.o + ((size_t)slot * R + row) * D + CPL * lane;
-                if constexpr (CPL == 4) { const float4 z = *reinterpret_cast<const float4*>(src); y[u][0] = z.x; y[u][1] = z.y; y[u][2] = z.z; y[u][3] = z.w; }
-                else { const float2 z = *reinterpret_cast<const float2*>(src); y[u][0] = z.x; y[u][1] = z.y; }
-                if (lane < 4) { const uint32_t bad = parts.bad[4 * slot + lane]; if (bad) atomicOr(&s_bad[lane], bad); }
-            }
-        }
-        const float top = fmaxf(fmaxf(fmaxf(M, st[0].x), fmaxf(st[1].x, st[2].x)), st[3].x);
-        if (top > -INFINITY) {
-            const float fix = ex2(M - top);
-            M = top; l *= fix;
-#pragma unroll
-            for (int e = 0; e < CPL; ++e) o[e] *= fix;
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float wgt = ex2(st[u].x - M);
-                l += st[u].y * wgt;
-#pragma unroll
-                for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
-            }
-        }
+    for (int x = c0 + (threadIdx.x >> 2); x <= c1; x += 64) {
+        const uint32_t bad = parts.bad[4 * (2 * x + (x == c0 ? 1 : 0)) + (threadIdx.x & 3)];
+        if (bad) atomicOr(&s_bad[threadIdx.x & 3], bad);
     }
-#pragma unroll
-    for (int e = 0; e < CPL; ++e) s_o[all][CPL * lane + e] = o[e];
-    if (lane == 0) { s_stat[all][0] = M; s_stat[all][1] = l; }
     __syncthreads();
-    if (row0 + all / W >= n * G) return;
-    const int first = all / W * W;
-    for (int c = threadIdx.x % (32 * W); c < D; c += 32 * W) {   // the row's threads: a channel each, or several
-        M = s_stat[first][0];
-        for (int x = 1; x < W; ++x) M = fmaxf(M, s_stat[first + x][0]);
-        float sum = 0.f;
-        l = 0.f;
-        for (int x = 0; x < W; ++x) {
-            const float wgt = s_stat[first + x][0] == -INFINITY ? 0.f : ex2(s_stat[first + x][0] - M);
-            l += s_stat[first + x][1] * wgt;
-            sum += s_o[first + x][c] * wgt;
-        }
-        sum *= 1.0f / l;
-        if (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3])
-            sum += bad_sum(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + c, s_bad, row / G, (size_t)Hkv * D);
-        const size_t at = ((size_t)b * ch.stride + row / G) * Hq + kh * G + row % G;
+    const bool any_bad = s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3];
+    auto write = [&](int row, int c, float sum, float M, float l) {
+        const int tok = row >> glog;
+        if (any_bad)
+            sum += bad_sum(reinterpret_cast<const __nv_bfloat16*>(ch.v) + ((size_t)b * ch.stride * Hkv + kh) * D + c, s_bad, tok, (size_t)Hkv * D);
+        const size_t at = (((size_t)b * ch.stride + tok) * Hkv + kh) * (1 << glog) + (row & ((1 << glog) - 1));
         reinterpret_cast<__nv_bfloat16*>(po.out)[at * D + c] = __float2bfloat16_rn(sum);
         if (po.lse && c == 0) po.lse[at] = (M + log2f(l)) * (1.0f / kLog2e);
+    };
+    for (int row0 = blockIdx.y * RPB; row0 < rows; row0 += RPB * gridDim.y) {
+        const int row = min(row0 + all / W, rows - 1);
+        float M = -INFINITY, l = 0.f, o[CPL];
+#pragma unroll
+        for (int e = 0; e < CPL; ++e) o[e] = 0.f;
+        for (int x0 = c0 + warp; x0 <= c1; x0 += 4 * W) {
+            float2 st[4];
+            float y[4][CPL];
+#pragma unroll
+            for (int u = 0; u < 4; ++u) {
+                const int x = x0 + u * W, slot = 2 * x + (x == c0 ? 1 : 0);
+                st[u] = make_float2(-INFINITY, 0.f);
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) y[u][e] = 0.f;
+                if (x <= c1) {
+                    st[u] = parts.stat[(size_t)slot * R + row];
+                    const float* src = parts.o + ((size_t)slot * R + row) * D + lane;
+#pragma unroll
+                    for (int e = 0; e < CPL; ++e) y[u][e] = src[32 * e];
+                }
+            }
+            const float top = fmaxf(fmaxf(fmaxf(M, st[0].x), fmaxf(st[1].x, st[2].x)), st[3].x);
+            if (top > -INFINITY) {
+                const float fix = ex2(M - top);
+                M = top; l *= fix;
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) o[e] *= fix;
+#pragma unroll
+                for (int u = 0; u < 4; ++u) {
+                    const float wgt = ex2(st[u].x - M);
+                    l += st[u].y * wgt;
+#pragma unroll
+                    for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
+                }
+            }
+        }
+        if constexpr (W == 1) {
+            const float inv = 1.0f / l;
+            if (row0 + all < rows)
+#pragma unroll
+                for (int e = 0; e < CPL; ++e) write(row, 32 * e + lane, o[e] * inv, M, l);
+        } else {
+            if (row0 != (int)blockIdx.y * RPB) __syncthreads();   // (the rows before are read)
+#pragma unroll
+            for (int e = 0; e < CPL; ++e) s_o[all][32 * e + lane] = o[e];
+            if (lane == 0) { s_stat[all][0] = M; s_stat[all][1] = l; }
+            __syncthreads();
+            const int first = all / W * W;
+            if (row0 + all / W < rows)
+                for (int c = threadIdx.x % (32 * W); c < D; c += 32 * W) {   // the row's threads: a channel each
+                    M = s_stat[first][0];
+                    for (int x = 1; x < W; ++x) M = fmaxf(M, s_stat[first + x][0]);
+                    float sum = 0.f;
+                    l = 0.f;
+                    for (int x = 0; x < W; ++x) {
+                        const float wgt = s_stat[first + x][0] == -INFINITY ? 0.f : ex2(s_stat[first + x][0] - M);
+                        l += s_stat[first + x][1] * wgt;
+                        sum += s_o[first + x][c] * wgt;
+                    }
+                    write(row, c, sum * (1.0f / l), M, l);
+                }
+        }
     }
 }
 
 template <int D, int TILE, int R>
 inline cudaError_t launch_join(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const PagedOut& o,
-                               const Parts& parts, const Deal& d, cudaStream_t stream) {
-    const int rows = max_n * (cv.Hq / cv.Hkv);
+                               const Parts& parts, const Deal& d, int sms, cudaStream_t stream) {
+    const int units = cv.B * cv.Hkv, G = cv.Hq / cv.Hkv, rows = max_n * G, most = (8 * sms + units - 1) / units;   // blocks of a unit
     if (d.blocks > 4 * d.units)   // (a unit has up to about blocks / units + 1 parts)
-        return launch_pdl(paged_join_kernel<D, TILE, R, 8>, dim3(cv.B * cv.Hkv, rows), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
-    return launch_pdl(paged_join_kernel<D, TILE, R, 2>, dim3(cv.B * cv.Hkv, (rows + 3) / 4), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv);
+        return launch_pdl(paged_join_kernel<D, TILE, R, 8>, dim3(units, std::min(rows, most)), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, group_log(G));
+    return launch_pdl(paged_join_kernel<D, TILE, R, 1>, dim3(units, std::min((rows + 7) / 8, most)), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, group_log(G));
 }
 
 // map over a pool: rows (page, KV head, token of the page) x channels
@@ -274,7 +295,6 @@ inline bool make_pool_map(CUtensorMap* map, const void* pool, const CacheView& c
     const uint32_t box[2] = {64u, (uint32_t)std::min(pv.page, keys)};
     return make_tensor_map_bf16(map, pool, 2, dims, strides, box);
 }
-inline int group_log(int G) { return G == 1 ? 0 : G == 2 ? 1 : G == 4 ? 2 : 3; }
 
 }  // namespace pieces
 

@@ -372,7 +372,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
                                      cv.stats, q_rows, (D / 64) * box * G * 128, n_q, slots, d.whole ? 1 : 0, group_log(G));
     *launches = d.whole ? 1 : 2;
     if (e != cudaSuccess || d.whole) return e;
-    return launch_join<D, kKeys, kRows>(cv, pv, ch, lens, max_n, o, parts, d, stream);
+    return launch_join<D, kKeys, kRows>(cv, pv, ch, lens, max_n, o, parts, d, sms, stream);
 }
 
 }  // namespace
