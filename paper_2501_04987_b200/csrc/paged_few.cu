@@ -170,10 +170,13 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             Ring rk(0, slots), rv(1, slots);
             int g = 0, piece = 0;         // tiles whose S^T is issued
             bool starts = false;                                   // the tile whose O^T comes next is the first of its piece
+            int o_piece = 0;              // that piece
             int steps = 0;                                         // and its groups of 16 keys
-            auto issue_o = [&](int of_piece) {
-                if (starts && !(ok = mbar_wait(bar(O_FREE), (of_piece & 1) ^ 1))) return;
-                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL), (g - 1) & 1))) return;
+            // of tile g - 1: its values and weights are there, and the first of a piece: the rows of the piece before are out
+            auto o_ready = [&]() {
+                return ready2(bar(FULL + rv.slot), rv.phase, bar(P_FULL), (g - 1) & 1) && (!starts || ready(bar(O_FREE), (o_piece & 1) ^ 1));
+            };
+            auto issue_o = [&]() {
                 tc_fence_after();
                 const uint32_t v = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
@@ -185,25 +188,38 @@ paged_few_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
             };
             for (; ok && w.get(); ++piece) {
                 const int qs = piece & 1;
-                if (!(ok = mbar_wait(bar(Q_FULL + qs), (piece >> 1) & 1))) break;
-                for (int t = w.t0; t < w.t1; ++t) {
-                    // the logits of the tile before are in registers: this one's take their place
-                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_READ), (g & 1) ^ 1))) break;
-                    tc_fence_after();
-                    const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (QB / 16);
+                for (int t = w.t0; t < w.t1 && ok; ++t) {
+                    // this tile's S - the logits of the tile before are in registers, and these take their place - and the O of the tile before, in
+                    // whichever order they can
+                    bool s_due = true, o_due = g > 0;
+                    for (uint32_t looks = 0; s_due || o_due;) {
+                        if (s_due && ready2(bar(FULL + rk.slot), rk.phase, bar(S_READ), (g & 1) ^ 1) && (t > w.t0 || ready(bar(Q_FULL + qs), (piece >> 1) & 1))) {
+                            tc_fence_after();
+                            const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (QB / 16);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tmem, desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), desc_of(q + (kk >> 2) * (R * 128 / 16) + (kk & 3) * 2), idesc_s, kk > 0);
-                    umma_commit(bar(USED + rk.slot));
-                    if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
-                    rk.next(); rk.next();
-                    if (g > 0) { issue_o(t == w.t0 ? piece - 1 : piece); if (!ok) break; }
-                    starts = t == w.t0;
+                            for (int kk = 0; kk < D / 16; ++kk)
+                                umma_bf16(tmem, desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), desc_of(q + (kk >> 2) * (R * 128 / 16) + (kk & 3) * 2), idesc_s, kk > 0);
+                            umma_commit(bar(USED + rk.slot));
+                            if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
+                            rk.next(); rk.next();
+                            s_due = false;
+                        } else if (o_due && o_ready()) {
+                            issue_o();
+                            o_due = false;
+                        } else if (++looks == kLookLimit) {
+                            ok = false;
+                            break;
+                        }
+                    }
+                    starts = t == w.t0; o_piece = piece;
                     steps = min(kTile / 16, (w.nvis - t * kTile + 15) / 16);
                     ++g;
                 }
             }
-            if (ok && g > 0) issue_o(piece - 1);
+            for (uint32_t looks = 0; ok && g > 0;) {
+                if (o_ready()) { issue_o(); break; }
+                ok = ++looks < kLookLimit;
+            }
             // every MMA has finished before its memory and tensor memory are given to anything else
             if (ok && g > 0) ok = mbar_wait(bar(O_DONE), (g - 1) & 1);
             if (!ok) atomicOr(&stats->error, 8u);

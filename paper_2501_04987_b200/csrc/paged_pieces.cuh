@@ -65,16 +65,20 @@ struct Walk {
     int b, kh, past, n, rows, nvis, tiles, t0, t1;  // of the piece: tiles [t0, t1) of the unit's
     __device__ Walk(const int* first_, const int* pasts_, const ChunkLens* lens_, int B_, int Hkv_, int glog_, bool whole_, int per)
         : first(first_), pasts(pasts_), lens(lens_), B(B_), Hkv(Hkv_), G(1 << glog_), glog(glog_), whole(whole_) {
-        item = min((int)blockIdx.x * per, first[B]); end = min(item + per, first[B]);
+        b = -1; item = min((int)blockIdx.x * per, first[B]); end = min(item + per, first[B]);
     }
     __device__ bool get() {
         while (item < end) {
-            int lo = 0, hi = B - 1;      // the last sequence that starts at or before the item
-            while (lo < hi) {
-                const int mid = (lo + hi + 1) >> 1;
-                if (first[mid] <= item) lo = mid; else hi = mid - 1;
+            if (b < 0) {                 // the last sequence that starts at or before the item
+                int lo = 0, hi = B - 1;
+                while (lo < hi) {
+                    const int mid = (lo + hi + 1) >> 1;
+                    if (first[mid] <= item) lo = mid; else hi = mid - 1;
+                }
+                b = lo;
+            } else {
+                while (b + 1 < B && first[b + 1] <= item) ++b;
             }
-            b = lo;
             n = lens->m[b]; past = pasts[b];
             rows = n << glog; nvis = past + n;
             tiles = (nvis + TILE - 1) / TILE;
@@ -117,11 +121,16 @@ __device__ inline void plan_items(const PagedView& pv, const ChunkLens& lens, in
 }
 
 // New tokens into their pages, by the block that reads the tile they lie in, before its loads are issued: `nthr` threads, four pieces
-// of 16 bytes on their way each.  A page that cannot be: nothing is written.
+// of 16 bytes on their way each; where a sequence brings few, its warps take pieces of units in turns.  A page that cannot be: nothing is
+// written.
 template <int D, int TILE>
 __device__ inline void append_tokens(Walk<TILE> a, const PagedView& pv, const ChunkView& ch, int Hkv, DevStats* stats, int t, int nthr) {
     constexpr int C = D / 8, U = 4;
-    while (a.get()) {
+    const bool turns = ch.stride * C <= 64;
+    const int turn = t >> 5, warps = nthr >> 5;
+    if (turns) { t &= 31; nthr = 32; }
+    for (int x = 0; a.get(); ++x) {
+        if (turns && x % warps != turn) continue;
         const int lo = max(0, a.t0 * TILE - a.past), hi = min(a.n, a.t1 * TILE - a.past);
         for (int e0 = t; e0 < (hi - lo) * C; e0 += U * nthr) {
             uint4 k[U], v[U];
@@ -287,6 +296,25 @@ inline cudaError_t launch_join(const CacheView& cv, const PagedView& pv, const C
         return launch_pdl(paged_join_kernel<D, TILE, R, 8>, dim3(units, std::min(rows, most)), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, group_log(G));
     return launch_pdl(paged_join_kernel<D, TILE, R, 1>, dim3(units, std::min((rows + 7) / 8, most)), dim3(256), 0, stream, pv, ch, lens, o, parts, cv.Hq, cv.Hkv, group_log(G));
 }
+
+// one or two barriers looked at, without waiting
+__device__ inline bool ready(uint32_t bar, uint32_t par) {
+    uint32_t a;
+    asm volatile("{\n\t.reg .pred p;\n\tmbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\tselp.u32 %0, 1, 0, p;\n\t}" : "=r"(a) : "r"(bar), "r"(par) : "memory");
+    return a;
+}
+__device__ inline bool ready2(uint32_t bar_a, uint32_t par_a, uint32_t bar_b, uint32_t par_b) {
+    uint32_t a;
+    asm volatile(
+        "{\n\t.reg .pred p, q;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 p, [%1], %2;\n\t"
+        "mbarrier.test_wait.parity.shared::cta.b64 q, [%3], %4;\n\t"
+        "and.pred p, p, q;\n\t"
+        "selp.u32 %0, 1, 0, p;\n\t}"
+        : "=r"(a) : "r"(bar_a), "r"(par_a), "r"(bar_b), "r"(par_b) : "memory");
+    return a;
+}
+constexpr uint32_t kLookLimit = 1u << 24;  // looks, of about 160 cycles each
 
 // map over a pool: rows (page, KV head, token of the page) x channels
 inline bool make_pool_map(CUtensorMap* map, const void* pool, const CacheView& cv, const PagedView& pv, int keys) {

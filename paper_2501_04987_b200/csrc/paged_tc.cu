@@ -152,12 +152,16 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             Ring rk(0, slots), rv(1, slots);
             int g = 0, piece = 0;         // tiles whose S is issued
             bool starts = false;          // the tile whose O comes next is the first of its piece
+            int o_piece = 0;              // that piece
             int steps = 0;                // and its groups of 16 keys
             int last = 0, last_phase = 0; // V of the last tile
-            auto issue_o = [&](int of_piece) {
+            // of tile g - 1: its values and weights are there, and the first of a piece: the rows of the piece before are out
+            auto o_ready = [&]() {
+                return ready2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + ((g - 1) & 1)), ((g - 1) >> 1) & 1) &&
+                       (!starts || ready(bar(O_FREE), (o_piece & 1) ^ 1));
+            };
+            auto issue_o = [&]() {
                 const int pb = (g - 1) & 1;
-                if (starts && !(ok = mbar_wait(bar(O_FREE), (of_piece & 1) ^ 1))) return;
-                if (!(ok = mbar_wait2(bar(FULL + rv.slot), rv.phase, bar(P_FULL + pb), ((g - 1) >> 1) & 1))) return;
                 tc_fence_after();
                 const uint32_t v = v_lo + rv.slot * (SLOT / 16);
 #pragma unroll
@@ -169,25 +173,38 @@ paged_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             };
             for (; ok && w.get(); ++piece) {
                 const int qs = q_slot(piece);
-                if (!(ok = mbar_wait(bar(Q_FULL + qs), q_phase(piece)))) break;
-                for (int t = w.t0; t < w.t1; ++t) {
-                    // the logits of the tile before are in registers: this one's take their place
-                    if (!(ok = mbar_wait2(bar(FULL + rk.slot), rk.phase, bar(S_READ), (g & 1) ^ 1))) break;
-                    tc_fence_after();
-                    const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (q_tile / 16);
+                for (int t = w.t0; t < w.t1 && ok; ++t) {
+                    // this tile's S - the logits of the tile before are in registers, and these take their place - and the O of the tile before, in
+                    // whichever order they can
+                    bool s_due = true, o_due = g > 0;
+                    for (uint32_t looks = 0; s_due || o_due;) {
+                        if (s_due && ready2(bar(FULL + rk.slot), rk.phase, bar(S_READ), (g & 1) ^ 1) && (t > w.t0 || ready(bar(Q_FULL + qs), q_phase(piece)))) {
+                            tc_fence_after();
+                            const uint32_t k = k_lo + rk.slot * (SLOT / 16), q = q_lo + qs * (q_tile / 16);
 #pragma unroll
-                    for (int kk = 0; kk < D / 16; ++kk)
-                        umma_bf16(tmem, desc_of(q + (kk >> 2) * q_half + (kk & 3) * 2), desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), idesc_s, kk > 0);
-                    umma_commit(bar(USED + rk.slot));
-                    if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
-                    rk.next(); rk.next();
-                    if (g > 0) { issue_o(t == w.t0 ? piece - 1 : piece); if (!ok) break; }
-                    starts = t == w.t0;
+                            for (int kk = 0; kk < D / 16; ++kk)
+                                umma_bf16(tmem, desc_of(q + (kk >> 2) * q_half + (kk & 3) * 2), desc_of(k + (kk >> 2) * (HALF / 16) + (kk & 3) * 2), idesc_s, kk > 0);
+                            umma_commit(bar(USED + rk.slot));
+                            if (t + 1 == w.t1) umma_commit(bar(Q_FREE + qs));
+                            rk.next(); rk.next();
+                            s_due = false;
+                        } else if (o_due && o_ready()) {
+                            issue_o();
+                            o_due = false;
+                        } else if (++looks == kLookLimit) {
+                            ok = false;
+                            break;
+                        }
+                    }
+                    starts = t == w.t0; o_piece = piece;
                     steps = min(kKeys / 16, (w.nvis - t * kKeys + 15) / 16);
                     ++g;
                 }
             }
-            if (ok && g > 0) issue_o(piece - 1);
+            for (uint32_t looks = 0; ok && g > 0;) {
+                if (o_ready()) { issue_o(); break; }
+                ok = ++looks < kLookLimit;
+            }
             // every MMA has finished before its memory and tensor memory are given to anything else
             if (ok && g > 0) ok = mbar_wait(bar(USED + last), last_phase);
             if (!ok) atomicOr(&stats->error, 8u);
