@@ -246,7 +246,8 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
 #pragma unroll
         for (int e = 1; e < E; ++e) ms.a = fmaxf(ms.a, r[e]);
         ms.a = warp_max(ms.a);
-        const float mine = ms.a == -INFINITY ? 0.f : ms.a;
+        const bool some = ms.a > -INFINITY;
+        const float mine = some ? ms.a : 0.f;
 #pragma unroll
         for (int e = 0; e < E; ++e) {
             r[e] = ex2((r[e] - mine) * sc);
@@ -255,9 +256,8 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
         ms = join(ms, s_join, slot, rank, split, SumOp{sc});
         // NaN, an infinite logit, or nothing above minus infinity
         if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;
-        const float top = ms.a, inv = 1.0f / ms.b, own = ex2((mine - top) * sc) * inv;
-#pragma unroll
-        for (int e = 0; e < E; ++e) r[e] = r[e] == 0.f ? 0.f : r[e] * own;  // (a warp without numbers has any reference)
+        const float top = ms.a, inv = 1.0f / ms.b;
+        float own = some ? ex2((mine - top) * sc) * inv : 0.f;   // r own: probabilities; multiplied only where a node needs them all
         float R = 1.f;
         int rejected = 0;
         bool lost = false;
@@ -295,10 +295,11 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                     get_beside<W, VEC>(q, whole, a.vocab, row.first(first + u0 * step), step * VEC, 0.f, qv);
 #pragma unroll
                     for (int e = 0; e < W * VEC; ++e) {
-                        r[u0 * VEC + e] = fmaxf(fmaf(r[u0 * VEC + e], over, -qv[e]), 0.f);
+                        r[u0 * VEC + e] = fmaxf(fmaf(r[u0 * VEC + e], own * over, -qv[e]), 0.f);
                         sum.a += r[u0 * VEC + e];
                     }
                 }
+                own = 1.f;
                 if (lane == 0) s_over[tid >> 5][rejected] = over;
                 __syncwarp();
                 ++rejected;
@@ -322,7 +323,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                 for (int u = 0; u < W; ++u)
 #pragma unroll
                     for (int e = 0; e < VEC; ++e) {
-                        const float z = __fdividef(r[(u0 + u) * VEC + e], e4[u * VEC + e]);   // (2 ulp: two that are closer count as equal)
+                        const float z = __fdividef(r[(u0 + u) * VEC + e] * own, e4[u * VEC + e]);   // (2 ulp: two that are closer count as equal)
                         if (z > best.a) { best.a = z; best.b = __int_as_float(row.first(first + (u0 + u) * step) + e); }
                     }
             }
@@ -333,6 +334,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
             row.template get<U>(first, step, r);
 #pragma unroll
             for (int e = 0; e < E; ++e) r[e] = ex2((r[e] - top) * sc) * inv;
+            own = 1.f;
             next = race();
         }
         if (next == 0x7fffffff) next = -1;
