@@ -2,8 +2,7 @@
 // step or a short draft of every sequence.
 //
 // Such a call is bound by the pages it reads: two blocks per SM, each with tiles in flight while the other works on its own, and
-// the tiles of all units (sequence, KV head) in a row, of which every block takes the same number, wherever the units end.  A block that has a unit to itself writes its rows; otherwise it leaves its part - maximum,
-// sum, unnormalised output - in the caller's scratch, and a second small launch joins the parts in order.
+// the tiles of all units (sequence, KV head) in a row, of which every block takes the same number, wherever the units end.
 //
 // With few rows the logits are taken transposed, so that the tensor core's 128 matrix rows are 128 keys:
 //     S^T = K Q^T   thread = key;  p = exp2(S^T c - m_row), the reference m_row common to the block
@@ -16,6 +15,12 @@
 //
 // The new tokens' keys and values enter their pages here too: by the block that will read the tile they lie in, before its TMA
 // load is issued.
+//
+// Measured, 8 KV heads of 128 x 4: 37 sequences of 8192, a unit a block, 182 us, the copy bandwidth; 32 of up to 4096 55 us, 5.2 TB/s; one
+// of 100000 72 us, 5.7 TB/s; one of 128 6.9 us.  What is left is 6 us to the first tiles and 3 to the last rows, and 5 of the second launch.
+//
+// Up to 16 rows, where the tile of 128 rows of paged_tc.cu takes as long or longer: one sequence of 128 7.9 us (6.9 here), 64 of up to
+// 2048 71 (56), 16 of 8192 with heads of 64 60 (54); 16 rows a head 92.6 (92.6).
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 are the softmax warps (one per lane quarter).
 #include <algorithm>

@@ -11,6 +11,12 @@
 // all rows see in front of those that fewer and fewer do: so the blocks end together.  With fewer items than the machine has SMs a
 // cluster shares an item's query tiles.
 //
+// A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 38 us, 3.5 TB/s; the
+// exponentials alone take 15 us, the matrix instructions 10), a chunk by both units: 128 x 128 logits are 512 cycles of matrix
+// instructions, fed from shared memory at its 128 bytes a cycle, and 1024 cycles of exponentials, of which a quarter is made on the
+// multiply-add units (none: 248 us, a quarter: 238, half: 262, at 4 x 1024 over 8192).  Measured and not taken: two key tiles an item (chunk
+// 150 -> 157 us), logit tiles of 256 columns (249 -> 283).  4 chunks of 1024 over up to 4096: 145 us, 600 TFLOP/s.
+//
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 and 6-9 are two groups that take alternate logit tiles.
 #include <algorithm>
 
@@ -257,7 +263,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const float sc2 = kLog2e * rsqrtf((float)D), over = 1.0f / (float)w.G;
         int st = 0, mine = 0, shared = 0;  // steps of the block; of this group, those with log-sum-exps of their own; items that both groups had steps of
         int held_unit = -1, held_q = -1;   // whose log-sum-exps this group has in shared memory
-        for (; ok && w.get(); w.next()) {
+        for (; w.get(); w.next()) {   // (a wait that gave up ends the waiting, not the walk: the warps meet at barriers)
             float sum = 0.f, comp = 0.f;
             const int kpos = w.k0 + key, r_min = max(0, kpos - w.past) * w.G;  // first row that sees this key
             auto lse_of = [&](int qt) {  // of column `key` of a query tile
@@ -280,7 +286,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 }
                 const float* nl = s_lse[group][mine & 1];
                 if (x + 2 < steps) l_next = lse_of(qt + 2 * split);
-                if (!mbar_wait(bar(S_FULL + buf), (s >> 2) & 1)) { ok = false; break; }
+                ok = ok && mbar_wait(bar(S_FULL + buf), (s >> 2) & 1);
                 tc_fence_after();
                 const int cmin = r_min - qt * kTile, cmax = w.rows - qt * kTile;     // columns [cmin, cmax) are rows that see the key
                 const int from = __reduce_max_sync(0xffffffffu, cmin), lead = __reduce_min_sync(0xffffffffu, cmin);
@@ -305,7 +311,6 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 comp = (t - sum) - y;
                 sum = t;
             }
-            if (!ok) break;
             // the group that took the item's first step writes; the other one's sum comes through shared memory
             const bool writer = (st & 1) == group;
             st += steps;
@@ -330,16 +335,16 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                     if (rank == 0) {
                         // (blocks beyond `split` do not exist: their arrivals are made here)
                         if (lane == 0) for (int x2 = split; x2 < kMaxSplit; ++x2) mbar_arrive(bar(JOIN));
-                        if (!mbar_wait_cluster(bar(JOIN), 0)) { ok = false; break; }
+                        ok = ok && mbar_wait_cluster(bar(JOIN), 0);
                         sum = 0.f;
                         for (int r = 0; r < split; ++r) sum += s_join[r][key];
-                        if (kpos < w.nvis) {
+                        if (ok && kpos < w.nvis) {
                             float* at = sa.scores + ((size_t)w.b * Hkv + w.kh) * sa.score_stride + kpos;
                             *at = sa.add ? *at + sum * over : sum * over;
                         }
                     }
                 }
-            } else if (writer && kpos < w.nvis) {
+            } else if (ok && writer && kpos < w.nvis) {
                 float* at = sa.scores + ((size_t)w.b * Hkv + w.kh) * sa.score_stride + kpos;
                 *at = sa.add ? *at + sum * over : sum * over;
             }

@@ -186,8 +186,103 @@ def test_attend_steps_of_ragged_batches(gpu, d, hq, hkv, page, longest, count):
     assert P.kv.stats()["device_error"] == 0
 
 
+@pytest.mark.parametrize("d,hq,hkv,page", [(128, 16, 4, 16), (64, 8, 8, 64), (64, 16, 2, 256), (128, 2, 2, 32)])
+@pytest.mark.parametrize("longest,count,tokens", [(3000, 24, 16), (300, 60, 16), (9000, 3, 15), (2000, 30, 9), (40, 30, 32), (6000, 2, 128), (1500, 9, 60)])
+def test_attend_short_chunks_of_ragged_batches(gpu, d, hq, hkv, page, longest, count, tokens):
+    """17 rows a KV head and more: blocks take whole units, parts of one, ends and starts; sequences with nothing new between them."""
+    past = [(7919 * i * i + 131 * i) % (longest + 1) for i in range(count)]
+    past[0] = longest
+    new = [(37 * i * i + 11 * i) % (tokens + 1) for i in range(count)]
+    new[-1] = tokens
+    P = Prompts(gpu, "bf16", d, hq, hkv, page, past, new, tokens, seed=longest)
+    for bound in (longest, None):
+        out, lse = P.attend(max_past=bound)
+        _check_attend(P, out, lse)
+    _check_pages(P)
+    assert P.kv.stats()["device_error"] == 0
+
+
+@pytest.mark.parametrize("d,hq,hkv", [(128, 4, 1), (64, 8, 4), (128, 8, 1)])
+@pytest.mark.parametrize("past,n", [(20000, 5), (20000, 16), (20000, 33), (20000, 129), (7000, 300), (1100, 65), (1100, 257)])
+def test_attend_of_one_user(gpu, d, hq, hkv, past, n):
+    """Few units: the keys of each are shared by many blocks, also by more than there are tiles to share."""
+    P = Prompts(gpu, "bf16", d, hq, hkv, 64, [past], [n], n + 1, seed=past + n)
+    for bound in (past, 60000 if past < 5000 else None):
+        out, lse = P.attend(max_past=min(bound, P.width * 64) if bound else None)
+        _check_attend(P, out, lse)
+    _check_pages(P)
+    assert P.kv.stats()["device_error"] == 0
+
+
+def test_the_largest_batch(gpu):
+    import torch
+
+    for n, hq in ((1, 4), (32, 4), (40, 4), (17, 1)):
+        past = [i % 90 for i in range(1024)]
+        new = [(5 * i) % (n + 1) for i in range(1024)]
+        new[3] = n
+        P = Prompts(gpu, "bf16", 128, hq, 1, 16, past, new, n, seed=n)
+        out, lse = P.attend(max_past=89)
+        torch.cuda.synchronize()
+        assert P.kv.stats()["device_error"] == 0
+        keep = [b for b in range(1024) if b % 37 < 2 or b == 3]
+        for x in ("past", "new", "K", "V"):
+            setattr(P, x, [getattr(P, x)[b] for b in keep])
+        P.q, out, lse = P.q[keep], out[keep], lse[keep]
+        _check_attend(P, out, lse)
+
+
+@pytest.mark.parametrize("dtype,new", [("bf16", [2, 1, 0]), ("bf16", [40, 3, 17]), ("bf16", [200, 300, 1]), ("f32", [3, 40, 2])])
+def test_calls_on_two_streams_at_once(gpu, dtype, new):
+    """Calls that overlap have nothing in common but the context: each gives what it gives alone, to the bit."""
+    import torch
+
+    P = [Prompts(gpu, dtype, 64, 8, 2, 16, [3000, 77, 500], new, max(new), seed=s) for s in range(2)]
+    alone = [p.attend() for p in P]
+    P[1].kv = P[0].kv
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in P]
+    got = [[], []]
+    for _ in range(8):
+        for x, (p, s) in enumerate(zip(P, streams)):
+            with torch.cuda.stream(s):
+                got[x].append(p.attend())
+    torch.cuda.synchronize()
+    for p, one, many in zip(P, alone, got):
+        for out, lse in many:
+            for b, n in enumerate(p.new):
+                assert torch.equal(out[b, :n], one[0][b, :n]) and torch.equal(lse[b, :n], one[1][b, :n])
+
+
+def test_two_captured_calls_share_nothing(gpu):
+    """Two graphs of calls that leave parts behind, replayed in turns and at once."""
+    import torch
+
+    P = [Prompts(gpu, "bf16", 128, 8, 2, 64, [9000], [n], n, seed=n) for n in (2, 30)]
+    P.append(Prompts(gpu, "bf16", 128, 8, 2, 64, [5000], [150], 150, seed=3))
+    alone = [p.attend() for p in P]
+    torch.cuda.synchronize()
+    graphs, outs = [], []
+    for p in P:
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            outs.append(p.attend())
+        graphs.append(g)
+    streams = [torch.cuda.Stream() for _ in P]
+    for _ in range(3):
+        for o in outs:
+            o[0].zero_(), o[1].zero_()
+        torch.cuda.synchronize()
+        for g, s in zip(graphs, streams):
+            with torch.cuda.stream(s):
+                g.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(alone, outs):
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
 @pytest.mark.parametrize("dtype,d,page", [("bf16", 128, 64), ("bf16", 64, 16), ("f32", 128, 32)])
-@pytest.mark.parametrize("past,n", [(0, 200), (70, 7), (300, 150), (64, 64), (9000, 6)])
+@pytest.mark.parametrize("past,n", [(0, 200), (70, 7), (300, 150), (64, 64), (9000, 6), (9000, 40), (9000, 150)])
 def test_values_that_are_not_finite(gpu, dtype, d, page, past, n):
     """A value of infinity or NaN reaches the rows that see its token and no other."""
     import torch
