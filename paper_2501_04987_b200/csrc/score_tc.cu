@@ -11,13 +11,14 @@
 // all rows see in front of those that fewer and fewer do: so the blocks end together.  With fewer items than the machine has SMs a
 // cluster shares an item's query tiles.
 //
-// A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 38 us, 3.5 TB/s; the
-// exponentials alone take 15 us, the matrix instructions 10), a chunk by both units: 128 x 128 logits are 512 cycles of matrix
-// instructions, fed from shared memory at its 128 bytes a cycle, and 1024 cycles of exponentials, of which a quarter is made on the
-// multiply-add units (none: 248 us, a quarter: 238, half: 262, at 4 x 1024 over 8192).  Measured and not taken: two key tiles an item (chunk
-// 150 -> 157 us), logit tiles of 256 columns (249 -> 283).  4 chunks of 1024 over up to 4096: 145 us, 600 TFLOP/s.
+// A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 38 us, 3.6 TB/s; the
+// exponentials alone take 15 us, the matrix instructions 10).  A chunk's logit tile of 128 x 128 takes 1480 cycles, of which shared memory
+// is busy for some 1300: 512 for the operands of the matrix instructions, 512 for the log-sum-exps that every warp reads, 256 for the
+// queries that come in.  The exponentials take 770, with one in four on the multiply-add units (none: 223 us, 216).  Measured and not taken:
+// a second thread that issues (211), scalar multiply-adds (228), two key tiles an item, each its own group (150 -> 157), logit tiles of
+// 256 columns (249 -> 283).  4 chunks of up to 1024 over up to 4096: 133 us, 660 TFLOP/s.
 //
-// Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 2-5 and 6-9 are two groups that take alternate logit tiles.
+// Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, from 2 on two or four groups of four that take logit tiles in turns.
 #include <algorithm>
 
 #include "exp2_fma.cuh"
@@ -30,7 +31,7 @@ namespace {
 
 using namespace vtc;
 
-constexpr int kThreads = 320;
+constexpr int threads(int groups) { return 64 + 128 * groups; }
 constexpr int kTile = 128;                 // keys of an item, query rows of a step
 constexpr uint32_t kTmemCols = 512;        // four logit tiles
 constexpr size_t kSmemMin = 120 * 1024;    // one block on an SM: it holds all of the tensor memory
@@ -40,7 +41,7 @@ constexpr int kMaxSplit = 8;
 constexpr int kTiles = 6, kMost = 4;
 
 enum Bar { K_FULL = 0, K_FREE = K_FULL + kMost, Q_FULL = K_FREE + kMost, Q_FREE = Q_FULL + kMost, S_FULL = Q_FREE + kMost, S_FREE = S_FULL + 4,
-           JOIN = S_FREE + 4, N_BARS = JOIN + 1 };
+           PART_FULL = S_FREE + 4, PART_FREE = PART_FULL + 2, JOIN = PART_FREE + 2, N_BARS = JOIN + 1 };
 
 // The items of a block in order, the same for every role: in a row (step 1; a sequence's key tiles head by head, where a division
 // per item would cost as much as its arithmetic), or every step-th (all heads of a key tile, then the next).
@@ -82,7 +83,7 @@ struct Walk {
 };
 
 // Sum of exp2(v sc2 + nl) of 32 columns; of those with `masked` only the ones in [lo, hi).  One pair in four goes to the multiply-add
-// units: of none 248 us, of half 262, of one in four 238 (4 x 1024 rows over 5120 keys, 8 KV heads).
+// units (4 x 1024 tokens over 4096, 8 KV heads of 128 x 4: of none 223 us, of one in four 216).
 template <bool MASKED>
 __device__ inline void add_columns(const uint32_t (&v)[32], const float* nl, float sc2, int lo, int hi, float2& a, float2& b) {
     const float2 sc = make_float2(sc2, sc2), one = make_float2(1.f, 1.f);
@@ -100,8 +101,8 @@ __device__ inline void add_columns(const uint32_t (&v)[32], const float* nl, flo
     }
 }
 
-template <int D>
-__global__ void __launch_bounds__(kThreads, 1)
+template <int D, int NG>
+__global__ void __launch_bounds__(threads(NG), 1)
 score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__ CUtensorMap tmK, PagedView pv, ChunkView ch, ChunkLens lens,
                 ScoreArgs sa, int B, int Hq, int Hkv, DevStats* stats, int q_bytes, int in_a_row, int split) {
     constexpr int HALVES = D / 64, SLOT = kTile * D * 2, HALF = kTile * 128;
@@ -109,8 +110,8 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     extern __shared__ unsigned char smem_raw[];
     __shared__ __align__(8) uint64_t bars[N_BARS];
     __shared__ uint32_t tmem_slot;
-    __shared__ __align__(16) float s_lse[2][2][kTile];     // [group][parity of its steps] minus log-sum-exps in units of log 2
-    __shared__ float s_part[2][kTile];                      // the second group's sums
+    __shared__ __align__(16) float s_lse[NG][2][kTile];     // [group][parity of its steps] minus log-sum-exps in units of log 2
+    __shared__ float s_part[2][NG][kTile];             // the groups' sums of an item
     __shared__ __align__(8) float s_join[kMaxSplit][kTile]; // (block 0 of a cluster) the blocks' sums
     const uint32_t base = (smem_addr_u32(smem_raw) + 1023u) & ~1023u;
     const int k_log = in_a_row ? 2 : 1, k_slots = 1 << k_log, q_log = 3 - k_log, q_slots = 1 << q_log;
@@ -123,6 +124,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     if (tid == 0) {
         for (int s = 0; s < kMost; ++s) { mbar_init(bar(K_FULL + s), 1); mbar_init(bar(K_FREE + s), 1); mbar_init(bar(Q_FULL + s), 1); mbar_init(bar(Q_FREE + s), 1); }
         for (int s = 0; s < 4; ++s) { mbar_init(bar(S_FULL + s), 1); mbar_init(bar(S_FREE + s), 4); }
+        for (int s = 0; s < 2; ++s) { mbar_init(bar(PART_FULL + s), 4 * (NG - 1)); mbar_init(bar(PART_FREE + s), 4); }
         mbar_init(bar(JOIN), 4 * kMaxSplit);
         mbar_fence_init();
     }
@@ -257,11 +259,11 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             if (!ok) atomicOr(&stats->error, 8u);
         }
     } else {
-        // ================= the two groups
+        // ================= the groups
         const int group = (warp - 2) >> 2, quarter = warp & 3, key = quarter * 32 + lane;
         const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
         const float sc2 = kLog2e * rsqrtf((float)D), over = 1.0f / (float)w.G;
-        int st = 0, mine = 0, shared = 0;  // steps of the block; of this group, those with log-sum-exps of their own; items that both groups had steps of
+        int st = 0, mine = 0, shared = 0;  // steps of the block; of this group, those with log-sum-exps of their own; items of several steps
         int held_unit = -1, held_q = -1;   // whose log-sum-exps this group has in shared memory
         for (; w.get(); w.next()) {   // (a wait that gave up ends the waiting, not the walk: the warps meet at barriers)
             float sum = 0.f, comp = 0.f;
@@ -271,13 +273,12 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 return qt < w.qb && r < w.rows ? sa.lse[((size_t)w.b * ch.stride + r / w.G) * Hq + w.kh * w.G + r % w.G] : INFINITY;
             };
             const int steps = w.qa + rank < w.qb ? split == 1 ? w.qb - w.qa : (w.qb - w.qa - rank + split - 1) / split : 0;
-            const bool both = steps > 1;         // each group has steps of this item
-            int x = (st & 1) == group ? 0 : 1;   // this group's first step of the item
+            int x = (group - st) & (NG - 1);   // this group's first step of the item
             const int unit = w.b * Hkv + w.kh, q_first = w.qa + rank + x * split;
             const bool held = steps == 1 && unit == held_unit && q_first == held_q;   // the log-sum-exps of the step before
             float l_next = x < steps && !held ? lse_of(q_first) : 0.f;
-            if (x < steps) { held_unit = unit; held_q = w.qa + rank + (x + (steps - 1 - x) / 2 * 2) * split; }
-            for (; x < steps; x += 2) {
+            if (x < steps) { held_unit = unit; held_q = w.qa + rank + (x + (steps - 1 - x) / NG * NG) * split; }
+            for (; x < steps; x += NG) {
                 const int qt = w.qa + rank + x * split, s = st + x, buf = s & 3;
                 if (!held) {
                     ++mine;
@@ -285,7 +286,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                     asm volatile("bar.sync %0, 128;" ::"r"(1 + group) : "memory");
                 }
                 const float* nl = s_lse[group][mine & 1];
-                if (x + 2 < steps) l_next = lse_of(qt + 2 * split);
+                if (x + NG < steps) l_next = lse_of(qt + NG * split);
                 ok = ok && mbar_wait(bar(S_FULL + buf), (s >> 2) & 1);
                 tc_fence_after();
                 const int cmin = r_min - qt * kTile, cmax = w.rows - qt * kTile;     // columns [cmin, cmax) are rows that see the key
@@ -311,16 +312,22 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
                 comp = (t - sum) - y;
                 sum = t;
             }
-            // the group that took the item's first step writes; the other one's sum comes through shared memory
-            const bool writer = (st & 1) == group;
+            // the group that took the item's first step writes; the others' sums come through shared memory, in their order
+            const bool writer = (st & (NG - 1)) == group;
             st += steps;
-            if (both) {
+            if (steps > 1) {
+                const int slot = shared & 1, use = shared >> 1 & 1;
                 if (!writer) {
-                    s_part[shared & 1][key] = sum;
-                    asm volatile("bar.sync 3, 256;" ::: "memory");
+                    ok = ok && mbar_wait(bar(PART_FREE + slot), use ^ 1);
+                    s_part[slot][group][key] = sum;
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(PART_FULL + slot));
                 } else {
-                    asm volatile("bar.sync 3, 256;" ::: "memory");
-                    sum += s_part[shared & 1][key];
+                    ok = ok && mbar_wait(bar(PART_FULL + slot), use);
+#pragma unroll
+                    for (int x2 = 1; x2 < NG; ++x2) sum += s_part[slot][(group + x2) & (NG - 1)][key];
+                    __syncwarp();
+                    if (lane == 0) mbar_arrive(bar(PART_FREE + slot));
                 }
                 ++shared;
             }
@@ -358,7 +365,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
     if (warp == 1) { tc_fence_after(); tmem_dealloc(tmem, kTmemCols); }
 }
 
-template <int D>
+template <int D, int NG>
 cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const ScoreArgs& a, int sms,
                      cudaStream_t stream) {
     const int G = cv.Hq / cv.Hkv, box = std::min(kTile / G, ch.stride);
@@ -369,7 +376,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     const uint64_t strides[1] = {(uint64_t)cv.d * 2};
     const uint32_t kbox[2] = {64u, (uint32_t)std::min(pv.page, kTile)};
     if (!make_tensor_map_bf16(&tmK, pv.kp, 2, dims, strides, kbox)) return cudaErrorInvalidValue;
-    auto kern = score_tc_kernel<D>;
+    auto kern = score_tc_kernel<D, NG>;
     const size_t smem = std::max(kSmemMin, (size_t)1024 + kTiles * kTile * D * 2 + 4 * (2 * (size_t)cv.B + 1));
     static bool smem_set[64] = {};  // per device: the opt-in is needed once
     int dev = 0;
@@ -389,7 +396,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     while (split < kMaxSplit && items * split * 2 <= sms && qtiles >= split * 4) split *= 2;
     cudaLaunchConfig_t cfg = {};
     cfg.gridDim = dim3((unsigned)(split > 1 ? items * split : std::min<long>(items, sms)));
-    cfg.blockDim = dim3(kThreads);
+    cfg.blockDim = dim3(threads(NG));
     cfg.dynamicSmemBytes = smem;
     cfg.stream = stream;
     cudaLaunchAttribute attr[2];
@@ -408,7 +415,12 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
 
 cudaError_t launch_score_tc(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const ScoreArgs& a,
                             int sms, cudaStream_t stream) {
-    return cv.d == 64 ? launch_t<64>(cv, pv, ch, lens, max_n, a, sms, stream) : launch_t<128>(cv, pv, ch, lens, max_n, a, sms, stream);
+    // Two groups for up to two query tiles, where the keys stream by (8 x 32 tokens x 4 heads over 8192: 38 us, with four 42; 2 x 64
+    // over 10000: 26 and 29), four for more, where each waits for its own arithmetic (4 x 512 over 4096: 120 with two, 117 with four; 4 x
+    // 1024: 234 and 216).
+    const bool window = max_n * (cv.Hq / cv.Hkv) <= 2 * kTile;
+    if (cv.d == 64) return window ? launch_t<64, 2>(cv, pv, ch, lens, max_n, a, sms, stream) : launch_t<64, 4>(cv, pv, ch, lens, max_n, a, sms, stream);
+    return window ? launch_t<128, 2>(cv, pv, ch, lens, max_n, a, sms, stream) : launch_t<128, 4>(cv, pv, ch, lens, max_n, a, sms, stream);
 }
 
 }  // namespace treekv
