@@ -22,7 +22,8 @@
 // 674 TFLOP/s (an item of 16 tiles at the mean pays some 5 us for its start and its rows, and half of two tiles on the diagonal); 64 tokens of
 // one over 60000 80 us, 3.1 TB/s.  Measured and not taken: blocks that stay and fetch their next item (566 us against 527, short
 // prompts 300 against 268), a share of the exponentials on the multiply-add units (574 to 621 against 551: the same warps feed both),
-// registers 216 / 72 (611) and 200 / 104.
+// registers 216 / 72 (611) and 200 / 104; eight warps a row tile, two threads a row (596 against 530), an issuer for each row tile (656: the
+// tiles no longer take turns).
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, 4-7 and 8-11 are the groups of the two row tiles, which take over
 // registers that the first four do not need.
