@@ -86,8 +86,7 @@ struct Walk {
             int at = item - first[b];
             if (whole) { kh = at; t0 = 0; t1 = tiles; ++item; return true; }
             const int each = tiles + kStart<TILE>;
-            kh = (int)__fdividef((float)at, (float)each);   // (off by one at most)
-            kh += (at >= (kh + 1) * each) - (at < kh * each);
+            kh = quotient(at, each);
             at -= kh * each + kStart<TILE>;
             t0 = max(0, at); t1 = min(tiles, at + end - item);
             item += tiles - at;

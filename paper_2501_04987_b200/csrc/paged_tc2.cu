@@ -69,9 +69,9 @@ struct Item {
     int b, kh, n, past, r0, rows, tok0, t_end, cached, tiles;  // tokens [tok0, t_end); key tiles over the pages, all
     // false: nothing to do
     __device__ bool get(const PagedView& pv, const ChunkLens& lens, int x, const Order& od, int G, int Hkv) {
-        const int wave = x / (od.group * od.per_unit), first = wave * od.group, here = min(od.group, od.units - first);
-        const int y = x - first * od.per_unit, at = y / here, unit = first + y - at * here;
-        b = unit / Hkv; kh = unit - b * Hkv;
+        const int wave = quotient(x, od.group * od.per_unit), first = wave * od.group, here = min(od.group, od.units - first);
+        const int y = x - first * od.per_unit, at = quotient(y, here), unit = first + y - at * here;
+        b = quotient(unit, Hkv); kh = unit - b * Hkv;
         n = lens.m[b];
         const int mine = (n * G + kRows - 1) / kRows;
         if (at >= mine) return false;
@@ -438,11 +438,12 @@ paged_tc2_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant_
                                 *at = __float2bfloat16_rn(__bfloat162float(*at) + y);
                             }
                         }
+                    const int gl = 31 - __clz(G);
                     __syncwarp();   // (a warp writes the rows that it has put together)
                     for (int e = lane; e < 32 * (D / 8); e += 32) {
                         const int rr = quarter * 32 + e / (D / 8), c = e % (D / 8), ru = it.r0 + g * kTile + rr;
                         if (rr < rows)
-                            reinterpret_cast<uint4*>(po.out)[((tok_at + ru / G) * Hq + it.kh * G + ru % G) * (D / 8) + c] =
+                            reinterpret_cast<uint4*>(po.out)[((tok_at + (ru >> gl)) * Hq + it.kh * G + (ru & (G - 1))) * (D / 8) + c] =
                                 *reinterpret_cast<const uint4*>(stage + rr * D * 2 + ((c ^ (rr & 7)) << 4));
                     }
                 } else {

@@ -58,7 +58,7 @@ struct Walk {
                 if (++kt == tiles) { kt = 0; ++kh; }
             } else {
                 const int at = item - first[b];
-                kt = at / Hkv; kh = at - kt * Hkv;
+                kt = quotient(at, Hkv); kh = at - kt * Hkv;
             }
         } else {
             int lo = max(b, 0), hi = B - 1;   // the last sequence that starts at or before the item
@@ -72,8 +72,8 @@ struct Walk {
             tiles = (nvis + kTile - 1) / kTile;
             qb = (rows + kTile - 1) / kTile;
             const int at = item - first[b];
-            if (step == 1) { kh = at / tiles; kt = at - kh * tiles; }
-            else { kt = at / Hkv; kh = at - kt * Hkv; }
+            if (step == 1) { kh = quotient(at, tiles); kt = at - kh * tiles; }
+            else { kt = quotient(at, Hkv); kh = at - kt * Hkv; }
         }
         k0 = kt * kTile;
         qa = max(0, k0 - past) * G / kTile;
@@ -263,6 +263,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
         const int group = (warp - 2) >> 2, quarter = warp & 3, key = quarter * 32 + lane;
         const uint32_t lane_off = (uint32_t)(quarter * 32) << 16;
         const float sc2 = kLog2e * rsqrtf((float)D), over = 1.0f / (float)w.G;
+        const int glog = 31 - __clz(w.G);
         int st = 0, mine = 0, shared = 0;  // steps of the block; of this group, those with log-sum-exps of their own; items of several steps
         int held_unit = -1, held_q = -1;   // whose log-sum-exps this group has in shared memory
         for (; w.get(); w.next()) {   // (a wait that gave up ends the waiting, not the walk: the warps meet at barriers)
@@ -270,7 +271,7 @@ score_tc_kernel(const __grid_constant__ CUtensorMap tmQ, const __grid_constant__
             const int kpos = w.k0 + key, r_min = max(0, kpos - w.past) * w.G;  // first row that sees this key
             auto lse_of = [&](int qt) {  // of column `key` of a query tile
                 const int r = qt * kTile + key;
-                return qt < w.qb && r < w.rows ? sa.lse[((size_t)w.b * ch.stride + r / w.G) * Hq + w.kh * w.G + r % w.G] : INFINITY;
+                return qt < w.qb && r < w.rows ? sa.lse[((size_t)w.b * ch.stride + (r >> glog)) * Hq + w.kh * w.G + (r & (w.G - 1))] : INFINITY;
             };
             const int steps = w.qa + rank < w.qb ? split == 1 ? w.qb - w.qa : (w.qb - w.qa - rank + split - 1) / split : 0;
             int x = (group - st) & (NG - 1);   // this group's first step of the item
