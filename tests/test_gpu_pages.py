@@ -573,7 +573,7 @@ def test_adopt(gpu, dtype, d, hq, hkv, page, budget, protect, lens, average):
     assert kv.stats()["device_error"] == 0
 
 
-@pytest.mark.parametrize("n,value", [(50000, None), (70001, 0.25), (20000, 0.0), (9000, None), (450000, None)])
+@pytest.mark.parametrize("n,value", [(50000, None), (70001, 0.25), (20000, 0.0), (9000, None), (450000, None), (900000, None), (900000, 0.5)])
 def test_adopt_long_and_equal_weights(gpu, n, value):
     """Few units: clusters share one; all weights equal: the oldest stay."""
     import torch
