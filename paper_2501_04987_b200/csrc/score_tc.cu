@@ -12,11 +12,12 @@
 // cluster shares an item's query tiles.
 //
 // A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 38 us, 3.6 TB/s; the
-// exponentials alone take 15 us, the matrix instructions 10).  A chunk's logit tile of 128 x 128 takes 1480 cycles, of which shared memory
-// is busy for some 1300: 512 for the operands of the matrix instructions, 512 for the log-sum-exps that every warp reads, 256 for the
-// queries that come in.  The exponentials take 770, with one in four on the multiply-add units (none: 223 us, 216).  Measured and not taken:
-// a second thread that issues (211), scalar multiply-adds (228), two key tiles an item, each its own group (150 -> 157), logit tiles of
-// 256 columns (249 -> 283).  4 chunks of up to 1024 over up to 4096: 133 us, 660 TFLOP/s.
+// exponentials alone take 15 us, the matrix instructions 10).  A chunk's logit tile of 128 x 128 takes 1480 cycles: 512 of matrix
+// instructions, 770 of exponentials with one in four on the multiply-add units, 512 for the log-sum-exps that every warp reads.  By the
+// counters no unit is busy for half the time, and none of these changed it by much (4 x 1024 over 4096, 216 us): no exponentials on the
+// multiply-add units (223), scalar multiply-adds (228), a second thread that issues (211), two key tiles a thread, which halves the
+// reads and the queries that come in (223; over 8192 395 against 407), logit tiles of 256 columns (249 -> 283, with two groups).
+// 4 chunks of up to 1024 over up to 4096: 132 us, 660 TFLOP/s.
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, from 2 on two or four groups of four that take logit tiles in turns.
 #include <algorithm>
