@@ -12,12 +12,12 @@
 // the way from one row to the next.  A cluster of blocks takes a sequence; a thread loads its E numbers of a row at once and
 // keeps what is left of their probabilities in registers, so a row is read once and its exponentials are taken once, whatever
 // happens at its node.  The row of the first child is asked into L2 while its parent's is worked on, the children's own logits are
-// fetched beside the row.  Sums and maxima are joined by pushing a block's pair into every block of the cluster: one barrier, then
-// each warp joins the pairs it finds at home, in one order.  All arithmetic is fp32.
+// fetched beside the row.  Sums and maxima are joined by sending a block's pair into every block of the cluster, where a barrier counts
+// the bytes, and each warp joins the pairs it finds at home, in one order.  All arithmetic is fp32.
 //
-// Measured: 8 nodes of 32000 in a chain, one sequence, 14 us; trees of 16 for 32 sequences, 128000 tokens, drawn from given probabilities,
-// 48 us.  A node of that size takes 5 us: 64 KB of logits an SM 1.5, 32000 exponentials an SM 1, the join 1.2; the race at the end 4.
-// Asking a node's draft row into L2 ahead of a rejection gave nothing (48.7 us).
+// Measured: 8 nodes of 32000 in a chain, one sequence, 12 us; trees of 16 for 32 sequences, 128000 tokens, drawn from given probabilities,
+// 44 us.  A node of that size takes some 4.5 us: 64 KB of logits an SM 1.5, 32000 exponentials an SM 1, the join 0.8; the race at the
+// end 4.  With a barrier of the cluster for a join 14 and 48 us.  Asking a node's draft row into L2 ahead of a rejection gave nothing.
 #include <algorithm>
 
 #include "paged.cuh"
@@ -134,14 +134,17 @@ struct AddOp {
     __device__ Pair operator()(Pair x) const { return {warp_sum(x.a), 0.f}; }
 };
 struct JoinSpace {
+    uint64_t bar[2];           // the blocks' pairs of a slot are there
     Pair warp[2][kWarps];
     Pair block[2][kMaxSplit];
 };
-// Joins one pair per thread over the cluster; every thread gets the result.  `slot` alternates from call to call: a slot is
-// written again two calls on, which the barrier of the call between comes before.
+// Joins one pair per thread over the cluster; every thread gets the result.  `calls` counts: a slot is written again two calls on, when
+// every block has sent its pair of the call between, and so is through with this one.  The pairs come with their bytes counted by
+// the receiver's barrier: a barrier of the whole cluster would wait for the rows asked into L2, too.
 template <typename Op>
-__device__ inline Pair join(Pair x, JoinSpace& js, int& slot, int rank, int split, Op op) {
-    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+__device__ inline Pair join(Pair x, JoinSpace& js, int& calls, int rank, int split, bool& ok, Op op) {
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5, slot = calls & 1, phase = calls >> 1 & 1;
+    ++calls;
     x = op(x);
     if (lane == 0) js.warp[slot][warp] = x;
     __syncthreads();
@@ -150,14 +153,16 @@ __device__ inline Pair join(Pair x, JoinSpace& js, int& slot, int rank, int spli
     } else {
         if (warp == 0) {
             x = op(lane < kWarps ? js.warp[slot][lane] : op.none());
+            const uint32_t bar = smem_addr_u32(&js.bar[slot]);
+            if (lane == 0) mbar_arrive_expect_tx(bar, split * sizeof(Pair));
             if (lane < split)
-                asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(map_to_cta(smem_addr_u32(&js.block[slot][rank]), lane)), "f"(x.a), "f"(x.b) : "memory");
+                asm volatile("st.async.shared::cluster.mbarrier::complete_tx::bytes.v2.f32 [%0], {%1, %2}, [%3];" ::"r"(
+                                 map_to_cta(smem_addr_u32(&js.block[slot][rank]), lane)), "f"(x.a), "f"(x.b), "r"(map_to_cta(bar, lane)) : "memory");
         }
+        ok = ok && mbar_wait_cluster(smem_addr_u32(&js.bar[slot]), phase);
         __syncwarp();
-        cluster_sync_all();
         x = op(lane < split ? js.block[slot][lane] : op.none());
     }
-    slot ^= 1;
     return x;
 }
 
@@ -185,6 +190,11 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
     const T* logits = reinterpret_cast<const T*>(a.logits) + (size_t)b * a.stride * a.vocab;
     const float* noise = a.noise + (size_t)b * a.vocab;
     const int first = rank * kThreads + tid, step = split * kThreads;
+    if (tid == 0) {
+        mbar_init(smem_addr_u32(&s_join.bar[0]), 1);
+        mbar_init(smem_addr_u32(&s_join.bar[1]), 1);
+        mbar_fence_init();
+    }
     if (tid < n) {
         const uint64_t below = (a.mask ? a.mask[(size_t)b * a.stride + tid] : low_bits(tid)) & low_bits(tid);
         s_parent[tid] = below ? 63 - __clzll((long long)below) : -1;
@@ -196,11 +206,12 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
     if (!greedy) // the one row of random numbers that is needed, a line of 128 bytes at a time
         for (int x = first * 32; x < a.vocab; x += step * 32) ask_l2(noise + x);
     __syncthreads();
-    if (split > 1) cluster_sync_all();  // every block is running before pairs are pushed to it
+    if (split > 1) cluster_sync_all();  // every block is running, and its barriers are there, before pairs are sent to it
     const float sc = greedy ? 1.f : kLog2e / a.temperature;
-    int at = 0, depth = 0, slot = 0, next = -1;
-    for (;;) {
-        if (tid == 0) s_path[depth] = at;       // (in memory at the end: a store under way would hold up the cluster's barriers)
+    int at = 0, depth = 0, calls = 0, next = -1;
+    bool ok = true;                         // no wait has given up
+    for (;;) {   // (a wait that gave up ends the waiting, not the walk: the warps meet at barriers)
+        if (tid == 0) s_path[depth] = at;       // (in memory at the end)
         const Row<T> row(logits + (size_t)at * a.vocab, a.vocab);
         const float* q = a.draft && !greedy ? a.draft + ((size_t)b * a.stride + at) * a.vocab : nullptr;
         float r[E];
@@ -234,7 +245,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                     if (f > best.a) { best.a = f; best.b = __int_as_float(row.first(first + u * step) + e); }
                 }
             if (wrong) { best.a = INFINITY; best.b = __int_as_float(-1); }   // a row with a NaN picks nothing
-            best = join(best, s_join, slot, rank, split, LargestOp());
+            best = join(best, s_join, calls, rank, split, ok, LargestOp());
             int token = __float_as_int(best.b);
             if (token == 0x7fffffff) token = -1;
             for (uint64_t left = kids; left; left &= left - 1) {
@@ -257,7 +268,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
             r[e] = ex2((r[e] - mine) * sc);
             ms.b += r[e];
         }
-        ms = join(ms, s_join, slot, rank, split, SumOp{sc});
+        ms = join(ms, s_join, calls, rank, split, ok, SumOp{sc});
         // NaN, an infinite logit, or nothing above minus infinity
         if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;
         const float top = ms.a, inv = 1.0f / ms.b;
@@ -308,7 +319,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                 __syncwarp();
                 ++rejected;
                 if (left & (left - 1)) {         // another child: how much is left
-                    sum = join(sum, s_join, slot, rank, split, AddOp());
+                    sum = join(sum, s_join, calls, rank, split, ok, AddOp());
                     R = sum.a;
                     if (!(R > 0.f)) { lost = true; break; }  // nothing is left
                 }
@@ -331,7 +342,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                         if (z > best.a) { best.a = z; best.b = __int_as_float(row.first(first + (u0 + u) * step) + e); }
                     }
             }
-            return __float_as_int(join(best, s_join, slot, rank, split, LargestOp()).b);
+            return __float_as_int(join(best, s_join, calls, rank, split, ok, LargestOp()).b);
         };
         next = lost ? 0x7fffffff : race();
         if (next == 0x7fffffff && rejected) {    // rounding has left nothing: the target's own probabilities
@@ -347,6 +358,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
     __syncthreads();
     if (rank == 0 && tid < a.stride) path[tid] = tid < depth ? s_path[tid] : -1;
     if (rank == 0 && tid == 0) { a.count[b] = depth; a.next[b] = next; }
+    if (!ok && tid == 0) atomicOr(&stats->error, 16u);
     if (split > 1) { __syncwarp(); cluster_sync_all(); }  // nobody leaves while pairs may be pushed to it
 }
 
