@@ -439,7 +439,7 @@ treekv_status treekv_pick_path(treekv_ctx* ctx, const void* dev_logits, treekv_d
 /* Counters and error words.  Synchronises `stream` to read the device-side counters.  *host_out is filled
  * whenever the read itself succeeded; the return value is TREEKV_ERR_TIMEOUT when device_error is non-zero, i.e.
  * when a kernel's bounded wait gave up (bits: 4 TMA producer, 8 MMA issuer, 16 softmax / epilogue warps of the
- * tensor-core prefill kernels, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v), or
+ * tensor-core kernels and the joins of treekv_pick_path, 32 misaligned shared memory, 64 the self-test below, 128 the decode kernel's fetch of the step's q, k, v), or
  * TREEKV_ERR_INVALID_ARG when its only bit is 256: an index in device memory was out of range and was not followed
  * (treekv_norm_rope, treekv_accept_path, the calls on pages, treekv_pick_path).  treekv_reset clears it; caches that a bad index of treekv_norm_rope has not
  * touched survive that as an image (treekv_export_state before it, treekv_import_state after it). */
