@@ -16,7 +16,7 @@
 // The new tokens' keys and values enter their pages here too: by the block that will read the tile they lie in, before its TMA
 // load is issued.
 //
-// Measured, 8 KV heads of 128 x 4: 37 sequences of 8192, a unit a block, 185 us, the copy bandwidth; 32 of up to 4096 55 us, 5.2 TB/s; one
+// Measured, 8 KV heads of 128 x 4: 37 sequences of 8192, a unit a block, 189 us, the copy bandwidth; 32 of up to 4096 55 us, 5.2 TB/s; one
 // of 100000 72 us, 5.7 TB/s; one of 128 6.9 us.  What is left is 6 us to the first tiles and 3 to the last rows, and 5 of the second launch.
 //
 // Up to 16 rows, where the tile of 128 rows of paged_tc.cu takes as long or longer: one sequence of 128 7.9 us (6.9 here), 64 of up to

@@ -32,15 +32,15 @@ __global__ void __launch_bounds__(kThreads)
 score_f32_kernel(PagedView pv, ChunkView ch, ChunkLens lens, ScoreArgs sa, int Hq, int Hkv, DevStats* stats, int split) {
     pdl_trigger();
     pdl_wait();
-    const int unit = blockIdx.z, b = unit / Hkv, kh = unit % Hkv, rank = blockIdx.x;
+    const int unit = blockIdx.z, b = unit / Hkv, kh = unit % Hkv, tile = (int)blockIdx.x / split, rank = (int)blockIdx.x - tile * split;
     const int n = lens.m[b], G = Hq / Hkv, rows = n * G;
     if (n == 0) return;    // the whole cluster
     const int past = paged_past(pv, b, n);
     if (past < 0) {
-        if (threadIdx.x == 0 && rank == 0 && blockIdx.y == 0) atomicOr(&stats->error, kErrBadIndex);
+        if (threadIdx.x == 0 && rank == 0 && tile == 0) atomicOr(&stats->error, kErrBadIndex);
         return;
     }
-    const int nvis = past + n, k_block = blockIdx.y * kWarps * kKeys;
+    const int nvis = past + n, k_block = tile * kWarps * kKeys;
     if (k_block >= nvis) return;
     extern __shared__ __align__(16) float smem[];
     __shared__ float s_lse[2][kRows];
@@ -161,7 +161,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     int split = 1;
     while (split < kMaxSplit && blocks * split * 2 <= 3L * sms && qtiles >= split * 2) split *= 2;
     cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(split, tiles, cv.B * cv.Hkv);
+    cfg.gridDim = dim3(split * tiles, 1, cv.B * cv.Hkv);   // (a long table has more tiles than the grid's other dimensions take)
     cfg.blockDim = dim3(kThreads);
     cfg.dynamicSmemBytes = smem_bytes<D>();
     cfg.stream = stream;

@@ -214,6 +214,27 @@ def test_attend_of_one_user(gpu, d, hq, hkv, past, n):
     assert P.kv.stats()["device_error"] == 0
 
 
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("new", [[3, 2], [60, 5]])
+def test_tables_of_millions_of_tokens(gpu, dtype, new):
+    """A table's width, and with it the largest past a launch has to expect, says nothing about how long its sequences are."""
+    import torch
+
+    P = Prompts(gpu, dtype, 64, 4, 2, 64, [700, 90], new, max(new), seed=1)
+    wide = torch.full((2, 70000), -7, dtype=torch.int32, device="cuda")
+    wide[:, :P.width] = P.table
+    P.table = wide
+    out, lse = P.attend()
+    _check_attend(P, out, lse)
+    s = torch.full((2, 2, 70000 * 64 + max(new)), 7.0, device="cuda")
+    P.kv.paged_score(P.q, lse, P.kp, P.table, P.past_dev, s, lens=new)
+    _check_score(P, lse, s)
+    for b, (p, n) in enumerate(zip(P.past, new)):
+        assert bool((s[b, :, p + n:] == 7).all())
+    P.kv.adopt_pages(P.kp, P.vp, P.table, s, [p + n for p, n in zip(P.past, new)])
+    assert P.kv.stats()["device_error"] == 0
+
+
 def test_the_largest_batch(gpu):
     import torch
 
