@@ -387,7 +387,9 @@ treekv_status treekv_paged_attend(treekv_ctx* ctx, const void* dev_q, const void
  * only its last rows are passed.
  *   dev_q, dev_lse, host_lens, stride   as in the treekv_paged_attend call of these rows, or of the last of them, with past the
  *                                       position of the first one passed.  A row whose log-sum-exp is infinite gives nothing
- *   dev_scores      [batch][n_kv_heads][score_stride] float, score_stride >= max_past + the longest length
+ *   dev_scores      [batch][n_kv_heads][score_stride] float: past + length <= score_stride, or the sequence sits the call out and
+ *                   device_error gets bit 256.  (TREEKV_ERR_INVALID_ARG where max_past + the shortest length of the call, those of 0
+ *                   aside, is more: no sequence could have such a past)
  * Positions at and beyond past + length are not written.  Every sum has one order: results do not vary from run to run.
  */
 treekv_status treekv_paged_score(treekv_ctx* ctx, const void* dev_q, const float* dev_lse, const void* dev_k_pages, int n_pages,

@@ -554,7 +554,8 @@ class TreeKV:
 
     def paged_score(self, q, lse, k_pages, table, past, scores, lens=None, max_past=None, add=False):
         """scores [batch, n_kv_heads, tokens] float32: written, or with add=True increased by, what the rows q gave to every token
-        of their sequence; past[b] is the position of the first of them."""
+        of their sequence; past[b] is the position of the first of them, and past[b] + lens[b] at most `tokens`.  max_past: no past
+        is larger (what the scores hold otherwise)."""
         want, t = self._want, self.torch
         B, Hq = self.batch, self.n_heads
         n = q.shape[1]
@@ -565,7 +566,7 @@ class TreeKV:
         ps = want(scores, t.float32, (B, self.n_kv_heads, steps), "scores")
         pn, kept = self._lens(lens, "chunk lengths")
         if max_past is None:
-            max_past = max(0, min(width * page, steps - n))
+            max_past = max(0, min(width * page, steps - (n if lens is None else min((x for x in lens if x), default=0))))
         st = lib.treekv_paged_score(self._h, pq, pl, kp, pages, page, pt, width, pp, max_past, ps, steps, 1 if add else 0, pn, n, self._stream())
         if st:
             _check(st, "treekv_paged_score")

@@ -36,6 +36,7 @@ treekv_status make_view(const treekv_ctx* ctx, const void* kp, const void* vp, i
     memset(pv, 0, sizeof(*pv));
     pv->kp = const_cast<void*>(kp); pv->vp = const_cast<void*>(vp); pv->table = table; pv->n_pages = n_pages; pv->page = page; pv->width = width;
     while ((1 << pv->plog) < page) ++pv->plog;
+    pv->limit = width * page;
     return TREEKV_OK;
 }
 
@@ -118,8 +119,13 @@ treekv_status treekv_paged_score(treekv_ctx* ctx, const void* dev_q, const float
     int max_n;
     st = chunk_lens(ctx, host_lens, stride, &lens, &max_n);
     if (st != TREEKV_OK) return st;
-    // a sequence whose rows reach past the scores would write behind them
-    if (score_stride < (int64_t)max_past + max_n) return TREEKV_ERR_INVALID_ARG;
+    // A sequence whose rows reach past the scores would write behind them: the device, which has the pasts, leaves it out.  Of a past that
+    // not even the shortest sequence could have, the host says so.
+    int least = max_n;
+    for (int b = 0; b < ctx->cv.B; ++b)
+        if (lens.m[b] && lens.m[b] < least) least = lens.m[b];
+    if (score_stride < (int64_t)max_past + least) return TREEKV_ERR_INVALID_ARG;
+    pv.limit = (int)std::min<int64_t>(pv.limit, score_stride);
     if (max_n == 0) return TREEKV_OK;
     if (!on_own_device(ctx)) return TREEKV_ERR_BAD_STATE;
     cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -16,6 +16,7 @@ struct PagedView {
     const int32_t* past;   // [B] tokens in the pages before this call
     int n_pages, page, plog, width;
     int max_past;          // no past is longer
+    int limit;             // tokens of a sequence, at most: what its row of the table, and of the scores, holds
 };
 
 // a chunk's tensors as the caller passed them
@@ -35,7 +36,7 @@ struct PagedOut {
 // tokens of sequence b in the pages before its n new ones; -1: what stands there cannot be (the sequence sits the call out)
 __device__ inline int paged_past(const PagedView& pv, int b, int n) {
     const int p = pv.past[b];
-    return p < 0 || p > pv.max_past || (long long)p + n > (long long)pv.width << pv.plog ? -1 : p;
+    return p < 0 || p > pv.max_past || p + n > pv.limit ? -1 : p;   // (both sums stay below 2^31)
 }
 // orders what earlier kernels stored to global memory (the new tokens' rows) before this thread's TMA loads of it
 __device__ inline void fence_proxy_async_global() { asm volatile("fence.proxy.async.global;" ::: "memory"); }

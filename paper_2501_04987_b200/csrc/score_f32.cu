@@ -154,10 +154,10 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
         if (e != cudaSuccess) return e;
         smem_set[dev] = true;
     }
-    const int G = cv.Hq / cv.Hkv, per = kWarps * kKeys, tiles = (pv.max_past + max_n + per - 1) / per, qtiles = (max_n * G + kRows - 1) / kRows;
+    const int G = cv.Hq / cv.Hkv, per = kWarps * kKeys, tiles = (std::min(pv.max_past + max_n, pv.limit) + per - 1) / per, qtiles = (max_n * G + kRows - 1) / kRows;
     long blocks = 0;
     for (int b = 0; b < cv.B; ++b)
-        if (lens.m[b]) blocks += (long)((pv.max_past + lens.m[b] + per - 1) / per) * cv.Hkv;
+        if (lens.m[b]) blocks += (long)((std::min(pv.max_past + lens.m[b], pv.limit) + per - 1) / per) * cv.Hkv;
     int split = 1;
     while (split < kMaxSplit && blocks * split * 2 <= 3L * sms && qtiles >= split * 2) split *= 2;
     cudaLaunchConfig_t cfg = {};

@@ -392,7 +392,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
     long items = 0;  // at most
     int active = 0;
     for (int b = 0; b < cv.B; ++b)
-        if (lens.m[b]) { items += (long)(pv.max_past + lens.m[b] + kTile - 1) / kTile * cv.Hkv; ++active; }
+        if (lens.m[b]) { items += (long)(std::min(pv.max_past + lens.m[b], pv.limit) + kTile - 1) / kTile * cv.Hkv; ++active; }
     const int qtiles = (max_n * G + kTile - 1) / kTile;
     int split = 1;
     while (split < kMaxSplit && items * split * 2 <= sms && qtiles >= split * 4) split *= 2;
