@@ -400,18 +400,17 @@ paged_f32_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, float* __restr
             }
         }
         const float top = fmaxf(fmaxf(fmaxf(M, st[0].x), fmaxf(st[1].x, st[2].x)), st[3].x);
-        if (top > -INFINITY) {
-            const float fix = exp2f(M - top);
-            M = top; l *= fix;
+        // (a part whose logits are all NaN has no maximum either: times a weight of zero its sum stays NaN)
+        const float at = top == -INFINITY ? 0.f : top, fix = exp2f(M - at);
+        M = top; l *= fix;
 #pragma unroll
-            for (int e = 0; e < CPL; ++e) o[e] *= fix;
+        for (int e = 0; e < CPL; ++e) o[e] *= fix;
 #pragma unroll
-            for (int u = 0; u < 4; ++u) {
-                const float wgt = exp2f(st[u].x - M);
-                l += st[u].y * wgt;
+        for (int u = 0; u < 4; ++u) {
+            const float wgt = exp2f(st[u].x - at);
+            l += st[u].y * wgt;
 #pragma unroll
-                for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
-            }
+            for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
         }
     }
 #pragma unroll

@@ -245,18 +245,17 @@ paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts
                 }
             }
             const float top = fmaxf(fmaxf(fmaxf(M, st[0].x), fmaxf(st[1].x, st[2].x)), st[3].x);
-            if (top > -INFINITY) {
-                const float fix = ex2(M - top);
-                M = top; l *= fix;
+            // (a part whose logits are all NaN has no reference either: times a weight of zero its sum stays NaN)
+            const float at = top == -INFINITY ? 0.f : top, fix = ex2(M - at);
+            M = top; l *= fix;
 #pragma unroll
-                for (int e = 0; e < CPL; ++e) o[e] *= fix;
+            for (int e = 0; e < CPL; ++e) o[e] *= fix;
 #pragma unroll
-                for (int u = 0; u < 4; ++u) {
-                    const float wgt = ex2(st[u].x - M);
-                    l += st[u].y * wgt;
+            for (int u = 0; u < 4; ++u) {
+                const float wgt = ex2(st[u].x - at);
+                l += st[u].y * wgt;
 #pragma unroll
-                    for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
-                }
+                for (int e = 0; e < CPL; ++e) o[e] += y[u][e] * wgt;
             }
         }
         if constexpr (W == 1) {

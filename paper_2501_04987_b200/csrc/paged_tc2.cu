@@ -492,20 +492,20 @@ paged_join2_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Part
             const size_t p = p0 + min(s0 + u, shares - 1);
             st[u] = parts.stat[p * kRows + row];
             y[u] = *reinterpret_cast<const float4*>(parts.o + (p * kRows + row) * D + 4 * c);
-            if (s0 + u >= shares) st[u].x = -INFINITY;
+            if (s0 + u >= shares) { st[u] = make_float2(-INFINITY, 0.f); y[u] = make_float4(0.f, 0.f, 0.f, 0.f); }
             top = fmaxf(top, st[u].x);
 #pragma unroll
             for (int w = 0; w < 8; ++w) bad[w] |= parts.bad[p * 8 + w];
         }
-        if (top == -INFINITY) continue;
-        const float fix = ex2(M - top);
+        // (no key of a part is seen, or there is none: reference minus infinity, the rest zeros.  Its logits are all NaN: the same reference,
+        // and times a weight of zero its sum stays NaN)
+        const float base = top == -INFINITY ? 0.f : top, fix = ex2(M - base);
         M = top; l *= fix;
 #pragma unroll
         for (int e = 0; e < 4; ++e) o[e] *= fix;
 #pragma unroll
         for (int u = 0; u < 4; ++u) {
-            if (st[u].x == -INFINITY) continue;   // (no key of the part is seen, or there is none)
-            const float f = ex2(st[u].x - M);
+            const float f = ex2(st[u].x - base);
             l += st[u].y * f;
             o[0] += y[u].x * f; o[1] += y[u].y * f; o[2] += y[u].z * f; o[3] += y[u].w * f;
         }

@@ -1,5 +1,7 @@
-"""Edges of the calls on pages: score rows exactly as wide as their prompts.
+"""Edges of the calls on pages: score rows exactly as wide as their prompts, keys that are NaN for a whole share of a row's keys.
 """
+import math
+
 import pytest
 
 from test_gpu_pages import BAD_INDEX, INVALID, Prompts, _check_score
@@ -51,3 +53,44 @@ def test_a_sequence_that_reaches_past_its_scores_sits_out(gpu, dtype):
         Q = Prompts(gpu, dtype, 64, 4, 2, 16, [126, 64, 90, 5], [0, 64, 38, 1], 64)
         Q.K, Q.q = P.K, P.q
         _check_score(Q, lse, s)
+
+
+# ---- attention: a share of the keys that holds nothing but NaN ---------------------------------------------------------
+@pytest.mark.parametrize("dtype,hq,hkv,past,n", [
+    ("bf16", 4, 1, 20000, 1), ("bf16", 4, 1, 6912, 4), ("bf16", 32, 32, 1280, 2), ("bf16", 16, 8, 4096, 3),            # up to 16 rows
+    ("bf16", 4, 1, 20000, 16), ("bf16", 8, 1, 6912, 5), ("bf16", 32, 32, 1280, 30), ("bf16", 32, 8, 4096, 20),         # up to 128
+    ("bf16", 4, 1, 6912, 300), ("bf16", 4, 1, 1280, 70), ("bf16", 16, 4, 4096, 200),                                   # beyond
+    ("f32", 4, 1, 20000, 2), ("f32", 4, 4, 6912, 1), ("f32", 8, 2, 20000, 9), ("f32", 4, 4, 640, 5)])
+def test_shares_of_nan_keys(gpu, dtype, hq, hkv, past, n):
+    """Wherever the keys of a row are cut: keys of NaN reach every row that sees one, and no other."""
+    import torch
+
+    P = Prompts(gpu, dtype, 64, hq, hkv, 64, [past], [n], n, seed=past + n)
+    clean, k = P.kp.clone(), P.k.clone()
+    plain = P.attend(max_past=past)
+    assert bool(plain[0].isfinite().all()) and bool(plain[1].isfinite().all())
+    pages = P.table[0].long()
+
+    def poison(a, b):       # keys [a, b) of the past
+        for x in range(a // 64, -(-b // 64)):
+            P.kp[pages[x], :, max(0, a - 64 * x):min(64, b - 64 * x)] = math.nan
+
+    ranges = [(0, past // 2), (0, past - 128), (past - 128, past), (past // 128 * 64, past), (0, 16), (past - 32, past), (0, past)]
+    ranges += [(0, x) for x in range(512, past, 512)]
+    for a, b in ranges:
+        P.kp.copy_(clean)
+        P.k.copy_(k)
+        poison(a, b)
+        for bound in (past, None):
+            out, lse = P.attend(max_past=bound)
+            assert bool(out.isnan().all()) and bool(lse.isnan().all()), (a, b, bound)
+    for first in {0, 1, n // 2, n - 1} & set(range(n)):
+        for last in {first + 1, n}:
+            P.kp.copy_(clean)
+            P.k.copy_(k)
+            P.k[0, first:last] = math.nan
+            for bound in (past, None):
+                out, lse = P.attend(max_past=bound)
+                assert bool(out[0, first:].isnan().all()) and bool(lse[0, first:].isnan().all()), (first, last, bound)
+                assert bool(out[0, :first].isfinite().all()) and bool(lse[0, :first].isfinite().all()), (first, last, bound)
+    assert P.kv.stats()["device_error"] == 0
