@@ -197,8 +197,8 @@ paged_join_kernel(PagedView pv, ChunkView ch, ChunkLens lens, PagedOut po, Parts
     constexpr int CPL = D / 32, RPB = 8 / W;   // a lane's channels; rows at a time
     pdl_trigger();
     const int unit = blockIdx.x, b = unit / Hkv, kh = unit - b * Hkv, n = lens.m[b], rows = n << glog;
-    if ((int)blockIdx.y * RPB >= rows) return;
     pdl_wait();
+    if ((int)blockIdx.y * RPB >= rows) return;
     const int past = paged_past(pv, b, n), per = parts.plan[kMaxBatch + 1], at0 = parts.plan[b];
     if (past < 0) return;
     const int tiles = (past + n + TILE - 1) / TILE, f = at0 + kh * (tiles + kStart<TILE>) + kStart<TILE>;
