@@ -29,6 +29,7 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxSplit = 16;
+constexpr float kLittle = 1.f / 16;  // share of a sum from which on it is not trusted to be what is left of it
 
 __device__ inline float ex2(float x) {
     float y;
@@ -273,7 +274,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
         if (!(ms.b > 0.f && ms.b < INFINITY && ms.a < INFINITY)) break;
         const float top = ms.a, inv = 1.0f / ms.b;
         float own = some ? ex2((mine - top) * sc) * inv : 0.f;   // r own: probabilities; multiplied only where a node needs them all
-        float R = 1.f;
+        float R = 1.f, added = 1.f;                              // what is left; what was when it was last added up
         int rejected = 0;
         bool lost = false;
         for (uint64_t left = kids; left; left &= left - 1) {
@@ -300,6 +301,15 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
                         if (v0 + e == t) r[u * VEC + e] = 0.f;
                 }
                 ++rejected;
+                // A difference keeps the errors of the sum and of the shares taken from it, some 2^-20 of what was added up: where most of that
+                // is gone and another child asks, what is left is added up anew.  (Every thread of the cluster has the same numbers.)
+                if ((left & (left - 1)) && R < added * kLittle) {
+                    Pair sum = {0.f, 0.f};
+#pragma unroll
+                    for (int e = 0; e < E; ++e) sum.a += r[e];
+                    sum.a *= own;
+                    added = R = join(sum, s_join, calls, rank, split, ok, AddOp()).a;
+                }
             } else {
                 const float over = 1.0f / R;
                 Pair sum = {0.f, 0.f};

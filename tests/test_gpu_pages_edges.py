@@ -1,7 +1,9 @@
-"""Edges of the calls on pages: score rows exactly as wide as their prompts, keys that are NaN for a whole share of a row's keys.
+"""Edges of the calls on pages and of the path of a draft: score rows exactly as wide as their prompts, keys that are NaN for a whole
+share of a row's keys, little mass behind rejected children.
 """
 import math
 
+import numpy as np
 import pytest
 
 from test_gpu_pages import BAD_INDEX, INVALID, Prompts, _check_score
@@ -94,3 +96,50 @@ def test_shares_of_nan_keys(gpu, dtype, hq, hkv, past, n):
                 assert bool(out[0, first:].isnan().all()) and bool(lse[0, first:].isnan().all()), (first, last, bound)
                 assert bool(out[0, :first].isfinite().all()) and bool(lse[0, :first].isfinite().all()), (first, last, bound)
     assert P.kv.stats()["device_error"] == 0
+
+
+# ---- the path of a draft ------------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("V", [50, 1000, 40001, 128000])
+@pytest.mark.parametrize("left", [[1e-3], [1e-5], [1e-6], [0.5, 1e-3], [0.1, 1e-2, 1e-4], [0.7, 0.6, 0.5, 0.3, 0.1, 0.01, 1e-3, 1e-4, 1e-5]])
+def test_little_mass_behind_rejected_children(gpu, dtype, V, left):
+    """A star whose first children are certain tokens and turned down by the largest number below one; left[i] is the mass behind the
+    i-th.  The child after them has half of what is left: numbers one in a thousand beside that decide (its share is off by its
+    exponential's argument of at most 20, 20 x 2^-24, the sums' some 2^-20 of what is held, and what is held by at most 16 times that)."""
+    import torch
+
+    m, heavy, B = len(left), 7, 64
+    tokens = [3 + 2 * i for i in range(m)] + [heavy + 2 * m]
+    masses = [1.0 - left[0]] + [left[i - 1] - left[i] for i in range(1, m)]
+    p = np.full(V, 0.5 * left[-1] / (V - m - 1))
+    p[tokens[:m]], p[tokens[m]] = masses, 0.5 * left[-1]
+    row = torch.tensor(np.log(p), device="cuda").float().to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    r = np.exp(row.double().cpu().numpy())
+    r /= r.sum()
+    kept, rest = [], r.copy()
+    for i in range(m):      # children that can be turned down: the largest number below one is above their share, told in 32 bits
+        share = rest[tokens[i]] / rest.sum()
+        if 1.0 - share > 4e-7:
+            kept.append(tokens[i])
+            rest[tokens[i]] = 0.0
+    share = rest[tokens[m]] / rest.sum()
+    n = len(kept) + 2
+    if n == 2 or not 0.01 < share < 0.99:
+        return              # (bf16 logits of a large vocabulary leave another distribution)
+    rng = np.random.default_rng(V)
+    u = share * (1.0 + np.where(np.arange(B) % 2, 1, -1) * np.exp(rng.uniform(math.log(1e-3), math.log(0.5), B)))
+    u = np.minimum(u, 0.999)
+    uniform = torch.full((B, n), 1.0 - 2.0 ** -24, device="cuda")
+    uniform[:, n - 1] = torch.tensor(u, device="cuda").float()
+    logits = row.expand(B, n, V).contiguous()
+    tok = torch.tensor([[0] + kept + [tokens[m]]], dtype=torch.int32, device="cuda").expand(B, n).contiguous()
+    mask = torch.tensor([[1] + [1 | 2 << i for i in range(n - 1)]], dtype=torch.int64, device="cuda").expand(B, n).contiguous()
+    noise = torch.ones((B, V), device="cuda")
+    kv = gpu.TreeKV(16, 2, 2, 64, "bf16", B, 0)
+    path, count, after = (x.cpu().numpy() for x in kv.pick_path(logits, tok, uniform, noise, mask=mask))
+    taken = u < share
+    assert np.array_equal(count == 2, taken)
+    assert (path[taken, 1] == n - 1).all()
+    rest[tokens[m]] = 0.0
+    if np.partition(rest, -2)[-2] < 0.99 * rest.max():
+        assert (after[~taken] == int(np.argmax(rest))).all()
