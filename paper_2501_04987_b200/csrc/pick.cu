@@ -208,7 +208,7 @@ __global__ void __launch_bounds__(kThreads, E <= 16 ? 2 : 1) pick_kernel(PickArg
         for (int x = first * 32; x < a.vocab; x += step * 32) ask_l2(noise + x);
     __syncthreads();
     if (split > 1) cluster_sync_all();  // every block is running, and its barriers are there, before pairs are sent to it
-    const float sc = greedy ? 1.f : kLog2e / a.temperature;
+    const float sc = greedy ? 1.f : fminf(kLog2e / a.temperature, 3e38f);   // (infinity times the largest logit's distance, 0, would be NaN)
     int at = 0, depth = 0, calls = 0, next = -1;
     bool ok = true;                         // no wait has given up
     for (;;) {   // (a wait that gave up ends the waiting, not the walk: the warps meet at barriers)

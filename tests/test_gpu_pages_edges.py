@@ -1,5 +1,5 @@
 """Edges of the calls on pages and of the path of a draft: score rows exactly as wide as their prompts, keys that are NaN for a whole
-share of a row's keys, little mass behind rejected children.
+share of a row's keys, little mass behind rejected children, the smallest temperatures.
 """
 import math
 
@@ -143,3 +143,27 @@ def test_little_mass_behind_rejected_children(gpu, dtype, V, left):
     rest[tokens[m]] = 0.0
     if np.partition(rest, -2)[-2] < 0.99 * rest.max():
         assert (after[~taken] == int(np.argmax(rest))).all()
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("given", [False, True])
+@pytest.mark.parametrize("temperature", [1e-30, 1e-38, 4e-39, 1e-41, 1.4e-45])
+def test_temperatures_next_to_zero(gpu, dtype, given, temperature):
+    """The one largest logit has all the mass."""
+    import torch
+
+    B, T, V = 3, 4, 5000
+    g = torch.Generator(device="cuda").manual_seed(4)
+    logits = torch.randn((B, T, V), generator=g, device="cuda").to(torch.float32 if dtype == "f32" else torch.bfloat16)
+    logits[:, :, 100] = -math.inf
+    best = torch.tensor([[17, 4000, 3, 4999], [0, 1, 2, 3], [88, 89, 90, 91]], device="cuda")
+    logits.scatter_(2, best[..., None], 20.0)
+    tokens = torch.zeros((B, T), dtype=torch.int32, device="cuda")
+    tokens[0, 1:] = best[0, :3].int()      # a chain that is accepted
+    tokens[1, 1], tokens[1, 2] = 0, 2      # accepted, then turned down
+    uniform, noise = torch.full((B, T), 0.5, device="cuda"), torch.empty((B, V), device="cuda").exponential_(generator=g)
+    q = torch.full((B, T, V), 1.0 / V, device="cuda") if given else None
+    kv = gpu.TreeKV(16, 2, 2, 64, "bf16", B, 0)
+    path, count, after = (x.tolist() for x in kv.pick_path(logits, tokens, uniform, noise, draft=q, temperature=temperature))
+    assert count == [4, 2, 1] and after == [4999, 1, 88]
+    assert path == [[0, 1, 2, 3], [0, 1, -1, -1], [0, -1, -1, -1]]
