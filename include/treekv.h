@@ -428,8 +428,8 @@ treekv_status treekv_adopt_pages(treekv_ctx* ctx, const void* dev_k_pages, const
  *   dev_uniform     [batch][stride] float in [0, 1)      dev_noise  [batch][vocab] float > 0, exponential; both may be NULL at
  *                   temperature 0
  *   dev_path        [batch][stride] int32: nodes of the path, -1 behind it     dev_count  [batch] int32: how many
- *   dev_next        [batch] int32: the token after the path; -1 where the row it would come from has a NaN or an infinite
- *                   logit above, or none above minus infinity
+ *   dev_next        [batch] int32: the token after the path; -1 where the row it would come from has a NaN, or no logit above
+ *                   minus infinity, or, but for temperature 0, one of plus infinity (which is the largest logit there)
  *   host_lens       [batch] int32 in 0..stride (0: count 0, next -1); NULL = all `stride`.  Read before returning.  stride: 1..64
  * vocab: 1..500000 (TREEKV_ERR_UNSUPPORTED above).  Tensors are 16-byte aligned; the rows of an odd vocabulary start anywhere.
  */
