@@ -350,8 +350,8 @@ int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64
  * Section 5 compares Algorithm 1 with.)
  *
  * Pages: dev_k_pages, dev_v_pages [n_pages][n_kv_heads][page_size][head_dim], the context's dtype, 16-byte aligned; page_size
- * 16, 32, 64, 128 or 256 (TREEKV_ERR_UNSUPPORTED otherwise), n_pages * n_kv_heads * page_size < 2^31.  dev_table
- * [batch][table_stride] int32: the page of the sequence's tokens [x page_size, (x + 1) page_size); entries behind its last
+ * 16, 32, 64, 128 or 256 (TREEKV_ERR_UNSUPPORTED otherwise), n_pages * n_kv_heads * page_size < 2^31 and
+ * table_stride * page_size <= 2^30 (the same).  dev_table [batch][table_stride] int32: the page of the sequence's tokens [x page_size, (x + 1) page_size); entries behind its last
  * token are not followed.  Keys carry their position encoding.  An entry outside 0..n_pages-1 is not followed: page 0 is
  * read in its place, nothing is written, and device_error gets bit 256.
  * dev_past [batch] int32, read on the device (a captured call can be replayed while the sequences grow): tokens in the
@@ -368,6 +368,8 @@ int treekv_selftest_fork_plan(const int32_t* host_source, int batch, const int64
  *   dev_lse         [batch][stride][n_heads] float: natural logarithm of the sum of exp(q k / sqrt(head_dim)); may be NULL
  *   host_lens       [batch] int32 in 0..stride (0 = sequence not in this call); NULL = all `stride`.  Read before returning.
  *                   stride: 1..32768
+ * In bf16 contexts the weights are rounded to bf16 where they are multiplied by the values, as in treekv_verify_tree; the sum
+ * that divides them is of the unrounded ones.
  * Rows beyond a sequence's length are neither read nor written.  A page that receives tokens must belong to one sequence of
  * the call; pages that are only read can be shared.  The outputs must not overlap the inputs.  A token's value never enters
  * rows in front of it, also where it is not finite.

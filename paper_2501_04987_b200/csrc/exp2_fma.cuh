@@ -8,7 +8,8 @@ namespace treekv {
 // 2^x of a pair on the multiply-add units, for the share of the exponentials that the special-function unit would keep waiting:
 // x = n + f with n the nearest integer (Cody and Waite's reduction, here without error) and 2^f by the polynomial of degree 5 with
 // value 1 at 0 and the least largest relative error on [-1/2, 1/2] (found by Lawson's iteration; 1.7e-7 with its roundings, as much
-// as the unit's own).  From 2^-127 down the result is 0; NaN stays NaN.
+// as the unit's own).  x stays below 128 (no larger result is made here; weights
+// are at most about 1).  From 2^-127 down the result is 0; NaN stays NaN.
 __device__ inline float2 exp2_fma(float2 x) {
     const float big = 12582912.f + 127.f;  // 1.5 * 2^23 + 127: adding it rounds to an integer, and n + 127 stands in the low bits
     asm("max.NaN.f32 %0, %0, 0fC2FE0000;" : "+f"(x.x));  // -127

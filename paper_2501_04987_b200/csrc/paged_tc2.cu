@@ -18,9 +18,10 @@
 // unnormalised output - go to the caller's scratch, and a second small launch joins them.
 //
 // A tile of 128 keys is 2048 cycles of matrix instructions for both row tiles - S fed from shared memory, P V from tensor memory - and as
-// many of exponentials.  8 KV heads of 128 x 4: 4 x 1024 tokens over 8192 510 us, 1150 TFLOP/s; 2 x 4096 tokens of 32 heads from nothing 410 us,
-// 674 TFLOP/s (an item of 16 tiles at the mean pays some 5 us for its start and its rows, and half of two tiles on the diagonal); 64 tokens of
-// one over 60000 80 us, 3.1 TB/s.  Measured and not taken: blocks that stay and fetch their next item (566 us against 527, short
+// many of exponentials.  8 KV heads of 128 x 4: 4 x 1024 tokens over 8192 521 us, 1120 TFLOP/s (a burst of 20;
+// repeated for a second, under the power cap, 589); 2 x 4096 tokens of 32 heads from nothing 421 us, 653 TFLOP/s; 64 tokens of one over 60000
+// 80 us, 3.1 TB/s.  Of the 700000 cycles of whole prompts the steps of 1024 items, 17 at the mean, are 412000 an SM, starts and rows, some 5 us an
+// item, 60000, and the order below, whose last wave is one unit, 58000; the other 170000 are not explained.  Measured and not taken: blocks that stay and fetch their next item (566 us against 527, short
 // prompts 300 against 268), a share of the exponentials on the multiply-add units (574 to 621 against 551: the same warps feed both),
 // registers 216 / 72 (611) and 200 / 104; eight warps a row tile, two threads a row (596 against 530), an issuer for each row tile (656: the
 // tiles no longer take turns).

@@ -29,7 +29,9 @@ namespace {
 
 constexpr int kThreads = 512, kWarps = kThreads / 32;
 constexpr int kMaxSplit = 16;
-constexpr float kLittle = 1.f / 16;  // share of a sum from which on it is not trusted to be what is left of it
+// Share of a sum below which a difference is not trusted to be what is left of it.  (15 children of a row of 128000 turned down that held
+// nearly everything, 32 sequences: 30.6 us; as differences alone 29.2, and off by several percent at a millionth.)
+constexpr float kLittle = 1.f / 16;
 
 __device__ inline float ex2(float x) {
     float y;

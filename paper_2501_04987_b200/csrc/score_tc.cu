@@ -11,13 +11,13 @@
 // all rows see in front of those that fewer and fewer do: so the blocks end together.  With fewer items than the machine has SMs a
 // cluster shares an item's query tiles.
 //
-// A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 38 us, 3.6 TB/s; the
+// A window of one query tile is bound by the bytes of K (8 windows of 32 tokens x 4 heads over 8192: 134 MB in 39 us, 3.5 TB/s; the
 // exponentials alone take 15 us, the matrix instructions 10).  A chunk's logit tile of 128 x 128 takes 1480 cycles: 512 of matrix
 // instructions, 770 of exponentials with one in four on the multiply-add units, 512 for the log-sum-exps that every warp reads.  By the
 // counters no unit is busy for half the time, and none of these changed it by much (4 x 1024 over 4096, 216 us): no exponentials on the
 // multiply-add units (223), scalar multiply-adds (228), a second thread that issues (211), two key tiles a thread, which halves the
 // reads and the queries that come in (223; over 8192 395 against 407), logit tiles of 256 columns (249 -> 283, with two groups).
-// 4 chunks of up to 1024 over up to 4096: 132 us, 660 TFLOP/s.
+// 4 chunks of up to 1024 over up to 4096: 135 us, 645 TFLOP/s.
 //
 // Warps: 0 issues TMA, 1 issues MMA and owns the tensor memory, from 2 on two or four groups of four that take logit tiles in turns.
 #include <algorithm>
@@ -417,7 +417,7 @@ cudaError_t launch_t(const CacheView& cv, const PagedView& pv, const ChunkView& 
 
 cudaError_t launch_score_tc(const CacheView& cv, const PagedView& pv, const ChunkView& ch, const ChunkLens& lens, int max_n, const ScoreArgs& a,
                             int sms, cudaStream_t stream) {
-    // Two groups for up to two query tiles, where the keys stream by (8 x 32 tokens x 4 heads over 8192: 38 us, with four 42; 2 x 64
+    // Two groups for up to two query tiles, where the keys stream by (8 x 32 tokens x 4 heads over 8192: 39 us, with four 42; 2 x 64
     // over 10000: 26 and 29), four for more, where each waits for its own arithmetic (4 x 512 over 4096: 120 with two, 117 with four; 4 x
     // 1024: 234 and 216).
     const bool window = max_n * (cv.Hq / cv.Hkv) <= 2 * kTile;
